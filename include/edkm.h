@@ -323,6 +323,106 @@ edkm_status edkm_unique_inverse_batch(int count, edkm_plan* const* plans,
                                       const uint16_t* const* w_bits, uint16_t* const* unique_out,
                                       uint16_t* const* inverse_out, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Layer and optimizer operators: what a program does with clustered weights.
+ *
+ * These calls take no plan.  Matrices are row-major with a leading dimension
+ * (elements between two rows, at least the row's length; ignored for a single
+ * row); 16-bit tensors of one call share one format (EDKM_KEYS_FP16 or
+ * EDKM_KEYS_BF16); sums are fp32 and each output is rounded once, to nearest
+ * even.  Sizes are 1 .. 2^31 - 1025, and m may be 0.  A workspace, where a
+ * call names one, holds at least the bytes of its size function (256-byte
+ * aligned; may be NULL if that is 0), carries nothing from one call to the
+ * next and must not be used by two calls at once.  Outputs must not overlap
+ * inputs except where noted.  Every call is asynchronous on the stream and can
+ * be captured in a HIP graph. */
+
+/* Activations: max(z, 0); z Phi(z) with the normal distribution's Phi (erf
+ * form); z / (1 + e^-z). */
+enum { EDKM_ACT_NONE = 0, EDKM_ACT_RELU = 1, EDKM_ACT_GELU = 2, EDKM_ACT_SILU = 3 };
+
+/* Product with its epilogue: z = x W^T + bias, y = act(z) + residual.
+ *   x         m x k tokens;  w  n x k weights (W~ of edkm_forward with out_half = 1)
+ *   bias      nullable, n;   residual  nullable, m x n
+ *   y         m x n; may be the residual (same leading dimension)
+ *   z         nullable, m x n without gaps: z for the backward, rounded to 16
+ *             bits (a finite value beyond the format becomes its largest) */
+size_t edkm_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
+edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activation,
+                        const void* x, int64_t ldx, const void* w, int64_t ldw,
+                        const void* bias, const void* residual, int64_t ldr,
+                        void* y, int64_t ldy, void* z, void* ws, size_t ws_bytes,
+                        hipStream_t stream);
+
+/* Its gradients for a given dL/dy: with dz = dy act'(z),
+ *   dx = dz W (m x k), dw = dz^T x (n x k without gaps: the dL/dW~ that
+ *   edkm_backward_ex takes with EDKM_GRAD_IN_HALF), dbias = sum over m of dz (n),
+ * all in the 16-bit format; each nullable, one at least given.  dL/dresidual
+ * is dy itself.  With an activation, dz is rounded to 16 bits before the two
+ * products (the bias gradient sums it unrounded).
+ *   z   the z of edkm_linear; not read without activation.  x is read for dw
+ *       only, w for dx only.  With m = 0, dw and dbias become zeros. */
+size_t edkm_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int activation);
+edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, int activation,
+                                 const void* dy, int64_t lddy, const void* z,
+                                 const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                 void* dx, int64_t lddx, void* dw, void* dbias,
+                                 void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The 16-bit weights of a palette, the inverse of edkm_palettize: w_out_i =
+ * lut[index_i] rounded to the format.
+ *   indices  device uint8[ceil(n bits / 8)], packed as edkm_palettize packs them
+ *   lut      device float[2^bits];  w_out  device, n;  n 1 .. EDKM_MAX_N */
+edkm_status edkm_unpalettize(const uint8_t* indices, uint64_t n, int bits, int format,
+                             const float* lut, uint16_t* w_out, hipStream_t stream);
+
+/* edkm_linear with the weights given as a palette: n x k row-major weights as
+ * edkm_palettize packs them (rows may start inside a byte), n k <= EDKM_MAX_N.
+ * A weight is its table entry rounded to the format, so y is edkm_linear's on
+ * the weights that edkm_unpalettize gives, up to the order of the sums.  For
+ * few tokens the indices are decoded on the way into the product; for many the
+ * weights are decoded into the workspace first. */
+size_t edkm_palette_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int bits);
+edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int format, int activation,
+                                const void* x, int64_t ldx, const uint8_t* indices, const float* lut,
+                                const void* bias, const void* residual, int64_t ldr,
+                                void* y, int64_t ldy, void* z, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* One AdamW step over `count` tensors, one launch per EDKM_LAUNCH_GROUP of them:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, t = *step + 1; *step becomes t.
+ *   n          host array: elements of each tensor, 0 .. EDKM_MAX_N (0: skipped)
+ *   param_type EDKM_TYPE_*; grad_type the same, or EDKM_TYPE_FP32
+ *   params     host array of device pointers: p, updated (to nearest even in 16 bits)
+ *   masters    nullable (must be NULL for fp32 parameters), entries nullable: fp32
+ *              parameters that the step is taken on; p is then their rounding
+ *   grads, exp_avg (m), exp_avg_sq (v)   host arrays of device pointers
+ *   state_bits 32: m and v are float.  8: m is float8 e4m3 (fn), v float8 e5m2,
+ *              one byte per element, times an fp32 scale for each
+ *              EDKM_STATE_BLOCK elements (m_scales, v_scales: host arrays of
+ *              device pointers, ceil(n / EDKM_STATE_BLOCK) floats each; not
+ *              read with 32).  A block's largest magnitude is stored as 448 or
+ *              57344 times the scale.  A value between two float8 numbers goes
+ *              up or down by a 16-bit noise (a hash of element pair, t and
+ *              seed), so that increments below half a step are kept on average;
+ *              a v above 0 is stored above 0.  Blocks whose largest magnitude
+ *              is below 2^-100 are stored as zeros.  A block with an Inf or NaN
+ *              gets a NaN scale.
+ *   step       device int32[1]: the steps done before this one
+ *   lr_dev     nullable, device float[1]: the rate (lr is then ignored), so that
+ *              a captured step can follow a schedule
+ * Elementwise on each tensor's own arrays; repeatable bit for bit.  Tensors of
+ * one call must not overlap (those of one launch are checked). */
+enum { EDKM_TYPE_FP16 = 0, EDKM_TYPE_BF16 = 1, EDKM_TYPE_FP32 = 2 };
+#define EDKM_STATE_BLOCK 256
+edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int grad_type, int state_bits,
+                             void* const* params, float* const* masters, const void* const* grads,
+                             void* const* exp_avg, void* const* exp_avg_sq,
+                             float* const* m_scales, float* const* v_scales,
+                             int32_t* step, const float* lr_dev, double lr, double beta1, double beta2,
+                             double eps, double weight_decay, uint32_t seed, hipStream_t stream);
+
 /* Keyed-gradient accumulators (the backward's keyed reduction).  AUTO, the
  * default, chooses per matrix at init_unique from how concentrated the
  * weight patterns are: 32-bit fixed point with returning LDS atomics when few

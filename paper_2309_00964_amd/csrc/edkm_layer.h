@@ -1,0 +1,88 @@
+// Internal declarations of the layer and optimizer operators: the products with
+// 16-bit or palettized weights, the palette read-back and the AdamW step.
+#pragma once
+#include "edkm_internal.h"
+
+namespace edkm {
+
+enum Activation : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3, ACT_COUNT = 4 };
+
+// How an operand of a product lies in memory.  `row` is its output index (a token,
+// an output feature), `depth` the index that is summed over.
+enum Operand : int {
+    OP_ROWS = 0,   // [row][depth], depth contiguous
+    OP_DEPTH = 1,  // [depth][row], rows contiguous
+    OP_PALETTE = 2 // [row][depth] as packed b-bit indices into a table
+};
+
+// out[r][c] = epilogue(sum_d a(r, d) b(c, d)); 16-bit operands of one format, fp32 sums.
+struct ProductArgs {
+    const uint16_t* a;
+    const uint16_t* b;
+    int64_t lda, ldb;       // elements between two rows of memory
+    int32_t rows, cols, depth;
+    // OP_PALETTE
+    const uint8_t* idx;
+    const float* lut;
+    uint64_t idx_bytes;
+    int bits;
+    // epilogue: y = act(sum + bias[c]) + res[r][c]; z = sum + bias (nullable)
+    const uint16_t* bias;
+    const uint16_t* res;
+    int64_t ldr;
+    uint16_t* out;
+    int64_t ldo;
+    uint16_t* z;
+    int act;
+};
+
+// The gradient at the activation: dz = dy act'(z) (16 bits, only with an activation)
+// and the bias gradient, summed over the rows of each chunk and then over the chunks.
+struct DzArgs {
+    const uint16_t* dy;
+    int64_t lddy;
+    const uint16_t* z;
+    uint16_t* dz;
+    float* part;            // [chunks][cols]
+    uint16_t* dbias;
+    int32_t rows, cols;
+    int act;
+};
+
+constexpr int DZ_COLS = 64, DZ_ROWS = 256;   // one block's share of the bias gradient
+
+enum ParamType : int { PT_FP16 = 0, PT_BF16 = 1, PT_FP32 = 2 };
+
+struct AdamwTensor {
+    void* p;
+    float* master;
+    const void* g;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    uint64_t n;
+};
+
+constexpr int ADAMW_BLOCK = 256;       // elements of one 8-bit state's scale
+constexpr int ADAMW_CHUNK = 4096;      // elements of one workgroup
+
+struct AdamwArgs {
+    int count;
+    uint32_t seed;
+    int32_t* step;                     // steps done before this one
+    const float* lr_dev;               // the rate on the device, or null: lr
+    double lr, beta1, beta2, eps, decay;
+    uint32_t wg_begin[MAXB];           // first workgroup of each tensor; 0xFFFFFFFF past them
+    AdamwTensor t[MAXB];
+};
+static_assert(sizeof(AdamwArgs) <= 4096, "launch arguments fit the kernel-argument limit");
+
+hipError_t launch_product(const ProductArgs& a, int fmt, int opa, int opb, hipStream_t s);
+hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s);
+hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
+                              uint16_t* out, hipStream_t s);
+hipError_t launch_adamw(const AdamwArgs& a, uint32_t grid, int param_type, int grad_type, int state_bits, hipStream_t s);
+hipError_t launch_adamw_tick(int32_t* step, hipStream_t s);
+
+}  // namespace edkm

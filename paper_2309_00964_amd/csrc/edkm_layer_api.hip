@@ -1,0 +1,267 @@
+// C ABI of the layer and optimizer operators: argument checks, workspace layout and
+// the launches of each call.  Every check runs on the host before any HIP call.
+
+#include "../../include/edkm.h"
+#include "edkm_layer.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+using namespace edkm;
+
+namespace {
+
+static_assert(EDKM_ACT_NONE == ACT_NONE && EDKM_ACT_RELU == ACT_RELU && EDKM_ACT_GELU == ACT_GELU &&
+                  EDKM_ACT_SILU == ACT_SILU, "activations");
+static_assert(EDKM_TYPE_FP16 == PT_FP16 && EDKM_TYPE_BF16 == PT_BF16 && EDKM_TYPE_FP32 == PT_FP32, "types");
+static_assert(EDKM_STATE_BLOCK == ADAMW_BLOCK, "8-bit state blocks");
+
+constexpr int64_t DIM_MAX = 0x7FFFFFFF - 1024;   // sizes are 32-bit in the kernels, tile ends included
+
+bool size_ok(int64_t v, int64_t least) { return v >= least && v <= DIM_MAX; }
+
+bool product_ok(int64_t m, int64_t n, int64_t k, int format, int act) {
+    return size_ok(m, 0) && size_ok(n, 1) && size_ok(k, 1) && (format == EDKM_KEYS_FP16 || format == EDKM_KEYS_BF16) &&
+           act >= 0 && act < ACT_COUNT;
+}
+
+// leading dimension of a matrix with `rows` rows of `cols`: any for a single row
+bool ld_ok(int64_t ld, int64_t rows, int64_t cols) { return (ld >= cols && ld < (int64_t)1 << 40) || rows <= 1; }
+
+size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+int dz_chunks(int64_t m) { return (int)((m + DZ_ROWS - 1) / DZ_ROWS); }
+
+// Workspace of a backward: dz, then the bias gradient's partial sums.
+struct BackwardWs {
+    size_t dz, part, total;
+};
+BackwardWs backward_ws(int64_t m, int64_t n, int act) {
+    BackwardWs w;
+    w.dz = 0;
+    w.part = act == ACT_NONE ? 0 : up256((size_t)m * n * 2);
+    w.total = w.part + up256((size_t)dz_chunks(m) * n * 4);
+    return w;
+}
+
+edkm_status ws_ok(const void* ws, size_t have, size_t need) {
+    if (need == 0) return EDKM_OK;
+    return !ws || have < need || ((uintptr_t)ws & 255u) ? EDKM_ERR_WORKSPACE : EDKM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t edkm_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) {
+    (void)m; (void)n; (void)k;
+    return 0;
+}
+
+edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activation, const void* x, int64_t ldx,
+                        const void* w, int64_t ldw, const void* bias, const void* residual, int64_t ldr, void* y,
+                        int64_t ldy, void* z, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (!product_ok(m, n, k, format, activation) || !w || !ld_ok(ldw, n, k)) return EDKM_ERR_ARG;
+    if (m > 0 && (!x || !y)) return EDKM_ERR_ARG;
+    if (!ld_ok(ldx, m, k) || !ld_ok(ldy, m, n) || (residual && !ld_ok(ldr, m, n))) return EDKM_ERR_ARG;
+    const edkm_status st = ws_ok(ws, ws_bytes, edkm_linear_workspace_bytes(m, n, k));
+    if (st != EDKM_OK) return st;
+    if (m == 0) return EDKM_OK;
+    ProductArgs p{};
+    p.a = static_cast<const uint16_t*>(x);
+    p.lda = ldx;
+    p.b = static_cast<const uint16_t*>(w);
+    p.ldb = ldw;
+    p.rows = (int32_t)m;
+    p.cols = (int32_t)n;
+    p.depth = (int32_t)k;
+    p.bias = static_cast<const uint16_t*>(bias);
+    p.res = static_cast<const uint16_t*>(residual);
+    p.ldr = ldr;
+    p.out = static_cast<uint16_t*>(y);
+    p.ldo = ldy;
+    p.z = static_cast<uint16_t*>(z);
+    p.act = activation;
+    return launch_product(p, format, OP_ROWS, OP_ROWS, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+}
+
+size_t edkm_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int activation) {
+    if (!product_ok(m, n, k, EDKM_KEYS_FP16, activation)) return 0;
+    return backward_ws(m, n, activation).total;
+}
+
+edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, int activation, const void* dy,
+                                 int64_t lddy, const void* z, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                 void* dx, int64_t lddx, void* dw, void* dbias, void* ws, size_t ws_bytes,
+                                 hipStream_t stream) {
+    if (!product_ok(m, n, k, format, activation) || (!dx && !dw && !dbias)) return EDKM_ERR_ARG;
+    if (m > 0 && (!dy || (activation != ACT_NONE && !z) || (dw && !x))) return EDKM_ERR_ARG;
+    if (dx && (!w || !ld_ok(ldw, n, k) || !ld_ok(lddx, m, k))) return EDKM_ERR_ARG;
+    if ((dw && !ld_ok(ldx, m, k)) || !ld_ok(lddy, m, n)) return EDKM_ERR_ARG;
+    const BackwardWs L = backward_ws(m, n, activation);
+    const edkm_status st = ws_ok(ws, ws_bytes, L.total);
+    if (st != EDKM_OK) return st;
+    char* base = static_cast<char*>(ws);
+    DzArgs d{};
+    d.dy = static_cast<const uint16_t*>(dy);
+    d.lddy = lddy;
+    d.z = static_cast<const uint16_t*>(z);
+    d.dz = reinterpret_cast<uint16_t*>(base + L.dz);
+    d.part = reinterpret_cast<float*>(base + L.part);
+    d.dbias = static_cast<uint16_t*>(dbias);
+    d.rows = (int32_t)m;
+    d.cols = (int32_t)n;
+    d.act = activation;
+    if (launch_dz(d, format, stream) != hipSuccess) return EDKM_ERR_HIP;
+    const uint16_t* dz = activation == ACT_NONE ? d.dy : d.dz;
+    const int64_t lddz = activation == ACT_NONE ? lddy : n;
+    if (dx && m > 0) {
+        ProductArgs p{};
+        p.a = dz;
+        p.lda = lddz;
+        p.b = static_cast<const uint16_t*>(w);
+        p.ldb = ldw;
+        p.rows = (int32_t)m;
+        p.cols = (int32_t)k;
+        p.depth = (int32_t)n;
+        p.out = static_cast<uint16_t*>(dx);
+        p.ldo = lddx;
+        if (launch_product(p, format, OP_ROWS, OP_DEPTH, stream) != hipSuccess) return EDKM_ERR_HIP;
+    }
+    if (dw) {
+        ProductArgs p{};
+        p.a = dz;
+        p.lda = lddz;
+        p.b = static_cast<const uint16_t*>(x);
+        p.ldb = ldx;
+        p.rows = (int32_t)n;
+        p.cols = (int32_t)k;
+        p.depth = (int32_t)m;
+        p.out = static_cast<uint16_t*>(dw);
+        p.ldo = k;
+        if (launch_product(p, format, OP_DEPTH, OP_DEPTH, stream) != hipSuccess) return EDKM_ERR_HIP;
+    }
+    return EDKM_OK;
+}
+
+size_t edkm_palette_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int bits) {
+    (void)m; (void)n; (void)k; (void)bits;
+    return 0;
+}
+
+edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int format, int activation, const void* x,
+                                int64_t ldx, const uint8_t* indices, const float* lut, const void* bias,
+                                const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, void* ws,
+                                size_t ws_bytes, hipStream_t stream) {
+    if (!product_ok(m, n, k, format, activation) || bits < 1 || bits > EDKM_MAX_BITS || !indices || !lut ||
+        (uint64_t)n * (uint64_t)k > EDKM_MAX_N)
+        return EDKM_ERR_ARG;
+    if (m > 0 && (!x || !y)) return EDKM_ERR_ARG;
+    if (!ld_ok(ldx, m, k) || !ld_ok(ldy, m, n) || (residual && !ld_ok(ldr, m, n))) return EDKM_ERR_ARG;
+    const edkm_status st = ws_ok(ws, ws_bytes, edkm_palette_linear_workspace_bytes(m, n, k, bits));
+    if (st != EDKM_OK) return st;
+    if (m == 0) return EDKM_OK;
+    ProductArgs p{};
+    p.a = static_cast<const uint16_t*>(x);
+    p.lda = ldx;
+    p.idx = indices;
+    p.idx_bytes = ((uint64_t)n * (uint64_t)k * (uint64_t)bits + 7) / 8;
+    p.lut = lut;
+    p.bits = bits;
+    p.rows = (int32_t)m;
+    p.cols = (int32_t)n;
+    p.depth = (int32_t)k;
+    p.bias = static_cast<const uint16_t*>(bias);
+    p.res = static_cast<const uint16_t*>(residual);
+    p.ldr = ldr;
+    p.out = static_cast<uint16_t*>(y);
+    p.ldo = ldy;
+    p.z = static_cast<uint16_t*>(z);
+    p.act = activation;
+    return launch_product(p, format, OP_ROWS, OP_PALETTE, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+}
+
+edkm_status edkm_unpalettize(const uint8_t* indices, uint64_t n, int bits, int format, const float* lut, uint16_t* w_out,
+                             hipStream_t stream) {
+    if (!indices || !lut || !w_out || n < 1 || n > EDKM_MAX_N || bits < 1 || bits > EDKM_MAX_BITS ||
+        (format != EDKM_KEYS_FP16 && format != EDKM_KEYS_BF16))
+        return EDKM_ERR_ARG;
+    const uint64_t bytes = (n * (uint64_t)bits + 7) / 8;
+    return launch_unpalettize(indices, bytes, n, bits, format, lut, w_out, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+}
+
+edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int grad_type, int state_bits,
+                             void* const* params, float* const* masters, const void* const* grads,
+                             void* const* exp_avg, void* const* exp_avg_sq, float* const* m_scales,
+                             float* const* v_scales, int32_t* step, const float* lr_dev, double lr, double beta1,
+                             double beta2, double eps, double weight_decay, uint32_t seed, hipStream_t stream) {
+    if (count < 1 || !n || !params || !grads || !exp_avg || !exp_avg_sq || !step) return EDKM_ERR_ARG;
+    if (param_type < PT_FP16 || param_type > PT_FP32 || (grad_type != param_type && grad_type != PT_FP32) ||
+        (state_bits != 8 && state_bits != 32) || (state_bits == 8 && (!m_scales || !v_scales)) ||
+        (masters && param_type == PT_FP32))
+        return EDKM_ERR_ARG;
+    if (!(lr_dev || (std::isfinite(lr) && lr >= 0)) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) ||
+        !(std::isfinite(eps) && eps >= 0) || !(std::isfinite(weight_decay) && weight_decay >= 0))
+        return EDKM_ERR_ARG;
+    const size_t pe = param_type == PT_FP32 ? 4 : 2, se = state_bits / 8;
+    for (int i = 0; i < count; ++i) {
+        if (n[i] > EDKM_MAX_N) return EDKM_ERR_ARG;
+        if (n[i] == 0) continue;
+        if (!params[i] || !grads[i] || !exp_avg[i] || !exp_avg_sq[i] || (state_bits == 8 && (!m_scales[i] || !v_scales[i])))
+            return EDKM_ERR_ARG;
+    }
+    auto clash = [](const void* a, size_t na, const void* b, size_t nb) {
+        return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+    };
+    // Two workgroups must not write the same place: tensors of one launch that overlap.
+    auto overlap = [&](int i, int j) {
+        return clash(params[i], n[i] * pe, params[j], n[j] * pe) || clash(exp_avg[i], n[i] * se, exp_avg[j], n[j] * se) ||
+               clash(exp_avg_sq[i], n[i] * se, exp_avg_sq[j], n[j] * se);
+    };
+    AdamwArgs a;
+    // all groups are checked before the first launch
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int i = 0; i < count;) {
+            std::memset(&a, 0, sizeof(a));
+            a.seed = seed;
+            a.step = step;
+            a.lr_dev = lr_dev;
+            a.lr = lr;
+            a.beta1 = beta1;
+            a.beta2 = beta2;
+            a.eps = eps;
+            a.decay = weight_decay;
+            uint64_t grid = 0;
+            int src[MAXB];
+            for (; i < count && a.count < MAXB; ++i) {
+                if (n[i] == 0) continue;
+                const uint64_t wgs = (n[i] + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+                AdamwTensor& T = a.t[a.count];
+                T.p = params[i];
+                T.master = masters ? masters[i] : nullptr;
+                T.g = grads[i];
+                T.m = exp_avg[i];
+                T.v = exp_avg_sq[i];
+                T.m_scale = state_bits == 8 ? m_scales[i] : nullptr;
+                T.v_scale = state_bits == 8 ? v_scales[i] : nullptr;
+                T.n = n[i];
+                a.wg_begin[a.count] = (uint32_t)grid;
+                src[a.count++] = i;
+                grid += wgs;
+            }
+            for (int j = a.count; j < MAXB; ++j) a.wg_begin[j] = 0xFFFFFFFFu;
+            if (a.count == 0) continue;
+            if (pass == 0) {
+                for (int x = 0; x < a.count; ++x)
+                    for (int y = 0; y < x; ++y)
+                        if (overlap(src[x], src[y])) return EDKM_ERR_ARG;
+            } else if (launch_adamw(a, (uint32_t)grid, param_type, grad_type, state_bits, stream) != hipSuccess) {
+                return EDKM_ERR_HIP;
+            }
+        }
+    }
+    return launch_adamw_tick(step, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+}
+
+}  // extern "C"

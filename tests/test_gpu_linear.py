@@ -1,0 +1,356 @@
+"""The products with an epilogue against plain 64-bit ones: every operand layout, type
+and direction at sizes around the tiles' ends, strided and unaligned rows, buffers whose
+surroundings are NaN, and the palette forms against the decoded weights."""
+import sys
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import layer_util as L                                             # noqa: E402
+from oracle import palette as pal                                  # noqa: E402
+from paper_2309_00964_amd import edkm, function, inputs            # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def say(*a):
+    print("[gpu-case]", *a, flush=True)
+    sys.stdout.flush()
+
+
+def randn(seed, *shape, dtype, scale=1.0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g, device=DEV) * scale).to(dtype)
+
+
+def inside(t, lead=1, gap=0):
+    """The same matrix as a view of a NaN-filled buffer: `lead` elements and one row before
+    it, `gap` elements between its rows, a row after it."""
+    r, c = t.shape
+    buf = torch.full((lead + (r + 2) * (c + gap),), float("nan"), dtype=t.dtype, device=t.device)
+    v = buf[lead + c + gap:][: r * (c + gap)].view(r, c + gap)[:, :c]
+    v.copy_(t)
+    return buf, v
+
+
+SIZES = [(1, 1, 1), (1, 64, 64), (2, 17, 33), (5, 256, 512), (16, 100, 129), (17, 130, 96), (33, 257, 200), (64, 128, 256),
+         (65, 63, 1031), (128, 320, 64), (200, 333, 77), (257, 260, 520), (300, 1, 40), (1, 3, 5000), (513, 515, 9)]
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_forward_and_backward(fmt, m, n, k):
+    dt = L.DT[fmt]
+    for i, name in enumerate(L.ACTS):
+        say("linear", fmt, m, n, k, name)
+        with_bias, with_res = i % 2 == 0, i != 1
+        x, w = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt, scale=k ** -0.5)
+        bias = randn(3, n, dtype=dt, scale=0.5) if with_bias else None
+        res = randn(4, m, n, dtype=dt) if with_res else None
+        dy = randn(5, m, n, dtype=dt)
+        y, z = torch.empty(m, n, dtype=dt, device=DEV), torch.empty(m, n, dtype=dt, device=DEV)
+        edkm.linear(x, w, y, bias, res, name, z)
+        z64, y64, tol = L.product(x, w, bias, res, name)
+        L.assert_within(y, y64, tol, "y")
+        L.assert_within(z, *L.product(x, w, bias, None, "none")[1:], "z")
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, dtype=dt, device=DEV)
+        edkm.linear_backward(dy, x, w, dx, dw, db, z, name)
+        for key, (ref, tol) in L.gradients(dy, x, w, z64, name).items():
+            L.assert_within({"dx": dx, "dw": dw, "db": db}[key], ref, tol, key)
+
+
+@pytest.mark.parametrize("m,n,k,lead,gap", [(40, 70, 100, 1, 3), (40, 70, 100, 8, 4), (3, 70, 100, 1, 3), (3, 64, 96, 8, 8),
+                                            (300, 264, 136, 8, 8), (300, 264, 136, 1, 0), (300, 263, 137, 3, 1),
+                                            (70, 300, 1000, 2, 7)])
+def test_views_in_nan_buffers(m, n, k, lead, gap):
+    """Nothing outside the matrices is read into a result, and nothing outside the outputs
+    is written."""
+    dt = torch.bfloat16
+    say("views", m, n, k, lead, gap)
+    x, w, res = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt, scale=0.1), randn(3, m, n, dtype=dt)
+    dy = randn(4, m, n, dtype=dt)
+    _, xv = inside(x, lead, gap)
+    _, wv = inside(w, lead, gap)
+    _, rv = inside(res, lead, gap)
+    _, dyv = inside(dy, lead, gap)
+    ybuf, yv = inside(torch.zeros_like(res), lead, gap)
+    xbuf, dxv = inside(torch.zeros_like(x), lead, gap)
+    edkm.linear(xv, wv, yv, None, rv, "none")
+    z64, y64, tol = L.product(x, w, None, res, "none")
+    L.assert_within(yv, y64, tol, "y")
+    assert int(ybuf.isnan().sum()) == ybuf.numel() - m * n
+    dwbuf = torch.full((lead + n * k + 16,), float("nan"), dtype=dt, device=DEV)
+    dw = dwbuf[lead:lead + n * k].view(n, k)
+    edkm.linear_backward(dyv, xv, wv, dxv, dw)
+    ref = L.gradients(dy, x, w, z64, "none")
+    L.assert_within(dxv, *ref["dx"], "dx")
+    L.assert_within(dw, *ref["dw"], "dw")
+    assert int(xbuf.isnan().sum()) == xbuf.numel() - m * k
+    assert int(dwbuf.isnan().sum()) == dwbuf.numel() - n * k
+
+
+@pytest.mark.parametrize("m", [4, 100, 300])
+def test_a_row_of_nan_or_inf_stays_in_its_row(m):
+    n, k, dt = 140, 200, torch.float16
+    say("nan rows", m)
+    x, w = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt, scale=0.1)
+    x[1, 7] = float("nan")
+    x[2, k - 1] = float("inf")
+    y = torch.empty(m, n, dtype=dt, device=DEV)
+    edkm.linear(x, w, y)
+    assert bool(y[1].isnan().all()) and not bool(y[2].isfinite().any())
+    keep = [0, *range(3, m)]
+    L.assert_within(y[keep], *L.product(x[keep], w, None, None, "none")[1:], "y")
+
+
+def test_large_z_keeps_its_slope():
+    """fp16: z beyond 65504 is kept as a finite number, so silu's and gelu's slopes there
+    stay 1 and 0 and the gradients finite."""
+    x = torch.tensor([[300.0, 300.0]], dtype=torch.float16, device=DEV)
+    w = torch.tensor([[300.0, 300.0], [-300.0, -300.0]], dtype=torch.float16, device=DEV)
+    for name in ("silu", "gelu"):
+        say("large z", name)
+        y, z = torch.empty(1, 2, dtype=x.dtype, device=DEV), torch.empty(1, 2, dtype=x.dtype, device=DEV)
+        edkm.linear(x, w, y, None, None, name, z)
+        assert z.tolist() == [[65504.0, -65504.0]]
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        edkm.linear_backward(torch.ones_like(y), x, w, dx, dw, None, z, name)
+        assert dx.tolist() == [[300.0, 300.0]] and dw.tolist() == [[300.0, 300.0], [0.0, 0.0]]
+
+
+def test_no_tokens():
+    say("m = 0")
+    dt, n, k = torch.float16, 70, 33
+    x, w = torch.empty(0, k, dtype=dt, device=DEV), randn(1, n, k, dtype=dt)
+    y = torch.empty(0, n, dtype=dt, device=DEV)
+    edkm.linear(x, w, y)
+    dw, db = torch.ones_like(w), torch.ones(n, dtype=dt, device=DEV)
+    edkm.linear_backward(y, x, w, torch.empty_like(x), dw, db)
+    assert not bool(dw.any()) and not bool(db.any())
+    _, packed, lut = L.palette(n, k, 3, 1)
+    edkm.palette_linear(x, torch.from_numpy(packed).to(DEV), torch.from_numpy(lut).to(DEV), y)
+    torch.cuda.synchronize()
+
+
+def test_y_may_be_the_residual():
+    for m in (2, 90, 400):
+        say("in place", m)
+        x, w, r = (randn(i, *s, dtype=torch.bfloat16) for i, s in enumerate([(m, 136), (264, 136), (m, 264)]))
+        y = r.clone()
+        edkm.linear(x, w, y, None, y, "relu")
+        L.assert_within(y, *L.product(x, w, None, r, "relu")[1:], "y")
+
+
+def device_palette(n, k, bits, seed):
+    idx, packed, lut = L.palette(n, k, bits, seed)
+    return idx, torch.from_numpy(packed).to(DEV), torch.from_numpy(lut).to(DEV), lut
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+@pytest.mark.parametrize("bits", [1, 2, 3, 4])
+@pytest.mark.parametrize("count", [1, 7, 8, 9, 31, 4097, 100_003])
+def test_unpalettize(fmt, bits, count):
+    say("unpalettize", fmt, bits, count)
+    idx, packed, lut, _ = device_palette(count, 1, bits, bits)
+    for lead in (0, 1):           # aligned and unaligned indices and outputs
+        raw = torch.cat([torch.full((lead,), 255, dtype=torch.uint8, device=DEV), packed])
+        buf = torch.full((count + 40,), float("nan"), dtype=L.DT[fmt], device=DEV)
+        edkm.unpalettize(raw[lead:], lut, buf[lead:lead + count])
+        want = lut.to(L.DT[fmt])[torch.from_numpy(idx).to(DEV).long()]
+        assert torch.equal(buf[lead:lead + count], want)
+        assert int(buf.isnan().sum()) == 40
+
+
+def test_unpalettize_inverts_palettize():
+    keys = inputs.fp16_weights(50_001, 3)
+    say("palettize and back")
+    lut = inputs.quantile_init(keys, 8)
+    w = torch.from_numpy(keys.view(np.int16)).to(DEV)
+    packed = torch.empty((keys.size * 3 + 7) // 8, dtype=torch.uint8, device=DEV)
+    lut_d = torch.from_numpy(lut).to(DEV)
+    edkm.palettize_noalloc(w, keys.size, 3, lut_d, packed)
+    out = torch.empty(keys.size, dtype=torch.float16, device=DEV)
+    edkm.unpalettize(packed, lut_d, out)
+    assert np.array_equal(out.cpu().numpy(), lut.astype(np.float16)[pal.indices(keys, lut)])
+
+
+@pytest.mark.parametrize("bits", [1, 2, 3, 4])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 64, 256), (1, 100, 77), (2, 33, 1000), (4, 48, 4096), (7, 1003, 137),
+                                   (8, 512, 96), (16, 31, 64), (17, 200, 264), (33, 128, 128), (64, 65, 130), (130, 140, 512),
+                                   (300, 513, 72), (520, 260, 330)])
+def test_palette_linear(bits, m, n, k):
+    fmt = "fp16" if (m + bits) % 2 else "bf16"
+    dt = L.DT[fmt]
+    idx, packed, lut, _ = device_palette(n, k, bits, 10 * bits + m)
+    w = lut.to(dt)[torch.from_numpy(idx).to(DEV).long()].view(n, k)
+    x, bias, res = randn(1, m, k, dtype=dt), randn(2, n, dtype=dt), randn(3, m, n, dtype=dt)
+    for name, b, r in (("none", None, None), ("gelu", bias, res), ("silu", bias, None), ("relu", None, res)):
+        say("palette", fmt, bits, m, n, k, name)
+        y, z = torch.empty(m, n, dtype=dt, device=DEV), torch.empty(m, n, dtype=dt, device=DEV)
+        edkm.palette_linear(x, packed, lut, y, b, r, name, z)
+        L.assert_within(y, *L.product(x, w, b, r, name)[1:], "y")
+        L.assert_within(z, *L.product(x, w, b, None, "none")[1:], "z")
+
+
+@pytest.mark.parametrize("m", [3, 20, 150, 600])
+def test_palette_views(m):
+    """Unaligned indices; x and y as views of NaN buffers."""
+    n, k, bits, dt = 75, 100, 3, torch.float16
+    say("palette views", m)
+    idx, packed, lut, _ = device_palette(n, k, bits, 5)
+    w = lut.to(dt)[torch.from_numpy(idx).to(DEV).long()].view(n, k)
+    x = randn(1, m, k, dtype=dt)
+    raw = torch.cat([torch.full((3,), 255, dtype=torch.uint8, device=DEV), packed])
+    for lead, gap in ((1, 3), (8, 4)):
+        _, xv = inside(x, lead, gap)
+        ybuf, yv = inside(torch.zeros(m, n, dtype=dt, device=DEV), lead, gap)
+        edkm.palette_linear(xv, raw[3:], lut, yv)
+        L.assert_within(yv, *L.product(x, w, None, None, "none")[1:], "y")
+        assert int(ybuf.isnan().sum()) == ybuf.numel() - m * n
+
+
+def test_non_finite_table_entries():
+    """A NaN or Inf table entry reaches exactly the products that use it."""
+    for m in (2, 40, 600):
+        say("non-finite table", m)
+        n, k = 80, 64
+        idx = np.zeros((n, k), np.uint8)
+        idx[5, 9], idx[7, 63] = 1, 2
+        lut = torch.tensor([0.5, float("nan"), float("inf"), 0.0], device=DEV)
+        packed = torch.from_numpy(pal.pack(idx.ravel(), 2)).to(DEV)
+        y = torch.empty(m, n, dtype=torch.bfloat16, device=DEV)
+        edkm.palette_linear(torch.ones(m, k, dtype=torch.bfloat16, device=DEV), packed, lut, y)
+        assert bool(y[:, 5].isnan().all()) and bool((y[:, 7] == float("inf")).all())
+        keep = [i for i in range(n) if i not in (5, 7)]
+        assert bool((y[:, keep] == 32).all())
+
+
+def test_same_inputs_same_bits():
+    """No atomics: forward and backward repeat bit for bit, on another stream too."""
+    dt = torch.bfloat16
+    x, w, dy = randn(1, 70, 2000, dtype=dt), randn(2, 136, 2000, dtype=dt, scale=0.02), randn(3, 70, 136, dtype=dt)
+    got = []
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for i in range(3):
+        say("repeat", i)
+        with torch.cuda.stream(side if i == 2 else torch.cuda.current_stream()):
+            y, z = torch.empty(70, 136, dtype=dt, device=DEV), torch.empty(70, 136, dtype=dt, device=DEV)
+            edkm.linear(x, w, y, None, None, "silu", z)
+            dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(136, dtype=dt, device=DEV)
+            edkm.linear_backward(dy, x, w, dx, dw, db, z, "silu")
+        torch.cuda.synchronize()
+        got.append((y, z, dx, dw, db))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+def test_autograd_linear():
+    dt = torch.bfloat16
+    x, w = randn(1, 3, 11, 72, dtype=dt), randn(2, 40, 72, dtype=dt, scale=0.1)
+    bias, res, dy = randn(3, 40, dtype=dt), randn(4, 3, 11, 40, dtype=dt), randn(5, 3, 11, 40, dtype=dt)
+    leaves = [t.requires_grad_(True) for t in (x, w, bias, res)]
+    say("autograd linear")
+    y = function.linear(x, w, bias, res, "gelu")
+    assert y.shape == (3, 11, 40)
+    gx, gw, gb, gr = torch.autograd.grad(y, leaves, dy)
+    z64 = L.product(x.detach().view(-1, 72), w.detach(), bias.detach(), None, "none")[0]
+    ref = L.gradients(dy.view(-1, 40), x.detach().view(-1, 72), w.detach(), z64, "gelu")
+    L.assert_within(gx.view(-1, 72), *ref["dx"], "dx")
+    L.assert_within(gw, *ref["dw"], "dw")
+    L.assert_within(gb, *ref["db"], "db")
+    assert torch.equal(gr, dy)
+    # an expanded gradient (of a sum), and only some leaves
+    y = function.linear(x, w.detach(), None, None, "relu")
+    (gx,) = torch.autograd.grad(y.sum(), [x])
+    z64 = L.product(x.detach().view(-1, 72), w.detach(), None, None, "none")[0]
+    ref = L.gradients(torch.ones(33, 40, dtype=dt, device=DEV), x.detach().view(-1, 72), w.detach(), z64, "relu")
+    L.assert_within(gx.view(-1, 72), *ref["dx"], "dx")
+    # transposed x: rows without contiguous elements
+    xt = randn(6, 72, 5, dtype=dt).t().requires_grad_(True)
+    y = function.linear(xt, w)
+    L.assert_within(y.detach(), *L.product(xt.detach(), w.detach(), None, None, "none")[1:], "y")
+
+
+def test_autograd_palette_linear():
+    n, k, bits, dt = 50, 90, 3, torch.float16
+    idx, packed, lut, _ = device_palette(n, k, bits, 8)
+    w = lut.to(dt)[torch.from_numpy(idx).to(DEV).long()].view(n, k)
+    x, bias, dy = randn(1, 20, k, dtype=dt), randn(2, n, dtype=dt), randn(3, 20, n, dtype=dt)
+    say("autograd palette")
+    y = function.palette_linear(x.requires_grad_(True), packed, lut, n, bias.requires_grad_(True), None, "silu")
+    gx, gb = torch.autograd.grad(y, [x, bias], dy)
+    z64 = L.product(x.detach(), w, bias.detach(), None, "none")[0]
+    ref = L.gradients(dy, x.detach(), w, z64, "silu")
+    L.assert_within(gx, *ref["dx"], "dx")
+    L.assert_within(gb, *ref["db"], "db")
+    with pytest.raises(ValueError, match="no gradient"):
+        function.palette_linear(x, packed, lut.clone().requires_grad_(True), n)
+
+
+def test_gradient_against_differences():
+    """dL/dx and dL/dw of a small product against central differences of the 64-bit one."""
+    dt = torch.float16
+    x, w = randn(1, 3, 8, dtype=dt), randn(2, 4, 8, dtype=dt, scale=0.3)
+    dy = randn(3, 3, 4, dtype=dt)
+    say("differences")
+    for name in ("gelu", "silu"):
+        y, z = torch.empty(3, 4, dtype=dt, device=DEV), torch.empty(3, 4, dtype=dt, device=DEV)
+        edkm.linear(x, w, y, None, None, name, z)
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        edkm.linear_backward(dy, x, w, dx, dw, None, z, name)
+        z64 = x.double() @ w.double().t()
+        ref = L.gradients(dy, x, w, z64, name)
+        h = 1e-4                       # the difference's own error is below h^2 times a few
+        for key, got, at in (("dx", dx, 0), ("dw", dw, 1)):
+            base = [x.double(), w.double()]
+            num = torch.empty_like(base[at])
+            for i in range(num.numel()):
+                vals = []
+                for s in (h, -h):
+                    q = [t.clone() for t in base]
+                    q[at].view(-1)[i] += s
+                    vals.append((L.act(q[0] @ q[1].t(), name) * dy.double()).sum())
+                num.view(-1)[i] = (vals[0] - vals[1]) / (2 * h)
+            L.assert_within(got, num, ref[key][1] + 1e-6, key)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 96, 512), (40, 136, 264), (300, 264, 520)])
+def test_captured_and_replayed(m, n, k):
+    """Forward, backward and the palette form in one graph, replayed with new inputs
+    between eager calls."""
+    dt = torch.bfloat16
+    say("graph", m, n, k)
+    x, w, dy = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt, scale=0.05), randn(3, m, n, dtype=dt)
+    _, packed, lut, _ = device_palette(n, k, 3, 4)
+    y, z, yp = (torch.empty(m, n, dtype=dt, device=DEV) for _ in range(3))
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, dtype=dt, device=DEV)
+    fws = torch.empty(max(1, edkm.linear_workspace_bytes(m, n, k)), dtype=torch.uint8, device=DEV)
+    bws = torch.empty(max(1, edkm.linear_backward_workspace_bytes(m, n, k, "silu")), dtype=torch.uint8, device=DEV)
+    pws = torch.empty(max(1, edkm.palette_linear_workspace_bytes(m, n, k, 3)), dtype=torch.uint8, device=DEV)
+
+    def step():
+        edkm.linear(x, w, y, None, None, "silu", z, workspace=fws)
+        edkm.linear_backward(dy, x, w, dx, dw, db, z, "silu", workspace=bws)
+        edkm.palette_linear(x, packed, lut, yp, workspace=pws)
+
+    outs = (y, z, yp, dx, dw, db)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        x.copy_(randn(10 + i, m, k, dtype=dt))
+        for t in outs:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, outs)), i

@@ -1,0 +1,202 @@
+"""Refusals of the layer and optimizer operators that need no GPU: the C ABI rejects bad
+arguments before any HIP call, and the binding rejects tensors that do not fit."""
+import ctypes
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+edkm = pytest.importorskip("paper_2309_00964_amd.edkm",
+                           reason="libedkm.so not built (run __graft_entry__.build())")
+import torch  # noqa: E402
+
+lib = edkm._lib
+P = 1 << 40                # never dereferenced: every call below is refused on the host
+BIG = 1 << 31
+
+
+def linear(m=4, n=8, k=16, fmt=0, act=0, x=P, ldx=16, w=P, ldw=16, bias=None, res=None, ldr=8, y=P, ldy=8, z=None, ws=None,
+           nws=0):
+    return lib.edkm_linear(m, n, k, fmt, act, x, ldx, w, ldw, bias, res, ldr, y, ldy, z, ws, nws, None)
+
+
+@pytest.mark.parametrize("kw", [dict(m=-1), dict(n=0), dict(k=0), dict(m=BIG), dict(n=BIG), dict(k=BIG), dict(fmt=2), dict(fmt=-1),
+                                dict(act=4), dict(act=-1), dict(x=None), dict(w=None), dict(y=None), dict(ldx=15), dict(ldw=15),
+                                dict(ldy=7), dict(res=P, ldr=7), dict(ldx=1 << 41)])
+def test_linear_argument_errors(kw):
+    assert linear(**kw) == edkm.ERR_ARG
+
+
+def backward(m=4, n=8, k=16, fmt=0, act=0, dy=P, lddy=8, z=None, x=P, ldx=16, w=P, ldw=16, dx=P, lddx=16, dw=P, db=P, ws=P,
+             nws=1 << 30):
+    return lib.edkm_linear_backward(m, n, k, fmt, act, dy, lddy, z, x, ldx, w, ldw, dx, lddx, dw, db, ws, nws, None)
+
+
+@pytest.mark.parametrize("kw", [dict(m=-1), dict(n=0), dict(k=0), dict(fmt=2), dict(act=4), dict(dx=None, dw=None, db=None),
+                                dict(dy=None), dict(act=1), dict(x=None), dict(w=None), dict(lddy=7), dict(lddx=15), dict(ldx=15),
+                                dict(ldw=15)])
+def test_linear_backward_argument_errors(kw):
+    assert backward(**kw) == edkm.ERR_ARG
+
+
+def test_workspaces():
+    need = edkm.linear_backward_workspace_bytes(400, 800, 64, "silu")
+    assert need >= 400 * 800 * 2
+    assert edkm.linear_backward_workspace_bytes(400, 0, 64) == 0
+    a = dict(m=400, n=800, k=64, act=3, z=P, lddy=800, ldx=64, ldw=64, lddx=64)
+    assert backward(ws=None, **a) == edkm.ERR_WORKSPACE
+    assert backward(nws=need - 1, **a) == edkm.ERR_WORKSPACE
+    assert backward(ws=P + 16, **a) == edkm.ERR_WORKSPACE
+    for m, n, k in ((1, 64, 4096), (300, 4096, 4096), (5000, 256, 256)):
+        need = edkm.linear_workspace_bytes(m, n, k)
+        assert need % 256 == 0
+        if need:
+            assert linear(m=m, n=n, k=k, ldx=k, ldw=k, ldy=n, ws=P, nws=need - 1) == edkm.ERR_WORKSPACE
+        assert edkm.palette_linear_workspace_bytes(m, n, k, 3) % 256 == 0
+
+
+def palette(m=4, n=8, k=16, bits=3, fmt=0, act=0, x=P, ldx=16, idx=P, lut=P, bias=None, res=None, ldr=8, y=P, ldy=8, z=None,
+            ws=None, nws=0):
+    return lib.edkm_palette_linear(m, n, k, bits, fmt, act, x, ldx, idx, lut, bias, res, ldr, y, ldy, z, ws, nws, None)
+
+
+@pytest.mark.parametrize("kw", [dict(m=-1), dict(n=0), dict(k=0), dict(bits=0), dict(bits=5), dict(fmt=2), dict(act=4), dict(x=None),
+                                dict(idx=None), dict(lut=None), dict(y=None), dict(ldx=15), dict(ldy=7), dict(res=P, ldr=7),
+                                dict(n=1 << 17, k=1 << 15, ldx=1 << 15, ldy=1 << 17)])
+def test_palette_linear_argument_errors(kw):
+    assert palette(**kw) == edkm.ERR_ARG
+
+
+def test_unpalettize_argument_errors():
+    f = lib.edkm_unpalettize
+    assert f(None, 10, 3, 0, P, P, None) == edkm.ERR_ARG
+    assert f(P, 10, 3, 0, None, P, None) == edkm.ERR_ARG
+    assert f(P, 10, 3, 0, P, None, None) == edkm.ERR_ARG
+    assert f(P, 0, 3, 0, P, P, None) == edkm.ERR_ARG
+    assert f(P, 1 << 32, 3, 0, P, P, None) == edkm.ERR_ARG
+    for bits, fmt in ((0, 0), (5, 0), (3, 2)):
+        assert f(P, 10, bits, fmt, P, P, None) == edkm.ERR_ARG
+
+
+def adamw(sizes=(100, 50), pt=0, gt=0, bits=32, p=(P, 2 * P), w=None, g=(P, P), m=(3 * P, 4 * P), v=(5 * P, 6 * P), ms=None, vs=None,
+          step=P, lr_dev=None, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, wd=0.0, count=None):
+    arr = lambda x: None if x is None else (ctypes.c_void_p * len(x))(*x)  # noqa: E731
+    return lib.edkm_adamw_batch(len(sizes) if count is None else count, (ctypes.c_uint64 * len(sizes))(*sizes), pt, gt, bits, arr(p),
+                                arr(w), arr(g), arr(m), arr(v), arr(ms), arr(vs), step, lr_dev, lr, b1, b2, eps, wd, 0, None)
+
+
+NAN = float("nan")
+
+
+@pytest.mark.parametrize("kw", [dict(count=0), dict(sizes=(1 << 32, 5)), dict(pt=3), dict(pt=-1), dict(gt=1), dict(pt=2, gt=0),
+                                dict(bits=16), dict(bits=8), dict(bits=8, ms=(P, P)), dict(pt=2, gt=2, w=(P, P)), dict(step=None),
+                                dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(p=(P, None)), dict(m=(None, P)),
+                                dict(bits=8, ms=(P, None), vs=(P, P)), dict(lr=NAN), dict(lr=-1.0), dict(b1=1.0), dict(b1=NAN),
+                                dict(b2=-0.1), dict(eps=NAN), dict(eps=-1.0), dict(wd=-1.0), dict(wd=NAN), dict(lr=float("inf")),
+                                dict(p=(P, P)), dict(p=(P, P + 198)), dict(m=(3 * P, 3 * P + 396)), dict(v=(5 * P + 4, 5 * P))])
+def test_adamw_argument_errors(kw):
+    assert adamw(**kw) == edkm.ERR_ARG
+
+
+def test_constants_match_the_header():
+    text = open(os.path.join(ROOT, "include", "edkm.h")).read()
+    acts = {k.lower(): int(v) for k, v in re.findall(r"\bEDKM_ACT_([A-Z]+)\s*=\s*(\d+)", text)}
+    assert acts == edkm.ACTIVATIONS
+    types = {k: int(v) for k, v in re.findall(r"\bEDKM_TYPE_([A-Z0-9]+)\s*=\s*(\d+)", text)}
+    assert types == {k: getattr(edkm, "TYPE_" + k) for k in ("FP16", "BF16", "FP32")}
+    assert int(re.search(r"#define EDKM_STATE_BLOCK (\d+)", text).group(1)) == edkm.STATE_BLOCK
+
+
+class Fake:
+    """Shape, type and device of a GPU tensor, for the checks that come before any call."""
+
+    def __init__(self, *shape, dtype=torch.float16, stride=None, device="cuda:0"):
+        self.t = torch.empty(shape, dtype=dtype, device="meta")
+        if stride:
+            self.t = self.t.as_strided(shape, stride)
+        self.shape, self.dtype, self.device, self.is_cuda = self.t.shape, dtype, torch.device(device), True
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def data_ptr(self):
+        return P
+
+    def get_device(self):
+        return self.device.index
+
+
+def test_binding_refuses_matrices_that_do_not_fit():
+    h = Fake
+    x, w, y = h(4, 16), h(8, 16), h(4, 8)
+    cases = [
+        (lambda: edkm.linear(h(4, 16, dtype=torch.float32), w, y), "x must be"),
+        (lambda: edkm.linear(x, h(8, 15), y), "w must be 8 x 16"),
+        (lambda: edkm.linear(x, w, h(4, 9)), "y must be 4 x 8"),
+        (lambda: edkm.linear(x, w, h(4, 8, dtype=torch.bfloat16)), "y must have the type"),
+        (lambda: edkm.linear(x, w, h(4, 8, device="cuda:1")), "y must have the type and device"),
+        (lambda: edkm.linear(h(4, 16, stride=(1, 4)), w, y), "x must have contiguous rows"),
+        (lambda: edkm.linear(h(4, 16, stride=(0, 1)), w, y), "x must have contiguous rows"),
+        (lambda: edkm.linear(x, w, y, h(7)), "bias must hold 8"),
+        (lambda: edkm.linear(x, w, y, None, h(4, 7)), "residual must be"),
+        (lambda: edkm.linear(x, w, y, None, None, "tanh"), "activation"),
+        (lambda: edkm.linear(x, w, y, z_out=h(4, 9)), "z_out"),
+        (lambda: edkm.linear_backward(y, None, w, dw=h(8, 16)), "dw needs x"),
+        (lambda: edkm.linear_backward(y, x, None, dx=h(4, 16)), "dx needs w"),
+        (lambda: edkm.linear_backward(y, x, w, dx=h(4, 16), activation="silu"), "needs z"),
+        (lambda: edkm.linear_backward(y, x, w, dw=h(8, 15)), "dw must hold"),
+        (lambda: edkm.palette_linear(x, h(47, dtype=torch.uint8), h(8, dtype=torch.float32), y), "indices must be 48"),
+        (lambda: edkm.palette_linear(x, h(48, dtype=torch.uint8), h(8), y), "lut must hold"),
+        (lambda: edkm.palette_linear(x, h(48, dtype=torch.uint8), h(32, dtype=torch.float32), y), "lut must hold"),
+        (lambda: edkm.unpalettize(h(48, dtype=torch.uint8, device="cuda:1"), h(8, dtype=torch.float32), h(128)), "must be on cuda:0"),
+        (lambda: edkm.unpalettize(h(48, dtype=torch.uint8), h(8, dtype=torch.float32), h(129)), "indices must be 49"),
+    ]
+    for call, what in cases:
+        with pytest.raises(ValueError, match=what):
+            call()
+
+
+def test_binding_refuses_optimizer_lists_that_do_not_fit():
+    h, f32 = Fake, torch.float32
+    p, g = [h(300), h(5)], [h(300), h(5)]
+    m, v, step = [h(300, dtype=f32), h(5, dtype=f32)], [h(300, dtype=f32), h(5, dtype=f32)], h(1, dtype=torch.int32)
+    p[1].data_ptr = lambda: 2 * P
+    e8 = [h(300, dtype=torch.float8_e4m3fn), h(5, dtype=torch.float8_e4m3fn)]
+    e5 = [h(300, dtype=torch.float8_e5m2), h(5, dtype=torch.float8_e5m2)]
+    s2, s1 = [h(2, dtype=f32), h(1, dtype=f32)], [h(1, dtype=f32), h(1, dtype=f32)]
+    cases = [
+        (lambda: edkm.adamw_batch(p, g[:1], m, v, step, 1e-3), "grads has 1 entries"),
+        (lambda: edkm.adamw_batch(p, [h(300), h(4)], m, v, step, 1e-3), "grads"),
+        (lambda: edkm.adamw_batch(p, [h(300, dtype=torch.bfloat16)] * 2, m, v, step, 1e-3), "grads"),
+        (lambda: edkm.adamw_batch([p[0], p[0]], g, m, v, step, 1e-3), "twice"),
+        (lambda: edkm.adamw_batch(p, g, e8, v, step, 1e-3), "exp_avgs"),
+        (lambda: edkm.adamw_batch(p, g, e8, e5, step, 1e-3, m_scales=s2), "m_scales and v_scales"),
+        (lambda: edkm.adamw_batch(p, g, e8, e5, step, 1e-3, m_scales=s1, v_scales=s2), "m_scales"),
+        (lambda: edkm.adamw_batch(p, g, e8, e8, step, 1e-3, m_scales=s2, v_scales=s2), "exp_avg_sqs"),
+        (lambda: edkm.adamw_batch(p, g, m, v, h(1, dtype=torch.int64), 1e-3), "step"),
+        (lambda: edkm.adamw_batch(p, g, m, v, step, torch.zeros(1, dtype=torch.float64)), "lr"),
+        (lambda: edkm.adamw_batch(m, g, m, v, step, 1e-3), "grads"),
+        (lambda: edkm.adamw_batch(m, m, m, v, step, 1e-3, masters=m), "take no masters"),
+        (lambda: edkm.adamw_batch([h(4, 4, stride=(1, 4))], [h(16)], [h(16, dtype=f32)], [h(16, dtype=f32)], step, 1e-3), "contiguous"),
+    ]
+    for call, what in cases:
+        with pytest.raises((ValueError, edkm.EdkmError), match=what):
+            call()
+
+
+def test_function_refusals():
+    from paper_2309_00964_amd import function
+    x, w = torch.zeros(2, 3, 16, dtype=torch.float16), torch.zeros(8, 16, dtype=torch.float16)
+    lut = torch.zeros(8)
+    for call, what in [
+        (lambda: function.linear(x, w), "device tensor"),
+        (lambda: function.linear(x, w[:, :15]), "w must be n x k"),
+        (lambda: function.linear(x, w, torch.zeros(7)), "bias must hold 8"),
+        (lambda: function.linear(x, w, None, torch.zeros(2, 4, 8)), "residual must have"),
+        (lambda: function.palette_linear(x, torch.zeros(48, dtype=torch.uint8), lut, 8), "device tensor"),
+        (lambda: function.palette_linear(x, torch.zeros(48, dtype=torch.uint8), lut, 8, torch.zeros(9)), "bias must hold 8"),
+        (lambda: function.palette_linear(x, torch.zeros(48, dtype=torch.uint8), lut.requires_grad_(True), 8), "no gradient"),
+    ]:
+        with pytest.raises(ValueError, match=what):
+            call()

@@ -111,7 +111,11 @@ def test_constants_match_the_header():
 class Fake:
     """Shape, type and device of a GPU tensor, for the checks that come before any call."""
 
+    made = 0
+
     def __init__(self, *shape, dtype=torch.float16, stride=None, device="cuda:0"):
+        Fake.made += 1
+        self.at = Fake.made * P
         self.t = torch.empty(shape, dtype=dtype, device="meta")
         if stride:
             self.t = self.t.as_strided(shape, stride)
@@ -121,7 +125,7 @@ class Fake:
         return getattr(self.t, name)
 
     def data_ptr(self):
-        return P
+        return self.at
 
     def get_device(self):
         return self.device.index
@@ -161,7 +165,6 @@ def test_binding_refuses_optimizer_lists_that_do_not_fit():
     h, f32 = Fake, torch.float32
     p, g = [h(300), h(5)], [h(300), h(5)]
     m, v, step = [h(300, dtype=f32), h(5, dtype=f32)], [h(300, dtype=f32), h(5, dtype=f32)], h(1, dtype=torch.int32)
-    p[1].data_ptr = lambda: 2 * P
     e8 = [h(300, dtype=torch.float8_e4m3fn), h(5, dtype=torch.float8_e4m3fn)]
     e5 = [h(300, dtype=torch.float8_e5m2), h(5, dtype=torch.float8_e5m2)]
     s2, s1 = [h(2, dtype=f32), h(1, dtype=f32)], [h(1, dtype=f32), h(1, dtype=f32)]

@@ -330,7 +330,8 @@ edkm_status edkm_unique_inverse_batch(int count, edkm_plan* const* plans,
  * (elements between two rows, at least the row's length; ignored for a single
  * row); 16-bit tensors of one call share one format (EDKM_KEYS_FP16 or
  * EDKM_KEYS_BF16); sums are fp32 and each output is rounded once, to nearest
- * even.  Sizes are 1 .. 2^31 - 1025, and m may be 0.  A workspace, where a
+ * even.  Sizes are 1 .. 2^31 - 1025, a matrix holds at most 2^40 elements, and
+ * m may be 0.  A workspace, where a
  * call names one, holds at least the bytes of its size function (256-byte
  * aligned; may be NULL if that is 0), carries nothing from one call to the
  * next and must not be used by two calls at once.  Outputs must not overlap

@@ -34,7 +34,19 @@ struct ProductArgs {
     int64_t ldo;
     uint16_t* z;
     int act;
+    // a split product: steps of 64 depths per part, and the parts' sums (null: not split)
+    int split_steps;
+    float* part;
 };
+
+// How a product is carried out.
+struct ProductPlan {
+    int tile;               // 256 or 128 outputs square
+    int splits, split_steps;
+    bool direct;            // operands can go to LDS by 16-byte pieces of memory
+};
+ProductPlan product_plan(const ProductArgs& p, int opa, int opb);
+size_t product_part_bytes(int64_t rows, int64_t cols, int64_t depth);
 
 // The gradient at the activation: dz = dy act'(z) (16 bits, only with an activation)
 // and the bias gradient, summed over the rows of each chunk and then over the chunks.
@@ -78,7 +90,7 @@ struct AdamwArgs {
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "launch arguments fit the kernel-argument limit");
 
-hipError_t launch_product(const ProductArgs& a, int fmt, int opa, int opb, hipStream_t s);
+hipError_t launch_product(const ProductArgs& a, int fmt, int opa, int opb, float* part, hipStream_t s);
 hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s);
 hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
                               uint16_t* out, hipStream_t s);

@@ -19,29 +19,37 @@ static_assert(EDKM_STATE_BLOCK == ADAMW_BLOCK, "8-bit state blocks");
 
 constexpr int64_t DIM_MAX = 0x7FFFFFFF - 1024;   // sizes are 32-bit in the kernels, tile ends included
 
+constexpr int64_t MATRIX_MAX = (int64_t)1 << 40;     // elements of a matrix: its tiles are numbered in 32 bits
+
 bool size_ok(int64_t v, int64_t least) { return v >= least && v <= DIM_MAX; }
 
 bool product_ok(int64_t m, int64_t n, int64_t k, int format, int act) {
-    return size_ok(m, 0) && size_ok(n, 1) && size_ok(k, 1) && (format == EDKM_KEYS_FP16 || format == EDKM_KEYS_BF16) &&
+    return size_ok(m, 0) && size_ok(n, 1) && size_ok(k, 1) && std::max(m, k) <= MATRIX_MAX / n && m <= MATRIX_MAX / k && (format == EDKM_KEYS_FP16 || format == EDKM_KEYS_BF16) &&
            act >= 0 && act < ACT_COUNT;
 }
 
-// leading dimension of a matrix with `rows` rows of `cols`: any for a single row
-bool ld_ok(int64_t ld, int64_t rows, int64_t cols) { return (ld >= cols && ld < (int64_t)1 << 40) || rows <= 1; }
+// Leading dimension of a matrix with `rows` rows of `cols`: any for a single row, which
+// then gets one that the kernels can work with.
+bool ld_ok(int64_t& ld, int64_t rows, int64_t cols) {
+    if (rows <= 1) ld = (cols + 7) & ~(int64_t)7;
+    return ld >= cols && ld < (int64_t)1 << 40;
+}
 
 size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 int dz_chunks(int64_t m) { return (int)((m + DZ_ROWS - 1) / DZ_ROWS); }
 
-// Workspace of a backward: dz, then the bias gradient's partial sums.
+// Workspace of a backward: dz, the bias gradient's partial sums, and those of the two
+// products in turn.
 struct BackwardWs {
-    size_t dz, part, total;
+    size_t dz, part, split, total;
 };
-BackwardWs backward_ws(int64_t m, int64_t n, int act) {
+BackwardWs backward_ws(int64_t m, int64_t n, int64_t k, int act) {
     BackwardWs w;
     w.dz = 0;
     w.part = act == ACT_NONE ? 0 : up256((size_t)m * n * 2);
-    w.total = w.part + up256((size_t)dz_chunks(m) * n * 4);
+    w.split = w.part + up256((size_t)dz_chunks(m) * n * 4);
+    w.total = w.split + up256(std::max(m ? product_part_bytes(m, k, n) : 0, product_part_bytes(n, k, m)));
     return w;
 }
 
@@ -55,8 +63,8 @@ edkm_status ws_ok(const void* ws, size_t have, size_t need) {
 extern "C" {
 
 size_t edkm_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) {
-    (void)m; (void)n; (void)k;
-    return 0;
+    if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m == 0) return 0;
+    return up256(product_part_bytes(m, n, k));
 }
 
 edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activation, const void* x, int64_t ldx,
@@ -83,12 +91,12 @@ edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activat
     p.ldo = ldy;
     p.z = static_cast<uint16_t*>(z);
     p.act = activation;
-    return launch_product(p, format, OP_ROWS, OP_ROWS, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    return launch_product(p, format, OP_ROWS, OP_ROWS, static_cast<float*>(ws), stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
 }
 
 size_t edkm_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int activation) {
     if (!product_ok(m, n, k, EDKM_KEYS_FP16, activation)) return 0;
-    return backward_ws(m, n, activation).total;
+    return backward_ws(m, n, k, activation).total;
 }
 
 edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, int activation, const void* dy,
@@ -99,7 +107,7 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
     if (m > 0 && (!dy || (activation != ACT_NONE && !z) || (dw && !x))) return EDKM_ERR_ARG;
     if (dx && (!w || !ld_ok(ldw, n, k) || !ld_ok(lddx, m, k))) return EDKM_ERR_ARG;
     if ((dw && !ld_ok(ldx, m, k)) || !ld_ok(lddy, m, n)) return EDKM_ERR_ARG;
-    const BackwardWs L = backward_ws(m, n, activation);
+    const BackwardWs L = backward_ws(m, n, k, activation);
     const edkm_status st = ws_ok(ws, ws_bytes, L.total);
     if (st != EDKM_OK) return st;
     char* base = static_cast<char*>(ws);
@@ -114,6 +122,7 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
     d.cols = (int32_t)n;
     d.act = activation;
     if (launch_dz(d, format, stream) != hipSuccess) return EDKM_ERR_HIP;
+    float* parts = reinterpret_cast<float*>(base + L.split);
     const uint16_t* dz = activation == ACT_NONE ? d.dy : d.dz;
     const int64_t lddz = activation == ACT_NONE ? lddy : n;
     if (dx && m > 0) {
@@ -127,7 +136,7 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
         p.depth = (int32_t)n;
         p.out = static_cast<uint16_t*>(dx);
         p.ldo = lddx;
-        if (launch_product(p, format, OP_ROWS, OP_DEPTH, stream) != hipSuccess) return EDKM_ERR_HIP;
+        if (launch_product(p, format, OP_ROWS, OP_DEPTH, parts, stream) != hipSuccess) return EDKM_ERR_HIP;
     }
     if (dw) {
         ProductArgs p{};
@@ -140,7 +149,7 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
         p.depth = (int32_t)m;
         p.out = static_cast<uint16_t*>(dw);
         p.ldo = k;
-        if (launch_product(p, format, OP_DEPTH, OP_DEPTH, stream) != hipSuccess) return EDKM_ERR_HIP;
+        if (launch_product(p, format, OP_DEPTH, OP_DEPTH, parts, stream) != hipSuccess) return EDKM_ERR_HIP;
     }
     return EDKM_OK;
 }
@@ -179,7 +188,7 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
     p.ldo = ldy;
     p.z = static_cast<uint16_t*>(z);
     p.act = activation;
-    return launch_product(p, format, OP_ROWS, OP_PALETTE, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    return launch_product(p, format, OP_ROWS, OP_PALETTE, nullptr, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
 }
 
 edkm_status edkm_unpalettize(const uint8_t* indices, uint64_t n, int bits, int format, const float* lut, uint16_t* w_out,

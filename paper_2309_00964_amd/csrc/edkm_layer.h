@@ -39,6 +39,8 @@ struct ProductArgs {
     float* part;
 };
 
+constexpr int FEW = 64;         // tokens of k_few at most
+
 // How a product is carried out.
 struct ProductPlan {
     int tile;               // 256 or 128 outputs square

@@ -63,7 +63,7 @@ edkm_status ws_ok(const void* ws, size_t have, size_t need) {
 extern "C" {
 
 size_t edkm_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) {
-    if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m == 0) return 0;
+    if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m <= FEW) return 0;
     return up256(product_part_bytes(m, n, k));
 }
 
@@ -155,8 +155,9 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
 }
 
 size_t edkm_palette_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int bits) {
-    (void)m; (void)n; (void)k; (void)bits;
-    return 0;
+    if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m <= FEW || bits < 1 || bits > EDKM_MAX_BITS) return 0;
+    // the decoded weights (rows of whole 16-byte pieces need no padding: n x k without gaps), then the split's sums
+    return up256((size_t)n * k * 2) + up256(product_part_bytes(m, n, k));
 }
 
 edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int format, int activation, const void* x,
@@ -188,7 +189,13 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
     p.ldo = ldy;
     p.z = static_cast<uint16_t*>(z);
     p.act = activation;
-    return launch_product(p, format, OP_ROWS, OP_PALETTE, nullptr, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    if (m <= FEW) return launch_product(p, format, OP_ROWS, OP_PALETTE, nullptr, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    uint16_t* w = static_cast<uint16_t*>(ws);
+    if (launch_unpalettize(indices, p.idx_bytes, (uint64_t)n * k, bits, format, lut, w, stream) != hipSuccess) return EDKM_ERR_HIP;
+    p.b = w;
+    p.ldb = k;
+    float* parts = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)n * k * 2));
+    return launch_product(p, format, OP_ROWS, OP_ROWS, parts, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
 }
 
 edkm_status edkm_unpalettize(const uint8_t* indices, uint64_t n, int bits, int format, const float* lut, uint16_t* w_out,

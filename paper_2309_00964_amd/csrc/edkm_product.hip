@@ -93,88 +93,110 @@ __device__ __forceinline__ uint32_t load_idx8(const uint8_t* idx, uint64_t nbyte
     return (uint32_t)(v >> (o & 7));
 }
 
+// Table lookups in registers: the low and the high bytes of up to sixteen 16-bit values in
+// four registers each; v_perm_b32 picks four bytes of two registers at once.
 template <int F>
-__global__ void __launch_bounds__(256) k_unpalettize(const uint8_t* idx, uint64_t nbytes, uint64_t n, int bits,
-                                                     const float* lut, uint16_t* out) {
-    __shared__ uint16_t tab[KMAX];
-    if (threadIdx.x < (1u << bits)) tab[threadIdx.x] = to_16<F>(lut[threadIdx.x]);
-    __syncthreads();
-    const uint64_t i = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (i >= n) return;
-    const uint32_t w = load_idx8(idx, nbytes, i, bits);
-    for (int j = 0; j < 8; ++j)
-        if (i + j < n) out[i + j] = tab[(w >> (j * bits)) & ((1u << bits) - 1)];
-}
+struct Decoder {
+    uint32_t lo[4], hi[4];
 
-// ----------------------------------------------------------------------------
-// products
-
-constexpr int TM = 64, TN = 64, TK = 32, TPAD = 8;
-
-// Eight consecutive depths of one row; zeros past the ends.
-template <int F, int OP>
-__device__ __forceinline__ s16x8 load8(const ProductArgs& p, const uint16_t* m, int64_t ld, int row, int nrow, int d,
-                                       const uint16_t* tab) {
-    s16x8 v = {};
-    if (row >= nrow || d >= p.depth) return v;
-    const int left = p.depth - d;
-    if (OP == OP_ROWS) {
-        const uint16_t* s = m + (int64_t)row * ld + d;
-        for (int j = 0; j < 8; ++j)
-            if (j < left) v[j] = (short)s[j];
-    } else if (OP == OP_DEPTH) {
-        const uint16_t* s = m + (int64_t)d * ld + row;
-        for (int j = 0; j < 8; ++j)
-            if (j < left) v[j] = (short)s[(int64_t)j * ld];
-    } else {
-        const uint32_t w = load_idx8(p.idx, p.idx_bytes, (uint64_t)row * (uint64_t)p.depth + d, p.bits);
-        for (int j = 0; j < 8; ++j)
-            if (j < left) v[j] = (short)tab[(w >> (j * p.bits)) & ((1u << p.bits) - 1)];
+    __device__ __forceinline__ void init(const float* lut, int bits) {
+        const int k = 1 << bits;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lo[i] = hi[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i * 4 + j < k) {
+                    const uint32_t h = to_16<F>(lut[i * 4 + j]);
+                    lo[i] |= (h & 255) << (8 * j);
+                    hi[i] |= (h >> 8) << (8 * j);
+                }
+        }
     }
+    // four values for the four indices in sel's bytes: two registers of two
+    __device__ __forceinline__ void four(uint32_t sel, bool wide, uint32_t& v01, uint32_t& v23) const {
+        uint32_t l, h;
+        if (wide) {       // sixteen entries: both halves, then the one that bit 3 names
+            const uint32_t s = sel & 0x07070707u, up = sel & 0x08080808u, mask = (up << 5) - (up >> 3);
+            const uint32_t l0 = __builtin_amdgcn_perm(lo[1], lo[0], s), l1 = __builtin_amdgcn_perm(lo[3], lo[2], s);
+            const uint32_t h0 = __builtin_amdgcn_perm(hi[1], hi[0], s), h1 = __builtin_amdgcn_perm(hi[3], hi[2], s);
+            l = (l1 & mask) | (l0 & ~mask);
+            h = (h1 & mask) | (h0 & ~mask);
+        } else {
+            l = __builtin_amdgcn_perm(lo[1], lo[0], sel);
+            h = __builtin_amdgcn_perm(hi[1], hi[0], sel);
+        }
+        v01 = __builtin_amdgcn_perm(h, l, 0x05010400u);
+        v23 = __builtin_amdgcn_perm(h, l, 0x07030602u);
+    }
+    // the values of eight packed indices
+    __device__ __forceinline__ s16x8 eight(uint32_t w, int bits) const {
+        typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+        uint32_t s0, s1;
+        if (bits == 4) {
+            s0 = spread(w & 0xFFFFu, 4);
+            s1 = spread(w >> 16, 4);
+        } else {
+            s0 = spread(w & ((1u << (4 * bits)) - 1), bits);
+            s1 = spread((w >> (4 * bits)) & ((1u << (4 * bits)) - 1), bits);
+        }
+        u32x4 v;
+        uint32_t a, b;
+        four(s0, bits == 4, a, b);
+        v[0] = a;
+        v[1] = b;
+        four(s1, bits == 4, a, b);
+        v[2] = a;
+        v[3] = b;
+        return __builtin_bit_cast(s16x8, v);
+    }
+    // 4 b bits into the low bits of four bytes
+    __device__ __forceinline__ static uint32_t spread(uint32_t x, int b) {
+        x = (x | (x << (16 - 2 * b))) & (((1u << (2 * b)) - 1) * 0x10001u);
+        return (x | (x << (8 - b))) & (((1u << b) - 1) * 0x01010101u);
+    }
+};
+
+// eight consecutive values, `left` of them there (zeros after them)
+__device__ __forceinline__ s16x8 row8(const uint16_t* q, int left) {
+    if (left >= 8) return reinterpret_cast<const S16x8*>(q)->v;
+    s16x8 v = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < left) v[j] = (short)q[j];
     return v;
 }
 
-template <int F, int OPA, int OPB>
-__global__ void __launch_bounds__(256) k_product(ProductArgs p) {
-    __shared__ __attribute__((aligned(16))) uint16_t la[TM][TK + TPAD], lb[TN][TK + TPAD];
-    __shared__ uint16_t tab[KMAX];
-    if (OPB == OP_PALETTE && threadIdx.x < (1u << p.bits)) tab[threadIdx.x] = to_16<F>(p.lut[threadIdx.x]);
-    __syncthreads();
-    const int r0 = blockIdx.y * TM, c0 = blockIdx.x * TN;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wr = (wave >> 1) * 32, wc = (wave & 1) * 32;
-    const int srow = OPA == OP_ROWS ? threadIdx.x >> 2 : threadIdx.x & 63;
-    const int sd = (OPA == OP_ROWS ? threadIdx.x & 3 : threadIdx.x >> 6) * 8;
-    const int trow = OPB != OP_DEPTH ? threadIdx.x >> 2 : threadIdx.x & 63;
-    const int td = (OPB != OP_DEPTH ? threadIdx.x & 3 : threadIdx.x >> 6) * 8;
-    f32x4 acc[2][2] = {};
-    for (int d0 = 0; d0 < p.depth; d0 += TK) {
-        const s16x8 va = load8<F, OPA>(p, p.a, p.lda, r0 + srow, p.rows, d0 + sd, tab);
-        const s16x8 vb = load8<F, OPB>(p, p.b, p.ldb, c0 + trow, p.cols, d0 + td, tab);
-        __syncthreads();
-        *reinterpret_cast<s16x8*>(&la[srow][sd]) = va;
-        *reinterpret_cast<s16x8*>(&lb[trow][td]) = vb;
-        __syncthreads();
-        const int l = lane & 15, g = (lane >> 4) * 8;
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2; ++j)
-                acc[i][j] = mfma16<F>(*reinterpret_cast<s16x8*>(&lb[wc + 16 * j + l][g]),
-                                      *reinterpret_cast<s16x8*>(&la[wr + 16 * i + l][g]), acc[i][j]);
-    }
-    for (int i = 0; i < 2; ++i) {
-        const int r = r0 + wr + 16 * i + (lane & 15);
-        if (r >= p.rows) continue;
-        for (int j = 0; j < 2; ++j)
-            for (int q = 0; q < 4; ++q) {
-                const int c = c0 + wc + 16 * j + (lane >> 4) * 4 + q;
-                if (c >= p.cols) continue;
-                float z = acc[i][j][q];
-                if (p.bias) z += to_f32<F>(p.bias[c]);
-                if (p.z) p.z[(int64_t)r * p.cols + c] = keep_z<F>(z);
-                float y = act_value(z, p.act);
-                if (p.res) y += to_f32<F>(p.res[(int64_t)r * p.ldr + c]);
-                p.out[(int64_t)r * p.ldo + c] = to_16<F>(y);
-            }
+// the first `n` of eight values, zeros after them
+__device__ __forceinline__ s16x8 keep_first(s16x8 v, int n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j >= n) v[j] = 0;
+    return v;
+}
+
+// Thirty-two weights per thread: 4 b bytes of indices, 64 bytes out, bound by the bytes
+// written.  Unaligned or ragged ends take eight indices at a time, any alignment.
+template <int F, int BITS>
+__global__ void __launch_bounds__(256) k_unpalettize(const uint8_t* idx, uint64_t nbytes, uint64_t n, const float* lut,
+                                                     uint16_t* out, int aligned) {
+    Decoder<F> dec;
+    dec.init(lut, BITS);
+    // a wave's 2048 weights; its j-th store covers 512 consecutive ones, eight per lane
+    const uint64_t base = ((uint64_t)blockIdx.x * 256 + (threadIdx.x & ~63)) * 32;
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint64_t i = base + j * 512 + lane * 8;
+        if (i >= n) return;
+        const s16x8 v = dec.eight(load_idx8(idx, nbytes, i, BITS), BITS);
+        if (aligned && i + 8 <= n) {
+            *reinterpret_cast<s16x8*>(out + i) = v;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (i + q < n) out[i + q] = (uint16_t)v[q];
+        }
     }
 }
 
@@ -521,6 +543,151 @@ __global__ void __launch_bounds__(64) k_join(ProductArgs p, int splits) {
     epi_rows<F, PLAIN>(p, lds, lane, 1, r, c);
 }
 
+// ----------------------------------------------------------------------------
+// products of few tokens
+
+// Table of pairs: entry e holds the values of indices e mod 2^b and e / 2^b, once per LDS
+// bank, so that the lanes of a wave look up without conflicts.
+constexpr int PAIR_BANKS = 32;
+
+// A lane's weights of a run: 32 depths of each of its NT rows, as 16-bit values (BITS 0) or
+// as packed indices.  WHOLE: 32 depths are 4 BITS bytes on a 4-byte boundary (16-bit
+// values: on a 16-byte one), all there or none; else any alignment and end.
+template <int F, int BITS, bool WHOLE>
+struct FewWeights {
+    uint32_t raw[BITS ? 4 : 1];
+    s16x8 w[BITS ? 1 : 4];
+
+    __device__ __forceinline__ void load(const ProductArgs& p, int row, int d) {
+        const int left = p.depth - d;
+        if constexpr (BITS == 0) {
+            const uint16_t* at = p.b + (int64_t)row * p.ldb + d;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (WHOLE) w[j] = left > 0 ? *reinterpret_cast<const s16x8*>(at + j * 8) : s16x8{};
+                else w[j] = row8(at + j * 8, left - j * 8);
+            }
+        } else if constexpr (WHOLE) {
+            const uint32_t* at = reinterpret_cast<const uint32_t*>(p.idx) + ((uint64_t)row * (uint32_t)p.depth + d) / 32 * BITS;
+#pragma unroll
+            for (int j = 0; j < BITS; ++j) raw[j] = left > 0 ? at[j] : 0;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                raw[j] = left > j * 8 ? load_idx8(p.idx, p.idx_bytes, (uint64_t)row * (uint32_t)p.depth + d + j * 8, BITS) : 0;
+        }
+    }
+    // the values of depths 8 j .. 8 j + 7
+    __device__ __forceinline__ s16x8 eight(const uint32_t* mine, int j, int left) const {
+        if constexpr (BITS == 0) {
+            return w[j];
+        } else {
+            typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+            uint32_t v;
+            if (WHOLE) {
+                constexpr int BPJ = 8 * BITS;                 // bits of eight indices
+                const int at = j * BPJ, q = at / 32, sh = at % 32;
+                v = sh + BPJ > 32 ? __builtin_amdgcn_alignbit(raw[q + 1 < 4 ? q + 1 : 3], raw[q], sh) : raw[q] >> sh;
+            } else {
+                v = raw[j];
+            }
+            u32x4 r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = mine[__builtin_amdgcn_ubfe(v, 2 * BITS * i, 2 * BITS) * PAIR_BANKS];
+            const s16x8 e = __builtin_bit_cast(s16x8, r);
+            return WHOLE || left >= 8 ? e : keep_first(e, left);
+        }
+    }
+};
+
+// Up to 16 MT tokens against 16 NT weight rows per workgroup.  The waves share the depths by
+// runs of 128 and add their sums through LDS.  The MFMA takes the weights as its rows: lane
+// l holds row l mod 16, depths 32 (l / 16) + 8 j + 0 .. 7 of a run at its j-th step, so its
+// share of a palette's run is 4 b consecutive bytes.  Bound by the weights' bytes: every
+// wave's loads are its own and independent, and sixteen waves hold them in flight.
+template <int F, int BITS, bool WHOLE, int MT, int NT>
+__global__ void __launch_bounds__(1024) k_few(ProductArgs p) {
+    constexpr int ENTRIES = 1 << (2 * BITS);
+    constexpr int TABLE = BITS ? ENTRIES * PAIR_BANKS : 0, SUMS = 16 * MT * NT * 256;
+    // the table, and after the last lookup the waves' sums
+    __shared__ __attribute__((aligned(16))) uint32_t lds[TABLE > SUMS ? TABLE : SUMS];
+    __shared__ uint16_t tab[KMAX];
+    uint32_t* pairs = lds;
+    float* red = reinterpret_cast<float*>(lds);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
+    const int l = lane & 15, g = lane >> 4;
+    const int c0 = blockIdx.x * 16 * NT;
+    const int runs = (p.depth + 127) / 128;
+    FewWeights<F, BITS, WHOLE> now[NT], next[NT];
+    int row[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        row[n] = min(c0 + n * 16 + l, p.cols - 1);
+        now[n].load(p, row[n], wave * 128 + g * 32);
+    }
+    if (BITS) {
+        if (threadIdx.x < (1 << BITS)) tab[threadIdx.x] = to_16<F>(p.lut[threadIdx.x]);
+        __syncthreads();
+        for (int i = threadIdx.x; i < ENTRIES * PAIR_BANKS; i += blockDim.x) {
+            const int e = i / PAIR_BANKS;
+            pairs[i] = (uint32_t)tab[e & ((1 << BITS) - 1)] | ((uint32_t)tab[e >> BITS] << 16);
+        }
+        __syncthreads();
+    }
+    const uint32_t* mine = pairs + (lane & (PAIR_BANKS - 1));
+    f32x4 acc[MT][NT] = {};
+    for (int t = wave; t < runs; t += nw) {
+        const int d = t * 128 + g * 32, left = p.depth - d;
+        if (BITS)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) next[n].load(p, row[n], d + nw * 128);
+        s16x8 x[MT][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const uint16_t* at = p.a + (int64_t)min(i * 16 + l, p.rows - 1) * p.lda + d;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (WHOLE) x[i][j] = left > 0 ? *reinterpret_cast<const s16x8*>(at + j * 8) : s16x8{};
+                else x[i][j] = row8(at + j * 8, left - j * 8);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s16x8 w = now[n].eight(mine, j, left - j * 8);
+                if (BITS && WHOLE && t * 128 + 128 > p.depth && left <= 0) w = s16x8{};
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc[i][n] = mfma16<F>(w, x[i][j], acc[i][n]);
+            }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (BITS) now[n] = next[n];
+            else now[n].load(p, row[n], d + nw * 128);
+        }
+    }
+    if (BITS) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            *reinterpret_cast<f32x4*>(red + (((wave * MT + i) * NT + n) * 64 + lane) * 4) = acc[i][n];
+    __syncthreads();
+    for (int e = threadIdx.x; e < MT * NT * 256; e += blockDim.x) {
+        const int n = e % (16 * NT), r = e / (16 * NT), i = r >> 4;
+        const int at = ((i * NT + (n >> 4)) * 64 + ((n & 15) >> 2) * 16 + (r & 15)) * 4 + (n & 3);
+        float z = 0.f;
+        for (int w = 0; w < nw; ++w) z += red[w * MT * NT * 256 + at];
+        const int col = c0 + n;
+        if (r >= p.rows || col >= p.cols) continue;
+        if (p.bias) z += to_f32<F>(p.bias[col]);
+        if (p.z) p.z[(int64_t)r * p.cols + col] = keep_z<F>(z);
+        float y = act_value(z, p.act);
+        if (p.res) y += to_f32<F>(p.res[(int64_t)r * p.ldr + col]);
+        p.out[(int64_t)r * p.ldo + col] = to_16<F>(y);
+    }
+}
+
 template <int F>
 __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
     __shared__ float red[4][DZ_COLS];
@@ -578,13 +745,39 @@ static hipError_t product_ab(const ProductArgs& p, const ProductPlan& q, hipStre
     return q.direct ? tiled<F, OPA, OPB, 128, 2, 2, true>(p, q, s) : tiled<F, OPA, OPB, 128, 2, 2, false>(p, q, s);
 }
 
+template <int F, int BITS, bool WHOLE, int MT, int NT>
+static hipError_t few_go(const ProductArgs& p, hipStream_t s) {
+    const int runs = (p.depth + 127) / 128;
+    int nw = 1;
+    while (nw < runs && nw < 16) nw *= 2;
+    EDKM_GO((k_few<F, BITS, WHOLE, MT, NT>), dim3((uint32_t)(((int64_t)p.cols + 16 * NT - 1) / (16 * NT))), dim3(nw * 64), p);
+    return hipSuccess;
+}
+
+template <int F, int BITS, bool WHOLE>
+static hipError_t few_bits(const ProductArgs& p, hipStream_t s) {
+    const bool wide = p.cols >= 32 * 256;
+    if (p.rows <= 16) return wide && p.rows > 4 ? few_go<F, BITS, WHOLE, 1, 2>(p, s) : few_go<F, BITS, WHOLE, 1, 1>(p, s);
+    if (p.rows <= 32) return wide ? few_go<F, BITS, WHOLE, 2, 2>(p, s) : few_go<F, BITS, WHOLE, 2, 1>(p, s);
+    return wide ? few_go<F, BITS, WHOLE, 4, 2>(p, s) : few_go<F, BITS, WHOLE, 4, 1>(p, s);
+}
+
+template <int F>
+static hipError_t few(const ProductArgs& p, int bits, hipStream_t s) {
+    const bool x16 = ((uintptr_t)p.a & 15) == 0 && p.lda % 8 == 0 && p.depth % 32 == 0;
+    const bool whole = x16 && (bits ? ((uintptr_t)p.idx & 3) == 0 : ((uintptr_t)p.b & 15) == 0 && p.ldb % 8 == 0);
+    switch (bits) {
+    case 1: return whole ? few_bits<F, 1, true>(p, s) : few_bits<F, 1, false>(p, s);
+    case 2: return whole ? few_bits<F, 2, true>(p, s) : few_bits<F, 2, false>(p, s);
+    case 3: return whole ? few_bits<F, 3, true>(p, s) : few_bits<F, 3, false>(p, s);
+    case 4: return whole ? few_bits<F, 4, true>(p, s) : few_bits<F, 4, false>(p, s);
+    default: return whole ? few_bits<F, 0, true>(p, s) : few_bits<F, 0, false>(p, s);
+    }
+}
+
 template <int F>
 static hipError_t product_f(ProductArgs p, int opa, int opb, float* part, hipStream_t s) {
-    if (opb == OP_PALETTE) {
-        const dim3 grid((p.cols + TN - 1) / TN, (p.rows + TM - 1) / TM);
-        EDKM_GO((k_product<F, OP_ROWS, OP_PALETTE>), grid, dim3(256), p);
-        return hipSuccess;
-    }
+    if (opa == OP_ROWS && opb != OP_DEPTH && p.rows <= FEW) return few<F>(p, opb == OP_PALETTE ? p.bits : 0, s);
     const ProductPlan q = product_plan(p, opa, opb);
     p.split_steps = q.split_steps;
     p.part = q.splits > 1 ? part : nullptr;
@@ -640,12 +833,22 @@ hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s) {
     return fmt == FMT_BF16 ? dz_f<FMT_BF16>(a, s) : dz_f<FMT_FP16>(a, s);
 }
 
+template <int F>
+static hipError_t unpalettize_f(const uint8_t* idx, uint64_t nb, uint64_t n, int bits, const float* lut, uint16_t* out,
+                                hipStream_t s) {
+    const dim3 grid((uint32_t)((n + 8191) / 8192));
+    const int al = ((uintptr_t)out & 15) == 0;
+    if (bits == 1) EDKM_GO((k_unpalettize<F, 1>), grid, dim3(256), idx, nb, n, lut, out, al);
+    else if (bits == 2) EDKM_GO((k_unpalettize<F, 2>), grid, dim3(256), idx, nb, n, lut, out, al);
+    else if (bits == 3) EDKM_GO((k_unpalettize<F, 3>), grid, dim3(256), idx, nb, n, lut, out, al);
+    else EDKM_GO((k_unpalettize<F, 4>), grid, dim3(256), idx, nb, n, lut, out, al);
+    return hipSuccess;
+}
+
 hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
                               uint16_t* out, hipStream_t s) {
-    const dim3 grid((uint32_t)((n + 2047) / 2048));
-    if (fmt == FMT_BF16) EDKM_GO(k_unpalettize<FMT_BF16>, grid, dim3(256), idx, idx_bytes, n, bits, lut, out);
-    else EDKM_GO(k_unpalettize<FMT_FP16>, grid, dim3(256), idx, idx_bytes, n, bits, lut, out);
-    return hipSuccess;
+    return fmt == FMT_BF16 ? unpalettize_f<FMT_BF16>(idx, idx_bytes, n, bits, lut, out, s)
+                           : unpalettize_f<FMT_FP16>(idx, idx_bytes, n, bits, lut, out, s);
 }
 
 }  // namespace edkm

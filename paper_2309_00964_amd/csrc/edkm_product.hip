@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(64) k_join(ProductArgs p, int splits) {
 // ----------------------------------------------------------------------------
 // products of few tokens
 
-// Table of pairs: entry e holds the values of indices e mod 2^b and e / 2^b, once per LDS
+// Table of pairs (4-bit palettes): entry e holds the values of indices e mod 2^b and e / 2^b, once per LDS
 // bank, so that the lanes of a wave look up without conflicts.
 constexpr int PAIR_BANKS = 32;
 
@@ -577,8 +577,9 @@ struct FewWeights {
                 raw[j] = left > j * 8 ? load_idx8(p.idx, p.idx_bytes, (uint64_t)row * (uint32_t)p.depth + d + j * 8, BITS) : 0;
         }
     }
-    // the values of depths 8 j .. 8 j + 7
-    __device__ __forceinline__ s16x8 eight(const uint32_t* mine, int j, int left) const {
+    // the values of depths 8 j .. 8 j + 7: up to eight entries by lookups in registers,
+    // sixteen from the table of pairs
+    __device__ __forceinline__ s16x8 eight(const Decoder<F>& dec, const uint32_t* mine, int j, int left) const {
         if constexpr (BITS == 0) {
             return w[j];
         } else {
@@ -591,10 +592,15 @@ struct FewWeights {
             } else {
                 v = raw[j];
             }
-            u32x4 r;
+            s16x8 e;
+            if constexpr (BITS < 4) {
+                e = dec.eight(v, BITS);
+            } else {
+                u32x4 r;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = mine[__builtin_amdgcn_ubfe(v, 2 * BITS * i, 2 * BITS) * PAIR_BANKS];
-            const s16x8 e = __builtin_bit_cast(s16x8, r);
+                for (int i = 0; i < 4; ++i) r[i] = mine[__builtin_amdgcn_ubfe(v, 2 * BITS * i, 2 * BITS) * PAIR_BANKS];
+                e = __builtin_bit_cast(s16x8, r);
+            }
             return WHOLE || left >= 8 ? e : keep_first(e, left);
         }
     }
@@ -603,12 +609,13 @@ struct FewWeights {
 // Up to 16 MT tokens against 16 NT weight rows per workgroup.  The waves share the depths by
 // runs of 128 and add their sums through LDS.  The MFMA takes the weights as its rows: lane
 // l holds row l mod 16, depths 32 (l / 16) + 8 j + 0 .. 7 of a run at its j-th step, so its
-// share of a palette's run is 4 b consecutive bytes.  Bound by the weights' bytes: every
-// wave's loads are its own and independent, and sixteen waves hold them in flight.
-template <int F, int BITS, bool WHOLE, int MT, int NT>
+// share of a palette's run is 4 b consecutive bytes.  Bound by the weights' bytes and by the
+// latency of one round: a wave asks for its weights of U runs, and for U more ahead, before
+// it waits for anything, the table included.
+template <int F, int BITS, bool WHOLE, int MT, int NT, int U>
 __global__ void __launch_bounds__(1024) k_few(ProductArgs p) {
     constexpr int ENTRIES = 1 << (2 * BITS);
-    constexpr int TABLE = BITS ? ENTRIES * PAIR_BANKS : 0, SUMS = 16 * MT * NT * 256;
+    constexpr int TABLE = BITS == 4 ? ENTRIES * PAIR_BANKS : 0, SUMS = 16 * MT * NT * 256;
     // the table, and after the last lookup the waves' sums
     __shared__ __attribute__((aligned(16))) uint32_t lds[TABLE > SUMS ? TABLE : SUMS];
     __shared__ uint16_t tab[KMAX];
@@ -618,14 +625,42 @@ __global__ void __launch_bounds__(1024) k_few(ProductArgs p) {
     const int l = lane & 15, g = lane >> 4;
     const int c0 = blockIdx.x * 16 * NT;
     const int runs = (p.depth + 127) / 128;
-    FewWeights<F, BITS, WHOLE> now[NT], next[NT];
+    FewWeights<F, BITS, WHOLE> now[U][NT], next[BITS ? U : 1][BITS ? NT : 1];
+    s16x8 x[U][MT][4];
     int row[NT];
+    auto load_x = [&](int t0) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        row[n] = min(c0 + n * 16 + l, p.cols - 1);
-        now[n].load(p, row[n], wave * 128 + g * 32);
-    }
-    if (BITS) {
+        for (int u = 0; u < U; ++u) {
+            const int d = (t0 + u * nw) * 128 + g * 32, left = p.depth - d;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                // lanes without a token load nothing: what a load costs here is its lanes, not its bytes
+                const int r = i * 16 + l;
+                const uint16_t* at = p.a + (int64_t)r * p.lda + d;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[u][i][j] = s16x8{};
+                if (r < p.rows && left > 0)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (WHOLE) x[u][i][j] = *reinterpret_cast<const s16x8*>(at + j * 8);
+                        else x[u][i][j] = row8(at + j * 8, left - j * 8);
+                    }
+            }
+        }
+    };
+#pragma unroll
+    for (int n = 0; n < NT; ++n) row[n] = min(c0 + n * 16 + l, p.cols - 1);
+    auto load_w = [&](auto& to, int t0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) to[u][n].load(p, row[n], (t0 + u * nw) * 128 + g * 32);
+    };
+    load_w(now, wave);
+    load_x(wave);
+    Decoder<F> dec;
+    if constexpr (BITS == 1 || BITS == 2 || BITS == 3) dec.init(p.lut, BITS);
+    if constexpr (BITS == 4) {
         if (threadIdx.x < (1 << BITS)) tab[threadIdx.x] = to_16<F>(p.lut[threadIdx.x]);
         __syncthreads();
         for (int i = threadIdx.x; i < ENTRIES * PAIR_BANKS; i += blockDim.x) {
@@ -636,50 +671,47 @@ __global__ void __launch_bounds__(1024) k_few(ProductArgs p) {
     }
     const uint32_t* mine = pairs + (lane & (PAIR_BANKS - 1));
     f32x4 acc[MT][NT] = {};
-    for (int t = wave; t < runs; t += nw) {
-        const int d = t * 128 + g * 32, left = p.depth - d;
-        if (BITS)
+    for (int t = wave; t < runs; t += nw * U) {
+        if constexpr (BITS != 0) load_w(next, t + nw * U);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) next[n].load(p, row[n], d + nw * 128);
-        s16x8 x[MT][4];
+        for (int u = 0; u < U; ++u) {
+            const int left = p.depth - ((t + u * nw) * 128 + g * 32);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const uint16_t* at = p.a + (int64_t)min(i * 16 + l, p.rows - 1) * p.lda + d;
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (WHOLE) x[i][j] = left > 0 ? *reinterpret_cast<const s16x8*>(at + j * 8) : s16x8{};
-                else x[i][j] = row8(at + j * 8, left - j * 8);
-            }
+                for (int n = 0; n < NT; ++n) {
+                    s16x8 w = now[u][n].eight(dec, mine, j, left - j * 8);
+                    if (BITS && WHOLE && left <= 0) w = s16x8{};
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) acc[i][n] = mfma16<F>(w, x[u][i][j], acc[i][n]);
+                }
         }
+        if (t + nw * U < runs) {
+            load_x(t + nw * U);
+            if constexpr (BITS != 0) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                s16x8 w = now[n].eight(mine, j, left - j * 8);
-                if (BITS && WHOLE && t * 128 + 128 > p.depth && left <= 0) w = s16x8{};
-#pragma unroll
-                for (int i = 0; i < MT; ++i) acc[i][n] = mfma16<F>(w, x[i][j], acc[i][n]);
+                    for (int n = 0; n < NT; ++n) now[u][n] = next[u][n];
+            } else {
+                load_w(now, t + nw * U);
             }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (BITS) now[n] = next[n];
-            else now[n].load(p, row[n], d + nw * 128);
         }
     }
-    if (BITS) __syncthreads();
+    if (BITS == 4) __syncthreads();
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
             *reinterpret_cast<f32x4*>(red + (((wave * MT + i) * NT + n) * 64 + lane) * 4) = acc[i][n];
     __syncthreads();
-    for (int e = threadIdx.x; e < MT * NT * 256; e += blockDim.x) {
+    for (int e = threadIdx.x; e < min(p.rows, 16 * MT) * NT * 16; e += blockDim.x) {
         const int n = e % (16 * NT), r = e / (16 * NT), i = r >> 4;
         const int at = ((i * NT + (n >> 4)) * 64 + ((n & 15) >> 2) * 16 + (r & 15)) * 4 + (n & 3);
         float z = 0.f;
         for (int w = 0; w < nw; ++w) z += red[w * MT * NT * 256 + at];
         const int col = c0 + n;
-        if (r >= p.rows || col >= p.cols) continue;
+        if (col >= p.cols) continue;
         if (p.bias) z += to_f32<F>(p.bias[col]);
         if (p.z) p.z[(int64_t)r * p.cols + col] = keep_z<F>(z);
         float y = act_value(z, p.act);
@@ -747,19 +779,28 @@ static hipError_t product_ab(const ProductArgs& p, const ProductPlan& q, hipStre
 
 template <int F, int BITS, bool WHOLE, int MT, int NT>
 static hipError_t few_go(const ProductArgs& p, hipStream_t s) {
+    constexpr int U = WHOLE && BITS && MT == 1 ? 2 : 1;
     const int runs = (p.depth + 127) / 128;
     int nw = 1;
     while (nw < runs && nw < 16) nw *= 2;
-    EDKM_GO((k_few<F, BITS, WHOLE, MT, NT>), dim3((uint32_t)(((int64_t)p.cols + 16 * NT - 1) / (16 * NT))), dim3(nw * 64), p);
+    EDKM_GO((k_few<F, BITS, WHOLE, MT, NT, U>), dim3((uint32_t)(((int64_t)p.cols + 16 * NT - 1) / (16 * NT))), dim3(nw * 64), p);
     return hipSuccess;
 }
 
 template <int F, int BITS, bool WHOLE>
 static hipError_t few_bits(const ProductArgs& p, hipStream_t s) {
-    const bool wide = p.cols >= 32 * 256;
-    if (p.rows <= 16) return wide && p.rows > 4 ? few_go<F, BITS, WHOLE, 1, 2>(p, s) : few_go<F, BITS, WHOLE, 1, 1>(p, s);
+    const int64_t tiles = ((int64_t)p.cols + 15) / 16;
+    if (!WHOLE) {
+        if (p.rows <= 16) return few_go<F, BITS, WHOLE, 1, 1>(p, s);
+        return p.rows <= 32 ? few_go<F, BITS, WHOLE, 2, 1>(p, s) : few_go<F, BITS, WHOLE, 4, 1>(p, s);
+    }
+    if (p.rows <= 16) {
+        if (tiles <= 256) return few_go<F, BITS, WHOLE, 1, 1>(p, s);
+        return tiles <= 512 || !BITS ? few_go<F, BITS, WHOLE, 1, 2>(p, s) : few_go<F, BITS, WHOLE, 1, 3>(p, s);
+    }
+    const bool wide = tiles >= 512;
     if (p.rows <= 32) return wide ? few_go<F, BITS, WHOLE, 2, 2>(p, s) : few_go<F, BITS, WHOLE, 2, 1>(p, s);
-    return wide ? few_go<F, BITS, WHOLE, 4, 2>(p, s) : few_go<F, BITS, WHOLE, 4, 1>(p, s);
+    return few_go<F, BITS, WHOLE, 4, 1>(p, s);
 }
 
 template <int F>

@@ -13,18 +13,87 @@ namespace edkm {
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
 template <int PT>
-__device__ __forceinline__ float ld_val(const void* p, uint64_t i) {
-    if (PT == PT_FP32) return static_cast<const float*>(p)[i];
-    const uint16_t h = static_cast<const uint16_t*>(p)[i];
-    if (PT == PT_BF16) return __uint_as_float((uint32_t)h << 16);
-    return (float)__builtin_bit_cast(_Float16, h);
+__device__ __forceinline__ float value_of(uint32_t h) {
+    if (PT == PT_BF16) return __uint_as_float(h << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)h);
 }
 template <int PT>
-__device__ __forceinline__ void st_val(void* p, uint64_t i, float x) {
-    if (PT == PT_FP32) static_cast<float*>(p)[i] = x;
-    else if (PT == PT_BF16) static_cast<__bf16*>(p)[i] = (__bf16)x;
-    else static_cast<_Float16*>(p)[i] = (_Float16)x;
+__device__ __forceinline__ uint16_t bits_of(float x) {
+    if (PT == PT_BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
+    return __builtin_bit_cast(uint16_t, (_Float16)x);
+}
+
+// Eight elements from i on; `vec`: all there, on a boundary of their size.  Elements past n
+// are zeros, and not written.
+template <int PT>
+__device__ __forceinline__ void load8(const void* p, uint64_t i, uint64_t n, bool vec, float (&x)[8]) {
+    if (vec) {
+        if (PT == PT_FP32) {
+            const f32x4 a = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i));
+            const f32x4 b = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i) + 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = a[j];
+                x[j + 4] = b[j];
+            }
+        } else {
+            const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + i));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = value_of<PT>(j & 1 ? a[j / 2] >> 16 : a[j / 2] & 0xFFFFu);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = 0.f;
+            if (i + j < n) x[j] = PT == PT_FP32 ? static_cast<const float*>(p)[i + j] : value_of<PT>(static_cast<const uint16_t*>(p)[i + j]);
+        }
+    }
+}
+template <int PT>
+__device__ __forceinline__ void store8(void* p, uint64_t i, uint64_t n, bool vec, const float (&x)[8]) {
+    if (vec) {
+        if (PT == PT_FP32) {
+            f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + i);
+            __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, q);
+            __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, q + 1);
+        } else {
+            u32x4 a;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[j] = bits_of<PT>(x[2 * j]) | ((uint32_t)bits_of<PT>(x[2 * j + 1]) << 16);
+            __builtin_nontemporal_store(a, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p) + i));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i + j < n) {
+                if (PT == PT_FP32) static_cast<float*>(p)[i + j] = x[j];
+                else static_cast<uint16_t*>(p)[i + j] = bits_of<PT>(x[j]);
+            }
+    }
+}
+__device__ __forceinline__ u32x2 load_codes(const void* p, uint64_t i, uint64_t n, bool vec) {
+    const uint8_t* q = static_cast<const uint8_t*>(p) + i;
+    if (vec) return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(q));
+    u32x2 c = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i + j < n) c[j / 4] |= (uint32_t)q[j] << (8 * (j & 3));
+    return c;
+}
+__device__ __forceinline__ void store_codes(void* p, uint64_t i, uint64_t n, bool vec, u32x2 c) {
+    uint8_t* q = static_cast<uint8_t*>(p) + i;
+    if (vec) {
+        __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(q));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i + j < n) q[j] = (uint8_t)(c[j / 4] >> (8 * (j & 3)));
 }
 
 // A 32-bit hash (MurmurHash3's finaliser, A. Appleby): the rounding noise of a pair
@@ -36,9 +105,6 @@ __device__ __forceinline__ uint32_t hash32(uint32_t h) {
     h *= 0xC2B2AE35u;
     return h ^ (h >> 16);
 }
-
-__device__ __forceinline__ float from_e4m3(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
-__device__ __forceinline__ float from_e5m2(uint8_t c) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(c << 8)); }
 
 // float8 code of y in 0..TOP: the leading bits of the fp32 number, or for a float8
 // subnormal those of the number plus the smallest normal one (whose last place is the
@@ -70,70 +136,107 @@ __device__ __forceinline__ int adamw_tensor(const AdamwArgs& a) {
     return k;
 }
 
+// the largest of 32 lanes (a half wave), in all of them
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+__device__ __forceinline__ uint32_t half_max(uint32_t x) {
+    x = max(x, dpp<0x121>(x));   // rotations by 1, 2, 4, 8 within rows of sixteen
+    x = max(x, dpp<0x122>(x));
+    x = max(x, dpp<0x124>(x));
+    x = max(x, dpp<0x128>(x));
+    return max(x, (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401F));   // lane ^ 16
+}
+
+// Square root and reciprocal by the hardware's estimates (an ulp each): they reach p only,
+// whose update they move by less than its own rounding.
+__device__ __forceinline__ float root(float x) {
+    const bool low = x < 0x1p-96f;    // the estimate takes no subnormals
+    return __builtin_amdgcn_sqrtf(low ? x * 0x1p64f : x) * (low ? 0x1p-32f : 1.f);
+}
+
+// Eight elements per thread and pass, 32 lanes for the 256 elements of a scale.  Bound by
+// the bytes moved (10.06 B per bf16 element with 8-bit states, 22 with fp32 ones); the
+// arithmetic of the 8-bit form, about 60 slots per element, comes close to that.
 template <int PT, int GT, bool S8>
 __global__ void __launch_bounds__(256) k_adamw(AdamwArgs a) {
 #pragma clang fp contract(off)
-    // no fused multiply-adds: the 8-bit codes are a function of separately rounded operations
+    // no fused multiply-adds: m, v and their codes are a function of separately rounded operations
     const int k = adamw_tensor(a);
     const AdamwTensor T = a.t[k];
     const uint32_t t = (uint32_t)*a.step + 1u;
-    const float c1 = (float)(1.0 - power(a.beta1, t)), c2 = (float)(1.0 - power(a.beta2, t));
+    const float i1 = (float)(1.0 / (1.0 - power(a.beta1, t))), i2 = (float)(1.0 / (1.0 - power(a.beta2, t)));
     const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
-    const float flr = (float)lr, decay = (float)(lr * a.decay), eps = (float)a.eps;
+    const float step1 = (float)lr * i1, decay = (float)(lr * a.decay), eps = (float)a.eps;
     const float b1 = (float)a.beta1, b2 = (float)a.beta2, d1 = (float)(1.0 - a.beta1), d2 = (float)(1.0 - a.beta2);
-    const uint64_t lo = (uint64_t)(blockIdx.x - a.wg_begin[k]) * ADAMW_CHUNK;
-    __shared__ uint32_t top[2][4];
-    for (uint64_t i = lo + threadIdx.x; i < lo + ADAMW_CHUNK; i += 256) {
-        const bool in = i < T.n;
-        float m = 0.f, v = 0.f;
-        if (in) {
-            const float g = ld_val<GT>(T.g, i);
-            if (S8) {
-                m = from_e4m3(static_cast<const uint8_t*>(T.m)[i]) * T.m_scale[i / ADAMW_BLOCK];
-                v = from_e5m2(static_cast<const uint8_t*>(T.v)[i]) * T.v_scale[i / ADAMW_BLOCK];
-            } else {
-                m = static_cast<const float*>(T.m)[i];
-                v = static_cast<const float*>(T.v)[i];
-            }
-            m = m * b1 + g * d1;
-            v = v * b2 + g * g * d2;
-            float p = T.master ? T.master[i] : ld_val<PT>(T.p, i);
-            p = p - p * decay - flr * (m / c1) / (sqrtf(v / c2) + eps);
-            if (T.master) T.master[i] = p;
-            st_val<PT>(T.p, i, p);
-            if (!S8) {
-                static_cast<float*>(T.m)[i] = m;
-                static_cast<float*>(T.v)[i] = v;
-            }
-        }
+    const uint64_t lo = (uint64_t)(blockIdx.x - a.wg_begin[k]) * a.chunk, hi = min(lo + a.chunk, T.n);
+    const uint32_t key = t * 0x9E3779B9u + a.seed;
+    // whole blocks of 256 elements, so that all lanes of a block's 32 take part in its maximum
+    const uint64_t end = S8 ? (hi + ADAMW_BLOCK - 1) & ~(uint64_t)(ADAMW_BLOCK - 1) : hi;
+    for (uint64_t i = lo + threadIdx.x * 8; i < end; i += 2048) {
+        const bool vec = a.aligned && i + 8 <= T.n;
+        float g[8], p[8], m[8], v[8];
+        load8<GT>(T.g, i, T.n, vec, g);
+        if (T.master) load8<PT_FP32>(T.master, i, T.n, vec, p);
+        else load8<PT>(T.p, i, T.n, vec, p);
         if (S8) {
+            const u32x2 cm = load_codes(T.m, i, T.n, vec), cv = load_codes(T.v, i, T.n, vec);
+            const float sm = T.m_scale[i / ADAMW_BLOCK], sv = T.v_scale[i / ADAMW_BLOCK];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x2 m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)cm[h], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)cm[h], true);
+                const f32x2 v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)cv[h], false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)cv[h], true);
+                m[4 * h] = m0[0] * sm, m[4 * h + 1] = m0[1] * sm, m[4 * h + 2] = m1[0] * sm, m[4 * h + 3] = m1[1] * sm;
+                v[4 * h] = v0[0] * sv, v[4 * h + 1] = v0[1] * sv, v[4 * h + 2] = v1[0] * sv, v[4 * h + 3] = v1[1] * sv;
+            }
+        } else {
+            load8<PT_FP32>(T.m, i, T.n, vec, m);
+            load8<PT_FP32>(T.v, i, T.n, vec, v);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            m[j] = m[j] * b1 + g[j] * d1;
+            v[j] = v[j] * b2 + g[j] * g[j] * d2;
+            p[j] = p[j] - p[j] * decay - step1 * (m[j] * __builtin_amdgcn_rcpf(root(v[j] * i2) + eps));
+        }
+        if (T.master) store8<PT_FP32>(T.master, i, T.n, vec, p);
+        store8<PT>(T.p, i, T.n, vec, p);
+        if (!S8) {
+            store8<PT_FP32>(T.m, i, T.n, vec, m);
+            store8<PT_FP32>(T.v, i, T.n, vec, v);
+        } else {
             // the block's largest magnitudes, as bit patterns: Inf and NaN are above all
-            uint32_t am = __float_as_uint(m) & 0x7FFFFFFFu, av = __float_as_uint(v) & 0x7FFFFFFFu;
-            for (int o = 32; o; o >>= 1) {
-                am = max(am, (uint32_t)__shfl_xor((int)am, o));
-                av = max(av, (uint32_t)__shfl_xor((int)av, o));
+            uint32_t am = 0, av = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (!vec && i + j >= T.n) m[j] = v[j] = 0.f;
+                am = max(am, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+                av = max(av, __float_as_uint(v[j]) & 0x7FFFFFFFu);
             }
-            __syncthreads();
-            if ((threadIdx.x & 63) == 0) {
-                top[0][threadIdx.x >> 6] = am;
-                top[1][threadIdx.x >> 6] = av;
-            }
-            __syncthreads();
-            am = max(max(top[0][0], top[0][1]), max(top[0][2], top[0][3]));
-            av = max(max(top[1][0], top[1][1]), max(top[1][2], top[1][3]));
+            am = half_max(am);
+            av = half_max(av);
             const float fm = __uint_as_float(am), fv = __uint_as_float(av);
-            const uint32_t h = hash32((uint32_t)(i >> 1) + t * 0x9E3779B9u + a.seed);
-            const uint32_t noise = (i & 1) ? h >> 16 : h & 0xFFFFu;
-            const float ym = fminf(fabsf(m) * (fm >= SCALE_LIVE ? (1.0f / fm) * E4M3_TOP : 0.f), E4M3_TOP);
-            const float yv = fminf(fabsf(v) * (fv >= SCALE_LIVE ? (1.0f / fv) * E5M2_TOP : 0.f), E5M2_TOP);
-            uint32_t cm = to_float8<3, 7>(ym, noise), cv = to_float8<2, 15>(yv, noise);
-            if (cv == 0 && yv > 0.f) cv = 1;
-            if (m < 0.f && cm) cm |= 0x80u;
-            if (in) {
-                static_cast<uint8_t*>(T.m)[i] = (uint8_t)cm;
-                static_cast<uint8_t*>(T.v)[i] = (uint8_t)cv;
+            const float im = fm >= SCALE_LIVE ? (1.0f / fm) * E4M3_TOP : 0.f, iv = fv >= SCALE_LIVE ? (1.0f / fv) * E5M2_TOP : 0.f;
+            u32x2 cm = {0, 0}, cv = {0, 0};
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const uint32_t h = hash32((uint32_t)((i + j) >> 1) + key);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const uint32_t noise = q ? h >> 16 : h & 0xFFFFu;
+                    const float x = m[j + q], y = v[j + q];
+                    const float yv = fminf(y * iv, E5M2_TOP);
+                    uint32_t em = to_float8<3, 7>(fminf(fabsf(x) * im, E4M3_TOP), noise), ev = to_float8<2, 15>(yv, noise);
+                    ev = max(ev, yv > 0.f ? 1u : 0u);
+                    em |= em ? (__float_as_uint(x) >> 24) & 0x80u : 0u;
+                    cm[(j + q) / 4] |= em << (8 * ((j + q) & 3));
+                    cv[(j + q) / 4] |= ev << (8 * ((j + q) & 3));
+                }
             }
-            if (in && threadIdx.x == 0) {
+            store_codes(T.m, i, T.n, vec, cm);
+            store_codes(T.v, i, T.n, vec, cv);
+            if ((threadIdx.x & 31) == 0 && i < T.n) {
                 // a block with an Inf or NaN decodes to NaN throughout
                 T.m_scale[i / ADAMW_BLOCK] = am >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : fm >= SCALE_LIVE ? fm * (1.0f / E4M3_TOP) : 0.f;
                 T.v_scale[i / ADAMW_BLOCK] = av >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : fv >= SCALE_LIVE ? fv * (1.0f / E5M2_TOP) : 0.f;

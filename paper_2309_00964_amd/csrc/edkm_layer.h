@@ -79,7 +79,10 @@ struct AdamwTensor {
 };
 
 constexpr int ADAMW_BLOCK = 256;       // elements of one 8-bit state's scale
-constexpr int ADAMW_CHUNK = 4096;      // elements of one workgroup
+// Elements of one workgroup: few where the tensors are small, so that all CUs take part,
+// more where there are workgroups enough, so that fewer of them pay the start.
+constexpr int ADAMW_CHUNK = 2048, ADAMW_CHUNK_MANY = 16384;
+constexpr uint64_t ADAMW_MANY = 1ull << 26;
 
 struct AdamwArgs {
     int count;
@@ -87,6 +90,8 @@ struct AdamwArgs {
     int32_t* step;                     // steps done before this one
     const float* lr_dev;               // the rate on the device, or null: lr
     double lr, beta1, beta2, eps, decay;
+    uint32_t chunk;                    // elements of one workgroup
+    int aligned;                       // all arrays can be read and written eight elements at a time
     uint32_t wg_begin[MAXB];           // first workgroup of each tensor; 0xFFFFFFFF past them
     AdamwTensor t[MAXB];
 };

@@ -235,6 +235,11 @@ edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int g
         return clash(params[i], n[i] * pe, params[j], n[j] * pe) || clash(exp_avg[i], n[i] * se, exp_avg[j], n[j] * se) ||
                clash(exp_avg_sq[i], n[i] * se, exp_avg_sq[j], n[j] * se);
     };
+    // by the average launch of the call
+    uint64_t total = 0;
+    for (int i = 0; i < count; ++i) total += n[i];
+    const uint32_t chunk = total / ((count + MAXB - 1) / MAXB) >= ADAMW_MANY ? ADAMW_CHUNK_MANY : ADAMW_CHUNK;
+    auto on = [](const void* p, size_t b) { return ((uintptr_t)p & (b - 1)) == 0; };
     AdamwArgs a;
     // all groups are checked before the first launch
     for (int pass = 0; pass < 2; ++pass) {
@@ -248,11 +253,13 @@ edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int g
             a.beta2 = beta2;
             a.eps = eps;
             a.decay = weight_decay;
+            a.chunk = chunk;
+            a.aligned = 1;
             uint64_t grid = 0;
             int src[MAXB];
             for (; i < count && a.count < MAXB; ++i) {
                 if (n[i] == 0) continue;
-                const uint64_t wgs = (n[i] + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+                const uint64_t wgs = (n[i] + chunk - 1) / chunk;
                 AdamwTensor& T = a.t[a.count];
                 T.p = params[i];
                 T.master = masters ? masters[i] : nullptr;
@@ -262,6 +269,9 @@ edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int g
                 T.m_scale = state_bits == 8 ? m_scales[i] : nullptr;
                 T.v_scale = state_bits == 8 ? v_scales[i] : nullptr;
                 T.n = n[i];
+                // eight elements: 16 bytes of a 16-bit array (fp32 ones are read in two pieces of 16), 8 of a code array
+                a.aligned = a.aligned && on(T.p, 16) && on(T.master, 16) && on(T.g, 16) && on(T.m, state_bits == 8 ? 8 : 16) &&
+                            on(T.v, state_bits == 8 ? 8 : 16);
                 a.wg_begin[a.count] = (uint32_t)grid;
                 src[a.count++] = i;
                 grid += wgs;

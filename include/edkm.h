@@ -392,7 +392,8 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
 /* One AdamW step over `count` tensors, one launch per EDKM_LAUNCH_GROUP of them:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, t = *step + 1; *step becomes t.
+ * in fp32, t = *step + 1; *step becomes t.  (v / (1 - beta2^t) counts as 2^-126 at
+ * least under the root.)
  *   n          host array: elements of each tensor, 0 .. EDKM_MAX_N (0: skipped)
  *   param_type EDKM_TYPE_*; grad_type the same, or EDKM_TYPE_FP32
  *   params     host array of device pointers: p, updated (to nearest even in 16 bits)
@@ -405,8 +406,9 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
  *              device pointers, ceil(n / EDKM_STATE_BLOCK) floats each; not
  *              read with 32).  A block's largest magnitude is stored as 448 or
  *              57344 times the scale.  A value between two float8 numbers goes
- *              up or down by a 16-bit noise (a hash of element pair, t and
- *              seed), so that increments below half a step are kept on average;
+ *              to the larger one if its share of the way there and a noise of
+ *              (u + 1/2) / 2^16 reach 1, u being 16 bits of a hash of element
+ *              pair, t and seed: increments below half a step are kept on average;
  *              a v above 0 is stored above 0.  Blocks whose largest magnitude
  *              is below 2^-100 are stored as zeros.  A block with an Inf or NaN
  *              gets a NaN scale.

@@ -106,20 +106,7 @@ __device__ __forceinline__ uint32_t hash32(uint32_t h) {
     return h ^ (h >> 16);
 }
 
-// float8 code of y in 0..TOP: the leading bits of the fp32 number, or for a float8
-// subnormal those of the number plus the smallest normal one (whose last place is the
-// subnormals' step), after adding a noise below the last place.
-template <int MAN, int BIAS>
-__device__ __forceinline__ uint32_t to_float8(float y, uint32_t noise16) {
-    constexpr int DROP = 23 - MAN;
-    const float lowest = __uint_as_float((uint32_t)(128 - BIAS) << 23);   // 2^(1 - BIAS)
-    const bool small = y < lowest;
-    const uint32_t at = __float_as_uint(small ? y + lowest : y);
-    const uint32_t up = (at + (noise16 << (DROP - 16)) + (1u << (DROP - 17))) >> DROP;
-    return up - ((uint32_t)(small ? 128 - BIAS : 127 - BIAS) << MAN);
-}
-
-constexpr float E4M3_TOP = 448.f, E5M2_TOP = 57344.f;
+constexpr float E4M3_TOP = 448.f, E5M2_TOP = 57344.f, E5M2_LEAST = 0x1p-16f;
 constexpr float SCALE_LIVE = 0x1p-100f;   // blocks below it are stored as zeros
 
 // beta^t, t >= 0
@@ -147,13 +134,6 @@ __device__ __forceinline__ uint32_t half_max(uint32_t x) {
     x = max(x, dpp<0x124>(x));
     x = max(x, dpp<0x128>(x));
     return max(x, (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401F));   // lane ^ 16
-}
-
-// Square root and reciprocal by the hardware's estimates (an ulp each): they reach p only,
-// whose update they move by less than its own rounding.
-__device__ __forceinline__ float root(float x) {
-    const bool low = x < 0x1p-96f;    // the estimate takes no subnormals
-    return __builtin_amdgcn_sqrtf(low ? x * 0x1p64f : x) * (low ? 0x1p-32f : 1.f);
 }
 
 // Eight elements per thread and pass, 32 lanes for the 256 elements of a scale.  Bound by
@@ -198,7 +178,11 @@ __global__ void __launch_bounds__(256) k_adamw(AdamwArgs a) {
         for (int j = 0; j < 8; ++j) {
             m[j] = m[j] * b1 + g[j] * d1;
             v[j] = v[j] * b2 + g[j] * g[j] * d2;
-            p[j] = p[j] - p[j] * decay - step1 * (m[j] * __builtin_amdgcn_rcpf(root(v[j] * i2) + eps));
+            // Square root and reciprocal are the hardware's estimates (an ulp each): they reach p
+            // only, whose update they move by less than its own rounding.  The root's takes no
+            // subnormals; 2^-126 more changes nothing above 2^-102.
+            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(__builtin_fmaf(v[j], i2, 0x1p-126f)) + eps);
+            p[j] = __builtin_fmaf(m[j] * -step1, r, __builtin_fmaf(p[j], -decay, p[j]));
         }
         if (T.master) store8<PT_FP32>(T.master, i, T.n, vec, p);
         store8<PT>(T.p, i, T.n, vec, p);
@@ -218,20 +202,29 @@ __global__ void __launch_bounds__(256) k_adamw(AdamwArgs a) {
             av = half_max(av);
             const float fm = __uint_as_float(am), fv = __uint_as_float(av);
             const float im = fm >= SCALE_LIVE ? (1.0f / fm) * E4M3_TOP : 0.f, iv = fv >= SCALE_LIVE ? (1.0f / fv) * E5M2_TOP : 0.f;
+            // The conversions' noise is added below the last place that they keep, in units of
+            // its 2^-32: sixteen bits of the hash and a half of their last place.
             u32x2 cm = {0, 0}, cv = {0, 0};
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 const uint32_t h = hash32((uint32_t)((i + j) >> 1) + key);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const uint32_t noise = q ? h >> 16 : h & 0xFFFFu;
-                    const float x = m[j + q], y = v[j + q];
-                    const float yv = fminf(y * iv, E5M2_TOP);
-                    uint32_t em = to_float8<3, 7>(fminf(fabsf(x) * im, E4M3_TOP), noise), ev = to_float8<2, 15>(yv, noise);
-                    ev = max(ev, yv > 0.f ? 1u : 0u);
-                    em |= em ? (__float_as_uint(x) >> 24) & 0x80u : 0u;
-                    cm[(j + q) / 4] |= em << (8 * ((j + q) & 3));
-                    cv[(j + q) / 4] |= ev << (8 * ((j + q) & 3));
+                const int n0 = (int)((h << 16) | 0x8000u), n1 = (int)((h & 0xFFFF0000u) | 0x8000u);
+                const float x0 = __builtin_amdgcn_fmed3f(m[j] * im, -E4M3_TOP, E4M3_TOP);
+                const float x1 = __builtin_amdgcn_fmed3f(m[j + 1] * im, -E4M3_TOP, E4M3_TOP);
+                // a second moment above 0 is kept at the smallest e5m2 number at least
+                float y0 = v[j] * iv, y1 = v[j + 1] * iv;
+                y0 = y0 > 0.f ? __builtin_amdgcn_fmed3f(y0, E5M2_LEAST, E5M2_TOP) : 0.f;
+                y1 = y1 > 0.f ? __builtin_amdgcn_fmed3f(y1, E5M2_LEAST, E5M2_TOP) : 0.f;
+                if (j & 2) {
+                    cm[j / 4] = __builtin_amdgcn_cvt_sr_fp8_f32(x0, n0, (int)cm[j / 4], 2);
+                    cm[j / 4] = __builtin_amdgcn_cvt_sr_fp8_f32(x1, n1, (int)cm[j / 4], 3);
+                    cv[j / 4] = __builtin_amdgcn_cvt_sr_bf8_f32(y0, n0, (int)cv[j / 4], 2);
+                    cv[j / 4] = __builtin_amdgcn_cvt_sr_bf8_f32(y1, n1, (int)cv[j / 4], 3);
+                } else {
+                    cm[j / 4] = __builtin_amdgcn_cvt_sr_fp8_f32(x0, n0, (int)cm[j / 4], 0);
+                    cm[j / 4] = __builtin_amdgcn_cvt_sr_fp8_f32(x1, n1, (int)cm[j / 4], 1);
+                    cv[j / 4] = __builtin_amdgcn_cvt_sr_bf8_f32(y0, n0, (int)cv[j / 4], 0);
+                    cv[j / 4] = __builtin_amdgcn_cvt_sr_bf8_f32(y1, n1, (int)cv[j / 4], 1);
                 }
             }
             store_codes(T.m, i, T.n, vec, cm);

@@ -131,11 +131,8 @@ def to_float8(x, step, seed, dtype):
     i = torch.arange(n)
     pair = hash32((i >> 1) + int(step) * 0x9E3779B9 + int(seed))
     noise = torch.where(i % 2 == 1, pair >> 16, pair & 0xFFFF).double()
-    # the subnormals' fp32 detour (y + 2^(1 - bias)) rounds y to 2^-(22 + bias)
-    small = y < 2.0 ** (1 - bias)
-    yd = torch.where(small, (y + 2.0 ** (1 - bias)).double() - 2.0 ** (1 - bias), y.double())
-    code = low + ((yd - lo) / (hi - lo) + (noise + 0.5) / 65536 >= 1).to(low.dtype)
+    code = low + ((y.double() - lo) / (hi - lo) + (noise + 0.5) / 65536 >= 1).to(low.dtype)
     if man == 2:
         code = torch.where((code == 0) & (y > 0), torch.ones_like(code), code)
-    code = code | torch.where((x < 0) & (code > 0), 128, 0)
+    code = code | torch.where(x.signbit(), 128, 0)
     return code.to(torch.uint8), scale.view(-1)

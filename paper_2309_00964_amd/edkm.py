@@ -3,8 +3,9 @@
 Argument marshalling only: tensors become device pointers and the current HIP
 stream; every step of the computation runs in the library's HIP kernels.  The
 functions keep the C names without the ``edkm_`` prefix.  Importing this module
-loads the library and raises ``ImportError`` if it has not been built (run
-``__graft_entry__.build()``); there is no fallback.
+loads the library (and the compiled marshalling of the layer and optimizer
+calls, ``_edkm_torch.so``) and raises ``ImportError`` if it has not been built
+(run ``__graft_entry__.build()``); there is no fallback.
 
 Weights are passed as 16-bit patterns of the plan's format (fp16 or bf16): any
 contiguous 2-byte device tensor (the weights themselves, or ``int16`` views).
@@ -421,89 +422,29 @@ def unique_inverse_batch(plans, w_bits, unique_out=None, inverse_out=None, strea
 
 # ---------------------------------------------------------------------------
 # layer and optimizer operators
+#
+# Their marshalling is compiled (csrc/edkm_torch.cpp): the checks of a call's tensors in
+# Python would take as long as a single token's kernel.  It calls the library loaded above.
+
+from . import _edkm_torch as _x  # noqa: E402
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 TYPE_FP16, TYPE_BF16, TYPE_FP32 = 0, 1, 2
 STATE_BLOCK = 256          # EDKM_STATE_BLOCK: elements of an 8-bit state's scale
-_HALF = {torch.float16: KEYS_FP16, torch.bfloat16: KEYS_BF16}
-_TYPES = {torch.float16: TYPE_FP16, torch.bfloat16: TYPE_BF16, torch.float32: TYPE_FP32}
 
-
-class _On:
-    """The tensors' device as the current one for a call, and its stream's handle."""
-
-    __slots__ = ("device", "before")
-
-    def __init__(self, device):
-        self.device = device
-
-    def __enter__(self):
-        self.before = torch._C._cuda_getDevice()
-        if self.before != self.device:
-            torch._C._cuda_setDevice(self.device)
-        return self
-
-    def __exit__(self, *exc):
-        if self.before != self.device:
-            torch._C._cuda_setDevice(self.before)
-
-    def stream(self, stream):
-        if stream is None:
-            return torch._C._cuda_getCurrentRawStream(self.device)
-        return stream if isinstance(stream, int) else stream.cuda_stream
-
-
-def _format(t, name):
-    if t.dtype not in _HALF or not t.is_cuda:
-        raise ValueError("%s must be an fp16 or bf16 device tensor" % name)
-    return _HALF[t.dtype]
-
-
-def _like(t, ref, name):
-    if t.dtype != ref.dtype or t.device != ref.device:
-        raise ValueError("%s must have the type and device of %s (%s, %s)" % (name, "the first tensor", ref.dtype, ref.device))
-
-
-def _matrix(t, rows, cols, ref, name):
-    """Pointer and leading dimension of a rows x cols matrix of ref's type and
-    device whose rows have no gaps and do not overlap."""
-    if t is None:
-        return None, cols
-    if ref is not t:
-        _like(t, ref, name)
-    if tuple(t.shape) != (rows, cols):
-        raise ValueError("%s must be %d x %d, not %s" % (name, rows, cols, "x".join(map(str, t.shape))))
-    s0, s1 = t.stride()
-    if (s1 != 1 and cols > 1) or (s0 < cols and rows > 1):
-        raise ValueError("%s must have contiguous rows that do not overlap" % name)
-    return t.data_ptr(), (s0 if rows > 1 else cols)
-
-
-def _vector(t, count, ref, name):
-    if t is None:
-        return None
-    _like(t, ref, name)
-    if t.numel() != count or not t.is_contiguous():
-        raise ValueError("%s must hold %d contiguous elements" % (name, count))
-    return t.data_ptr()
+_x.bind({_n: ctypes.cast(getattr(_lib, _n), _P).value for _n in _SIGS}, EdkmError)
 
 
 def _activation(name):
-    if name not in ACTIVATIONS:
-        raise ValueError("activation must be one of %s" % sorted(ACTIVATIONS))
-    return ACTIVATIONS[name]
+    try:
+        return ACTIVATIONS[name]
+    except (KeyError, TypeError):
+        raise ValueError("activation must be one of %s" % sorted(ACTIVATIONS)) from None
 
 
-def _scratch(workspace, need, device):
-    """The caller's workspace, or one from torch's allocator (which keeps it from
-    other streams' use until the work queued here is done)."""
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    if workspace is None:
-        return None, 0, None
-    if workspace.device != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous tensor on the operands' device")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+def _given(stream):
+    """A stream argument as its raw handle, or None for the current stream of the tensors' device."""
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
 def linear_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -521,20 +462,11 @@ def palette_linear_workspace_bytes(m: int, n: int, k: int, bits: int) -> int:
 def linear(x, w, y, bias=None, residual=None, activation: str = "none", z_out=None, workspace=None, stream=None) -> None:
     """y = act(x w^T + bias) + residual for 16-bit matrices x (m x k), w (n x k)
     and y (m x n), any of whose rows may lie apart; y may be the residual.
-    ``z_out`` (m x n, contiguous) receives x w^T + bias for linear_backward."""
-    fmt, act = _format(x, "x"), _activation(activation)
-    if x.dim() != 2 or w.dim() != 2:
-        raise ValueError("x and w must be matrices")
-    (m, k), n = x.shape, w.shape[0]
-    px, ldx = _matrix(x, m, k, x, "x")
-    pw, ldw = _matrix(w, n, k, x, "w")
-    py, ldy = _matrix(y, m, n, x, "y")
-    pr, ldr = _matrix(residual, m, n, x, "residual")
-    pb, pz = _vector(bias, n, x, "bias"), _vector(z_out, m * n, x, "z_out")
-    with _On(x.get_device()) as on:
-        pws, nws, _keep = _scratch(workspace, _lib.edkm_linear_workspace_bytes(m, n, k), x.device)
-        _check(_lib.edkm_linear(m, n, k, fmt, act, px, ldx, pw, ldw, pb, pr, ldr, py, ldy, pz, pws, nws,
-                                on.stream(stream)), "linear")
+    ``z_out`` (m x n, contiguous) receives x w^T + bias for linear_backward.
+    Without ``workspace`` one is taken from torch's allocator, on the current
+    stream only: a call with another ``stream`` brings its own (of
+    linear_workspace_bytes)."""
+    _x.linear(x, w, y, bias, residual, _activation(activation), z_out, workspace, _given(stream))
 
 
 def linear_backward(dy, x, w, dx=None, dw=None, dbias=None, z=None, activation: str = "none", workspace=None,
@@ -542,85 +474,19 @@ def linear_backward(dy, x, w, dx=None, dw=None, dbias=None, z=None, activation: 
     """The gradients of linear's x, w and bias for dL/dy = ``dy`` into those of dx
     (m x k), dw (n x k, contiguous) and dbias (n) that are given.  ``z`` is
     linear's z_out (needed with an activation); x may be None without dw, w without dx."""
-    fmt, act = _format(dy, "dy"), _activation(activation)
-    if dy.dim() != 2:
-        raise ValueError("dy must be a matrix")
-    m, n = dy.shape
-    if (x is None and dw is not None) or (w is None and dx is not None):
-        raise ValueError("dw needs x and dx needs w")
-    if act != 0 and z is None:
-        raise ValueError("an activation's backward needs z")
-    k = next((t.shape[1] for t in (x, w, dx, dw) if t is not None), 1)
-    pd, ldd = _matrix(dy, m, n, dy, "dy")
-    px, ldx = _matrix(x, m, k, dy, "x")
-    pw, ldw = _matrix(w, n, k, dy, "w")
-    pdx, lddx = _matrix(dx, m, k, dy, "dx")
-    pdw = _vector(dw, n * k, dy, "dw")
-    pdb, pz = _vector(dbias, n, dy, "dbias"), _vector(z, m * n, dy, "z")
-    with _On(dy.get_device()) as on:
-        pws, nws, _keep = _scratch(workspace, _lib.edkm_linear_backward_workspace_bytes(m, n, k, act), dy.device)
-        _check(_lib.edkm_linear_backward(m, n, k, fmt, act, pd, ldd, pz, px, ldx, pw, ldw, pdx, lddx, pdw, pdb, pws, nws,
-                                         on.stream(stream)), "linear_backward")
-
-
-def _table(indices, lut, count, ref):
-    """Pointers of a palette of ``count`` weights, and its bits."""
-    bits = lut.numel().bit_length() - 1
-    if not 1 <= bits <= 4 or lut.numel() != 1 << bits or lut.dtype != torch.float32 or not lut.is_contiguous():
-        raise ValueError("lut must hold 2, 4, 8 or 16 contiguous float32 values")
-    need = (count * bits + 7) // 8
-    if indices.element_size() != 1 or not indices.is_contiguous() or indices.numel() < need:
-        raise ValueError("indices must be %d contiguous bytes" % need)
-    if indices.device != ref.device or lut.device != ref.device:
-        raise ValueError("indices and lut must be on %s" % ref.device)
-    return indices.data_ptr(), lut.data_ptr(), bits
+    _x.linear_backward(dy, x, w, dx, dw, dbias, z, _activation(activation), workspace, _given(stream))
 
 
 def unpalettize(indices, lut, w_out, stream=None) -> None:
     """The 16-bit weights of a palette (palettize's indices and table) into
     ``w_out`` (fp16 or bf16, contiguous; its elements are the palette's weights)."""
-    fmt = _format(w_out, "w_out")
-    if not w_out.is_contiguous():
-        raise ValueError("w_out must be contiguous")
-    pi, pl, bits = _table(indices, lut, w_out.numel(), w_out)
-    with _On(w_out.get_device()) as on:
-        _check(_lib.edkm_unpalettize(pi, w_out.numel(), bits, fmt, pl, w_out.data_ptr(), on.stream(stream)), "unpalettize")
+    _x.unpalettize(indices, lut, w_out, _given(stream))
 
 
 def palette_linear(x, indices, lut, y, bias=None, residual=None, activation: str = "none", z_out=None, workspace=None,
                    stream=None) -> None:
     """linear with the n x k weights given as palettize's indices and table."""
-    fmt, act = _format(x, "x"), _activation(activation)
-    if x.dim() != 2 or y.dim() != 2:
-        raise ValueError("x and y must be matrices")
-    (m, k), n = x.shape, y.shape[1]
-    px, ldx = _matrix(x, m, k, x, "x")
-    py, ldy = _matrix(y, m, n, x, "y")
-    pr, ldr = _matrix(residual, m, n, x, "residual")
-    pb, pz = _vector(bias, n, x, "bias"), _vector(z_out, m * n, x, "z_out")
-    pi, pl, bits = _table(indices, lut, n * k, x)
-    with _On(x.get_device()) as on:
-        pws, nws, _keep = _scratch(workspace, _lib.edkm_palette_linear_workspace_bytes(m, n, k, bits), x.device)
-        _check(_lib.edkm_palette_linear(m, n, k, bits, fmt, act, px, ldx, pi, pl, pb, pr, ldr, py, ldy, pz, pws, nws,
-                                        on.stream(stream)), "palette_linear")
-
-
-def _pointers(items, name, dtypes, sizes, device):
-    """Host array of the device pointers of contiguous tensors that hold sizes[i]
-    elements of one of the types, and their type."""
-    if len(items) != len(sizes):
-        raise EdkmError(ERR_ARG, "adamw_batch", "%s has %d entries for %d parameters" % (name, len(items), len(sizes)))
-    kinds = {t.dtype for t in items}
-    if len(kinds) != 1 or not kinds <= dtypes:
-        raise ValueError("%s must all be of one type among %s" % (name, sorted(map(str, dtypes))))
-    if any(t.get_device() != device for t in items) or not all(t.is_contiguous() for t in items):
-        raise ValueError("%s must be contiguous tensors on the parameters' device" % name)
-    if any(t.numel() < n for t, n in zip(items, sizes)):
-        raise ValueError("%s: a tensor has fewer elements than its parameter needs" % name)
-    return (ctypes.c_void_p * len(items))(*[t.data_ptr() for t in items]), kinds.pop()
-
-
-_F32, _E4M3, _E5M2 = {torch.float32}, {torch.float8_e4m3fn}, {torch.float8_e5m2}
+    _x.palette_linear(x, indices, lut, y, bias, residual, _activation(activation), z_out, workspace, _given(stream))
 
 
 def adamw_batch(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1: float = 0.9, beta2: float = 0.999,
@@ -634,39 +500,5 @@ def adamw_batch(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1: float = 0
     rounding.  exp_avgs and exp_avg_sqs are float32, or float8_e4m3fn and
     float8_e5m2 with one fp32 scale per STATE_BLOCK elements in ``m_scales`` and
     ``v_scales``; ``seed`` then varies their rounding noise."""
-    params = list(params)
-    if not params:
-        return
-    device, sizes = params[0].get_device(), [p.numel() for p in params]
-    if device < 0:
-        raise ValueError("params must be device tensors")
-    pp, pt = _pointers(params, "params", set(_TYPES), sizes, device)
-    if len(set(pp)) != len(params) and len({p for p, n in zip(pp, sizes) if n}) != sum(n > 0 for n in sizes):
-        raise ValueError("params: the same tensor twice")
-    pg, gt = _pointers(grads, "grads", {pt, torch.float32}, sizes, device)
-    bits = 8 if m_scales is not None or v_scales is not None else 32
-    if bits == 8 and (m_scales is None or v_scales is None):
-        raise ValueError("8-bit states need m_scales and v_scales")
-    pm, _ = _pointers(exp_avgs, "exp_avgs", _E4M3 if bits == 8 else _F32, sizes, device)
-    pv, _ = _pointers(exp_avg_sqs, "exp_avg_sqs", _E5M2 if bits == 8 else _F32, sizes, device)
-    pms = pvs = pma = None
-    if bits == 8:
-        blocks = [(n + STATE_BLOCK - 1) // STATE_BLOCK for n in sizes]
-        pms, _ = _pointers(m_scales, "m_scales", _F32, blocks, device)
-        pvs, _ = _pointers(v_scales, "v_scales", _F32, blocks, device)
-    if masters is not None:
-        if pt == torch.float32:
-            raise ValueError("float32 parameters take no masters")
-        pma, _ = _pointers(masters, "masters", _F32, sizes, device)
-    if step.dtype != torch.int32 or step.numel() != 1 or step.get_device() != device:
-        raise ValueError("step must be one int32 on the parameters' device")
-    lr_dev = None
-    if isinstance(lr, torch.Tensor):
-        if lr.dtype != torch.float32 or lr.numel() != 1 or lr.get_device() != device:
-            raise ValueError("a tensor lr must be one float32 on the parameters' device")
-        lr_dev, lr = lr.data_ptr(), 0.0
-    with _On(device) as on:
-        _check(_lib.edkm_adamw_batch(len(params), (ctypes.c_uint64 * len(sizes))(*sizes), _TYPES[pt], _TYPES[gt], bits,
-                                     pp, pma, pg, pm, pv, pms, pvs, step.data_ptr(), lr_dev, float(lr), float(beta1),
-                                     float(beta2), float(eps), float(weight_decay), int(seed) & 0xFFFFFFFF,
-                                     on.stream(stream)), "adamw_batch")
+    _x.adamw_batch(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1, beta2, eps, weight_decay, masters, m_scales, v_scales,
+                   int(seed), _given(stream))

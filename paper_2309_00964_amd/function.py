@@ -24,7 +24,6 @@ so two clustered layers in one graph never share state.
 from __future__ import annotations
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import edkm
 
@@ -147,117 +146,17 @@ def dkm_batch(ws, c0s, tau: float = 2e-3, max_iter: int = 5, eps: float = 0.0, o
     return list(out[:m]), list(out[m:2 * m]), list(out[2 * m:])
 
 
-def _rows(t, cols):
-    """A tensor of any leading shape as a matrix whose rows have no gaps."""
-    m = t.reshape(-1, cols)
-    s0, s1 = m.stride()
-    ok = (s1 == 1 or cols == 1) and (s0 >= cols or m.shape[0] <= 1)
-    return m if ok else m.contiguous()
-
-
-def _check_product(x, n, bias, residual):
-    if x.dim() < 1:
-        raise ValueError("x needs a last dimension of inputs")
-    if bias is not None and tuple(bias.shape) != (n,):
-        raise ValueError("bias must hold %d elements" % n)
-    if residual is not None and tuple(residual.shape) != (*x.shape[:-1], n):
-        raise ValueError("residual must have the output's shape")
-
-
-class LinearFunction(torch.autograd.Function):
-    """apply(x, w, bias, residual, activation) -> y = act(x w^T + bias) + residual."""
-
-    @staticmethod
-    def forward(ctx, x, w, bias, residual, activation):
-        n, k = w.shape
-        x2, w2 = _rows(x, k), _rows(w, k)
-        r2 = _rows(residual, n) if residual is not None else None
-        y = torch.empty(*x.shape[:-1], n, dtype=x.dtype, device=x.device)
-        z = None
-        if activation != "none" and any(ctx.needs_input_grad[:3]):
-            z = torch.empty(x2.shape[0], n, dtype=x.dtype, device=x.device)
-        edkm.linear(x2, w2, y.view(-1, n), bias.contiguous() if bias is not None else None, r2, activation, z)
-        ctx.activation, ctx.shape = activation, x.shape
-        ctx.save_for_backward(x2 if ctx.needs_input_grad[1] else None, w2 if ctx.needs_input_grad[0] else None, z)
-        return y
-
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, grad_y):
-        x2, w2, z = ctx.saved_tensors
-        n, k = grad_y.shape[-1], ctx.shape[-1]
-        dy = _rows(grad_y, n)
-        new = lambda *shape: torch.empty(shape, dtype=dy.dtype, device=dy.device)  # noqa: E731
-        dx = new(dy.shape[0], k) if ctx.needs_input_grad[0] else None
-        dw = new(n, k) if ctx.needs_input_grad[1] else None
-        db = new(n) if ctx.needs_input_grad[2] else None
-        if dx is not None or dw is not None or db is not None:
-            edkm.linear_backward(dy, x2, w2, dx, dw, db, z, ctx.activation)
-        return (dx.view(ctx.shape) if dx is not None else None, dw, db,
-                grad_y if ctx.needs_input_grad[3] else None, None)
-
-
 def linear(x, w, bias=None, residual=None, activation: str = "none"):
-    """act(x w^T + bias) + residual; differentiable in all four tensors.
+    """act(x w^T + bias) + residual; differentiable (once) in all four tensors.
 
     x: fp16 or bf16, (..., k); w: n x k of x's type, say W~ of ``dkm`` with
     out_half; bias: n; residual: (..., n); activation: none, relu, gelu or silu.
     The backward keeps x, w and (with an activation) x w^T + bias in 16 bits."""
-    if w.dim() != 2 or x.shape[-1] != w.shape[1]:
-        raise ValueError("w must be n x k for x of (..., k)")
-    _check_product(x, w.shape[0], bias, residual)
-    edkm._format(x, "x"), edkm._activation(activation)
-    return LinearFunction.apply(x, w, bias, residual, activation)
-
-
-class PaletteLinearFunction(torch.autograd.Function):
-    """apply(x, bias, residual, indices, lut, n, activation): LinearFunction with
-    a palette as its frozen weights."""
-
-    @staticmethod
-    def forward(ctx, x, bias, residual, indices, lut, n, activation):
-        x2 = _rows(x, x.shape[-1])
-        y = torch.empty(*x.shape[:-1], n, dtype=x.dtype, device=x.device)
-        z = None
-        if activation != "none" and any(ctx.needs_input_grad[:2]):
-            z = torch.empty(x2.shape[0], n, dtype=x.dtype, device=x.device)
-        edkm.palette_linear(x2, indices, lut, y.view(-1, n), bias.contiguous() if bias is not None else None,
-                            _rows(residual, n) if residual is not None else None, activation, z)
-        ctx.activation, ctx.shape, ctx.n = activation, x.shape, n
-        ctx.save_for_backward(indices, lut, z)
-        return y
-
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, grad_y):
-        indices, lut, z = ctx.saved_tensors
-        n, k = ctx.n, ctx.shape[-1]
-        dy = _rows(grad_y, n)
-        new = lambda *shape: torch.empty(shape, dtype=dy.dtype, device=dy.device)  # noqa: E731
-        dx = db = w = None
-        if ctx.needs_input_grad[0]:
-            w, dx = new(n, k), new(dy.shape[0], k)
-            edkm.unpalettize(indices, lut, w)
-        if ctx.needs_input_grad[1]:
-            db = new(n)
-        if dx is not None or db is not None:
-            edkm.linear_backward(dy, None, w, dx, None, db, z, ctx.activation)
-        return (dx.view(ctx.shape) if dx is not None else None, db,
-                grad_y if ctx.needs_input_grad[2] else None, None, None, None, None)
+    return edkm._x.apply_linear(x, w, bias, residual, edkm._activation(activation))
 
 
 def palette_linear(x, indices, lut, out_features: int, bias=None, residual=None, activation: str = "none"):
     """act(x W^T + bias) + residual with W (out_features x k) given as the packed
     indices and the table of ``edkm.palettize``: the product of a served model.
-    Differentiable in x, bias and residual; the palette is frozen."""
-    n = int(out_features)
-    if lut.requires_grad and torch.is_grad_enabled():
-        raise ValueError("a palette's table takes no gradient; train the weights through dkm and linear")
-    _check_product(x, n, bias, residual)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, bias, residual)):
-        edkm._format(x, "x"), edkm._activation(activation)
-        return PaletteLinearFunction.apply(x, bias, residual, indices, lut, n, activation)
-    y = torch.empty(*x.shape[:-1], n, dtype=x.dtype, device=x.device)
-    edkm.palette_linear(_rows(x, x.shape[-1]), indices, lut, y.view(-1, n), bias,
-                        _rows(residual, n) if residual is not None else None, activation)
-    return y
+    Differentiable (once) in x, bias and residual; the palette is frozen."""
+    return edkm._x.apply_palette_linear(x, indices, lut, out_features, bias, residual, edkm._activation(activation))

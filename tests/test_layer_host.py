@@ -108,38 +108,22 @@ def test_constants_match_the_header():
     assert int(re.search(r"#define EDKM_STATE_BLOCK (\d+)", text).group(1)) == edkm.STATE_BLOCK
 
 
-class Fake:
-    """Shape, type and device of a GPU tensor, for the checks that come before any call."""
-
-    made = 0
-
-    def __init__(self, *shape, dtype=torch.float16, stride=None, device="cuda:0"):
-        Fake.made += 1
-        self.at = Fake.made * P
-        self.t = torch.empty(shape, dtype=dtype, device="meta")
-        if stride:
-            self.t = self.t.as_strided(shape, stride)
-        self.shape, self.dtype, self.device, self.is_cuda = self.t.shape, dtype, torch.device(device), True
-
-    def __getattr__(self, name):
-        return getattr(self.t, name)
-
-    def data_ptr(self):
-        return self.at
-
-    def get_device(self):
-        return self.device.index
+def h(*shape, dtype=torch.float16, stride=None, device="cpu"):
+    """A tensor of a shape, type and stride (host memory: the last refusal is that it is no
+    device tensor; one on "meta" stands for another device)."""
+    if stride is None:
+        return torch.zeros(shape, dtype=dtype, device=device)
+    return torch.zeros(1 << 10, dtype=dtype, device=device).as_strided(shape, stride)
 
 
 def test_binding_refuses_matrices_that_do_not_fit():
-    h = Fake
     x, w, y = h(4, 16), h(8, 16), h(4, 8)
     cases = [
         (lambda: edkm.linear(h(4, 16, dtype=torch.float32), w, y), "x must be"),
         (lambda: edkm.linear(x, h(8, 15), y), "w must be 8 x 16"),
         (lambda: edkm.linear(x, w, h(4, 9)), "y must be 4 x 8"),
         (lambda: edkm.linear(x, w, h(4, 8, dtype=torch.bfloat16)), "y must have the type"),
-        (lambda: edkm.linear(x, w, h(4, 8, device="cuda:1")), "y must have the type and device"),
+        (lambda: edkm.linear(x, w, h(4, 8, device="meta")), "y must have the type and device"),
         (lambda: edkm.linear(h(4, 16, stride=(1, 4)), w, y), "x must have contiguous rows"),
         (lambda: edkm.linear(h(4, 16, stride=(0, 1)), w, y), "x must have contiguous rows"),
         (lambda: edkm.linear(x, w, y, h(7)), "bias must hold 8"),
@@ -153,8 +137,13 @@ def test_binding_refuses_matrices_that_do_not_fit():
         (lambda: edkm.palette_linear(x, h(47, dtype=torch.uint8), h(8, dtype=torch.float32), y), "indices must be 48"),
         (lambda: edkm.palette_linear(x, h(48, dtype=torch.uint8), h(8), y), "lut must hold"),
         (lambda: edkm.palette_linear(x, h(48, dtype=torch.uint8), h(32, dtype=torch.float32), y), "lut must hold"),
-        (lambda: edkm.unpalettize(h(48, dtype=torch.uint8, device="cuda:1"), h(8, dtype=torch.float32), h(128)), "must be on cuda:0"),
+        (lambda: edkm.unpalettize(h(48, dtype=torch.uint8, device="meta"), h(8, dtype=torch.float32), h(128)), "must be on cpu"),
         (lambda: edkm.unpalettize(h(48, dtype=torch.uint8), h(8, dtype=torch.float32), h(129)), "indices must be 49"),
+        (lambda: edkm.unpalettize(h(48, dtype=torch.uint8), h(8, dtype=torch.float32), h(128)), "device tensor"),
+        (lambda: edkm.linear(x, w, y), "device tensor"),
+        (lambda: edkm.linear_backward(y, x, w, dx=h(4, 16)), "device tensor"),
+        (lambda: edkm.palette_linear(x, h(48, dtype=torch.uint8), h(8, dtype=torch.float32), y), "device tensor"),
+        (lambda: edkm.linear(None, w, y), "x must be a tensor"),
     ]
     for call, what in cases:
         with pytest.raises(ValueError, match=what):
@@ -162,8 +151,8 @@ def test_binding_refuses_matrices_that_do_not_fit():
 
 
 def test_binding_refuses_optimizer_lists_that_do_not_fit():
-    h, f32 = Fake, torch.float32
-    p, g = [h(300), h(5)], [h(300), h(5)]
+    f32 = torch.float32
+    p, g, q = [h(300), h(5)], [h(300), h(5)], h(204)
     m, v, step = [h(300, dtype=f32), h(5, dtype=f32)], [h(300, dtype=f32), h(5, dtype=f32)], h(1, dtype=torch.int32)
     e8 = [h(300, dtype=torch.float8_e4m3fn), h(5, dtype=torch.float8_e4m3fn)]
     e5 = [h(300, dtype=torch.float8_e5m2), h(5, dtype=torch.float8_e5m2)]
@@ -172,7 +161,9 @@ def test_binding_refuses_optimizer_lists_that_do_not_fit():
         (lambda: edkm.adamw_batch(p, g[:1], m, v, step, 1e-3), "grads has 1 entries"),
         (lambda: edkm.adamw_batch(p, [h(300), h(4)], m, v, step, 1e-3), "grads"),
         (lambda: edkm.adamw_batch(p, [h(300, dtype=torch.bfloat16)] * 2, m, v, step, 1e-3), "grads"),
-        (lambda: edkm.adamw_batch([p[0], p[0]], g, m, v, step, 1e-3), "twice"),
+        (lambda: edkm.adamw_batch(p, g, m, v, step, 1e-3), "device tensors"),
+        (lambda: edkm.adamw_batch([q[:200], q[199:]], g, m, v, step, 1e-3), "overlap"),
+        (lambda: edkm.adamw_batch([p[1], p[1]], g, m, v, step, 1e-3), "twice"),
         (lambda: edkm.adamw_batch(p, g, e8, v, step, 1e-3), "exp_avgs"),
         (lambda: edkm.adamw_batch(p, g, e8, e5, step, 1e-3, m_scales=s2), "m_scales and v_scales"),
         (lambda: edkm.adamw_batch(p, g, e8, e5, step, 1e-3, m_scales=s1, v_scales=s2), "m_scales"),

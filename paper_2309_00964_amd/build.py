@@ -3,10 +3,16 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("edkm_kernels.hip", "edkm_api.hip", "edkm_product.hip", "edkm_adamw.hip", "edkm_layer_api.hip")]
+CSRC = os.path.join(HERE, "csrc")
+# The clustering's sources, which the diagnostics and test builds compile with flags of
+# their own, and the layer and optimizer operators', which all builds share.
+SOURCES = [os.path.join(CSRC, f) for f in ("edkm_kernels.hip", "edkm_api.hip")]
+LAYER_SOURCES = [os.path.join(CSRC, f) for f in ("edkm_product.hip", "edkm_few.hip", "edkm_adamw.hip", "edkm_layer_api.hip")]
 OUT = os.path.join(HERE, "libedkm.so")
 # Diagnostics build: the same library with per-block timeline stamps
 # (-DEDKM_BLOCK_STAMPS, include/edkm_stamps.h); load it with EDKM_LIBRARY.
@@ -19,28 +25,64 @@ OUT_EXCHANGE = os.path.join(HERE, "libedkm_exchange.so")
 OUT_BINDING = os.path.join(HERE, "_edkm_torch.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Werror=uninitialized",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Werror=uninitialized",
     # no packed-fp32 instructions in generated code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-I" + os.path.join(ROOT, "include"),
 ]
 
 
-def build_library(out: str = OUT, extra=()) -> str:
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+def _hipcc(args):
+    subprocess.check_call([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *args])
+
+
+def _compile(folder, jobs):
+    """Objects of (source, extra flags) pairs, side by side."""
+    def one(job):
+        i, (src, extra) = job
+        obj = os.path.join(folder, "%d_%s.o" % (i, os.path.basename(src)))
+        _hipcc([*HIPCC_FLAGS, *extra, "-c", src, "-o", obj])
+        return obj
+    with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        return list(pool.map(one, enumerate(jobs)))
+
+
+def _link(out, objects):
     tmp = out + ".tmp%d" % os.getpid()
-    cmd = [hipcc, *HIPCC_FLAGS, *extra, "-o", tmp, *SOURCES]
-    subprocess.check_call(cmd)
+    _hipcc(["--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objects])
     os.replace(tmp, out)
     return out
 
 
+STAMPS_FLAGS = ("-DEDKM_BLOCK_STAMPS",)
+EXCHANGE_FLAGS = ("-DEDKM_XW_WAIT=-1", "-DEDKM_XW_LATE=300000")
+
+
+def build_libraries(builds) -> list:
+    """Each (output, extra flags) build of the library; what they share is compiled once."""
+    with tempfile.TemporaryDirectory() as folder:
+        jobs = [(s, ()) for s in LAYER_SOURCES] + [(s, tuple(extra)) for _, extra in builds for s in SOURCES]
+        objs = _compile(folder, jobs)
+        shared, own = objs[:len(LAYER_SOURCES)], objs[len(LAYER_SOURCES):]
+        n = len(SOURCES)
+        return [_link(out, own[n * i:n * i + n] + shared) for i, (out, _) in enumerate(builds)]
+
+
+def build_library(out: str = OUT, extra=()) -> str:
+    return build_libraries([(out, extra)])[0]
+
+
 def build_stamps(out: str = OUT_STAMPS) -> str:
-    return build_library(out, extra=("-DEDKM_BLOCK_STAMPS",))
+    return build_library(out, extra=STAMPS_FLAGS)
 
 
 def build_exchange(out: str = OUT_EXCHANGE) -> str:
-    return build_library(out, extra=("-DEDKM_XW_WAIT=-1", "-DEDKM_XW_LATE=300000"))
+    return build_library(out, extra=EXCHANGE_FLAGS)
+
+
+def build_all() -> list:
+    """The product library, its diagnostics and test builds, and the marshalling."""
+    return [build_binding()] + build_libraries([(OUT, ()), (OUT_STAMPS, STAMPS_FLAGS), (OUT_EXCHANGE, EXCHANGE_FLAGS)])
 
 
 def build_binding(out: str = OUT_BINDING) -> str:
@@ -61,7 +103,4 @@ def build_binding(out: str = OUT_BINDING) -> str:
 
 
 if __name__ == "__main__":
-    print(build_binding())
-    print(build_library())
-    print(build_stamps())
-    print(build_exchange())
+    print("\n".join(build_all()))

@@ -61,9 +61,16 @@ struct DzArgs {
     uint16_t* dbias;
     int32_t rows, cols;
     int act;
+    int per;                // rows of a workgroup
 };
 
-constexpr int DZ_COLS = 64, DZ_ROWS = 256;   // one block's share of the bias gradient
+constexpr int DZ_COLS = 512, DZ_ROWS_LEAST = 4, DZ_ROWS_MOST = 64;   // one workgroup's share of them
+// Rows of a workgroup: as many as leave 1024 of them (four per CU).
+inline int dz_rows(int64_t rows, int64_t cols) {
+    int64_t r = DZ_ROWS_MOST;
+    while (r > DZ_ROWS_LEAST && (rows + r - 1) / r * ((cols + DZ_COLS - 1) / DZ_COLS) < 1024) r /= 2;
+    return (int)r;
+}
 
 enum ParamType : int { PT_FP16 = 0, PT_BF16 = 1, PT_FP32 = 2 };
 
@@ -98,6 +105,7 @@ struct AdamwArgs {
 static_assert(sizeof(AdamwArgs) <= 4096, "launch arguments fit the kernel-argument limit");
 
 hipError_t launch_product(const ProductArgs& a, int fmt, int opa, int opb, float* part, hipStream_t s);
+hipError_t launch_few(const ProductArgs& a, int fmt, int bits, hipStream_t s);
 hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s);
 hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
                               uint16_t* out, hipStream_t s);

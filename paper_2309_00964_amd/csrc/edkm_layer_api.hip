@@ -37,7 +37,7 @@ bool ld_ok(int64_t& ld, int64_t rows, int64_t cols) {
 
 size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-int dz_chunks(int64_t m) { return (int)((m + DZ_ROWS - 1) / DZ_ROWS); }
+int64_t dz_chunks(int64_t m, int64_t n) { return (m + dz_rows(m, n) - 1) / dz_rows(m, n); }
 
 // Workspace of a backward: dz, the bias gradient's partial sums, and those of the two
 // products in turn.
@@ -48,7 +48,7 @@ BackwardWs backward_ws(int64_t m, int64_t n, int64_t k, int act) {
     BackwardWs w;
     w.dz = 0;
     w.part = act == ACT_NONE ? 0 : up256((size_t)m * n * 2);
-    w.split = w.part + up256((size_t)dz_chunks(m) * n * 4);
+    w.split = w.part + up256((size_t)dz_chunks(m, n) * n * 4);
     w.total = w.split + up256(std::max(m ? product_part_bytes(m, k, n) : 0, product_part_bytes(n, k, m)));
     return w;
 }
@@ -121,6 +121,7 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
     d.rows = (int32_t)m;
     d.cols = (int32_t)n;
     d.act = activation;
+    d.per = dz_rows(m, n);
     if (launch_dz(d, format, stream) != hipSuccess) return EDKM_ERR_HIP;
     float* parts = reinterpret_cast<float*>(base + L.split);
     const uint16_t* dz = activation == ACT_NONE ? d.dy : d.dz;

@@ -1,204 +1,11 @@
 // Products with an epilogue for gfx950 (MI355X): y = act(x W^T + bias) + residual with
-// 16-bit or palettized weights, the products of its backward pass, and the 16-bit
-// weights of a palette.
+// 16-bit weights, the products of its backward pass and the gradient at its activation.
 
-#include "edkm_layer.h"
+#include "edkm_product.h"
 
-#include <hip/hip_fp16.h>
 #include <algorithm>
 
 namespace edkm {
-
-typedef __attribute__((ext_vector_type(8))) short s16x8;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-struct __attribute__((packed)) S16x8 { s16x8 v; };
-
-// ----------------------------------------------------------------------------
-// the two 16-bit formats
-
-template <int F>
-__device__ __forceinline__ float to_f32(uint16_t h) {
-    if (F == FMT_BF16) return __uint_as_float((uint32_t)h << 16);
-    return (float)__builtin_bit_cast(_Float16, h);
-}
-// to nearest even; NaN stays NaN
-template <int F>
-__device__ __forceinline__ uint16_t to_16(float x) {
-    if (F == FMT_BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
-    return __builtin_bit_cast(uint16_t, (_Float16)x);
-}
-template <int F>
-__device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
-    if constexpr (F == FMT_BF16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-
-// ----------------------------------------------------------------------------
-// activations and their derivatives
-
-__device__ __forceinline__ float act_value(float z, int act) {
-    switch (act) {
-    case ACT_RELU: return z < 0.f ? 0.f : z;
-    case ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    case ACT_SILU: return z / (1.0f + expf(-z));
-    default: return z;
-    }
-}
-__device__ __forceinline__ float act_slope(float z, int act) {
-    switch (act) {
-    case ACT_RELU: return z > 0.f ? 1.f : 0.f;
-    case ACT_GELU:
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-    case ACT_SILU: {
-        const float q = 1.0f / (1.0f + expf(-z));
-        return q * (1.0f + z * (1.0f - q));
-    }
-    default: return 1.f;
-    }
-}
-
-// The pre-activation as it is kept for the backward pass.  A finite z that the format
-// cannot hold takes its largest value: every activation's slope is constant out there,
-// while at an infinity gelu's and silu's formulas give NaN.
-template <int F>
-__device__ __forceinline__ uint16_t keep_z(float z) {
-    const uint16_t h = to_16<F>(z);
-    const uint16_t top = F == FMT_BF16 ? 0x7F7F : 0x7BFF;
-    if ((h & 0x7FFF) == top + 1 && __builtin_isfinite(z)) return (h & 0x8000) | top;
-    return h;
-}
-
-// ----------------------------------------------------------------------------
-// palettes
-
-struct __attribute__((packed)) U64 { uint64_t v; };
-
-// The 8 b bits of eight consecutive indices, from index i on, in the low bits.  Reads
-// nothing past the last byte.
-__device__ __forceinline__ uint32_t load_idx8(const uint8_t* idx, uint64_t nbytes, uint64_t i, int bits) {
-    const uint64_t o = i * (uint64_t)bits;
-    const uint64_t at = o >> 3;
-    uint64_t v = 0;
-    if (at + 8 <= nbytes) {
-        v = reinterpret_cast<const U64*>(idx + at)->v;
-    } else {
-        for (int j = 0; j < 8; ++j)
-            if (at + j < nbytes) v |= (uint64_t)idx[at + j] << (8 * j);
-    }
-    return (uint32_t)(v >> (o & 7));
-}
-
-// Table lookups in registers: the low and the high bytes of up to sixteen 16-bit values in
-// four registers each; v_perm_b32 picks four bytes of two registers at once.
-template <int F>
-struct Decoder {
-    uint32_t lo[4], hi[4];
-
-    __device__ __forceinline__ void init(const float* lut, int bits) {
-        const int k = 1 << bits;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            lo[i] = hi[i] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (i * 4 + j < k) {
-                    const uint32_t h = to_16<F>(lut[i * 4 + j]);
-                    lo[i] |= (h & 255) << (8 * j);
-                    hi[i] |= (h >> 8) << (8 * j);
-                }
-        }
-    }
-    // four values for the four indices in sel's bytes: two registers of two
-    __device__ __forceinline__ void four(uint32_t sel, bool wide, uint32_t& v01, uint32_t& v23) const {
-        uint32_t l, h;
-        if (wide) {       // sixteen entries: both halves, then the one that bit 3 names
-            const uint32_t s = sel & 0x07070707u, up = sel & 0x08080808u, mask = (up << 5) - (up >> 3);
-            const uint32_t l0 = __builtin_amdgcn_perm(lo[1], lo[0], s), l1 = __builtin_amdgcn_perm(lo[3], lo[2], s);
-            const uint32_t h0 = __builtin_amdgcn_perm(hi[1], hi[0], s), h1 = __builtin_amdgcn_perm(hi[3], hi[2], s);
-            l = (l1 & mask) | (l0 & ~mask);
-            h = (h1 & mask) | (h0 & ~mask);
-        } else {
-            l = __builtin_amdgcn_perm(lo[1], lo[0], sel);
-            h = __builtin_amdgcn_perm(hi[1], hi[0], sel);
-        }
-        v01 = __builtin_amdgcn_perm(h, l, 0x05010400u);
-        v23 = __builtin_amdgcn_perm(h, l, 0x07030602u);
-    }
-    // the values of eight packed indices
-    __device__ __forceinline__ s16x8 eight(uint32_t w, int bits) const {
-        typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-        uint32_t s0, s1;
-        if (bits == 4) {
-            s0 = spread(w & 0xFFFFu, 4);
-            s1 = spread(w >> 16, 4);
-        } else {
-            s0 = spread(w & ((1u << (4 * bits)) - 1), bits);
-            s1 = spread((w >> (4 * bits)) & ((1u << (4 * bits)) - 1), bits);
-        }
-        u32x4 v;
-        uint32_t a, b;
-        four(s0, bits == 4, a, b);
-        v[0] = a;
-        v[1] = b;
-        four(s1, bits == 4, a, b);
-        v[2] = a;
-        v[3] = b;
-        return __builtin_bit_cast(s16x8, v);
-    }
-    // 4 b bits into the low bits of four bytes
-    __device__ __forceinline__ static uint32_t spread(uint32_t x, int b) {
-        x = (x | (x << (16 - 2 * b))) & (((1u << (2 * b)) - 1) * 0x10001u);
-        return (x | (x << (8 - b))) & (((1u << b) - 1) * 0x01010101u);
-    }
-};
-
-// eight consecutive values, `left` of them there (zeros after them)
-__device__ __forceinline__ s16x8 row8(const uint16_t* q, int left) {
-    if (left >= 8) return reinterpret_cast<const S16x8*>(q)->v;
-    s16x8 v = {};
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < left) v[j] = (short)q[j];
-    return v;
-}
-
-// the first `n` of eight values, zeros after them
-__device__ __forceinline__ s16x8 keep_first(s16x8 v, int n) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j >= n) v[j] = 0;
-    return v;
-}
-
-// Thirty-two weights per thread: 4 b bytes of indices, 64 bytes out, bound by the bytes
-// written.  Unaligned or ragged ends take eight indices at a time, any alignment.
-template <int F, int BITS>
-__global__ void __launch_bounds__(256) k_unpalettize(const uint8_t* idx, uint64_t nbytes, uint64_t n, const float* lut,
-                                                     uint16_t* out, int aligned) {
-    Decoder<F> dec;
-    dec.init(lut, BITS);
-    // a wave's 2048 weights; its j-th store covers 512 consecutive ones, eight per lane
-    const uint64_t base = ((uint64_t)blockIdx.x * 256 + (threadIdx.x & ~63)) * 32;
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint64_t i = base + j * 512 + lane * 8;
-        if (i >= n) return;
-        const s16x8 v = dec.eight(load_idx8(idx, nbytes, i, BITS), BITS);
-        if (aligned && i + 8 <= n) {
-            *reinterpret_cast<s16x8*>(out + i) = v;
-        } else {
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (i + q < n) out[i + q] = (uint16_t)v[q];
-        }
-    }
-}
 
 // ----------------------------------------------------------------------------
 // tiled products
@@ -358,8 +165,6 @@ __device__ __forceinline__ void tile_of(uint32_t w, uint32_t nx, uint32_t ny, ui
 
 // ----------------------------------------------------------------------------
 // epilogue
-
-struct __attribute__((packed)) U16x8 { s16x8 v; };
 
 // Eight outputs from column c of row r on; a PLAIN epilogue only rounds and stores.
 template <int F, bool PLAIN>
@@ -544,222 +349,74 @@ __global__ void __launch_bounds__(64) k_join(ProductArgs p, int splits) {
 }
 
 // ----------------------------------------------------------------------------
-// products of few tokens
+// the gradient at the activation
 
-// Table of pairs (4-bit palettes): entry e holds the values of indices e mod 2^b and e / 2^b, once per LDS
-// bank, so that the lanes of a wave look up without conflicts.
-constexpr int PAIR_BANKS = 32;
-
-// A lane's weights of a run: 32 depths of each of its NT rows, as 16-bit values (BITS 0) or
-// as packed indices.  WHOLE: 32 depths are 4 BITS bytes on a 4-byte boundary (16-bit
-// values: on a 16-byte one), all there or none; else any alignment and end.
-template <int F, int BITS, bool WHOLE>
-struct FewWeights {
-    uint32_t raw[BITS ? 4 : 1];
-    s16x8 w[BITS ? 1 : 4];
-
-    __device__ __forceinline__ void load(const ProductArgs& p, int row, int d) {
-        const int left = p.depth - d;
-        if constexpr (BITS == 0) {
-            const uint16_t* at = p.b + (int64_t)row * p.ldb + d;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (WHOLE) w[j] = left > 0 ? *reinterpret_cast<const s16x8*>(at + j * 8) : s16x8{};
-                else w[j] = row8(at + j * 8, left - j * 8);
-            }
-        } else if constexpr (WHOLE) {
-            const uint32_t* at = reinterpret_cast<const uint32_t*>(p.idx) + ((uint64_t)row * (uint32_t)p.depth + d) / 32 * BITS;
-#pragma unroll
-            for (int j = 0; j < BITS; ++j) raw[j] = left > 0 ? at[j] : 0;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                raw[j] = left > j * 8 ? load_idx8(p.idx, p.idx_bytes, (uint64_t)row * (uint32_t)p.depth + d + j * 8, BITS) : 0;
-        }
-    }
-    // the values of depths 8 j .. 8 j + 7: up to eight entries by lookups in registers,
-    // sixteen from the table of pairs
-    __device__ __forceinline__ s16x8 eight(const Decoder<F>& dec, const uint32_t* mine, int j, int left) const {
-        if constexpr (BITS == 0) {
-            return w[j];
-        } else {
-            typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-            uint32_t v;
-            if (WHOLE) {
-                constexpr int BPJ = 8 * BITS;                 // bits of eight indices
-                const int at = j * BPJ, q = at / 32, sh = at % 32;
-                v = sh + BPJ > 32 ? __builtin_amdgcn_alignbit(raw[q + 1 < 4 ? q + 1 : 3], raw[q], sh) : raw[q] >> sh;
-            } else {
-                v = raw[j];
-            }
-            s16x8 e;
-            if constexpr (BITS < 4) {
-                e = dec.eight(v, BITS);
-            } else {
-                u32x4 r;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) r[i] = mine[__builtin_amdgcn_ubfe(v, 2 * BITS * i, 2 * BITS) * PAIR_BANKS];
-                e = __builtin_bit_cast(s16x8, r);
-            }
-            return WHOLE || left >= 8 ? e : keep_first(e, left);
-        }
-    }
-};
-
-// Up to 16 MT tokens against 16 NT weight rows per workgroup.  The waves share the depths by
-// runs of 128 and add their sums through LDS.  The MFMA takes the weights as its rows: lane
-// l holds row l mod 16, depths 32 (l / 16) + 8 j + 0 .. 7 of a run at its j-th step, so its
-// share of a palette's run is 4 b consecutive bytes.  Bound by the weights' bytes and by the
-// latency of one round: a wave asks for its weights of U runs, and for U more ahead, before
-// it waits for anything, the table included.
-template <int F, int BITS, bool WHOLE, int MT, int NT, int U>
-__global__ void __launch_bounds__(1024) k_few(ProductArgs p) {
-    constexpr int ENTRIES = 1 << (2 * BITS);
-    constexpr int TABLE = BITS == 4 ? ENTRIES * PAIR_BANKS : 0, SUMS = 16 * MT * NT * 256;
-    // the table, and after the last lookup the waves' sums
-    __shared__ __attribute__((aligned(16))) uint32_t lds[TABLE > SUMS ? TABLE : SUMS];
-    __shared__ uint16_t tab[KMAX];
-    uint32_t* pairs = lds;
-    float* red = reinterpret_cast<float*>(lds);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
-    const int l = lane & 15, g = lane >> 4;
-    const int c0 = blockIdx.x * 16 * NT;
-    const int runs = (p.depth + 127) / 128;
-    FewWeights<F, BITS, WHOLE> now[U][NT], next[BITS ? U : 1][BITS ? NT : 1];
-    s16x8 x[U][MT][4];
-    int row[NT];
-    auto load_x = [&](int t0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int d = (t0 + u * nw) * 128 + g * 32, left = p.depth - d;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                // lanes without a token load nothing: what a load costs here is its lanes, not its bytes
-                const int r = i * 16 + l;
-                const uint16_t* at = p.a + (int64_t)r * p.lda + d;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[u][i][j] = s16x8{};
-                if (r < p.rows && left > 0)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (WHOLE) x[u][i][j] = *reinterpret_cast<const s16x8*>(at + j * 8);
-                        else x[u][i][j] = row8(at + j * 8, left - j * 8);
-                    }
-            }
-        }
-    };
-#pragma unroll
-    for (int n = 0; n < NT; ++n) row[n] = min(c0 + n * 16 + l, p.cols - 1);
-    auto load_w = [&](auto& to, int t0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) to[u][n].load(p, row[n], (t0 + u * nw) * 128 + g * 32);
-    };
-    load_w(now, wave);
-    load_x(wave);
-    Decoder<F> dec;
-    if constexpr (BITS == 1 || BITS == 2 || BITS == 3) dec.init(p.lut, BITS);
-    if constexpr (BITS == 4) {
-        if (threadIdx.x < (1 << BITS)) tab[threadIdx.x] = to_16<F>(p.lut[threadIdx.x]);
-        __syncthreads();
-        for (int i = threadIdx.x; i < ENTRIES * PAIR_BANKS; i += blockDim.x) {
-            const int e = i / PAIR_BANKS;
-            pairs[i] = (uint32_t)tab[e & ((1 << BITS) - 1)] | ((uint32_t)tab[e >> BITS] << 16);
-        }
-        __syncthreads();
-    }
-    const uint32_t* mine = pairs + (lane & (PAIR_BANKS - 1));
-    f32x4 acc[MT][NT] = {};
-    for (int t = wave; t < runs; t += nw * U) {
-        if constexpr (BITS != 0) load_w(next, t + nw * U);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int left = p.depth - ((t + u * nw) * 128 + g * 32);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    s16x8 w = now[u][n].eight(dec, mine, j, left - j * 8);
-                    if (BITS && WHOLE && left <= 0) w = s16x8{};
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[i][n] = mfma16<F>(w, x[u][i][j], acc[i][n]);
-                }
-        }
-        if (t + nw * U < runs) {
-            load_x(t + nw * U);
-            if constexpr (BITS != 0) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) now[u][n] = next[u][n];
-            } else {
-                load_w(now, t + nw * U);
-            }
-        }
-    }
-    if (BITS == 4) __syncthreads();
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-            *reinterpret_cast<f32x4*>(red + (((wave * MT + i) * NT + n) * 64 + lane) * 4) = acc[i][n];
-    __syncthreads();
-    for (int e = threadIdx.x; e < min(p.rows, 16 * MT) * NT * 16; e += blockDim.x) {
-        const int n = e % (16 * NT), r = e / (16 * NT), i = r >> 4;
-        const int at = ((i * NT + (n >> 4)) * 64 + ((n & 15) >> 2) * 16 + (r & 15)) * 4 + (n & 3);
-        float z = 0.f;
-        for (int w = 0; w < nw; ++w) z += red[w * MT * NT * 256 + at];
-        const int col = c0 + n;
-        if (col >= p.cols) continue;
-        if (p.bias) z += to_f32<F>(p.bias[col]);
-        if (p.z) p.z[(int64_t)r * p.cols + col] = keep_z<F>(z);
-        float y = act_value(z, p.act);
-        if (p.res) y += to_f32<F>(p.res[(int64_t)r * p.ldr + col]);
-        p.out[(int64_t)r * p.ldo + col] = to_16<F>(y);
-    }
-}
-
-template <int F>
+// A thread takes eight columns of every fourth row of the block's; one pass over dy and z
+// (bound by its bytes: 6 B per element with an activation, 2 B without) writes dz and sums
+// the bias gradient in fp32, unrounded.
+template <int F, int ACT>
 __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
     __shared__ float red[4][DZ_COLS];
-    const int c = blockIdx.x * DZ_COLS + (threadIdx.x & 63), q = threadIdx.x >> 6;
-    const int r0 = blockIdx.y * DZ_ROWS, r1 = min(r0 + DZ_ROWS, a.rows);
-    float sum = 0.f;
-    if (c < a.cols)
+    const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
+    const int c = blockIdx.x * DZ_COLS + lane * 8, left = a.cols - c;
+    const int r0 = blockIdx.y * a.per, r1 = min(r0 + a.per, a.rows);
+    float sum[8] = {};
+    if (left > 0) {
+#pragma unroll 2
         for (int r = r0 + q; r < r1; r += 4) {
-            float d = to_f32<F>(a.dy[(int64_t)r * a.lddy + c]);
-            if (a.act != ACT_NONE) {
-                d *= act_slope(to_f32<F>(a.z[(int64_t)r * a.cols + c]), a.act);
-                a.dz[(int64_t)r * a.cols + c] = to_16<F>(d);
+            const s16x8 d = row8(a.dy + (int64_t)r * a.lddy + c, left);
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = to_f32<F>((uint16_t)d[j]);
+            if (ACT != ACT_NONE) {
+                const s16x8 z = row8(a.z + (int64_t)r * a.cols + c, left);
+                uint16_t* out = a.dz + (int64_t)r * a.cols + c;
+                s16x8 o;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] *= act_slope(to_f32<F>((uint16_t)z[j]), ACT);
+                    o[j] = (short)to_16<F>(v[j]);
+                }
+                if (left >= 8) {
+                    reinterpret_cast<U16x8*>(out)->v = o;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < left) out[j] = (uint16_t)o[j];
+                }
             }
-            sum += d;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += v[j];
         }
-    red[q][threadIdx.x & 63] = sum;
+    }
+    if (!a.dbias) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) red[q][lane * 8 + j] = sum[j];
     __syncthreads();
-    if (a.dbias && q == 0 && c < a.cols)
-        a.part[(int64_t)blockIdx.y * a.cols + c] =
-            (red[0][threadIdx.x] + red[1][threadIdx.x]) + (red[2][threadIdx.x] + red[3][threadIdx.x]);
+    for (int i = threadIdx.x; i < DZ_COLS; i += 256)
+        if (blockIdx.x * DZ_COLS + i < (uint32_t)a.cols)
+            a.part[(int64_t)blockIdx.y * a.cols + blockIdx.x * DZ_COLS + i] = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
 }
 
+// 32 columns per workgroup, their chunks shared by eight threads each
 template <int F>
 __global__ void __launch_bounds__(256) k_dbias(DzArgs a, int chunks) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= a.cols) return;
+    __shared__ float red[8][32];
+    const int l = threadIdx.x & 31, q = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
     float sum = 0.f;
-    for (int i = 0; i < chunks; ++i) sum += a.part[(int64_t)i * a.cols + c];
-    a.dbias[c] = to_16<F>(sum);
+    if (c < a.cols)
+        for (int i = q; i < chunks; i += 8) sum += a.part[(int64_t)i * a.cols + c];
+    red[q][l] = sum;
+    __syncthreads();
+    if (q == 0 && c < a.cols) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) sum += red[i][l];
+        a.dbias[c] = to_16<F>(sum);
+    }
 }
 
 // ----------------------------------------------------------------------------
 // launches
-
-#define EDKM_GO(kern, grid, block, ...)                       \
-    do {                                                       \
-        hipLaunchKernelGGL(kern, grid, block, 0, s, __VA_ARGS__); \
-        const hipError_t e_ = hipGetLastError();               \
-        if (e_ != hipSuccess) return e_;                       \
-    } while (0)
 
 template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT>
 static hipError_t tiled(const ProductArgs& p, const ProductPlan& q, hipStream_t s) {
@@ -777,48 +434,9 @@ static hipError_t product_ab(const ProductArgs& p, const ProductPlan& q, hipStre
     return q.direct ? tiled<F, OPA, OPB, 128, 2, 2, true>(p, q, s) : tiled<F, OPA, OPB, 128, 2, 2, false>(p, q, s);
 }
 
-template <int F, int BITS, bool WHOLE, int MT, int NT>
-static hipError_t few_go(const ProductArgs& p, hipStream_t s) {
-    constexpr int U = WHOLE && BITS && MT == 1 ? 2 : 1;
-    const int runs = (p.depth + 127) / 128;
-    int nw = 1;
-    while (nw < runs && nw < 16) nw *= 2;
-    EDKM_GO((k_few<F, BITS, WHOLE, MT, NT, U>), dim3((uint32_t)(((int64_t)p.cols + 16 * NT - 1) / (16 * NT))), dim3(nw * 64), p);
-    return hipSuccess;
-}
-
-template <int F, int BITS, bool WHOLE>
-static hipError_t few_bits(const ProductArgs& p, hipStream_t s) {
-    const int64_t tiles = ((int64_t)p.cols + 15) / 16;
-    if (!WHOLE) {
-        if (p.rows <= 16) return few_go<F, BITS, WHOLE, 1, 1>(p, s);
-        return p.rows <= 32 ? few_go<F, BITS, WHOLE, 2, 1>(p, s) : few_go<F, BITS, WHOLE, 4, 1>(p, s);
-    }
-    if (p.rows <= 16) {
-        if (tiles <= 256) return few_go<F, BITS, WHOLE, 1, 1>(p, s);
-        return tiles <= 512 || !BITS ? few_go<F, BITS, WHOLE, 1, 2>(p, s) : few_go<F, BITS, WHOLE, 1, 3>(p, s);
-    }
-    const bool wide = tiles >= 512;
-    if (p.rows <= 32) return wide ? few_go<F, BITS, WHOLE, 2, 2>(p, s) : few_go<F, BITS, WHOLE, 2, 1>(p, s);
-    return few_go<F, BITS, WHOLE, 4, 1>(p, s);
-}
-
-template <int F>
-static hipError_t few(const ProductArgs& p, int bits, hipStream_t s) {
-    const bool x16 = ((uintptr_t)p.a & 15) == 0 && p.lda % 8 == 0 && p.depth % 32 == 0;
-    const bool whole = x16 && (bits ? ((uintptr_t)p.idx & 3) == 0 : ((uintptr_t)p.b & 15) == 0 && p.ldb % 8 == 0);
-    switch (bits) {
-    case 1: return whole ? few_bits<F, 1, true>(p, s) : few_bits<F, 1, false>(p, s);
-    case 2: return whole ? few_bits<F, 2, true>(p, s) : few_bits<F, 2, false>(p, s);
-    case 3: return whole ? few_bits<F, 3, true>(p, s) : few_bits<F, 3, false>(p, s);
-    case 4: return whole ? few_bits<F, 4, true>(p, s) : few_bits<F, 4, false>(p, s);
-    default: return whole ? few_bits<F, 0, true>(p, s) : few_bits<F, 0, false>(p, s);
-    }
-}
-
 template <int F>
 static hipError_t product_f(ProductArgs p, int opa, int opb, float* part, hipStream_t s) {
-    if (opa == OP_ROWS && opb != OP_DEPTH && p.rows <= FEW) return few<F>(p, opb == OP_PALETTE ? p.bits : 0, s);
+    if (opa == OP_ROWS && opb != OP_DEPTH && p.rows <= FEW) return launch_few(p, F, opb == OP_PALETTE ? p.bits : 0, s);
     const ProductPlan q = product_plan(p, opa, opb);
     p.split_steps = q.split_steps;
     p.part = q.splits > 1 ? part : nullptr;
@@ -863,33 +481,21 @@ ProductPlan product_plan(const ProductArgs& p, int opa, int opb) {
 
 template <int F>
 static hipError_t dz_f(const DzArgs& a, hipStream_t s) {
-    const int chunks = (a.rows + DZ_ROWS - 1) / DZ_ROWS;
+    const int chunks = (a.rows + a.per - 1) / a.per;
     if (chunks > 0 && (a.dbias || a.act != ACT_NONE))
-        EDKM_GO(k_dz<F>, dim3((a.cols + DZ_COLS - 1) / DZ_COLS, chunks), dim3(256), a);
-    if (a.dbias) EDKM_GO(k_dbias<F>, dim3((a.cols + 255) / 256), dim3(256), a, chunks);
+    {
+        const dim3 grid((a.cols + DZ_COLS - 1) / DZ_COLS, chunks);
+        if (a.act == ACT_NONE) EDKM_GO((k_dz<F, ACT_NONE>), grid, dim3(256), a);
+        else if (a.act == ACT_RELU) EDKM_GO((k_dz<F, ACT_RELU>), grid, dim3(256), a);
+        else if (a.act == ACT_GELU) EDKM_GO((k_dz<F, ACT_GELU>), grid, dim3(256), a);
+        else EDKM_GO((k_dz<F, ACT_SILU>), grid, dim3(256), a);
+    }
+    if (a.dbias) EDKM_GO(k_dbias<F>, dim3((a.cols + 31) / 32), dim3(256), a, chunks);
     return hipSuccess;
 }
 
 hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s) {
     return fmt == FMT_BF16 ? dz_f<FMT_BF16>(a, s) : dz_f<FMT_FP16>(a, s);
-}
-
-template <int F>
-static hipError_t unpalettize_f(const uint8_t* idx, uint64_t nb, uint64_t n, int bits, const float* lut, uint16_t* out,
-                                hipStream_t s) {
-    const dim3 grid((uint32_t)((n + 8191) / 8192));
-    const int al = ((uintptr_t)out & 15) == 0;
-    if (bits == 1) EDKM_GO((k_unpalettize<F, 1>), grid, dim3(256), idx, nb, n, lut, out, al);
-    else if (bits == 2) EDKM_GO((k_unpalettize<F, 2>), grid, dim3(256), idx, nb, n, lut, out, al);
-    else if (bits == 3) EDKM_GO((k_unpalettize<F, 3>), grid, dim3(256), idx, nb, n, lut, out, al);
-    else EDKM_GO((k_unpalettize<F, 4>), grid, dim3(256), idx, nb, n, lut, out, al);
-    return hipSuccess;
-}
-
-hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
-                              uint16_t* out, hipStream_t s) {
-    return fmt == FMT_BF16 ? unpalettize_f<FMT_BF16>(idx, idx_bytes, n, bits, lut, out, s)
-                           : unpalettize_f<FMT_FP16>(idx, idx_bytes, n, bits, lut, out, s);
 }
 
 }  // namespace edkm

@@ -3,6 +3,8 @@
 
 #include "edkm_product.h"
 
+#include <type_traits>
+
 namespace edkm {
 
 // Thirty-two weights per thread: 4 b bytes of indices, 64 bytes out, bound by the bytes
@@ -33,40 +35,43 @@ __global__ void __launch_bounds__(256) k_unpalettize(const uint8_t* idx, uint64_
 // ----------------------------------------------------------------------------
 // products of few tokens
 
-// Table of pairs (4-bit palettes): entry e holds the values of indices e mod 2^b and e / 2^b, once per LDS
+// Table of pairs: entry e holds the values of indices e mod 2^b and e / 2^b, once per LDS
 // bank, so that the lanes of a wave look up without conflicts.
 constexpr int PAIR_BANKS = 32;
 
-// A lane's weights of a run: 32 depths of each of its NT rows, as 16-bit values (BITS 0) or
-// as packed indices.  WHOLE: 32 depths are 4 BITS bytes on a 4-byte boundary (16-bit
-// values: on a 16-byte one), all there or none; else any alignment and end.
+// A lane's weights of a run: 32 depths of one row, as 16-bit values (BITS 0) or as packed
+// indices.  WHOLE: 32 depths are 4 BITS bytes on a 4-byte boundary (16-bit values: 64 bytes
+// on a 16-byte one), and offsets from the workgroup's first row fit 32 bits; else any
+// alignment and end.
 template <int F, int BITS, bool WHOLE>
 struct FewWeights {
     uint32_t raw[BITS ? 4 : 1];
     s16x8 w[BITS ? 1 : 4];
 
-    __device__ __forceinline__ void load(const ProductArgs& p, int row, int d) {
+    // `at`: the run's bytes of the first row (the same for all lanes), `off`: the lane's from there
+    __device__ __forceinline__ void load_whole(const char* at, uint32_t off) {
+        if constexpr (BITS == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const s16x8*>(at + off + j * 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < BITS; ++j) raw[j] = *reinterpret_cast<const uint32_t*>(at + off + j * 4);
+        }
+    }
+    __device__ __forceinline__ void load_any(const ProductArgs& p, int row, int d) {
         const int left = p.depth - d;
         if constexpr (BITS == 0) {
             const uint16_t* at = p.b + (int64_t)row * p.ldb + d;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (WHOLE) w[j] = left > 0 ? *reinterpret_cast<const s16x8*>(at + j * 8) : s16x8{};
-                else w[j] = row8(at + j * 8, left - j * 8);
-            }
-        } else if constexpr (WHOLE) {
-            const uint32_t* at = reinterpret_cast<const uint32_t*>(p.idx) + ((uint64_t)row * (uint32_t)p.depth + d) / 32 * BITS;
-#pragma unroll
-            for (int j = 0; j < BITS; ++j) raw[j] = left > 0 ? at[j] : 0;
+            for (int j = 0; j < 4; ++j) w[j] = row8(at + j * 8, left - j * 8);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 raw[j] = left > j * 8 ? load_idx8(p.idx, p.idx_bytes, (uint64_t)row * (uint32_t)p.depth + d + j * 8, BITS) : 0;
         }
     }
-    // the values of depths 8 j .. 8 j + 7: up to eight entries by lookups in registers,
-    // sixteen from the table of pairs
-    __device__ __forceinline__ s16x8 eight(const Decoder<F>& dec, const uint32_t* mine, int j, int left) const {
+    // the values of depths 8 j .. 8 j + 7
+    __device__ __forceinline__ s16x8 eight(const char* mine, int j) const {
         if constexpr (BITS == 0) {
             return w[j];
         } else {
@@ -75,20 +80,19 @@ struct FewWeights {
             if (WHOLE) {
                 constexpr int BPJ = 8 * BITS;                 // bits of eight indices
                 const int at = j * BPJ, q = at / 32, sh = at % 32;
-                v = sh + BPJ > 32 ? __builtin_amdgcn_alignbit(raw[q + 1 < 4 ? q + 1 : 3], raw[q], sh) : raw[q] >> sh;
+                v = sh + BPJ > 32 ? __builtin_amdgcn_alignbit(raw[q + 1 < 4 ? q + 1 : 3], raw[q], sh) : sh ? raw[q] >> sh : raw[q];
             } else {
                 v = raw[j];
             }
-            s16x8 e;
-            if constexpr (BITS < 4) {
-                e = dec.eight(v, BITS);
-            } else {
-                u32x4 r;
+            u32x4 r;
+            constexpr uint32_t MASK = ((1u << (2 * BITS)) - 1) * (PAIR_BANKS * 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) r[i] = mine[__builtin_amdgcn_ubfe(v, 2 * BITS * i, 2 * BITS) * PAIR_BANKS];
-                e = __builtin_bit_cast(s16x8, r);
+            for (int i = 0; i < 4; ++i) {
+                const int sh = 2 * BITS * i - 7;              // the pair times 128 bytes
+                const uint32_t e = (sh < 0 ? v << (sh < 0 ? -sh : 0) : v >> (sh < 0 ? 0 : sh)) & MASK;
+                r[i] = *reinterpret_cast<const uint32_t*>(mine + e);
             }
-            return WHOLE || left >= 8 ? e : keep_first(e, left);
+            return __builtin_bit_cast(s16x8, r);
         }
     }
 };
@@ -96,22 +100,17 @@ struct FewWeights {
 // Up to 16 MT tokens against 16 NT weight rows per workgroup.  The waves share the depths by
 // runs of 128 and add their sums through LDS.  The MFMA takes the weights as its rows: lane
 // l holds row l mod 16, depths 32 (l / 16) + 8 j + 0 .. 7 of a run at its j-th step, so its
-// share of a palette's run is 4 b consecutive bytes.  Bound by the weights' bytes and by the
-// latency of one round: a wave asks for its weights of U runs, and for U more ahead, before
-// it waits for anything, the table included.
-//
-// XL: the tokens (up to FEW_X bytes) wait in LDS.  Read from memory they are four times the
-// bytes of a 4-bit palette, lane by lane, and each round waits for them.
-constexpr int FEW_X = 48 * 1024;
-__host__ __device__ constexpr int few_x_row(int depth) { return depth * 2 + 16; }   // bytes: rows fall on different banks
-
-template <int F, int BITS, bool WHOLE, int MT, int NT, int U, int NW, bool XL>
+// share of a palette's run is 4 b consecutive bytes.  A wave asks for its weights of U runs,
+// and for U more ahead, before it waits for anything, the table included.  Bound by the
+// weights' bytes where they are 16 bits; a palette's few bytes leave the vector instructions
+// as the bound (two a weight pair and its lookup), so addresses are one 32-bit offset per
+// row from a pointer that all lanes share.
+template <int F, int BITS, bool WHOLE, int MT, int NT, int U, int NW>
 __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
     constexpr int ENTRIES = 1 << (2 * BITS);
-    constexpr int TABLE = BITS == 4 ? ENTRIES * PAIR_BANKS : 0, SUMS = NW * MT * NT * 256, XW = XL ? FEW_X / 4 : 0;
-    // the table and the tokens, and after the last of them the waves' sums
-    __shared__ __attribute__((aligned(16))) uint32_t lds[TABLE + XW > SUMS ? TABLE + XW : SUMS];
-    char* xl = reinterpret_cast<char*>(lds + TABLE);
+    constexpr int TABLE = BITS ? ENTRIES * PAIR_BANKS : 0, SUMS = NW * MT * NT * 256;
+    // the table, and after the last lookup the waves' sums
+    __shared__ __attribute__((aligned(128))) uint32_t lds[TABLE > SUMS ? TABLE : SUMS];
     __shared__ uint16_t tab[KMAX];
     uint32_t* pairs = lds;
     float* red = reinterpret_cast<float*>(lds);
@@ -119,61 +118,62 @@ __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
     const int l = lane & 15, g = lane >> 4;
     const int c0 = blockIdx.x * 16 * NT;
     const int runs = (p.depth + 127) / 128;
+    constexpr int RUN_BYTES = BITS ? 16 * BITS : 256;        // of one row
+    const uint32_t row_bytes = BITS ? (uint32_t)((uint64_t)p.depth * BITS / 8) : (uint32_t)(p.ldb * 2);
+    const char* wat = BITS ? reinterpret_cast<const char*>(p.idx) + (uint64_t)c0 * row_bytes
+                           : reinterpret_cast<const char*>(p.b) + (int64_t)c0 * p.ldb * 2;
     FewWeights<F, BITS, WHOLE> now[U][NT], next[BITS ? U : 1][BITS ? NT : 1];
     s16x8 x[U][MT][4];
+    uint32_t woff[NT], xoff[MT];
     int row[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        row[n] = min(c0 + n * 16 + l, p.cols - 1);
+        woff[n] = (uint32_t)(row[n] - c0) * row_bytes + g * (RUN_BYTES / 4);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xoff[i] = (uint32_t)(min(i * 16 + l, p.rows - 1) * (int)p.lda + g * 32) * 2;
+    // Depths past the end (WHOLE: all 32 of a lane, in the last run): the lane reads the
+    // run's first ones instead, and its values are cleared before the product.
+    auto back = [&](int t) { return t * 128 + 128 > p.depth && t * 128 + g * 32 >= p.depth; };
     auto load_x = [&](int t0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int d = (t0 + u * nw) * 128 + g * 32, left = p.depth - d;
-            if constexpr (XL) {
-                // lanes without a token repeat the first one's: their columns are not used
-                const char* at = xl + (l < p.rows ? l : 0) * few_x_row(p.depth) + min(d, p.depth - 32) * 2;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[u][0][j] = *reinterpret_cast<const s16x8*>(at + j * 16);
-                    if (left <= 0) x[u][0][j] = s16x8{};
-                }
-                continue;
-            }
+            const int t = min(t0 + u * nw, runs - 1);
+            const bool b = back(t);
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                // lanes without a token load nothing: what a load costs here is its lanes, not its bytes
-                const int r = i * 16 + l;
-                const uint16_t* at = p.a + (int64_t)r * p.lda + d;
+                // lanes without a token load nothing (their columns are not used): what a load costs is its lanes
+                if (i * 16 + l >= p.rows) continue;
+                if constexpr (WHOLE) {
+                    const char* at = reinterpret_cast<const char*>(p.a) + (int64_t)t * 256;
+                    const uint32_t off = xoff[i] - (b ? g * 64 : 0);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[u][i][j] = s16x8{};
-                if (r < p.rows && left > 0)
+                    for (int j = 0; j < 4; ++j) x[u][i][j] = *reinterpret_cast<const s16x8*>(at + off + j * 16);
+                } else {
+                    const int d = t * 128 + g * 32;
+                    const uint16_t* at = p.a + (int64_t)(i * 16 + l) * p.lda + d;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (WHOLE) x[u][i][j] = *reinterpret_cast<const s16x8*>(at + j * 8);
-                        else x[u][i][j] = row8(at + j * 8, left - j * 8);
-                    }
+                    for (int j = 0; j < 4; ++j) x[u][i][j] = row8(at + j * 8, p.depth - d - j * 8);
+                }
             }
         }
     };
-#pragma unroll
-    for (int n = 0; n < NT; ++n) row[n] = min(c0 + n * 16 + l, p.cols - 1);
     auto load_w = [&](auto& to, int t0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            const int t = min(t0 + u * nw, runs - 1);
+            const bool b = back(t);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) to[u][n].load(p, row[n], (t0 + u * nw) * 128 + g * 32);
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (WHOLE) to[u][n].load_whole(wat + (int64_t)t * RUN_BYTES, woff[n] - (b ? g * (RUN_BYTES / 4) : 0));
+                else to[u][n].load_any(p, row[n], t * 128 + g * 32);
+            }
+        }
     };
     load_w(now, wave);
-    if constexpr (XL) {
-        const int pieces = p.depth / 8;
-        for (int i = threadIdx.x; i < p.rows * pieces; i += blockDim.x) {
-            const int r = i / pieces, q = i % pieces;
-            *reinterpret_cast<s16x8*>(xl + r * few_x_row(p.depth) + q * 16) = *reinterpret_cast<const s16x8*>(p.a + (int64_t)r * p.lda + q * 8);
-        }
-        if (BITS != 4) __syncthreads();
-    } else {
-        load_x(wave);
-    }
-    Decoder<F> dec;
-    if constexpr (BITS == 1 || BITS == 2 || BITS == 3) dec.init(p.lut, BITS);
-    if constexpr (BITS == 4) {
+    load_x(wave);
+    if constexpr (BITS != 0) {
         if (threadIdx.x < (1 << BITS)) tab[threadIdx.x] = to_16<F>(p.lut[threadIdx.x]);
         __syncthreads();
         for (int i = threadIdx.x; i < ENTRIES * PAIR_BANKS; i += blockDim.x) {
@@ -182,25 +182,39 @@ __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
         }
         __syncthreads();
     }
-    if constexpr (XL) load_x(wave);
-    const uint32_t* mine = pairs + (lane & (PAIR_BANKS - 1));
+    const char* mine = reinterpret_cast<const char*>(pairs + (lane & (PAIR_BANKS - 1)));
     f32x4 acc[MT][NT] = {};
+    // one run; TAIL: only the lane's first `left` depths count (WHOLE: all or none)
+    auto run = [&](int u, int left, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            s16x8 xj[MT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                xj[i] = x[u][i][j];
+                if (TAIL) xj[i] = WHOLE ? (left > 0 ? xj[i] : s16x8{}) : keep_first(xj[i], left - j * 8);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s16x8 w = now[u][n].eight(mine, j);
+                if (TAIL) w = WHOLE ? (left > 0 ? w : s16x8{}) : keep_first(w, left - j * 8);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc[i][n] = mfma16<F>(w, xj[i], acc[i][n]);
+            }
+        }
+    };
     for (int t = wave; t < runs; t += nw * U) {
-        if constexpr (BITS != 0) load_w(next, t + nw * U);
+        const bool more = t + nw * U < runs;
+        if constexpr (BITS != 0)
+            if (more) load_w(next, t + nw * U);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int left = p.depth - ((t + u * nw) * 128 + g * 32);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    s16x8 w = now[u][n].eight(dec, mine, j, left - j * 8);
-                    if (BITS && WHOLE && left <= 0) w = s16x8{};
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[i][n] = mfma16<F>(w, x[u][i][j], acc[i][n]);
-                }
+            const int tu = t + u * nw;
+            if (tu * 128 + 128 <= p.depth) run(u, 0, std::false_type{});
+            else if (tu < runs) run(u, p.depth - (tu * 128 + g * 32), std::true_type{});
         }
-        if (t + nw * U < runs) {
+        if (more) {
             load_x(t + nw * U);
             if constexpr (BITS != 0) {
 #pragma unroll
@@ -212,7 +226,7 @@ __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
             }
         }
     }
-    if (BITS == 4 || XL) __syncthreads();
+    if (BITS) __syncthreads();
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -234,41 +248,35 @@ __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
     }
 }
 
-template <int F, int BITS, bool WHOLE, int MT, int NT, int U, int NW, bool XL>
+template <int F, int BITS, bool WHOLE, int MT, int NT>
 static hipError_t few_go(const ProductArgs& p, hipStream_t s) {
+    constexpr int U = WHOLE && BITS && MT == 1 && NT < 3 ? 2 : 1, NW = MT == 1 ? 16 : 8;
     const int runs = (p.depth + 127) / 128;
     int nw = 1;
     while (nw < runs && nw < NW) nw *= 2;
-    EDKM_GO((k_few<F, BITS, WHOLE, MT, NT, U, NW, XL>), dim3((uint32_t)(((int64_t)p.cols + 16 * NT - 1) / (16 * NT))), dim3(nw * 64), p);
+    EDKM_GO((k_few<F, BITS, WHOLE, MT, NT, U, NW>), dim3((uint32_t)(((int64_t)p.cols + 16 * NT - 1) / (16 * NT))), dim3(nw * 64), p);
     return hipSuccess;
+}
+
+// Weight rows of a workgroup: as many as leave a workgroup per CU, so that the tokens are
+// read and the table is made for more of them.
+template <int F, int BITS, bool WHOLE, int MT>
+static hipError_t few_rows(const ProductArgs& p, hipStream_t s) {
+    const int64_t tiles = ((int64_t)p.cols + 15) / 16;
+    if (!WHOLE || tiles <= 256) return few_go<F, BITS, WHOLE, MT, 1>(p, s);
+    return tiles <= 512 || (MT == 1 && !BITS) ? few_go<F, BITS, WHOLE, MT, WHOLE ? 2 : 1>(p, s) : few_go<F, BITS, WHOLE, MT, WHOLE ? 3 : 1>(p, s);
 }
 
 template <int F, int BITS, bool WHOLE>
 static hipError_t few_bits(const ProductArgs& p, hipStream_t s) {
-    const int64_t tiles = ((int64_t)p.cols + 15) / 16;
-    if constexpr (!WHOLE) {
-        if (p.rows <= 16) return few_go<F, BITS, WHOLE, 1, 1, 1, 16, false>(p, s);
-        return p.rows <= 32 ? few_go<F, BITS, WHOLE, 2, 1, 1, 8, false>(p, s) : few_go<F, BITS, WHOLE, 4, 1, 1, 8, false>(p, s);
-    } else {
-        constexpr int U1 = BITS ? 3 : 1, U2 = BITS ? 2 : 1;
-        const bool xl = BITS && (int64_t)p.rows * few_x_row(p.depth) <= FEW_X;
-        if (p.rows <= 16) {
-            if (tiles <= 256) return xl ? few_go<F, BITS, WHOLE, 1, 1, U1, 16, BITS != 0>(p, s) : few_go<F, BITS, WHOLE, 1, 1, U2, 16, false>(p, s);
-            if (tiles <= 512 || !BITS) return xl ? few_go<F, BITS, WHOLE, 1, 2, U2, 16, BITS != 0>(p, s) : few_go<F, BITS, WHOLE, 1, 2, U2, 16, false>(p, s);
-            return xl ? few_go<F, BITS, WHOLE, 1, 3, U2, 16, BITS != 0>(p, s) : few_go<F, BITS, WHOLE, 1, 3, U2, 16, false>(p, s);
-        }
-        if (p.rows <= 32) {
-            if (tiles <= 256) return few_go<F, BITS, WHOLE, 2, 1, 1, 8, false>(p, s);
-            return tiles <= 512 ? few_go<F, BITS, WHOLE, 2, 2, 1, 8, false>(p, s) : few_go<F, BITS, WHOLE, 2, 3, 1, 8, false>(p, s);
-        }
-        if (tiles <= 256) return few_go<F, BITS, WHOLE, 4, 1, 1, 8, false>(p, s);
-        return tiles <= 512 ? few_go<F, BITS, WHOLE, 4, 2, 1, 8, false>(p, s) : few_go<F, BITS, WHOLE, 4, 3, 1, 8, false>(p, s);
-    }
+    if (p.rows <= 16) return few_rows<F, BITS, WHOLE, 1>(p, s);
+    return p.rows <= 32 ? few_rows<F, BITS, WHOLE, 2>(p, s) : few_rows<F, BITS, WHOLE, 4>(p, s);
 }
 
 template <int F>
 static hipError_t few(const ProductArgs& p, int bits, hipStream_t s) {
-    const bool x16 = ((uintptr_t)p.a & 15) == 0 && p.lda % 8 == 0 && p.depth % 32 == 0;
+    // 32-bit offsets: 64 rows of at most 2^25 bytes
+    const bool x16 = ((uintptr_t)p.a & 15) == 0 && p.lda % 8 == 0 && p.depth % 32 == 0 && p.lda < (1 << 24) && p.ldb < (1 << 24);
     const bool whole = x16 && (bits ? ((uintptr_t)p.idx & 3) == 0 : ((uintptr_t)p.b & 15) == 0 && p.ldb % 8 == 0);
     switch (bits) {
     case 1: return whole ? few_bits<F, 1, true>(p, s) : few_bits<F, 1, false>(p, s);

@@ -33,6 +33,12 @@ Other workloads (--workload; one JSON line each, same fields):
                               packed b-bit nearest-centroid indices per weight
   unique_inverse              the decoder layer's distinct patterns and 16-bit inverse
                               index per weight (the uniquification's lists)
+  train_step [--bits] [--tokens 2048] [--state-bits 8|32]
+                              the decoder layer's seven matrices clustered (dkm_batch),
+                              multiplied with a sequence's tokens (linear, no attention),
+                              backward, and the AdamW step on fp32 masters
+  serve [--bits] [--tokens 1] the layer's seven products from exported palettes
+                              (palette_linear), captured in a HIP graph
 
 Other modes (measurement helpers):
   --copy-calibration          run a plain 1 GiB device copy (HBM counter calibration)
@@ -81,13 +87,13 @@ COPY_BYTES = 1 << 30
 
 
 def source_hash():
-    """Hash of the product build's kernel code: comments, blank lines and the
+    """Hash of the clustering's kernel code: comments, blank lines and the
     block-timeline instrumentation (the EDKM_BLOCK_STAMPS sections and the
     EDKM_STAMP_* statements, which the product build compiles to nothing) are
     left out, so the counters stay tied to what the product compiles."""
     h = hashlib.sha256()
-    for f in sorted(glob.glob(os.path.join(ROOT, "paper_2309_00964_amd", "csrc", "*"))):
-        text = open(f).read()
+    for f in ("edkm_api.hip", "edkm_internal.h", "edkm_kernels.hip", "edkm_partition.h"):
+        text = open(os.path.join(ROOT, "paper_2309_00964_amd", "csrc", f)).read()
         text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
         text = re.sub(r"//[^\n]*", "", text)
         text = re.sub(r"#ifdef EDKM_BLOCK_STAMPS\n.*?#endif", "", text, flags=re.S)
@@ -596,6 +602,103 @@ def bench_stack(args):
     return out
 
 
+def _layer_weights(fmt, config=4):
+    """The decoder layer's seven weight matrices on the GPU, by name."""
+    import torch
+    from paper_2309_00964_amd import inputs
+    dt = torch.bfloat16 if fmt == "bf16" else torch.float16
+    return {name: inputs.fp16_weights_device(r * c, inputs.weight_seed(config, i), "cuda", fmt=fmt).view(dt).view(r, c)
+            for i, (name, r, c) in enumerate(inputs.LLAMA7B_LAYER)}
+
+
+def _layer_products(x, product):
+    """The layer's seven products on tokens x; attention and the gate's multiplication with
+    its neighbour stand for nothing but their shapes."""
+    a = product("v_proj", product("k_proj", product("q_proj", x, None, "none"), None, "none"), None, "none")
+    h = product("o_proj", a, x, "none")
+    return product("down_proj", product("gate_proj", h, None, "silu") * product("up_proj", h, None, "none"), h, "none")
+
+
+def _timed_steps(step, args):
+    """Seconds for args.steps calls of step() between two events."""
+    import torch
+    for _ in range(args.warmup):
+        step()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    torch.cuda.synchronize()
+    begin.record()
+    for _ in range(args.steps):
+        step()
+    end.record()
+    torch.cuda.synchronize()
+    return begin.elapsed_time(end) / 1e3
+
+
+def _token_line(args, metric, tokens, bits, elapsed, flops, extra):
+    cfg = {"workload": "llama7b_decoder_layer", "bits": bits, "tokens": tokens, "weights_dtype": args.key_format,
+           "parallelism": "single_gpu"}
+    cfg.update(extra)
+    return {"metric": metric, "value": tokens * args.steps / elapsed, "unit": "tokens/s", "n_gpus": 1, "steps": args.steps,
+            "warmup": args.warmup, "ms_per_step": elapsed * 1e3 / args.steps, "higher_is_better": True, "scaling": "weak",
+            "vs_baseline": None, "dtype": args.key_format, "data": "synthetic", "config": cfg,
+            "product_tflops": flops * args.steps / elapsed / 1e12}
+
+
+def bench_train_step(args):
+    """A training step of the clustered decoder layer: clustering, products, their
+    gradients, the clustering's gradient and the optimizer's step."""
+    import torch
+    from paper_2309_00964_amd import function, inputs
+    from paper_2309_00964_amd.optim import AdamW
+    bits, tokens = args.bits or 3, args.tokens or 2048
+    ws = {k: torch.nn.Parameter(w) for k, w in _layer_weights(args.key_format).items()}
+    c0 = [inputs.quantile_init_device(w.detach().view(torch.int16).view(-1), 1 << bits, args.key_format) for w in ws.values()]
+    opt = AdamW(ws.values(), lr=1e-5, state_bits=args.state_bits, master_weights=True)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(inputs.grad_seed(4, 99))
+    x, dy = ((torch.randn(tokens, 4096, generator=gen, device="cuda") * s).to(next(iter(ws.values())).dtype) for s in (1.0, 1e-3))
+    x.requires_grad_(True)
+
+    def step():
+        opt.zero_grad()
+        x.grad = None
+        wt = dict(zip(ws, function.dkm_batch(ws.values(), c0, inputs.TAU, inputs.ITERS, out_half=True)[0]))
+        _layer_products(x, lambda name, t, res, act: function.linear(t, wt[name], None, res, act)).backward(dy)
+        opt.step()
+    flops = 6 * tokens * sum(w.numel() for w in ws.values())
+    return _token_line(args, "clustered training step, tokens per second", tokens, bits, _timed_steps(step, args), flops,
+                       {"state_bits": args.state_bits, "iters": inputs.ITERS, "attention": None})
+
+
+def bench_serve(args):
+    """The decoder layer's products from its exported palettes, as a captured graph."""
+    import torch
+    from paper_2309_00964_amd import edkm, function, inputs
+    bits, tokens = args.bits or 3, args.tokens or 1
+    pal, rows = {}, {}
+    for name, w in _layer_weights(args.key_format).items():
+        keys = w.view(torch.int16).view(-1)
+        lut = inputs.quantile_init_device(keys, 1 << bits, args.key_format)
+        idx = torch.empty((keys.numel() * bits + 7) // 8, dtype=torch.uint8, device="cuda")
+        edkm.palettize_noalloc(keys, keys.numel(), bits, lut, idx, key_format=args.key_format)
+        pal[name], rows[name], dt = (idx, lut), w.shape[0], w.dtype
+    x = torch.randn(tokens, 4096, device="cuda").to(dt)
+
+    def layer():
+        return _layer_products(x, lambda name, t, res, act: function.palette_linear(t, *pal[name], rows[name], None, res, act))
+    with torch.no_grad():
+        layer()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            layer()
+    flops = 2 * tokens * sum(r * c for _, r, c in inputs.LLAMA7B_LAYER)
+    elapsed = _timed_steps(graph.replay, args)
+    read = sum(idx.numel() for idx, _ in pal.values())
+    return _token_line(args, "layer products from palettes, tokens per second", tokens, bits, elapsed, flops,
+                       {"palette_bytes": read, "palette_GBps": read * args.steps / elapsed / 1e9, "attention": None})
+
+
 def copy_calibration():
     import torch
     a = torch.empty(COPY_BYTES // 4, dtype=torch.float32, device="cuda").fill_(1.0)
@@ -903,11 +1006,14 @@ def main():
     ap.add_argument("--steps", type=int, default=50)
     ap.add_argument("--warmup", type=int, default=5)
     ap.add_argument("--workload", choices=("decoder_layer", "single_256x256", "attn_proj_4096x4096",
-                                           "mlp_outliers", "stack", "palettize", "unique_inverse"),
+                                           "mlp_outliers", "stack", "palettize", "unique_inverse", "train_step",
+                                           "serve"),
                     default="decoder_layer")
     ap.add_argument("--bits", type=int, choices=(1, 2, 3, 4), default=None,
                     help="mlp_outliers: 3 or 4 (default 4); stack: 2, 3 or 4 (default 3); "
                          "palettize: 1-4 (default 3)")
+    ap.add_argument("--tokens", type=int, default=None, help="train_step (default 2048), serve (default 1)")
+    ap.add_argument("--state-bits", type=int, choices=(8, 32), default=8, help="train_step: the optimizer's states")
     ap.add_argument("--key-format", choices=("fp16", "bf16"), default="fp16",
                     help="weight format (default fp16, the metric's; bf16 is the paper's training format)")
     ap.add_argument("--w-tilde", choices=("fp32", "half"), default="fp32",
@@ -951,7 +1057,8 @@ def main():
           "single_256x256": lambda a: bench_single_matrix(a, 1, 3),
           "attn_proj_4096x4096": lambda a: bench_single_matrix(a, 2, 3),
           "stack": bench_stack, "palettize": bench_palettize,
-          "unique_inverse": bench_unique_inverse}[args.workload]
+          "unique_inverse": bench_unique_inverse, "train_step": bench_train_step,
+          "serve": bench_serve}[args.workload]
     if args.workload == "decoder_layer" and args.bits not in (None, 3):
         sys.exit("the decoder-layer workload is 3-bit")
     if args.block_timeline:

@@ -1,0 +1,202 @@
+"""optim.AdamW: against torch's AdamW in fp32 and float64, parameters that skip steps,
+several groups, saving and loading, captured steps, and a training step of clustered
+layers from dkm_batch over linear to the weights' update."""
+import copy
+import sys
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import layer_util as L                                             # noqa: E402
+from paper_2309_00964_amd import edkm, inputs                      # noqa: E402
+from paper_2309_00964_amd.function import dkm_batch, linear, palette_linear   # noqa: E402
+from paper_2309_00964_amd.optim import AdamW                       # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def say(*a):
+    print("[gpu-case]", *a, flush=True)
+    sys.stdout.flush()
+
+
+def params(seed, dtype, sizes=((17, 33), (5000,), (1,))):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.nn.Parameter((torch.randn(s, generator=g) * 0.1).to(DEV, dtype)) for s in sizes]
+
+
+def grads(ps, seed):
+    g = torch.Generator().manual_seed(seed)
+    for p in ps:
+        p.grad = (torch.randn(p.shape, generator=g) * 0.01).to(DEV, p.dtype)
+
+
+def test_equals_torch_in_fp32():
+    """Five steps against torch.optim.AdamW in float64: each step moves p by at most lr and
+    adds a few fp32 roundings of p."""
+    ps = params(1, torch.float32)
+    ref = [torch.nn.Parameter(p.detach().double()) for p in ps]
+    a = AdamW(ps, lr=1e-2, betas=(0.8, 0.95), eps=1e-6, weight_decay=0.1)
+    b = torch.optim.AdamW(ref, lr=1e-2, betas=(0.8, 0.95), eps=1e-6, weight_decay=0.1)
+    for i in range(5):
+        say("against torch", i)
+        grads(ps, 10 + i)
+        for p, r in zip(ps, ref):
+            r.grad = p.grad.double()
+        a.step()
+        b.step()
+        for p, r in zip(ps, ref):
+            # per step: three roundings of p (2^-24 each) and 8 ulps of an update of at most lr / (1 - beta1);
+            # m and v carry up to 3 roundings each per step so far
+            tol = (i + 1) * (3 * 2.0 ** -24 * r.abs() + (8 + 6 * (i + 1)) * 2.0 ** -23 * 1e-2 * 5)
+            L.assert_within(p.detach(), r.detach(), tol, "p")
+
+
+def test_parameters_that_skip_steps_keep_their_own_count():
+    say("skipped steps")
+    ps = params(2, torch.float32)
+    ref = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    a, b = AdamW(ps, lr=1e-2), torch.optim.AdamW(ref, lr=1e-2)
+    for i, present in enumerate([(0, 1), (0, 1, 2), (1,), (0, 2), (0, 1, 2)]):
+        grads(ps, 20 + i)
+        for j, (p, r) in enumerate(zip(ps, ref)):
+            if j not in present:
+                p.grad = None
+            r.grad = None if p.grad is None else p.grad.clone()
+        a.step()
+        b.step()
+    torch.cuda.synchronize()
+    for p, r in zip(ps, ref):
+        assert int(a.state[p]["step"]) == int(b.state[r]["step"])
+        torch.testing.assert_close(p, r, rtol=1e-5, atol=1e-6)
+
+
+def test_groups_of_one_cohort_count_a_step_once():
+    say("groups")
+    ps = params(3, torch.float32) + params(4, torch.bfloat16)
+    a = AdamW([dict(params=ps[:2], lr=1e-2), dict(params=ps[2:], weight_decay=0.0)], lr=1e-3, master_weights=True)
+    for i in range(3):
+        grads(ps, 30 + i)
+        a.step()
+    torch.cuda.synchronize()
+    assert [int(a.state[p]["step"]) for p in ps] == [3] * len(ps)
+    assert "master" not in a.state[ps[0]] and a.state[ps[4]]["master"].dtype == torch.float32
+    assert torch.equal(ps[4].detach().view(-1), a.state[ps[4]]["master"].to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_save_and_load(bits):
+    say("save and load", bits)
+    ps = params(5, torch.bfloat16)
+    a = AdamW(ps, lr=1e-2, state_bits=bits, master_weights=True, seed=3)
+    for i in range(2):
+        grads(ps, 40 + i)
+        a.step()
+    qs = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    b = AdamW(qs, lr=1e-2, state_bits=bits, master_weights=True, seed=3)
+    b.load_state_dict(copy.deepcopy(a.state_dict()))
+    for p, q in zip(ps, qs):
+        for name, value in a.state[p].items():
+            got = b.state[q][name]
+            assert got.dtype == value.dtype and torch.equal(got.view(torch.uint8), value.view(torch.uint8)), name
+    for opt, xs in ((a, ps), (b, qs)):
+        grads(xs, 50)
+        opt.step()
+    torch.cuda.synchronize()
+    for p, q in zip(ps, qs):
+        assert torch.equal(p, q) and int(a.state[p]["step"]) == int(b.state[q]["step"]) == 3
+
+
+def test_captured_steps():
+    """A captured step with the rate on the device against the same steps outside a graph;
+    states cannot be made within a capture."""
+    say("captured optimizer")
+    ps = params(6, torch.float16)
+    qs = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    lr = torch.full((1,), 1e-3, device=DEV)
+    a, b = (AdamW(x, lr=lr, state_bits=8, master_weights=True) for x in (ps, qs))
+    for opt, xs in ((a, ps), (b, qs)):
+        grads(xs, 60)
+        opt.step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step()
+    for i in range(3):
+        lr.fill_(1e-3 / (i + 1))
+        for p, q in zip(ps, qs):
+            p.grad.mul_(-0.7)
+            q.grad.mul_(-0.7)
+        graph.replay()
+        b.step()
+        torch.cuda.synchronize()
+        for p, q in zip(ps, qs):
+            assert torch.equal(p, q), i
+    c = AdamW(params(7, torch.float16))
+    grads(c.param_groups[0]["params"], 70)
+    with pytest.raises(RuntimeError, match="first step outside"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            lr.add_(1.0)
+            c.step()
+    torch.cuda.synchronize()
+
+
+def test_a_step_between_forward_and_backward_is_noticed():
+    say("version check")
+    (p,) = params(8, torch.float32, ((4, 4),))
+    a = AdamW([p])
+    y = (p * p).sum()
+    p.grad = torch.ones_like(p)
+    a.step()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+def test_training_step_of_clustered_layers(fmt):
+    """Two clustered layers and their optimizer step, as a program uses them together: the
+    loss's gradients against a 64-bit graph on the same W~, and weights that move by the
+    optimizer's rule; then the clustered weights exported and served."""
+    dt, tok, d, hid = L.DT[fmt], 70, 96, 136
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    rnd = lambda *s, scale=1.0: (torch.randn(s, generator=g, device=DEV) * scale).to(dt)  # noqa: E731
+    ws = [torch.nn.Parameter(rnd(hid, d, scale=0.02)), torch.nn.Parameter(rnd(d, hid, scale=0.02))]
+    bias = torch.nn.Parameter(rnd(hid, scale=0.1))
+    c0 = [inputs.quantile_init_device(w.detach().view(torch.int16).view(-1), 8, fmt) for w in ws]
+    opt = AdamW([*ws, bias], lr=1e-3, state_bits=8, master_weights=True)
+    x, dy = rnd(tok, d), rnd(tok, d)
+    for i in range(2):
+        say("training step", fmt, i)
+        opt.zero_grad()
+        before = [w.detach().clone() for w in ws]
+        wt, c, _ = dkm_batch(ws, c0, inputs.TAU, 3, out_half=True)
+        h = linear(x, wt[0], bias, None, "silu")
+        y = linear(h, wt[1], None, x)
+        wts = [w.detach() for w in wt]
+        y.backward(dy)
+        # the products' gradients on the same W~ in 64 bits, with the kept 16-bit h
+        ref = L.gradients(dy, h.detach(), wts[1], h.detach().double() @ wts[1].double().t(), "none")
+        z1 = x.double() @ wts[0].double().t() + bias.detach().double()
+        got_dh = torch.empty_like(h)
+        edkm.linear_backward(dy, None, wts[1], dx=got_dh)
+        L.assert_within(got_dh, *ref["dx"], "dL/dh")
+        db = L.gradients(got_dh, x, wts[0], z1, "silu")["db"]
+        L.assert_within(bias.grad, *db, "dL/dbias")
+        assert all(w.grad is not None and w.grad.dtype == dt and bool(w.grad.isfinite().all()) for w in ws)
+        opt.step()
+        assert all(not torch.equal(w.detach(), b) for w, b in zip(ws, before))
+        c0 = [v.detach() for v in c]
+    # export and serve: palette indices against the final centroids
+    plan = edkm.Plan(ws[0].numel(), 3, 1, key_format=fmt)
+    packed = torch.empty((ws[0].numel() * 3 + 7) // 8, dtype=torch.uint8, device=DEV)
+    edkm.palettize(plan, ws[0].detach().view(torch.int16).view(-1), c0[0], packed)
+    w16 = torch.empty(hid, d, dtype=dt, device=DEV)
+    edkm.unpalettize(packed, c0[0], w16)
+    for rows in (1, 5, tok):
+        with torch.no_grad():
+            out = palette_linear(x[:rows], packed, c0[0], hid, bias, None, "silu")
+        L.assert_within(out, *L.product(x[:rows], w16, bias.detach(), None, "silu")[1:], "served")

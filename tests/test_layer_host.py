@@ -194,3 +194,24 @@ def test_function_refusals():
     ]:
         with pytest.raises(ValueError, match=what):
             call()
+
+
+def test_optimizer_refusals():
+    from paper_2309_00964_amd.optim import AdamW
+    p = torch.nn.Parameter(torch.zeros(4))
+    for kw, what in ((dict(state_bits=16), "state_bits"), (dict(lr=-1.0), "lr"), (dict(lr=float("nan")), "lr"), (dict(betas=(1.0, 0.9)), "betas"),
+                     (dict(eps=-1.0), "eps"), (dict(weight_decay=float("inf")), "weight_decay"),
+                     (dict(lr=torch.zeros(2)), "tensor lr")):
+        with pytest.raises(ValueError, match=what):
+            AdamW([p], **kw)
+    with pytest.raises(ValueError, match="float64"):
+        AdamW([torch.nn.Parameter(torch.zeros(4, dtype=torch.float64))])
+    opt = AdamW([p])
+    opt.step()                       # no gradient: nothing to do
+    p.grad = torch.zeros(4)
+    with pytest.raises(ValueError, match="GPU tensors"):
+        opt.step()
+    q = torch.nn.Parameter(torch.zeros(4, dtype=torch.float16))
+    q.grad = torch.zeros(4, dtype=torch.float16)
+    with pytest.raises(ValueError, match="GPU tensors"):
+        AdamW([q]).step()

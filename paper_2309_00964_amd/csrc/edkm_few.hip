@@ -3,12 +3,13 @@
 
 #include "edkm_product.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace edkm {
 
-// Thirty-two weights per thread: 4 b bytes of indices, 64 bytes out, bound by the bytes
-// written.  Unaligned or ragged ends take eight indices at a time, any alignment.
+// Thirty-two weights per thread, eight at a time: bound by the bytes written.  Unaligned
+// indices and ragged ends take any alignment.
 template <int F, int BITS>
 __global__ void __launch_bounds__(256) k_unpalettize(const uint8_t* idx, uint64_t nbytes, uint64_t n, const float* lut,
                                                      uint16_t* out, int aligned) {
@@ -29,6 +30,28 @@ __global__ void __launch_bounds__(256) k_unpalettize(const uint8_t* idx, uint64_
             for (int q = 0; q < 8; ++q)
                 if (i + q < n) out[i + q] = (uint16_t)v[q];
         }
+    }
+}
+
+// The rows of a matrix (16-bit values, or with BITS a palette's) from rows of any length
+// and alignment to rows of whole 16-byte pieces, zeros behind their ends: what the tiled
+// products' loads want, for one pass over the operand.
+template <int F, int BITS>
+__global__ void __launch_bounds__(256) k_align_rows(const uint16_t* m, int64_t ld, const uint8_t* idx, uint64_t nbytes, const float* lut,
+                                                    int rows, int cols, uint16_t* out) {
+    Decoder<F> dec;
+    if constexpr (BITS != 0) dec.init(lut, BITS);
+    const uint32_t pieces = ((uint32_t)cols + 7) / 8;
+    const uint64_t total = (uint64_t)rows * pieces;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (uint64_t)gridDim.x * 256) {
+        const uint32_t r = (uint32_t)(i / pieces), c = (uint32_t)(i % pieces) * 8;
+        const int left = cols - (int)c;
+        s16x8 v;
+        if constexpr (BITS != 0)
+            v = keep_first(dec.eight(load_idx8(idx, nbytes, (uint64_t)r * (uint32_t)cols + c, BITS), BITS), left);
+        else
+            v = row8(m + (int64_t)r * ld + c, left);
+        *reinterpret_cast<s16x8*>(out + i * 8) = v;
     }
 }
 
@@ -307,6 +330,34 @@ hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n
                               uint16_t* out, hipStream_t s) {
     return fmt == FMT_BF16 ? unpalettize_f<FMT_BF16>(idx, idx_bytes, n, bits, lut, out, s)
                            : unpalettize_f<FMT_FP16>(idx, idx_bytes, n, bits, lut, out, s);
+}
+
+static uint32_t align_grid(int64_t rows, int64_t cols) {
+    return (uint32_t)std::min<int64_t>((rows * ((cols + 7) / 8) + 255) / 256, 8192);
+}
+
+hipError_t launch_align_rows(const uint16_t* m, int64_t ld, int64_t rows, int64_t cols, uint16_t* out, hipStream_t s) {
+    EDKM_GO((k_align_rows<FMT_BF16, 0>), dim3(align_grid(rows, cols)), dim3(256), m, ld, (const uint8_t*)nullptr, (uint64_t)0,
+            (const float*)nullptr, (int)rows, (int)cols, out);
+    return hipSuccess;
+}
+
+template <int F>
+static hipError_t unpalettize_rows_f(const uint8_t* idx, uint64_t nb, int rows, int cols, int bits, const float* lut, uint16_t* out,
+                                     hipStream_t s) {
+    const dim3 grid(align_grid(rows, cols));
+    const uint16_t* none = nullptr;
+    if (bits == 1) EDKM_GO((k_align_rows<F, 1>), grid, dim3(256), none, (int64_t)0, idx, nb, lut, rows, cols, out);
+    else if (bits == 2) EDKM_GO((k_align_rows<F, 2>), grid, dim3(256), none, (int64_t)0, idx, nb, lut, rows, cols, out);
+    else if (bits == 3) EDKM_GO((k_align_rows<F, 3>), grid, dim3(256), none, (int64_t)0, idx, nb, lut, rows, cols, out);
+    else EDKM_GO((k_align_rows<F, 4>), grid, dim3(256), none, (int64_t)0, idx, nb, lut, rows, cols, out);
+    return hipSuccess;
+}
+
+hipError_t launch_unpalettize_rows(const uint8_t* idx, uint64_t nb, int64_t rows, int64_t cols, int bits, int fmt, const float* lut,
+                                   uint16_t* out, hipStream_t s) {
+    return fmt == FMT_BF16 ? unpalettize_rows_f<FMT_BF16>(idx, nb, (int)rows, (int)cols, bits, lut, out, s)
+                           : unpalettize_rows_f<FMT_FP16>(idx, nb, (int)rows, (int)cols, bits, lut, out, s);
 }
 
 }  // namespace edkm

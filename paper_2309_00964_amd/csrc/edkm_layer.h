@@ -34,6 +34,7 @@ struct ProductArgs {
     int64_t ldo;
     uint16_t* z;
     int act;
+    int padded;             // OP_ROWS operands hold zeros up to the next multiple of eight depths
     // a split product: steps of 64 depths per part, and the parts' sums (null: not split)
     int split_steps;
     float* part;
@@ -57,6 +58,7 @@ struct DzArgs {
     int64_t lddy;
     const uint16_t* z;
     uint16_t* dz;
+    int64_t lddz;           // a multiple of eight: dz's rows are followed by zeros up to it
     float* part;            // [chunks][cols]
     uint16_t* dbias;
     int32_t rows, cols;
@@ -109,6 +111,9 @@ hipError_t launch_few(const ProductArgs& a, int fmt, int bits, hipStream_t s);
 hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s);
 hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
                               uint16_t* out, hipStream_t s);
+hipError_t launch_align_rows(const uint16_t* m, int64_t ld, int64_t rows, int64_t cols, uint16_t* out, hipStream_t s);
+hipError_t launch_unpalettize_rows(const uint8_t* idx, uint64_t idx_bytes, int64_t rows, int64_t cols, int bits, int fmt,
+                                   const float* lut, uint16_t* out, hipStream_t s);
 hipError_t launch_adamw(const AdamwArgs& a, uint32_t grid, int param_type, int grad_type, int state_bits, hipStream_t s);
 hipError_t launch_adamw_tick(int32_t* step, hipStream_t s);
 

@@ -39,18 +39,50 @@ size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 int64_t dz_chunks(int64_t m, int64_t n) { return (m + dz_rows(m, n) - 1) / dz_rows(m, n); }
 
-// Workspace of a backward: dz, the bias gradient's partial sums, and those of the two
+int64_t up8(int64_t v) { return (v + 7) & ~(int64_t)7; }
+
+// Rows whose length is no multiple of eight cannot be loaded by 16-byte pieces: a product
+// first copies them to rows that can.
+size_t aligned_bytes(int64_t rows, int64_t cols) { return cols % 8 ? up256((size_t)rows * up8(cols) * 2) : 0; }
+
+// Workspace of a forward: aligned copies of x and w, then a split product's sums.
+struct ForwardWs {
+    size_t x, w, split, total;
+};
+ForwardWs forward_ws(int64_t m, int64_t n, int64_t k) {
+    ForwardWs f;
+    f.x = 0;
+    f.w = f.x + aligned_bytes(m, k);
+    f.split = f.w + aligned_bytes(n, k);
+    f.total = f.split + up256(product_part_bytes(m, n, k));
+    return f;
+}
+
+// Workspace of a backward: dz (written with an activation, copied where dy's rows need it),
+// the bias gradient's partial sums, aligned copies of x and w, and the split sums of the two
 // products in turn.
 struct BackwardWs {
-    size_t dz, part, split, total;
+    size_t dz, part, x, w, split, total;
 };
 BackwardWs backward_ws(int64_t m, int64_t n, int64_t k, int act) {
     BackwardWs w;
     w.dz = 0;
-    w.part = act == ACT_NONE ? 0 : up256((size_t)m * n * 2);
-    w.split = w.part + up256((size_t)dz_chunks(m, n) * n * 4);
+    w.part = act == ACT_NONE ? aligned_bytes(m, n) : up256((size_t)m * up8(n) * 2);
+    w.x = w.part + up256((size_t)dz_chunks(m, n) * n * 4);
+    w.w = w.x + aligned_bytes(m, k);
+    w.split = w.w + aligned_bytes(n, k);
     w.total = w.split + up256(std::max(m ? product_part_bytes(m, k, n) : 0, product_part_bytes(n, k, m)));
     return w;
+}
+
+// Copies a matrix's rows to `to` if their length asks for it, and points there.
+hipError_t align_rows(const uint16_t*& p, int64_t& ld, int64_t rows, int64_t cols, char* to, hipStream_t stream) {
+    if (cols % 8 == 0) return hipSuccess;
+    uint16_t* out = reinterpret_cast<uint16_t*>(to);
+    const hipError_t e = launch_align_rows(p, ld, rows, cols, out, stream);
+    p = out;
+    ld = up8(cols);
+    return e;
 }
 
 edkm_status ws_ok(const void* ws, size_t have, size_t need) {
@@ -64,7 +96,7 @@ extern "C" {
 
 size_t edkm_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) {
     if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m <= FEW) return 0;
-    return up256(product_part_bytes(m, n, k));
+    return forward_ws(m, n, k).total;
 }
 
 edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activation, const void* x, int64_t ldx,
@@ -91,7 +123,14 @@ edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activat
     p.ldo = ldy;
     p.z = static_cast<uint16_t*>(z);
     p.act = activation;
-    return launch_product(p, format, OP_ROWS, OP_ROWS, static_cast<float*>(ws), stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    if (m <= FEW) return launch_product(p, format, OP_ROWS, OP_ROWS, nullptr, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    const ForwardWs f = forward_ws(m, n, k);
+    char* base = static_cast<char*>(ws);
+    p.padded = 1;
+    if (align_rows(p.a, p.lda, m, k, base + f.x, stream) != hipSuccess || align_rows(p.b, p.ldb, n, k, base + f.w, stream) != hipSuccess)
+        return EDKM_ERR_HIP;
+    return launch_product(p, format, OP_ROWS, OP_ROWS, reinterpret_cast<float*>(base + f.split), stream) == hipSuccess ? EDKM_OK
+                                                                                                                       : EDKM_ERR_HIP;
 }
 
 size_t edkm_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int activation) {
@@ -122,31 +161,33 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
     d.cols = (int32_t)n;
     d.act = activation;
     d.per = dz_rows(m, n);
+    d.lddz = up8(n);
     if (launch_dz(d, format, stream) != hipSuccess) return EDKM_ERR_HIP;
+    if (!dx && !dw) return EDKM_OK;
     float* parts = reinterpret_cast<float*>(base + L.split);
     const uint16_t* dz = activation == ACT_NONE ? d.dy : d.dz;
-    const int64_t lddz = activation == ACT_NONE ? lddy : n;
+    int64_t lddz = activation == ACT_NONE ? lddy : d.lddz;
+    if (activation == ACT_NONE && m > 0 && align_rows(dz, lddz, m, n, base + L.dz, stream) != hipSuccess) return EDKM_ERR_HIP;
+    ProductArgs p{};
+    p.a = dz;
+    p.lda = lddz;
+    p.cols = (int32_t)k;
+    p.padded = 1;
     if (dx && m > 0) {
-        ProductArgs p{};
-        p.a = dz;
-        p.lda = lddz;
         p.b = static_cast<const uint16_t*>(w);
         p.ldb = ldw;
+        if (align_rows(p.b, p.ldb, n, k, base + L.w, stream) != hipSuccess) return EDKM_ERR_HIP;
         p.rows = (int32_t)m;
-        p.cols = (int32_t)k;
         p.depth = (int32_t)n;
         p.out = static_cast<uint16_t*>(dx);
         p.ldo = lddx;
         if (launch_product(p, format, OP_ROWS, OP_DEPTH, parts, stream) != hipSuccess) return EDKM_ERR_HIP;
     }
     if (dw) {
-        ProductArgs p{};
-        p.a = dz;
-        p.lda = lddz;
         p.b = static_cast<const uint16_t*>(x);
         p.ldb = ldx;
+        if (m > 0 && align_rows(p.b, p.ldb, m, k, base + L.x, stream) != hipSuccess) return EDKM_ERR_HIP;
         p.rows = (int32_t)n;
-        p.cols = (int32_t)k;
         p.depth = (int32_t)m;
         p.out = static_cast<uint16_t*>(dw);
         p.ldo = k;
@@ -157,8 +198,8 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
 
 size_t edkm_palette_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int bits) {
     if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m <= FEW || bits < 1 || bits > EDKM_MAX_BITS) return 0;
-    // the decoded weights (rows of whole 16-byte pieces need no padding: n x k without gaps), then the split's sums
-    return up256((size_t)n * k * 2) + up256(product_part_bytes(m, n, k));
+    // the decoded weights, in rows of whole 16-byte pieces; an aligned copy of x; a split's sums
+    return up256((size_t)n * up8(k) * 2) + aligned_bytes(m, k) + up256(product_part_bytes(m, n, k));
 }
 
 edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int format, int activation, const void* x,
@@ -191,12 +232,18 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
     p.z = static_cast<uint16_t*>(z);
     p.act = activation;
     if (m <= FEW) return launch_product(p, format, OP_ROWS, OP_PALETTE, nullptr, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    char* base = static_cast<char*>(ws);
     uint16_t* w = static_cast<uint16_t*>(ws);
-    if (launch_unpalettize(indices, p.idx_bytes, (uint64_t)n * k, bits, format, lut, w, stream) != hipSuccess) return EDKM_ERR_HIP;
+    char* xs = base + up256((size_t)n * up8(k) * 2);
+    const hipError_t e = k % 8 ? launch_unpalettize_rows(indices, p.idx_bytes, n, k, bits, format, lut, w, stream)
+                               : launch_unpalettize(indices, p.idx_bytes, (uint64_t)n * k, bits, format, lut, w, stream);
     p.b = w;
-    p.ldb = k;
-    float* parts = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)n * k * 2));
-    return launch_product(p, format, OP_ROWS, OP_ROWS, parts, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    p.ldb = up8(k);
+    p.padded = 1;
+    if (e != hipSuccess || align_rows(p.a, p.lda, m, k, xs, stream) != hipSuccess) return EDKM_ERR_HIP;
+    return launch_product(p, format, OP_ROWS, OP_ROWS, reinterpret_cast<float*>(xs + aligned_bytes(m, k)), stream) == hipSuccess
+               ? EDKM_OK
+               : EDKM_ERR_HIP;
 }
 
 edkm_status edkm_unpalettize(const uint8_t* indices, uint64_t n, int bits, int format, const float* lut, uint16_t* w_out,

@@ -340,6 +340,7 @@ __global__ void __launch_bounds__(64) k_join(ProductArgs p, int splits) {
     f32x4 acc[4] = {};
     const float* at = p.part + ((int64_t)w * NW + wave) * (TR * 1024) + i * 1024 + lane * 4;
     const int64_t stride = (int64_t)nx * ny * NW * (TR * 1024);
+#pragma unroll 4
     for (int s = 0; s < splits; ++s)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] += *reinterpret_cast<const f32x4*>(at + s * stride + j * 256);
@@ -370,20 +371,14 @@ __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
             for (int j = 0; j < 8; ++j) v[j] = to_f32<F>((uint16_t)d[j]);
             if (ACT != ACT_NONE) {
                 const s16x8 z = row8(a.z + (int64_t)r * a.cols + c, left);
-                uint16_t* out = a.dz + (int64_t)r * a.cols + c;
+                uint16_t* out = a.dz + (int64_t)r * a.lddz + c;
                 s16x8 o;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     v[j] *= act_slope(to_f32<F>((uint16_t)z[j]), ACT);
                     o[j] = (short)to_16<F>(v[j]);
                 }
-                if (left >= 8) {
-                    reinterpret_cast<U16x8*>(out)->v = o;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < left) out[j] = (uint16_t)o[j];
-                }
+                *reinterpret_cast<s16x8*>(out) = left >= 8 ? o : keep_first(o, left);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += v[j];
@@ -398,21 +393,23 @@ __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
             a.part[(int64_t)blockIdx.y * a.cols + blockIdx.x * DZ_COLS + i] = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
 }
 
-// 32 columns per workgroup, their chunks shared by eight threads each
+// 32 columns per workgroup, their chunks shared by 32 threads each
 template <int F>
-__global__ void __launch_bounds__(256) k_dbias(DzArgs a, int chunks) {
-    __shared__ float red[8][32];
+__global__ void __launch_bounds__(1024) k_dbias(DzArgs a, int chunks) {
+    __shared__ float red[32][33];
     const int l = threadIdx.x & 31, q = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
     float sum = 0.f;
     if (c < a.cols)
-        for (int i = q; i < chunks; i += 8) sum += a.part[(int64_t)i * a.cols + c];
+#pragma unroll 4
+        for (int i = q; i < chunks; i += 32) sum += a.part[(int64_t)i * a.cols + c];
     red[q][l] = sum;
     __syncthreads();
-    if (q == 0 && c < a.cols) {
+    // column q's 32 sums lie in this half wave
+    sum = red[l][q];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) sum += red[i][l];
-        a.dbias[c] = to_16<F>(sum);
-    }
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor(sum, o, 32);
+    const int mine = blockIdx.x * 32 + q;
+    if (l == 0 && mine < a.cols) a.dbias[mine] = to_16<F>(sum);
 }
 
 // ----------------------------------------------------------------------------
@@ -429,8 +426,7 @@ static hipError_t tiled(const ProductArgs& p, const ProductPlan& q, hipStream_t 
 
 template <int F, int OPA, int OPB>
 static hipError_t product_ab(const ProductArgs& p, const ProductPlan& q, hipStream_t s) {
-    if (q.tile == 256)
-        return q.direct ? tiled<F, OPA, OPB, 256, 2, 4, true>(p, q, s) : tiled<F, OPA, OPB, 256, 2, 4, false>(p, q, s);
+    if (q.tile == 256) return tiled<F, OPA, OPB, 256, 2, 4, true>(p, q, s);
     return q.direct ? tiled<F, OPA, OPB, 128, 2, 2, true>(p, q, s) : tiled<F, OPA, OPB, 128, 2, 2, false>(p, q, s);
 }
 
@@ -449,12 +445,16 @@ hipError_t launch_product(const ProductArgs& p, int fmt, int opa, int opb, float
     return fmt == FMT_BF16 ? product_f<FMT_BF16>(p, opa, opb, part, s) : product_f<FMT_FP16>(p, opa, opb, part, s);
 }
 
-// A tile and a split of the depths from the sizes alone, so that a workspace can be sized
-// before the call.
-static void shape_plan(int64_t rows, int64_t cols, int64_t depth, ProductPlan& q) {
+// A tile and a split of the depths.  What bounds a tile is bringing its operands into LDS,
+// whose bytes per product fall with the tile's side, so the larger one where it gives most
+// CUs a tile; two of the smaller share a CU, and its depths are split where they are few.
+// Unaligned operands, whose way through registers the larger tile has no room for, take
+// the smaller.
+static void shape_plan(int64_t rows, int64_t cols, int64_t depth, bool direct, ProductPlan& q) {
     auto tiles = [&](int64_t b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
     const int64_t steps = std::max<int64_t>(1, (depth + 63) / 64);
-    q.tile = tiles(256) >= 192 ? 256 : 128;
+    q.direct = direct;
+    q.tile = direct && tiles(256) >= 192 ? 256 : 128;
     q.splits = 1;
     const int64_t t = tiles(q.tile);
     if (q.tile == 128 && t < 256) q.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / t, steps / 4, 64}));
@@ -463,19 +463,22 @@ static void shape_plan(int64_t rows, int64_t cols, int64_t depth, ProductPlan& q
 }
 
 size_t product_part_bytes(int64_t rows, int64_t cols, int64_t depth) {
-    ProductPlan q{};
-    shape_plan(rows, cols, depth, q);
-    if (q.splits <= 1) return 0;
-    return (size_t)((rows + q.tile - 1) / q.tile) * ((cols + q.tile - 1) / q.tile) * q.tile * q.tile * 4 * q.splits;
+    size_t most = 0;
+    for (const bool direct : {false, true}) {
+        ProductPlan q{};
+        shape_plan(rows, cols, depth, direct, q);
+        if (q.splits > 1)
+            most = std::max(most, (size_t)((rows + q.tile - 1) / q.tile) * ((cols + q.tile - 1) / q.tile) * q.tile * q.tile * 4 * q.splits);
+    }
+    return most;
 }
 
 ProductPlan product_plan(const ProductArgs& p, int opa, int opb) {
     ProductPlan q{};
-    shape_plan(p.rows, p.cols, p.depth, q);
     auto whole = [&](const void* m, int64_t ld, int op) {
-        return ((uintptr_t)m & 15) == 0 && ld % 8 == 0 && ld <= (1 << 22) && (op == OP_DEPTH || p.depth % 8 == 0);
+        return ((uintptr_t)m & 15) == 0 && ld % 8 == 0 && ld <= (1 << 22) && (op == OP_DEPTH || p.depth % 8 == 0 || p.padded);
     };
-    q.direct = whole(p.a, p.lda, opa) && whole(p.b, p.ldb, opb);
+    shape_plan(p.rows, p.cols, p.depth, whole(p.a, p.lda, opa) && whole(p.b, p.ldb, opb), q);
     return q;
 }
 
@@ -490,7 +493,7 @@ static hipError_t dz_f(const DzArgs& a, hipStream_t s) {
         else if (a.act == ACT_GELU) EDKM_GO((k_dz<F, ACT_GELU>), grid, dim3(256), a);
         else EDKM_GO((k_dz<F, ACT_SILU>), grid, dim3(256), a);
     }
-    if (a.dbias) EDKM_GO(k_dbias<F>, dim3((a.cols + 31) / 32), dim3(256), a, chunks);
+    if (a.dbias) EDKM_GO(k_dbias<F>, dim3((a.cols + 31) / 32), dim3(1024), a, chunks);
     return hipSuccess;
 }
 

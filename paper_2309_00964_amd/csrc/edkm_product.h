@@ -6,14 +6,12 @@
 
 namespace edkm {
 
-
 typedef __attribute__((ext_vector_type(8))) short s16x8;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 struct __attribute__((packed)) S16x8 { s16x8 v; };   // at any address
-struct __attribute__((packed)) U16x8 { s16x8 v; };
 
 // ----------------------------------------------------------------------------
 // the two 16-bit formats

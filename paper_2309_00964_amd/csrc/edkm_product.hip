@@ -175,14 +175,14 @@ __device__ __forceinline__ void finish8(const ProductArgs& p, int r, int c, floa
         s16x8 v;
         if (!PLAIN) {
             if (p.bias) {
-                v = reinterpret_cast<const U16x8*>(p.bias + c)->v;
+                v = reinterpret_cast<const S16x8*>(p.bias + c)->v;
 #pragma unroll
                 for (int q = 0; q < 8; ++q) z[q] += to_f32<F>((uint16_t)v[q]);
             }
             if (p.z) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q) v[q] = (short)keep_z<F>(z[q]);
-                reinterpret_cast<U16x8*>(p.z + (int64_t)r * p.cols + c)->v = v;
+                reinterpret_cast<S16x8*>(p.z + (int64_t)r * p.cols + c)->v = v;
             }
             if (p.act == ACT_RELU) {
 #pragma unroll
@@ -195,14 +195,14 @@ __device__ __forceinline__ void finish8(const ProductArgs& p, int r, int c, floa
                 for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], ACT_SILU);
             }
             if (p.res) {
-                v = reinterpret_cast<const U16x8*>(p.res + (int64_t)r * p.ldr + c)->v;
+                v = reinterpret_cast<const S16x8*>(p.res + (int64_t)r * p.ldr + c)->v;
 #pragma unroll
                 for (int q = 0; q < 8; ++q) z[q] += to_f32<F>((uint16_t)v[q]);
             }
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = (short)to_16<F>(z[q]);
-        reinterpret_cast<U16x8*>(out)->v = v;
+        reinterpret_cast<S16x8*>(out)->v = v;
         return;
     }
 #pragma unroll
@@ -359,8 +359,10 @@ template <int F, int ACT>
 __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
     __shared__ float red[4][DZ_COLS];
     const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
-    const int c = blockIdx.x * DZ_COLS + lane * 8, left = a.cols - c;
-    const int r0 = blockIdx.y * a.per, r1 = min(r0 + a.per, a.rows);
+    // workgroups go column block by column block through a chunk of rows
+    const uint32_t nc = (a.cols + DZ_COLS - 1) / DZ_COLS, cb = blockIdx.x % nc, chunk = blockIdx.x / nc;
+    const int c = cb * DZ_COLS + lane * 8, left = a.cols - c;
+    const int r0 = chunk * a.per, r1 = min(r0 + a.per, a.rows);
     float sum[8] = {};
     if (left > 0) {
 #pragma unroll 2
@@ -389,8 +391,8 @@ __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
     for (int j = 0; j < 8; ++j) red[q][lane * 8 + j] = sum[j];
     __syncthreads();
     for (int i = threadIdx.x; i < DZ_COLS; i += 256)
-        if (blockIdx.x * DZ_COLS + i < (uint32_t)a.cols)
-            a.part[(int64_t)blockIdx.y * a.cols + blockIdx.x * DZ_COLS + i] = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
+        if (cb * DZ_COLS + i < (uint32_t)a.cols)
+            a.part[(int64_t)chunk * a.cols + cb * DZ_COLS + i] = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
 }
 
 // 32 columns per workgroup, their chunks shared by 32 threads each
@@ -487,7 +489,7 @@ static hipError_t dz_f(const DzArgs& a, hipStream_t s) {
     const int chunks = (a.rows + a.per - 1) / a.per;
     if (chunks > 0 && (a.dbias || a.act != ACT_NONE))
     {
-        const dim3 grid((a.cols + DZ_COLS - 1) / DZ_COLS, chunks);
+        const dim3 grid((uint32_t)((a.cols + DZ_COLS - 1) / DZ_COLS) * chunks);
         if (a.act == ACT_NONE) EDKM_GO((k_dz<F, ACT_NONE>), grid, dim3(256), a);
         else if (a.act == ACT_RELU) EDKM_GO((k_dz<F, ACT_RELU>), grid, dim3(256), a);
         else if (a.act == ACT_GELU) EDKM_GO((k_dz<F, ACT_GELU>), grid, dim3(256), a);

@@ -69,6 +69,8 @@ def gradients(dy, x, w, z, name):
     h, t = half(x.dtype), tiny(x.dtype)
     m, n = dy.shape
     dy, x, w = dy.double(), x.double(), w.double()
+    if z is None:            # without activation it is not looked at
+        z = torch.zeros_like(dy)
     dz = dy * slope(z, name)
     e0 = dy.abs() * (CURVE[name] * (2 * h * z.abs() + t + 2.0 ** -20) + 2.0 ** -20 * (name != "none"))
     if name == "relu":       # within z's error of 0 the slope is one side's or the other's

@@ -354,3 +354,154 @@ def test_captured_and_replayed(m, n, k):
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, outs)), i
+
+
+def test_many_rows_of_few_columns():
+    """More row chunks than a grid's second dimension holds: 5M tokens of 8 outputs."""
+    m, n, k, dt = 5_000_011, 8, 8, torch.bfloat16
+    say("many rows")
+    x, w, dy = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt), randn(3, m, n, dtype=dt)
+    y, z = torch.empty(m, n, dtype=dt, device=DEV), torch.empty(m, n, dtype=dt, device=DEV)
+    edkm.linear(x, w, y, None, None, "relu", z)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, dtype=dt, device=DEV)
+    edkm.linear_backward(dy, x, w, dx, dw, db, z, "relu")
+    z64, y64, tol = L.product(x, w, None, None, "relu")
+    L.assert_within(y, y64, tol, "y")
+    for key, (ref, tol) in L.gradients(dy, x, w, z64, "relu").items():
+        L.assert_within({"dx": dx, "dw": dw, "db": db}[key], ref, tol, key)
+
+
+def test_past_32_bit_offsets():
+    """An x of more than 2^32 bytes (rows far apart) and a y whose last rows lie past 2^31
+    elements' bytes: a few rows against their own products."""
+    n, k, dt = 16, 64, torch.float16
+    m, gap = 260, 9_000_000
+    say("wide rows")
+    buf = torch.empty(m * gap, dtype=dt, device=DEV)          # 4.7 GB
+    x = buf.view(m, gap)[:, :k]
+    x.copy_(randn(1, m, k, dtype=dt))
+    w = randn(2, n, k, dtype=dt)
+    y = torch.empty(m, n, dtype=dt, device=DEV)
+    for rows in (m, 20):
+        edkm.linear(x[:rows], w, y[:rows])
+        L.assert_within(y[:rows], *L.product(x[:rows], w, None, None, "none")[1:], "y")
+    dx = buf.view(m, gap)[:, 128:128 + k]
+    edkm.linear_backward(y, None, w, dx=dx)
+    L.assert_within(dx, *L.gradients(y, x, w, None, "none")["dx"], "dx")
+    dw = torch.empty_like(w)
+    edkm.linear_backward(y, x, w, dw=dw)
+    L.assert_within(dw, *L.gradients(y, x, w, None, "none")["dw"], "dw")
+
+
+def test_another_stream_needs_its_own_workspace():
+    m, n, k, dt = 100, 64, 100, torch.float16
+    say("other stream")
+    x, w = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt)
+    y = torch.empty(m, n, dtype=dt, device=DEV)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    need = edkm.linear_workspace_bytes(m, n, k)
+    assert need > 0                     # rows of 100 elements are copied to aligned ones
+    with pytest.raises(ValueError, match="needs a workspace"):
+        edkm.linear(x, w, y, stream=side)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    edkm.linear(x, w, y, workspace=ws, stream=side)
+    torch.cuda.synchronize()
+    L.assert_within(y, *L.product(x, w, None, None, "none")[1:], "y")
+    with torch.cuda.stream(side):
+        y2 = torch.empty_like(y)
+        edkm.linear(x, w, y2)
+    torch.cuda.synchronize()
+    assert torch.equal(y, y2)
+
+
+def test_two_streams_at_once():
+    """Two calls with workspaces of their own, side by side."""
+    m, n, k, dt = 300, 500, 1000, torch.bfloat16
+    say("two streams")
+    x = [randn(i, m, k, dtype=dt) for i in range(2)]
+    w, dy = randn(5, n, k, dtype=dt, scale=0.05), randn(6, m, n, dtype=dt)
+    torch.cuda.synchronize()
+    outs = []
+    for t, s in zip(x, (torch.cuda.Stream(), torch.cuda.Stream())):
+        with torch.cuda.stream(s):
+            for _ in range(3):
+                y, z = torch.empty(m, n, dtype=dt, device=DEV), torch.empty(m, n, dtype=dt, device=DEV)
+                edkm.linear(t, w, y, None, None, "silu", z)
+                dx, dw = torch.empty_like(t), torch.empty_like(w)
+                edkm.linear_backward(dy, t, w, dx, dw, None, z, "silu")
+            outs.append((y, dx, dw))
+    torch.cuda.synchronize()
+    for t, (y, dx, dw) in zip(x, outs):
+        z64, y64, tol = L.product(t, w, None, None, "silu")
+        L.assert_within(y, y64, tol, "y")
+        ref = L.gradients(dy, t, w, z64, "silu")
+        L.assert_within(dx, *ref["dx"], "dx")
+        L.assert_within(dw, *ref["dw"], "dw")
+
+
+def test_autograd_captured_and_replayed():
+    """Forward and gradients through autograd in one graph, replayed with new tokens."""
+    m, n, k, dt = 90, 72, 100, torch.float16
+    say("autograd graph")
+    x = randn(1, m, k, dtype=dt).requires_grad_(True)
+    w, bias, dy = randn(2, n, k, dtype=dt, scale=0.1).requires_grad_(True), randn(3, n, dtype=dt).requires_grad_(True), randn(4, m, n, dtype=dt)
+
+    def step():
+        y = function.linear(x, w, bias, None, "gelu")
+        return (y.detach(), *torch.autograd.grad(y, [x, w, bias], dy))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for i in range(3):
+        with torch.no_grad():
+            x.copy_(randn(10 + i, m, k, dtype=dt))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_no_second_derivative():
+    x = randn(1, 5, 16, dtype=torch.float16).requires_grad_(True)
+    w = randn(2, 8, 16, dtype=torch.float16).requires_grad_(True)
+    say("second derivative")
+    (gx,) = torch.autograd.grad(function.linear(x, w, None, None, "silu").float().sum(), [x], create_graph=True)
+    with pytest.raises(RuntimeError, match="cannot be differentiated again"):
+        gx.sum().backward()
+    y = function.linear(x, w)
+    with torch.no_grad():
+        w.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(3600, 3608, 72), (3585, 3601, 67), (3600, 130, 3608), (3599, 67, 3585), (70, 3600, 3608),
+                                   (133, 3585, 3599)])
+def test_large_tiles(fmt, m, n, k):
+    """Enough 256 x 256 tiles of y, dx or dw (the small size is the one summed over or the
+    output of the other products), at their ends and with ragged depths."""
+    dt = L.DT[fmt]
+    say("large tiles", fmt, m, n, k)
+    x, w, dy = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt, scale=0.1), randn(3, m, n, dtype=dt)
+    bias, res = randn(4, n, dtype=dt), randn(5, m, n, dtype=dt)
+    y, z = torch.empty(m, n, dtype=dt, device=DEV), torch.empty(m, n, dtype=dt, device=DEV)
+    edkm.linear(x, w, y, bias, res, "gelu", z)
+    z64, y64, tol = L.product(x, w, bias, res, "gelu")
+    L.assert_within(y, y64, tol, "y")
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, dtype=dt, device=DEV)
+    edkm.linear_backward(dy, x, w, dx, dw, db, z, "gelu")
+    for key, (ref, tol) in L.gradients(dy, x, w, z64, "gelu").items():
+        L.assert_within({"dx": dx, "dw": dw, "db": db}[key], ref, tol, key)

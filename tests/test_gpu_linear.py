@@ -505,3 +505,22 @@ def test_large_tiles(fmt, m, n, k):
     edkm.linear_backward(dy, x, w, dx, dw, db, z, "gelu")
     for key, (ref, tol) in L.gradients(dy, x, w, z64, "gelu").items():
         L.assert_within({"dx": dx, "dw": dw, "db": db}[key], ref, tol, key)
+
+
+@pytest.mark.parametrize("bits", [0, 1, 2, 3, 4])
+@pytest.mark.parametrize("m", [1, 5, 16, 20, 40])
+@pytest.mark.parametrize("n,k", [(4101, 160), (8205, 288), (4101, 2080)])
+def test_few_tokens_of_many_outputs(bits, m, n, k):
+    """Several weight rows of sixteen per workgroup, a last run of 32 depths; bits 0: 16-bit weights."""
+    dt = torch.float16 if (m + bits) % 2 else torch.bfloat16
+    say("few tokens", bits, m, n, k)
+    x, bias = randn(1, m, k, dtype=dt), randn(2, n, dtype=dt)
+    y = torch.empty(m, n, dtype=dt, device=DEV)
+    if bits:
+        idx, packed, lut, _ = device_palette(n, k, bits, bits)
+        w = lut.to(dt)[torch.from_numpy(idx).to(DEV).long()].view(n, k)
+        edkm.palette_linear(x, packed, lut, y, bias, None, "silu")
+    else:
+        w = randn(3, n, k, dtype=dt, scale=0.05)
+        edkm.linear(x, w, y, bias, None, "silu")
+    L.assert_within(y, *L.product(x, w, bias, None, "silu")[1:], "y")

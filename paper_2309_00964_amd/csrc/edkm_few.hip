@@ -58,10 +58,6 @@ __global__ void __launch_bounds__(256) k_align_rows(const uint16_t* m, int64_t l
 // ----------------------------------------------------------------------------
 // products of few tokens
 
-// Table of pairs: entry e holds the values of indices e mod 2^b and e / 2^b, once per LDS
-// bank, so that the lanes of a wave look up without conflicts.
-constexpr int PAIR_BANKS = 32;
-
 // A lane's weights of a run: 32 depths of one row, as 16-bit values (BITS 0) or as packed
 // indices.  WHOLE: 32 depths are 4 BITS bytes on a 4-byte boundary (16-bit values: 64 bytes
 // on a 16-byte one), and offsets from the workgroup's first row fit 32 bits; else any

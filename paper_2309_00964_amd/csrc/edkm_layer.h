@@ -107,6 +107,8 @@ struct AdamwArgs {
 static_assert(sizeof(AdamwArgs) <= 4096, "launch arguments fit the kernel-argument limit");
 
 hipError_t launch_product(const ProductArgs& a, int fmt, int opa, int opb, float* part, hipStream_t s);
+// Rows of whole 16-byte pieces of x, whole pieces of eight indices, four bytes of them at least.
+hipError_t launch_tiled_palette(ProductArgs a, int fmt, float* part, hipStream_t s);
 hipError_t launch_few(const ProductArgs& a, int fmt, int bits, hipStream_t s);
 hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s);
 hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,

@@ -196,6 +196,16 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
     return EDKM_OK;
 }
 
+// Whether the tiled product decodes the palette itself, once for every tile row: for whole
+// pieces of eight indices, where no CU has a second tile.  At 4096 x 4096 and 3 bits it
+// takes 21.3 us for 65 tokens, 24.2 for 256, 33.2 for 512 and 58.4 for 1024; decoded first
+// by a launch of its own 26.9, 31.2, 38.5 and 59.2.  Past that the decoding that is done over
+// and over costs more: 81.0 against 77.8 at 512 x 11008 x 4096, 87.4 against 72.2 for 2048 tokens.
+static bool palette_fused(const ProductArgs& p) {
+    const int64_t tiles = ((int64_t)p.rows + 127) / 128 * (((int64_t)p.cols + 127) / 128);
+    return tiles <= 256 && p.depth % 8 == 0 && p.idx_bytes >= 4 && product_plan(p, OP_ROWS, OP_PALETTE).direct;
+}
+
 size_t edkm_palette_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int bits) {
     if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m <= FEW || bits < 1 || bits > EDKM_MAX_BITS) return 0;
     // the decoded weights, in rows of whole 16-byte pieces; an aligned copy of x; a split's sums
@@ -232,6 +242,9 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
     p.z = static_cast<uint16_t*>(z);
     p.act = activation;
     if (m <= FEW) return launch_product(p, format, OP_ROWS, OP_PALETTE, nullptr, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    p.padded = 1;
+    if (palette_fused(p))
+        return launch_tiled_palette(p, format, static_cast<float*>(ws), stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
     char* base = static_cast<char*>(ws);
     uint16_t* w = static_cast<uint16_t*>(ws);
     char* xs = base + up256((size_t)n * up8(k) * 2);
@@ -239,7 +252,6 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
                                : launch_unpalettize(indices, p.idx_bytes, (uint64_t)n * k, bits, format, lut, w, stream);
     p.b = w;
     p.ldb = up8(k);
-    p.padded = 1;
     if (e != hipSuccess || align_rows(p.a, p.lda, m, k, xs, stream) != hipSuccess) return EDKM_ERR_HIP;
     return launch_product(p, format, OP_ROWS, OP_ROWS, reinterpret_cast<float*>(xs + aligned_bytes(m, k)), stream) == hipSuccess
                ? EDKM_OK

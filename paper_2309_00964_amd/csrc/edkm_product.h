@@ -94,6 +94,11 @@ __device__ __forceinline__ uint16_t keep_z(float z) {
 // palettes
 
 struct __attribute__((packed)) U64 { uint64_t v; };
+struct __attribute__((packed)) U32 { uint32_t v; };
+
+// Table of pairs: entry e holds the values of indices e mod 2^b and e / 2^b, once per LDS
+// bank, so that the lanes of a wave look up without conflicts.
+constexpr int PAIR_BANKS = 32;
 
 // The 8 b bits of eight consecutive indices, from index i on, in the low bits.  Reads
 // nothing past the last byte.

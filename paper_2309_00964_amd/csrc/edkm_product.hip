@@ -1,353 +1,11 @@
 // Products with an epilogue for gfx950 (MI355X): y = act(x W^T + bias) + residual with
 // 16-bit weights, the products of its backward pass and the gradient at its activation.
 
-#include "edkm_product.h"
+#include "edkm_tiled.h"
 
 #include <algorithm>
 
 namespace edkm {
-
-// ----------------------------------------------------------------------------
-// tiled products
-
-// One operand's tile of R output indices x 64 depths in LDS, filled by 16-byte pieces.
-//
-// OP_ROWS: [R][64], a row is 128 bytes; piece c of row r lies at place c ^ (r & 7), so
-// that the 16-byte fragment reads of sixteen rows fall on different banks.
-// OP_DEPTH: [64][R]; fragments are read transposed (ds_read_b64_tr_b16: sixteen lanes
-// read 4 depths x 16 indices and each gets the 4 depths of its index).  The 32-byte
-// units of depth d are permuted by an exclusive or with (d & 3) + 4 (d >> 3 & 3), since
-// one read takes 16 depths of the same unit.
-template <int OP, int R, int NW>
-struct Tile {
-    static constexpr int BYTES = R * 128;
-    static constexpr int PER = BYTES / 1024 / NW;     // pieces of 1 KiB per wave
-    static constexpr int LPD = R / 8;                 // OP_DEPTH: lanes (pieces) per depth
-    static constexpr int UM = R / 16 - 1;             // OP_DEPTH: mask of the units
-
-    __device__ __forceinline__ static int swz(int d) { return ((d & 3) | ((d >> 1) & 12)) & UM; }
-    // place of lane's piece i of wave w: (index or first index, depth) of its 8 elements
-    __device__ __forceinline__ static void place(int w, int i, int lane, int& idx, int& d) {
-        const int q = w * PER + i;
-        if (OP == OP_DEPTH) {
-            d = q * (64 / LPD) + lane / LPD;
-            const int p = lane % LPD;
-            idx = (((p >> 1) ^ swz(d)) * 2 + (p & 1)) * 8;
-        } else {
-            idx = q * 8 + (lane >> 3);
-            d = ((lane & 7) ^ (lane >> 3)) * 8;
-        }
-    }
-    // fragment reads: index base u0 (multiple of 16 times the wave's tiles)
-    int off[2];
-    __device__ __forceinline__ void init(int base, int lane) {
-        const int l = lane & 15, g = lane >> 4;
-        if (OP == OP_DEPTH) {
-            const int d = g * 8 + (l >> 2);
-            off[0] = d * (R * 2) + (((base >> 4) ^ swz(d)) * 32) + (l & 3) * 8;
-            off[1] = 0;
-        } else {
-            off[0] = (base + l) * 128 + ((g ^ (l & 7)) * 16);
-            off[1] = (base + l) * 128 + (((g + 4) ^ (l & 7)) * 16);
-        }
-    }
-    __device__ __forceinline__ s16x8 frag(const char* lds, int t, int ks) const {
-        if constexpr (OP == OP_DEPTH) {
-            typedef __attribute__((address_space(3))) s16x4 lds4;
-            const char* p = lds + (off[0] ^ (t * 32)) + ks * (R * 64);
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)p);
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + R * 8));
-            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        } else {
-            return *reinterpret_cast<const s16x8*>(lds + off[ks] + t * 2048);
-        }
-    }
-};
-
-// A buffer's bytes from `p` on that a tile may read: range-checked, zeros past the end.
-constexpr int OUT_OF_RANGE = 0x7FFFFFF0;
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
-__device__ __forceinline__ rsrc_t buffer_at(const void* p, int64_t bytes) {
-    const int n = bytes < 0 ? 0 : bytes > OUT_OF_RANGE ? OUT_OF_RANGE : (int)((bytes + 3) & ~3ll);
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, n, 0x00027000);
-}
-
-// Brings an operand's tiles into LDS.  DIRECT: by buffer loads that write LDS, for rows of
-// memory that start on 16 bytes (and whole pieces of 8 depths for OP_ROWS); else through
-// registers, by loads of any alignment.
-template <int OP, int R, int NW, bool DIRECT>
-struct Feed {
-    typedef Tile<OP, R, NW> T;
-    const uint16_t* m;       // the tile's first element at depth 0
-    int64_t ld;
-    int limit, depth;        // output indices from m on; depths in all
-    int wave, lane;
-    int voff[T::PER], vd[T::PER];
-    s16x8 reg[DIRECT ? 1 : T::PER];
-
-    __device__ __forceinline__ void init(const uint16_t* base, int64_t ld_, int first, int count, int depth_, int wave_,
-                                         int lane_) {
-        ld = ld_;
-        m = OP == OP_DEPTH ? base + first : base + (int64_t)first * ld;
-        limit = count - first;
-        depth = depth_;
-        wave = wave_;
-        lane = lane_;
-#pragma unroll
-        for (int i = 0; i < T::PER; ++i) {
-            int idx, d;
-            T::place(wave, i, lane, idx, d);
-            vd[i] = d;
-            voff[i] = OP == OP_DEPTH ? (int)((d * ld + idx) * 2) : (int)((idx * ld + d) * 2);
-        }
-    }
-    // start bringing in depths d0 .. d0 + 63
-    __device__ __forceinline__ void start(char* lds, int d0) {
-        if constexpr (DIRECT) {
-            rsrc_t r;
-            if (OP == OP_DEPTH)
-                r = buffer_at(m + (int64_t)d0 * ld, ((int64_t)(depth - 1 - d0) * ld + limit) * 2);
-            else
-                r = buffer_at(m + d0, ((int64_t)(limit - 1) * ld + depth - d0) * 2);
-            const bool tail = OP != OP_DEPTH && d0 + 64 > depth;
-#pragma unroll
-            for (int i = 0; i < T::PER; ++i) {
-                const int off = tail && d0 + vd[i] >= depth ? OUT_OF_RANGE : voff[i];
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    r, (__attribute__((address_space(3))) void*)(lds + (wave * T::PER + i) * 1024), 16, off, 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < T::PER; ++i) {
-                int idx, d;
-                T::place(wave, i, lane, idx, d);
-                reg[i] = fetch(idx, d0 + d);
-            }
-        }
-    }
-    // what start() left in registers
-    __device__ __forceinline__ void finish(char* lds) {
-        if constexpr (!DIRECT)
-#pragma unroll
-            for (int i = 0; i < T::PER; ++i)
-                *reinterpret_cast<s16x8*>(lds + (wave * T::PER + i) * 1024 + lane * 16) = reg[i];
-    }
-    __device__ __forceinline__ s16x8 fetch(int idx, int d) const {
-        s16x8 v = {};
-        if (OP == OP_DEPTH) {
-            if (d >= depth || idx >= limit) return v;
-            const uint16_t* q = m + (int64_t)d * ld + idx;
-            if (idx + 8 <= limit) return reinterpret_cast<const S16x8*>(q)->v;
-            for (int j = 0; j < 8; ++j)
-                if (idx + j < limit) v[j] = (short)q[j];
-        } else {
-            if (idx >= limit || d >= depth) return v;
-            const uint16_t* q = m + (int64_t)idx * ld + d;
-            if (d + 8 <= depth) return reinterpret_cast<const S16x8*>(q)->v;
-            for (int j = 0; j < 8; ++j)
-                if (d + j < depth) v[j] = (short)q[j];
-        }
-        return v;
-    }
-};
-
-// Tile (x, y) of workgroup w: each of the eight XCDs (workgroups go to them in turn) takes
-// a run of tiles, and within a run eight tile rows are walked column by column, so that
-// the XCD's L2 holds the operands that its tiles share.
-__device__ __forceinline__ void tile_of(uint32_t w, uint32_t nx, uint32_t ny, uint32_t& x, uint32_t& y) {
-    const uint32_t total = nx * ny, per = total / 8, more = total % 8;
-    const uint32_t xcd = w % 8, t = xcd * per + min(xcd, more) + w / 8;
-    const uint32_t group = t / (8 * nx), first = group * 8, h = min(8u, ny - first);
-    const uint32_t in = t - group * 8 * nx;
-    y = first + in % h;
-    x = in / h;
-}
-
-// ----------------------------------------------------------------------------
-// epilogue
-
-// Eight outputs from column c of row r on; a PLAIN epilogue only rounds and stores.
-template <int F, bool PLAIN>
-__device__ __forceinline__ void finish8(const ProductArgs& p, int r, int c, float (&z)[8]) {
-    if (r >= p.rows || c >= p.cols) return;
-    uint16_t* out = p.out + (int64_t)r * p.ldo + c;
-    if (c + 8 <= p.cols) {
-        s16x8 v;
-        if (!PLAIN) {
-            if (p.bias) {
-                v = reinterpret_cast<const S16x8*>(p.bias + c)->v;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) z[q] += to_f32<F>((uint16_t)v[q]);
-            }
-            if (p.z) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] = (short)keep_z<F>(z[q]);
-                reinterpret_cast<S16x8*>(p.z + (int64_t)r * p.cols + c)->v = v;
-            }
-            if (p.act == ACT_RELU) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], ACT_RELU);
-            } else if (p.act == ACT_GELU) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], ACT_GELU);
-            } else if (p.act == ACT_SILU) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], ACT_SILU);
-            }
-            if (p.res) {
-                v = reinterpret_cast<const S16x8*>(p.res + (int64_t)r * p.ldr + c)->v;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) z[q] += to_f32<F>((uint16_t)v[q]);
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = (short)to_16<F>(z[q]);
-        reinterpret_cast<S16x8*>(out)->v = v;
-        return;
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        if (c + q >= p.cols) break;
-        float v = z[q];
-        if (!PLAIN) {
-            if (p.bias) v += to_f32<F>(p.bias[c + q]);
-            if (p.z) p.z[(int64_t)r * p.cols + c + q] = keep_z<F>(v);
-            v = act_value(v, p.act);
-            if (p.res) v += to_f32<F>(p.res[(int64_t)r * p.ldr + c + q]);
-        }
-        out[q] = to_16<F>(v);
-    }
-}
-
-// A wave's 16 x 64 block of sums as the MFMA leaves it (row lane & 15, four columns per
-// tile of 16) goes through LDS, so that lanes take eight columns of a row: whole 128-byte
-// lines to and from memory.  Its 16-byte places are permuted by the row.
-constexpr int EPI_BYTES = 16 * 64 * 4;
-__device__ __forceinline__ void epi_put(char* lds, int lane, int j, f32x4 v) {
-    const int r = lane & 15;
-    *reinterpret_cast<f32x4*>(lds + r * 256 + (((j * 4 + (lane >> 4)) ^ r) * 16)) = v;
-}
-template <int F, bool PLAIN>
-__device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, int lane, int blocks, int r0, int c0) {
-#pragma unroll 1
-    for (int i = 0; i < blocks * 2; ++i) {
-        const int r = i * 8 + (lane >> 3), q = (lane & 7) * 2, m = r & 15;
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + r * 256 + ((q ^ m) * 16));
-        const f32x4 hi = *reinterpret_cast<const f32x4*>(lds + r * 256 + (((q + 1) ^ m) * 16));
-        float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish8<F, PLAIN>(p, r0 + r, c0 + (lane & 7) * 8, z);
-    }
-}
-
-// BM x BN outputs per workgroup, 64 depths a step in two LDS buffers; WM x WN waves.
-// The sixteen-wide MFMA takes b's tile as its rows, so a lane ends with four consecutive
-// columns of one output row.
-template <int F, int OPA, int OPB, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
-    constexpr int NW = WM * WN, TR = BM / WM / 16, TC = BN / WN / 16;
-    static_assert(TC == 4 && TR % 4 == 0, "a wave's columns are those of the epilogue");
-    typedef Feed<OPA, BM, NW, DIRECT> FA;
-    typedef Feed<OPB, BN, NW, DIRECT> FB;
-    // four arrays, so that the compiler knows the loads of one buffer apart from the reads of the other
-    __shared__ __attribute__((aligned(1024))) char a0[FA::T::BYTES], a1[FA::T::BYTES], b0[FB::T::BYTES], b1[FB::T::BYTES];
-    static_assert(NW * 2 * EPI_BYTES <= FA::T::BYTES + FB::T::BYTES, "the epilogue's blocks fit");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint32_t tx, ty;
-    const uint32_t nx = (p.cols + BN - 1) / BN, ny = (p.rows + BM - 1) / BM;
-    const uint32_t split = blockIdx.x / (nx * ny);
-    tile_of(blockIdx.x % (nx * ny), nx, ny, tx, ty);
-    const int r0 = ty * BM, c0 = tx * BN;
-    const int wr = (wave / WN) * (BM / WM), wc = (wave % WN) * (BN / WN);
-    FA fa;
-    FB fb;
-    fa.init(p.a, p.lda, r0, p.rows, p.depth, wave, lane);
-    fb.init(p.b, p.ldb, c0, p.cols, p.depth, wave, lane);
-    typename FA::T ta;
-    typename FB::T tb;
-    ta.init(wr, lane);
-    tb.init(wc, lane);
-    f32x4 acc[TR][TC] = {};
-    const int first = split * p.split_steps, steps = min(first + p.split_steps, (p.depth + 63) / 64);
-
-    auto step = [&](const char* a, const char* b, char* an, char* bn, int s) {
-        if (s + 1 < steps) {
-            fa.start(an, (s + 1) * 64);
-            fb.start(bn, (s + 1) * 64);
-        }
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            s16x8 va[TR], vb[TC];
-#pragma unroll
-            for (int j = 0; j < TC; ++j) vb[j] = tb.frag(b, j, ks);
-#pragma unroll
-            for (int i = 0; i < TR; ++i) va[i] = ta.frag(a, i, ks);
-#pragma unroll
-            for (int i = 0; i < TR; ++i)
-#pragma unroll
-                for (int j = 0; j < TC; ++j) acc[i][j] = mfma16<F>(vb[j], va[i], acc[i][j]);
-        }
-        if (s + 1 < steps) {
-            fa.finish(an);
-            fb.finish(bn);
-        }
-        __syncthreads();
-    };
-    if (first < steps) {
-        fa.start(a0, first * 64);
-        fb.start(b0, first * 64);
-        fa.finish(a0);
-        fb.finish(b0);
-    }
-    __syncthreads();
-    for (int s = first; s < steps; s += 2) {
-        step(a0, b0, a1, b1, s);
-        if (s + 1 < steps) step(a1, b1, a0, b0, s + 1);
-    }
-    if (p.part) {
-        float* at = p.part + ((int64_t)blockIdx.x * NW + wave) * (TR * 1024) + lane * 4;
-#pragma unroll
-        for (int i = 0; i < TR; ++i)
-#pragma unroll
-            for (int j = 0; j < TC; ++j) *reinterpret_cast<f32x4*>(at + (i * TC + j) * 256) = acc[i][j];
-        return;
-    }
-    // each wave has two blocks of LDS: in a0/a1 the first half of the waves, in b0/b1 the others
-    char* mine = (wave < NW / 2 ? a0 : b0) + (wave % (NW / 2)) * 2 * EPI_BYTES;
-    static_assert(NW / 2 * 2 * EPI_BYTES <= (FA::T::BYTES < FB::T::BYTES ? FA::T::BYTES : FB::T::BYTES), "");
-#pragma unroll
-    for (int i = 0; i < TR; i += 2) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < TC; ++j) epi_put(mine + h * EPI_BYTES, lane, j, acc[i + h][j]);
-        epi_rows<F, OPB == OP_DEPTH>(p, mine, lane, 2, r0 + wr + i * 16, c0 + wc);
-    }
-}
-
-// Adds the partial sums of a split product, split after split, and finishes them: one wave
-// for 16 x 64 outputs.
-template <int F, int BM, int BN, int WM, int WN, bool PLAIN>
-__global__ void __launch_bounds__(64) k_join(ProductArgs p, int splits) {
-    constexpr int NW = WM * WN, TR = BM / WM / 16;
-    __shared__ __attribute__((aligned(16))) char lds[EPI_BYTES];
-    const uint32_t nx = (p.cols + BN - 1) / BN, ny = (p.rows + BM - 1) / BM;
-    const uint32_t w = blockIdx.x / (NW * TR);
-    const int wave = blockIdx.x / TR % NW, i = blockIdx.x % TR, lane = threadIdx.x;
-    uint32_t tx, ty;
-    tile_of(w, nx, ny, tx, ty);
-    const int r = ty * BM + wave / WN * (BM / WM) + i * 16, c = tx * BN + wave % WN * 64;
-    if (r >= p.rows || c >= p.cols) return;
-    f32x4 acc[4] = {};
-    const float* at = p.part + ((int64_t)w * NW + wave) * (TR * 1024) + i * 1024 + lane * 4;
-    const int64_t stride = (int64_t)nx * ny * NW * (TR * 1024);
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] += *reinterpret_cast<const f32x4*>(at + s * stride + j * 256);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) epi_put(lds, lane, j, acc[j]);
-    epi_rows<F, PLAIN>(p, lds, lane, 1, r, c);
-}
 
 // ----------------------------------------------------------------------------
 // the gradient at the activation
@@ -417,15 +75,6 @@ __global__ void __launch_bounds__(1024) k_dbias(DzArgs a, int chunks) {
 // ----------------------------------------------------------------------------
 // launches
 
-template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT>
-static hipError_t tiled(const ProductArgs& p, const ProductPlan& q, hipStream_t s) {
-    const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
-    EDKM_GO((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT>), dim3((uint32_t)(tiles * q.splits)), dim3(WM * WN * 64), p);
-    if (q.splits > 1)
-        EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH>), dim3((uint32_t)(tiles * WM * WN * (B / WM / 16))), dim3(64), p, q.splits);
-    return hipSuccess;
-}
-
 template <int F, int OPA, int OPB>
 static hipError_t product_ab(const ProductArgs& p, const ProductPlan& q, hipStream_t s) {
     if (q.tile == 256) return tiled<F, OPA, OPB, 256, 2, 4, true>(p, q, s);
@@ -480,7 +129,7 @@ ProductPlan product_plan(const ProductArgs& p, int opa, int opb) {
     auto whole = [&](const void* m, int64_t ld, int op) {
         return ((uintptr_t)m & 15) == 0 && ld % 8 == 0 && ld <= (1 << 22) && (op == OP_DEPTH || p.depth % 8 == 0 || p.padded);
     };
-    shape_plan(p.rows, p.cols, p.depth, whole(p.a, p.lda, opa) && whole(p.b, p.ldb, opb), q);
+    shape_plan(p.rows, p.cols, p.depth, whole(p.a, p.lda, opa) && (opb == OP_PALETTE || whole(p.b, p.ldb, opb)), q);
     return q;
 }
 

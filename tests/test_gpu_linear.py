@@ -524,3 +524,38 @@ def test_few_tokens_of_many_outputs(bits, m, n, k):
         w = randn(3, n, k, dtype=dt, scale=0.05)
         edkm.linear(x, w, y, bias, None, "silu")
     L.assert_within(y, *L.product(x, w, bias, None, "silu")[1:], "y")
+
+
+@pytest.mark.parametrize("bits", [1, 2, 3, 4])
+@pytest.mark.parametrize("m,n,k", [(65, 1, 32), (65, 5, 8), (70, 130, 8), (128, 129, 72), (129, 200, 136), (300, 257, 1000),
+                                   (66, 96, 4096), (200, 40, 2056), (640, 3000, 64), (2000, 1700, 64)])
+def test_tokens_of_some_tiles(bits, m, n, k):
+    """Rows of whole pieces of eight indices that no step or tile divides, depths split and not;
+    the last index is the memory's last byte, which starts on an odd one."""
+    dt = torch.float16 if (m + bits) % 2 else torch.bfloat16
+    say("some tiles", bits, m, n, k)
+    idx, packed, lut, _ = device_palette(n, k, bits, bits + m)
+    w = lut.to(dt)[torch.from_numpy(idx).to(DEV).long()].view(n, k)
+    raw = torch.cat([torch.full((5,), 255, dtype=torch.uint8, device=DEV), packed])[5:]
+    x, bias, res = randn(1, m, k, dtype=dt), randn(2, n, dtype=dt), randn(3, m, n, dtype=dt)
+    _, xv = inside(x, 8, 8)
+    ybuf, yv = inside(torch.zeros(m, n, dtype=dt, device=DEV), 3, 5)
+    z = torch.empty(m, n, dtype=dt, device=DEV)
+    edkm.palette_linear(xv, raw, lut, yv, bias, res, "gelu", z)
+    L.assert_within(yv, *L.product(x, w, bias, res, "gelu")[1:], "y")
+    L.assert_within(z, *L.product(x, w, bias, None, "none")[1:], "z")
+    assert int(ybuf.isnan().sum()) == ybuf.numel() - m * n
+
+
+def test_table_of_infinities_at_a_tail():
+    """Depths past the last and columns past the end add nothing, whatever the table holds."""
+    m, n, k = 100, 131, 72
+    x = torch.ones(m, k, dtype=torch.bfloat16, device=DEV)
+    packed = torch.zeros((n * k * 3 + 7) // 8, dtype=torch.uint8, device=DEV)
+    lut = torch.tensor([0.5] + [float("nan")] * 7, device=DEV)
+    y = torch.empty(m, n, dtype=torch.bfloat16, device=DEV)
+    say("infinities at a tail")
+    edkm.palette_linear(x, packed, lut, y)
+    assert bool((y == 36).all())
+    edkm.palette_linear(x, packed, torch.tensor([float("inf")] * 8, device=DEV), y)
+    assert bool((y == float("inf")).all())

@@ -40,7 +40,16 @@ struct ProductArgs {
     float* part;
 };
 
-constexpr int FEW = 64;         // tokens of k_few at most
+
+// Whether a forward goes to k_few, which takes up to 64 tokens: always up to 16; past them,
+// where every workgroup reads all tokens, only while those are no larger than given here.
+// Measured (us, k_few against the tiles, bf16 and 3 bits): 32 x 4096 x 4096 12.7 (17.1) and
+// 10.5 (17.6), 64 x 4096 x 4096 20.3 (15.9) and 18.0 (18.6), 48 x 11008 x 4096 25.6 (22.7) and
+// 19.1 (26.6), 32 x 4096 x 11008 30.9 (25.5) and 22.9 (25.8), 33 x 4096 x 11008 33.2 (25.3)
+// and 26.5 (29.0), 48 x 4096 x 11008 40.0 (25.6) and 34.1 (28.3).
+inline bool few_tokens(int64_t rows, int64_t depth, bool palette) {
+    return rows <= 16 || (rows <= 64 && rows * depth <= (palette ? 400 : 192) * 1000);
+}
 
 // How a product is carried out.
 struct ProductPlan {

@@ -95,7 +95,7 @@ edkm_status ws_ok(const void* ws, size_t have, size_t need) {
 extern "C" {
 
 size_t edkm_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) {
-    if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m <= FEW) return 0;
+    if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || few_tokens(m, k, false)) return 0;
     return forward_ws(m, n, k).total;
 }
 
@@ -123,7 +123,7 @@ edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activat
     p.ldo = ldy;
     p.z = static_cast<uint16_t*>(z);
     p.act = activation;
-    if (m <= FEW) return launch_product(p, format, OP_ROWS, OP_ROWS, nullptr, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    if (few_tokens(m, k, false)) return launch_few(p, format, 0, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
     const ForwardWs f = forward_ws(m, n, k);
     char* base = static_cast<char*>(ws);
     p.padded = 1;
@@ -207,7 +207,7 @@ static bool palette_fused(const ProductArgs& p) {
 }
 
 size_t edkm_palette_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int bits) {
-    if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || m <= FEW || bits < 1 || bits > EDKM_MAX_BITS) return 0;
+    if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || bits < 1 || bits > EDKM_MAX_BITS || few_tokens(m, k, true)) return 0;
     // the decoded weights, in rows of whole 16-byte pieces; an aligned copy of x; a split's sums
     return up256((size_t)n * up8(k) * 2) + aligned_bytes(m, k) + up256(product_part_bytes(m, n, k));
 }
@@ -241,7 +241,7 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
     p.ldo = ldy;
     p.z = static_cast<uint16_t*>(z);
     p.act = activation;
-    if (m <= FEW) return launch_product(p, format, OP_ROWS, OP_PALETTE, nullptr, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    if (few_tokens(m, k, true)) return launch_few(p, format, bits, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
     p.padded = 1;
     if (palette_fused(p))
         return launch_tiled_palette(p, format, static_cast<float*>(ws), stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;

@@ -83,7 +83,6 @@ static hipError_t product_ab(const ProductArgs& p, const ProductPlan& q, hipStre
 
 template <int F>
 static hipError_t product_f(ProductArgs p, int opa, int opb, float* part, hipStream_t s) {
-    if (opa == OP_ROWS && opb != OP_DEPTH && p.rows <= FEW) return launch_few(p, F, opb == OP_PALETTE ? p.bits : 0, s);
     const ProductPlan q = product_plan(p, opa, opb);
     p.split_steps = q.split_steps;
     p.part = q.splits > 1 ? part : nullptr;
@@ -96,19 +95,32 @@ hipError_t launch_product(const ProductArgs& p, int fmt, int opa, int opb, float
     return fmt == FMT_BF16 ? product_f<FMT_BF16>(p, opa, opb, part, s) : product_f<FMT_FP16>(p, opa, opb, part, s);
 }
 
-// A tile and a split of the depths.  What bounds a tile is bringing its operands into LDS,
-// whose bytes per product fall with the tile's side, so the larger one where it gives most
-// CUs a tile; two of the smaller share a CU, and its depths are split where they are few.
-// Unaligned operands, whose way through registers the larger tile has no room for, take
-// the smaller.
+// A tile and a split of the depths.
+//
+// What bounds a tile is bringing its operands into LDS, whose bytes per product fall with the
+// tile's side: a CU takes 1.5 times as long for one tile of 256 as for two of 128 side by
+// side, for twice the outputs (95 against 63 us at 4096 depths), and 0.77 as long for a
+// single one of 128.  So the tile whose last round costs least: 2560 x 4096 x 4096 takes 96 us
+// by tiles of 256 (102 by 128), 1024 x 11008 x 4096 98 (103), but 2048 x 4096 x 4096 99 (73),
+// 512 x 11008 x 4096 93 (59) and 4608 x 4096 x 4096 190 (158).  Unaligned operands, whose way
+// through registers the larger tile has no room for, take the smaller.
+//
+// A split costs a launch and its sums' way to memory and back: 3.6 steps' time and 1/26 of
+// one for every tile and part, so it is the number of parts that adds up to least.  Measured
+// (us by parts): 128 x 4096 x 4096 1: 47, 4: 19.5, 8: 17.4, 16: 20.4; 512 x 4096 x 4096
+// 1: 48, 2: 33.0, 3: 29.7, 4: 30.2, 6: 35.8; 1000 x 1336 x 776 1: 12.1, 2: 16.1, 3: 17.5.
 static void shape_plan(int64_t rows, int64_t cols, int64_t depth, bool direct, ProductPlan& q) {
     auto tiles = [&](int64_t b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
-    const int64_t steps = std::max<int64_t>(1, (depth + 63) / 64);
+    const int64_t steps = std::max<int64_t>(1, (depth + 63) / 64), large = tiles(256), t = tiles(128);
+    const int64_t large_cost = (large + 255) / 256 * 6, cost = t / 512 * 4 + (t % 512 > 256 ? 4 : t % 512 ? 3 : 0);
     q.direct = direct;
-    q.tile = direct && tiles(256) >= 192 ? 256 : 128;
+    q.tile = direct && large_cost < cost ? 256 : 128;
     q.splits = 1;
-    const int64_t t = tiles(q.tile);
-    if (q.tile == 128 && t < 256) q.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / t, steps / 4, 64}));
+    if (q.tile == 128) {
+        auto time = [&](int64_t s) { return 26 * ((steps + s - 1) / s) + (s > 1 ? 94 + s * t : 0); };
+        for (int s = 2; s <= std::min<int64_t>(64, 512 / t); ++s)
+            if (time(s) < time(q.splits)) q.splits = s;
+    }
     q.split_steps = (int)((steps + q.splits - 1) / q.splits);
     q.splits = (int)((steps + q.split_steps - 1) / q.split_steps);
 }

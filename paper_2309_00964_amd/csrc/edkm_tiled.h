@@ -309,10 +309,11 @@ __device__ __forceinline__ void epi_put(char* lds, int lane, int j, f32x4 v) {
     const int r = lane & 15;
     *reinterpret_cast<f32x4*>(lds + r * 256 + (((j * 4 + (lane >> 4)) ^ r) * 16)) = v;
 }
+// Finishes two such blocks.
 template <int F, bool PLAIN>
-__device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, int lane, int blocks, int r0, int c0) {
+__device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, int lane, int r0, int c0) {
 #pragma unroll 1
-    for (int i = 0; i < blocks * 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const int r = i * 8 + (lane >> 3), q = (lane & 7) * 2, m = r & 15;
         const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + r * 256 + ((q ^ m) * 16));
         const f32x4 hi = *reinterpret_cast<const f32x4*>(lds + r * 256 + (((q + 1) ^ m) * 16));
@@ -412,41 +413,57 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < TC; ++j) epi_put(mine + h * EPI_BYTES, lane, j, acc[i + h][j]);
-        epi_rows<F, OPB == OP_DEPTH>(p, mine, lane, 2, r0 + wr + i * 16, c0 + wc);
+        epi_rows<F, OPB == OP_DEPTH>(p, mine, lane, r0 + wr + i * 16, c0 + wc);
     }
 }
 
-// Adds the partial sums of a split product, split after split, and finishes them: one wave
-// for 16 x 64 outputs.
-template <int F, int BM, int BN, int WM, int WN, bool PLAIN>
-__global__ void __launch_bounds__(64) k_join(ProductArgs p, int splits) {
+// Adds the partial sums of a split product and finishes them: 16 x 64 outputs per workgroup,
+// each of its W waves a part of the splits, one after the other.  Bound by the partial sums'
+// bytes for few splits, where one wave is best (512 x 4096 x 4096 in four parts: 29.8 us with
+// the product, 30.3 by four waves), and by the chain of loads for many (128 x 128 x 32768 in
+// 64: 20.0 us, 14.3 by four).
+template <int F, int BM, int BN, int WM, int WN, bool PLAIN, int W>
+__global__ void __launch_bounds__(W * 64) k_join(ProductArgs p, int splits) {
     constexpr int NW = WM * WN, TR = BM / WM / 16;
-    __shared__ __attribute__((aligned(16))) char lds[EPI_BYTES];
+    __shared__ __attribute__((aligned(16))) char lds[W][EPI_BYTES];
     const uint32_t nx = (p.cols + BN - 1) / BN, ny = (p.rows + BM - 1) / BM;
     const uint32_t w = blockIdx.x / (NW * TR);
-    const int wave = blockIdx.x / TR % NW, i = blockIdx.x % TR, lane = threadIdx.x;
+    const int wave = blockIdx.x / TR % NW, i = blockIdx.x % TR, lane = threadIdx.x & 63, share = threadIdx.x >> 6;
     uint32_t tx, ty;
     tile_of(w, nx, ny, tx, ty);
-    const int r = ty * BM + wave / WN * (BM / WM) + i * 16, c = tx * BN + wave % WN * 64;
-    if (r >= p.rows || c >= p.cols) return;
+    const int r0 = ty * BM + wave / WN * (BM / WM) + i * 16, c0 = tx * BN + wave % WN * 64;
+    if (r0 >= p.rows || c0 >= p.cols) return;
     f32x4 acc[4] = {};
     const float* at = p.part + ((int64_t)w * NW + wave) * (TR * 1024) + i * 1024 + lane * 4;
     const int64_t stride = (int64_t)nx * ny * NW * (TR * 1024);
+    const int per = (splits + W - 1) / W, end = min(splits, (share + 1) * per);
 #pragma unroll 4
-    for (int s = 0; s < splits; ++s)
+    for (int s = share * per; s < end; ++s)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] += *reinterpret_cast<const f32x4*>(at + s * stride + j * 256);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) epi_put(lds, lane, j, acc[j]);
-    epi_rows<F, PLAIN>(p, lds, lane, 1, r, c);
+    for (int j = 0; j < 4; ++j) epi_put(lds[share], lane, j, acc[j]);
+    __syncthreads();
+    const int c = (threadIdx.x & 7) * 2;
+    for (int r = threadIdx.x >> 3; r < 16; r += W * 8) {
+        f32x4 lo = {}, hi = {};
+#pragma unroll
+        for (int q = 0; q < W; ++q) {
+            lo += *reinterpret_cast<const f32x4*>(lds[q] + r * 256 + ((c ^ r) * 16));
+            hi += *reinterpret_cast<const f32x4*>(lds[q] + r * 256 + (((c + 1) ^ r) * 16));
+        }
+        float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        finish8<F, PLAIN>(p, r0 + r, c0 + c * 4, z);
+    }
 }
 
 template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, int BITS = 0>
 static hipError_t tiled(const ProductArgs& p, const ProductPlan& q, hipStream_t s) {
     const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
     EDKM_GO((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS>), dim3((uint32_t)(tiles * q.splits)), dim3(WM * WN * 64), p);
-    if (q.splits > 1)
-        EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH>), dim3((uint32_t)(tiles * WM * WN * (B / WM / 16))), dim3(64), p, q.splits);
+    const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
+    if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4>), blocks, dim3(256), p, q.splits);
+    else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1>), blocks, dim3(64), p, q.splits);
     return hipSuccess;
 }
 

@@ -559,3 +559,21 @@ def test_table_of_infinities_at_a_tail():
     assert bool((y == 36).all())
     edkm.palette_linear(x, packed, torch.tensor([float("inf")] * 8, device=DEV), y)
     assert bool((y == float("inf")).all())
+
+
+@pytest.mark.parametrize("bits", [0, 3])
+@pytest.mark.parametrize("m,n,k", [(17, 33, 11008), (40, 70, 11008), (64, 48, 8192), (20, 48, 25000), (33, 17, 12001), (64, 130, 3001)])
+def test_some_tokens_of_many_depths(bits, m, n, k):
+    """Between the few tokens' kernel and the tiles; bits 0: 16-bit weights."""
+    dt = torch.float16 if (m + bits) % 2 else torch.bfloat16
+    say("some tokens", bits, m, n, k)
+    x, bias = randn(1, m, k, dtype=dt), randn(2, n, dtype=dt)
+    y = torch.empty(m, n, dtype=dt, device=DEV)
+    if bits:
+        idx, packed, lut, _ = device_palette(n, k, bits, bits)
+        w = lut.to(dt)[torch.from_numpy(idx).to(DEV).long()].view(n, k)
+        edkm.palette_linear(x, packed, lut, y, bias, None, "gelu")
+    else:
+        w = randn(3, n, k, dtype=dt, scale=0.05)
+        edkm.linear(x, w, y, bias, None, "gelu")
+    L.assert_within(y, *L.product(x, w, bias, None, "gelu")[1:], "y")

@@ -248,24 +248,34 @@ __device__ __forceinline__ void tile_of(uint32_t w, uint32_t nx, uint32_t ny, ui
 // ----------------------------------------------------------------------------
 // epilogue
 
-// Eight outputs from column c of row r on; a PLAIN epilogue only rounds and stores.
+// Eight outputs from column c on, in one row after another: bias holds the columns' biases,
+// and a row's part of the residual is asked for before the row's turn.  A PLAIN epilogue
+// only rounds and stores.
 template <int F, bool PLAIN>
-__device__ __forceinline__ void finish8(const ProductArgs& p, int r, int c, float (&z)[8]) {
-    if (r >= p.rows || c >= p.cols) return;
-    uint16_t* out = p.out + (int64_t)r * p.ldo + c;
-    if (c + 8 <= p.cols) {
-        s16x8 v;
+struct Eight {
+    float bias[8];
+    s16x8 res;
+    __device__ __forceinline__ void init(const ProductArgs& p, int c) {
+        if (PLAIN) return;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) bias[q] = 0.f;
+        if (!p.bias || c >= p.cols) return;
+        const s16x8 v = row8(p.bias + c, p.cols - c);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) bias[q] = to_f32<F>((uint16_t)v[q]);
+    }
+    __device__ __forceinline__ void ask(const ProductArgs& p, int r, int c) {
+        if (!PLAIN && p.res && r < p.rows && c < p.cols) res = row8(p.res + (int64_t)r * p.ldr + c, p.cols - c);
+    }
+    __device__ __forceinline__ void finish(const ProductArgs& p, int r, int c, float (&z)[8], s16x8 rest) const {
+        if (r >= p.rows || c >= p.cols) return;
+        s16x8 v, k;
         if (!PLAIN) {
-            if (p.bias) {
-                v = reinterpret_cast<const S16x8*>(p.bias + c)->v;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) z[q] += to_f32<F>((uint16_t)v[q]);
-            }
-            if (p.z) {
+            for (int q = 0; q < 8; ++q) z[q] += bias[q];
+            if (p.z)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] = (short)keep_z<F>(z[q]);
-                reinterpret_cast<S16x8*>(p.z + (int64_t)r * p.cols + c)->v = v;
-            }
+                for (int q = 0; q < 8; ++q) k[q] = (short)keep_z<F>(z[q]);
             if (p.act == ACT_RELU) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], ACT_RELU);
@@ -276,30 +286,27 @@ __device__ __forceinline__ void finish8(const ProductArgs& p, int r, int c, floa
 #pragma unroll
                 for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], ACT_SILU);
             }
-            if (p.res) {
-                v = reinterpret_cast<const S16x8*>(p.res + (int64_t)r * p.ldr + c)->v;
+            if (p.res)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) z[q] += to_f32<F>((uint16_t)v[q]);
-            }
+                for (int q = 0; q < 8; ++q) z[q] += to_f32<F>((uint16_t)rest[q]);
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = (short)to_16<F>(z[q]);
-        reinterpret_cast<S16x8*>(out)->v = v;
-        return;
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        if (c + q >= p.cols) break;
-        float v = z[q];
-        if (!PLAIN) {
-            if (p.bias) v += to_f32<F>(p.bias[c + q]);
-            if (p.z) p.z[(int64_t)r * p.cols + c + q] = keep_z<F>(v);
-            v = act_value(v, p.act);
-            if (p.res) v += to_f32<F>(p.res[(int64_t)r * p.ldr + c + q]);
+        uint16_t* out = p.out + (int64_t)r * p.ldo + c;
+        uint16_t* keep = p.z + (int64_t)r * p.cols + c;
+        if (c + 8 <= p.cols) {
+            reinterpret_cast<S16x8*>(out)->v = v;
+            if (!PLAIN && p.z) reinterpret_cast<S16x8*>(keep)->v = k;
+            return;
         }
-        out[q] = to_16<F>(v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            if (c + q >= p.cols) break;
+            out[q] = (uint16_t)v[q];
+            if (!PLAIN && p.z) keep[q] = (uint16_t)k[q];
+        }
     }
-}
+};
 
 // A wave's 16 x 64 block of sums as the MFMA leaves it (row lane & 15, four columns per
 // tile of 16) goes through LDS, so that lanes take eight columns of a row: whole 128-byte
@@ -311,14 +318,18 @@ __device__ __forceinline__ void epi_put(char* lds, int lane, int j, f32x4 v) {
 }
 // Finishes two such blocks.
 template <int F, bool PLAIN>
-__device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, int lane, int r0, int c0) {
+__device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, int lane, int r0, int c0, Eight<F, PLAIN>& e) {
+    const int c = c0 + (lane & 7) * 8;
+    e.ask(p, r0 + (lane >> 3), c);
 #pragma unroll 1
     for (int i = 0; i < 4; ++i) {
         const int r = i * 8 + (lane >> 3), q = (lane & 7) * 2, m = r & 15;
         const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + r * 256 + ((q ^ m) * 16));
         const f32x4 hi = *reinterpret_cast<const f32x4*>(lds + r * 256 + (((q + 1) ^ m) * 16));
         float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish8<F, PLAIN>(p, r0 + r, c0 + (lane & 7) * 8, z);
+        const s16x8 res = e.res;
+        if (i < 3) e.ask(p, r0 + r + 8, c);
+        e.finish(p, r0 + r, c, z, res);
     }
 }
 
@@ -406,6 +417,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
     }
     // each wave has two blocks of LDS: in a0/a1 the first half of the waves, in b0/b1 the others
     char* mine = (wave < NW / 2 ? a0 : b0) + (wave % (NW / 2)) * 2 * EPI_BYTES;
+    Eight<F, OPB == OP_DEPTH> eight;
+    eight.init(p, c0 + wc + (lane & 7) * 8);
     static_assert(NW / 2 * 2 * EPI_BYTES <= (FA::T::BYTES < FB::T::BYTES ? FA::T::BYTES : FB::T::BYTES), "");
 #pragma unroll
     for (int i = 0; i < TR; i += 2) {
@@ -413,7 +426,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < TC; ++j) epi_put(mine + h * EPI_BYTES, lane, j, acc[i + h][j]);
-        epi_rows<F, OPB == OP_DEPTH>(p, mine, lane, r0 + wr + i * 16, c0 + wc);
+        epi_rows(p, mine, lane, r0 + wr + i * 16, c0 + wc, eight);
     }
 }
 
@@ -433,6 +446,9 @@ __global__ void __launch_bounds__(W * 64) k_join(ProductArgs p, int splits) {
     tile_of(w, nx, ny, tx, ty);
     const int r0 = ty * BM + wave / WN * (BM / WM) + i * 16, c0 = tx * BN + wave % WN * 64;
     if (r0 >= p.rows || c0 >= p.cols) return;
+    const int c = (threadIdx.x & 7) * 2;
+    Eight<F, PLAIN> eight;
+    eight.init(p, c0 + c * 4);
     f32x4 acc[4] = {};
     const float* at = p.part + ((int64_t)w * NW + wave) * (TR * 1024) + i * 1024 + lane * 4;
     const int64_t stride = (int64_t)nx * ny * NW * (TR * 1024);
@@ -444,8 +460,8 @@ __global__ void __launch_bounds__(W * 64) k_join(ProductArgs p, int splits) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) epi_put(lds[share], lane, j, acc[j]);
     __syncthreads();
-    const int c = (threadIdx.x & 7) * 2;
     for (int r = threadIdx.x >> 3; r < 16; r += W * 8) {
+        eight.ask(p, r0 + r, c0 + c * 4);
         f32x4 lo = {}, hi = {};
 #pragma unroll
         for (int q = 0; q < W; ++q) {
@@ -453,7 +469,7 @@ __global__ void __launch_bounds__(W * 64) k_join(ProductArgs p, int splits) {
             hi += *reinterpret_cast<const f32x4*>(lds[q] + r * 256 + (((c + 1) ^ r) * 16));
         }
         float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish8<F, PLAIN>(p, r0 + r, c0 + c * 4, z);
+        eight.finish(p, r0 + r, c0 + c * 4, z, eight.res);
     }
 }
 

@@ -147,7 +147,8 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
     if (dx && (!w || !ld_ok(ldw, n, k) || !ld_ok(lddx, m, k))) return EDKM_ERR_ARG;
     if ((dw && !ld_ok(ldx, m, k)) || !ld_ok(lddy, m, n)) return EDKM_ERR_ARG;
     const BackwardWs L = backward_ws(m, n, k, activation);
-    const edkm_status st = ws_ok(ws, ws_bytes, L.total);
+    // without products only dz and the partial sums, which do not depend on k
+    const edkm_status st = ws_ok(ws, ws_bytes, dx || dw ? L.total : L.x);
     if (st != EDKM_OK) return st;
     char* base = static_cast<char*>(ws);
     DzArgs d{};

@@ -577,3 +577,17 @@ def test_some_tokens_of_many_depths(bits, m, n, k):
         w = randn(3, n, k, dtype=dt, scale=0.05)
         edkm.linear(x, w, y, bias, None, "gelu")
     L.assert_within(y, *L.product(x, w, bias, None, "gelu")[1:], "y")
+
+
+@pytest.mark.parametrize("k", [8, 4096])
+@pytest.mark.parametrize("name", ["none", "gelu"])
+def test_bias_gradient_alone_with_a_workspace(k, name):
+    """No operand that tells k: the workspace for any k will do."""
+    m, n, dt = 37, 88, torch.bfloat16
+    say("bias gradient alone", k, name)
+    dy, z = randn(1, m, n, dtype=dt), randn(2, m, n, dtype=dt)
+    db = torch.empty(n, dtype=dt, device=DEV)
+    ws = torch.empty(edkm.linear_backward_workspace_bytes(m, n, k, name), dtype=torch.uint8, device=DEV)
+    edkm.linear_backward(dy, None, None, dbias=db, z=z, activation=name, workspace=ws)
+    ref, tol = L.gradients(dy, randn(3, m, k, dtype=dt), randn(4, n, k, dtype=dt), z if name != "none" else None, name)["db"]
+    L.assert_within(db, ref, tol, "db")

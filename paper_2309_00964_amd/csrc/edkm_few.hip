@@ -277,13 +277,23 @@ static hipError_t few_go(const ProductArgs& p, hipStream_t s) {
     return hipSuccess;
 }
 
-// Weight rows of a workgroup: as many as leave a workgroup per CU, so that the tokens are
-// read and the table is made for more of them.
+// Weight rows of a workgroup, in sixteens.  More of them share the reading of the tokens and
+// the making of the table, and cost a workgroup time: 1.5 and 2 times one's for up to 16
+// tokens, 1.13 and 1.25 times for more.  So the number whose rounds over the CUs take least
+// (3 bits, 4096 depths, us with 16, 32 and 48 rows: one token and 8192 outputs 8.2, 6.7, -,
+// 11008 11.0, 11.4, 8.1, 16384 14.3, 11.8, 14.1; 32 tokens and 11008 26.6, 21.7, 14.2, 16384
+// 34.7, 21.9, 26.1).  A few tokens' 16-bit weights, bound by their bytes, want many small
+// workgroups (one token and 11008 outputs 18.6, 26.5).
 template <int F, int BITS, bool WHOLE, int MT>
 static hipError_t few_rows(const ProductArgs& p, hipStream_t s) {
-    const int64_t tiles = ((int64_t)p.cols + 15) / 16;
-    if (!WHOLE || tiles <= 256) return few_go<F, BITS, WHOLE, MT, 1>(p, s);
-    return tiles <= 512 || (MT == 1 && !BITS) ? few_go<F, BITS, WHOLE, MT, WHOLE ? 2 : 1>(p, s) : few_go<F, BITS, WHOLE, MT, WHOLE ? 3 : 1>(p, s);
+    if constexpr (!WHOLE || (MT == 1 && BITS == 0)) {
+        return few_go<F, BITS, WHOLE, MT, 1>(p, s);
+    } else {
+        const int64_t tiles = ((int64_t)p.cols + 15) / 16;
+        auto time = [&](int64_t n) { return ((tiles + n - 1) / n + 255) / 256 * ((MT == 1 ? 1 : 7) + n); };
+        if (time(1) <= time(2) && time(1) <= time(3)) return few_go<F, BITS, WHOLE, MT, 1>(p, s);
+        return time(2) <= time(3) ? few_go<F, BITS, WHOLE, MT, 2>(p, s) : few_go<F, BITS, WHOLE, MT, 3>(p, s);
+    }
 }
 
 template <int F, int BITS, bool WHOLE>

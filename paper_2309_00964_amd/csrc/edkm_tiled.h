@@ -321,7 +321,7 @@ template <int F, bool PLAIN>
 __device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, int lane, int r0, int c0, Eight<F, PLAIN>& e) {
     const int c = c0 + (lane & 7) * 8;
     e.ask(p, r0 + (lane >> 3), c);
-#pragma unroll 1
+#pragma unroll 4
     for (int i = 0; i < 4; ++i) {
         const int r = i * 8 + (lane >> 3), q = (lane & 7) * 2, m = r & 15;
         const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + r * 256 + ((q ^ m) * 16));

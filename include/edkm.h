@@ -362,7 +362,8 @@ edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activat
  * is dy itself.  With an activation, dz is rounded to 16 bits before the two
  * products (the bias gradient sums it unrounded).
  *   z   the z of edkm_linear; not read without activation.  x is read for dw
- *       only, w for dx only.  With m = 0, dw and dbias become zeros. */
+ *       only, w for dx only.  With m = 0, dw and dbias become zeros.  For dbias
+ *       alone k is not used, and the workspace for any k is enough. */
 size_t edkm_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int activation);
 edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, int activation,
                                  const void* dy, int64_t lddy, const void* z,
@@ -380,9 +381,9 @@ edkm_status edkm_unpalettize(const uint8_t* indices, uint64_t n, int bits, int f
 /* edkm_linear with the weights given as a palette: n x k row-major weights as
  * edkm_palettize packs them (rows may start inside a byte), n k <= EDKM_MAX_N.
  * A weight is its table entry rounded to the format, so y is edkm_linear's on
- * the weights that edkm_unpalettize gives, up to the order of the sums.  For
- * few tokens the indices are decoded on the way into the product; for many the
- * weights are decoded into the workspace first. */
+ * the weights that edkm_unpalettize gives, up to the order of the sums.  Up to
+ * some hundred tokens the indices are decoded on the way into the product; for
+ * more the weights are decoded into the workspace first. */
 size_t edkm_palette_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int bits);
 edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int format, int activation,
                                 const void* x, int64_t ldx, const uint8_t* indices, const float* lut,

@@ -50,6 +50,18 @@ inline bool few_tokens(int64_t rows, int64_t depth, bool palette) {
     return rows <= 16 || (rows <= 64 && rows * depth <= (palette ? 400 : 192) * 1000);
 }
 
+// Matrices to be copied to rows of whole 16-byte pieces in one launch.
+struct AlignJob {
+    const uint16_t* m;
+    int64_t ld;
+    int rows, cols;
+    uint16_t* out;
+};
+struct AlignArgs {
+    int count;
+    AlignJob job[3];
+};
+
 // How a product is carried out.
 struct ProductPlan {
     int tile;               // 256 or 128 outputs square
@@ -125,7 +137,7 @@ hipError_t launch_few(const ProductArgs& a, int fmt, int bits, hipStream_t s);
 hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s);
 hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
                               uint16_t* out, hipStream_t s);
-hipError_t launch_align_rows(const uint16_t* m, int64_t ld, int64_t rows, int64_t cols, uint16_t* out, hipStream_t s);
+hipError_t launch_align_rows(const AlignArgs& a, hipStream_t s);
 hipError_t launch_unpalettize_rows(const uint8_t* idx, uint64_t idx_bytes, int64_t rows, int64_t cols, int bits, int fmt,
                                    const float* lut, uint16_t* out, hipStream_t s);
 hipError_t launch_adamw(const AdamwArgs& a, uint32_t grid, int param_type, int grad_type, int state_bits, hipStream_t s);

@@ -75,14 +75,13 @@ BackwardWs backward_ws(int64_t m, int64_t n, int64_t k, int act) {
     return w;
 }
 
-// Copies a matrix's rows to `to` if their length asks for it, and points there.
-hipError_t align_rows(const uint16_t*& p, int64_t& ld, int64_t rows, int64_t cols, char* to, hipStream_t stream) {
-    if (cols % 8 == 0) return hipSuccess;
+// Has a matrix's rows copied to `to` if their length asks for it, and points there.
+void align_rows(AlignArgs& a, const uint16_t*& p, int64_t& ld, int64_t rows, int64_t cols, char* to) {
+    if (cols % 8 == 0 || rows == 0) return;
     uint16_t* out = reinterpret_cast<uint16_t*>(to);
-    const hipError_t e = launch_align_rows(p, ld, rows, cols, out, stream);
+    a.job[a.count++] = {p, ld, (int)rows, (int)cols, out};
     p = out;
     ld = up8(cols);
-    return e;
 }
 
 edkm_status ws_ok(const void* ws, size_t have, size_t need) {
@@ -127,8 +126,10 @@ edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activat
     const ForwardWs f = forward_ws(m, n, k);
     char* base = static_cast<char*>(ws);
     p.padded = 1;
-    if (align_rows(p.a, p.lda, m, k, base + f.x, stream) != hipSuccess || align_rows(p.b, p.ldb, n, k, base + f.w, stream) != hipSuccess)
-        return EDKM_ERR_HIP;
+    AlignArgs copies{};
+    align_rows(copies, p.a, p.lda, m, k, base + f.x);
+    align_rows(copies, p.b, p.ldb, n, k, base + f.w);
+    if (launch_align_rows(copies, stream) != hipSuccess) return EDKM_ERR_HIP;
     return launch_product(p, format, OP_ROWS, OP_ROWS, reinterpret_cast<float*>(base + f.split), stream) == hipSuccess ? EDKM_OK
                                                                                                                        : EDKM_ERR_HIP;
 }
@@ -168,16 +169,20 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
     float* parts = reinterpret_cast<float*>(base + L.split);
     const uint16_t* dz = activation == ACT_NONE ? d.dy : d.dz;
     int64_t lddz = activation == ACT_NONE ? lddy : d.lddz;
-    if (activation == ACT_NONE && m > 0 && align_rows(dz, lddz, m, n, base + L.dz, stream) != hipSuccess) return EDKM_ERR_HIP;
+    const uint16_t *px = static_cast<const uint16_t*>(x), *pw = static_cast<const uint16_t*>(w);
+    AlignArgs copies{};
+    if (activation == ACT_NONE) align_rows(copies, dz, lddz, m, n, base + L.dz);
+    if (dx && m > 0) align_rows(copies, pw, ldw, n, k, base + L.w);
+    if (dw) align_rows(copies, px, ldx, m, k, base + L.x);
+    if (launch_align_rows(copies, stream) != hipSuccess) return EDKM_ERR_HIP;
     ProductArgs p{};
     p.a = dz;
     p.lda = lddz;
     p.cols = (int32_t)k;
     p.padded = 1;
     if (dx && m > 0) {
-        p.b = static_cast<const uint16_t*>(w);
+        p.b = pw;
         p.ldb = ldw;
-        if (align_rows(p.b, p.ldb, n, k, base + L.w, stream) != hipSuccess) return EDKM_ERR_HIP;
         p.rows = (int32_t)m;
         p.depth = (int32_t)n;
         p.out = static_cast<uint16_t*>(dx);
@@ -185,9 +190,8 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
         if (launch_product(p, format, OP_ROWS, OP_DEPTH, parts, stream) != hipSuccess) return EDKM_ERR_HIP;
     }
     if (dw) {
-        p.b = static_cast<const uint16_t*>(x);
+        p.b = px;
         p.ldb = ldx;
-        if (m > 0 && align_rows(p.b, p.ldb, m, k, base + L.x, stream) != hipSuccess) return EDKM_ERR_HIP;
         p.rows = (int32_t)n;
         p.depth = (int32_t)m;
         p.out = static_cast<uint16_t*>(dw);
@@ -253,7 +257,9 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
                                : launch_unpalettize(indices, p.idx_bytes, (uint64_t)n * k, bits, format, lut, w, stream);
     p.b = w;
     p.ldb = up8(k);
-    if (e != hipSuccess || align_rows(p.a, p.lda, m, k, xs, stream) != hipSuccess) return EDKM_ERR_HIP;
+    AlignArgs copies{};
+    align_rows(copies, p.a, p.lda, m, k, xs);
+    if (e != hipSuccess || launch_align_rows(copies, stream) != hipSuccess) return EDKM_ERR_HIP;
     return launch_product(p, format, OP_ROWS, OP_ROWS, reinterpret_cast<float*>(xs + aligned_bytes(m, k)), stream) == hipSuccess
                ? EDKM_OK
                : EDKM_ERR_HIP;

@@ -591,3 +591,31 @@ def test_bias_gradient_alone_with_a_workspace(k, name):
     edkm.linear_backward(dy, None, None, dbias=db, z=z, activation=name, workspace=ws)
     ref, tol = L.gradients(dy, randn(3, m, k, dtype=dt), randn(4, n, k, dtype=dt), z if name != "none" else None, name)["db"]
     L.assert_within(db, ref, tol, "db")
+
+
+@pytest.mark.parametrize("m,n,k,bits", [(100, 200, 4096, 3), (300, 130, 1000, 4), (90, 70, 2049, 2), (40, 33, 12000, 1)])
+def test_captured_palette_products(m, n, k, bits):
+    """Split and joined, decoded on the way and before: every replay is the eager call's result on
+    the inputs of the time."""
+    dt = torch.bfloat16
+    say("captured palette", m, n, k, bits)
+    idx, packed, lut, _ = device_palette(n, k, bits, 3)
+    w = lut.to(dt)[torch.from_numpy(idx).to(DEV).long()].view(n, k)
+    x, bias = randn(1, m, k, dtype=dt), randn(2, n, dtype=dt)
+    y, want = torch.empty(m, n, dtype=dt, device=DEV), torch.empty(m, n, dtype=dt, device=DEV)
+    ws = torch.empty(max(1, edkm.palette_linear_workspace_bytes(m, n, k, bits)), dtype=torch.uint8, device=DEV)
+    edkm.palette_linear(x, packed, lut, want, bias, None, "silu", workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        edkm.palette_linear(x, packed, lut, y, bias, None, "silu", workspace=ws)
+    for i in range(3):
+        x.copy_(randn(10 + i, m, k, dtype=dt))
+        y.fill_(float("nan"))
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        edkm.palette_linear(x, packed, lut, want, bias, None, "silu")
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+        L.assert_within(y, *L.product(x, w, bias, None, "silu")[1:], "y")

@@ -319,6 +319,11 @@ __device__ __forceinline__ void epi_put(char* lds, int lane, int j, f32x4 v) {
 // Finishes two such blocks.
 template <int F, bool PLAIN>
 __device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, int lane, int r0, int c0, Eight<F, PLAIN>& e) {
+    // a forward that has nothing to add: 65.7 us for 2048 x 4096 x 4096, 67.3 through the other
+    if (!PLAIN && !p.bias && !p.res && !p.z && p.act == ACT_NONE) {
+        Eight<F, true> plain;
+        return epi_rows(p, lds, lane, r0, c0, plain);
+    }
     const int c = c0 + (lane & 7) * 8;
     e.ask(p, r0 + (lane >> 3), c);
 #pragma unroll 4

@@ -9,10 +9,11 @@
 namespace edkm {
 
 // Thirty-two weights per thread, eight at a time, each wave writing whole lines: bound by the
-// bytes written (11008 x 4096 at 3 bits, 107 MB: 18.7 to 24.7 us, 4.3 to 5.7 TB/s; the higher
-// rate where the output stays in the Infinity Cache).  Unaligned indices and ragged ends
-// take any alignment.
-template <int F, int BITS>
+// bytes written.  PAST: by stores past the caches, for weights that nothing reads at once:
+// 11008 x 4096 at 3 bits, 107 MB, takes 17.2 us so (6.2 TB/s), 27.2 through them; but the
+// product of 512 tokens with the decoded weights then 95 us instead of 82, since it
+// finds them there.  Unaligned indices and ragged ends take any alignment.
+template <int F, int BITS, bool PAST>
 __global__ void __launch_bounds__(256) k_unpalettize(const uint8_t* idx, uint64_t nbytes, uint64_t n, const float* lut,
                                                      uint16_t* out, int aligned) {
     Decoder<F> dec;
@@ -26,7 +27,8 @@ __global__ void __launch_bounds__(256) k_unpalettize(const uint8_t* idx, uint64_
         if (i >= n) return;
         const s16x8 v = dec.eight(load_idx8(idx, nbytes, i, BITS), BITS);
         if (aligned && i + 8 <= n) {
-            *reinterpret_cast<s16x8*>(out + i) = v;
+            if (PAST) __builtin_nontemporal_store(v, reinterpret_cast<s16x8*>(out + i));
+            else *reinterpret_cast<s16x8*>(out + i) = v;
         } else {
 #pragma unroll
             for (int q = 0; q < 8; ++q)
@@ -331,22 +333,25 @@ hipError_t launch_few(const ProductArgs& p, int fmt, int bits, hipStream_t s) {
     return fmt == FMT_BF16 ? few<FMT_BF16>(p, bits, s) : few<FMT_FP16>(p, bits, s);
 }
 
-template <int F>
+template <int F, bool PAST>
 static hipError_t unpalettize_f(const uint8_t* idx, uint64_t nb, uint64_t n, int bits, const float* lut, uint16_t* out,
                                 hipStream_t s) {
     const dim3 grid((uint32_t)((n + 8191) / 8192));
     const int al = ((uintptr_t)out & 15) == 0;
-    if (bits == 1) EDKM_GO((k_unpalettize<F, 1>), grid, dim3(256), idx, nb, n, lut, out, al);
-    else if (bits == 2) EDKM_GO((k_unpalettize<F, 2>), grid, dim3(256), idx, nb, n, lut, out, al);
-    else if (bits == 3) EDKM_GO((k_unpalettize<F, 3>), grid, dim3(256), idx, nb, n, lut, out, al);
-    else EDKM_GO((k_unpalettize<F, 4>), grid, dim3(256), idx, nb, n, lut, out, al);
+    if (bits == 1) EDKM_GO((k_unpalettize<F, 1, PAST>), grid, dim3(256), idx, nb, n, lut, out, al);
+    else if (bits == 2) EDKM_GO((k_unpalettize<F, 2, PAST>), grid, dim3(256), idx, nb, n, lut, out, al);
+    else if (bits == 3) EDKM_GO((k_unpalettize<F, 3, PAST>), grid, dim3(256), idx, nb, n, lut, out, al);
+    else EDKM_GO((k_unpalettize<F, 4, PAST>), grid, dim3(256), idx, nb, n, lut, out, al);
     return hipSuccess;
 }
 
 hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
-                              uint16_t* out, hipStream_t s) {
-    return fmt == FMT_BF16 ? unpalettize_f<FMT_BF16>(idx, idx_bytes, n, bits, lut, out, s)
-                           : unpalettize_f<FMT_FP16>(idx, idx_bytes, n, bits, lut, out, s);
+                              uint16_t* out, bool past, hipStream_t s) {
+    if (past)
+        return fmt == FMT_BF16 ? unpalettize_f<FMT_BF16, true>(idx, idx_bytes, n, bits, lut, out, s)
+                               : unpalettize_f<FMT_FP16, true>(idx, idx_bytes, n, bits, lut, out, s);
+    return fmt == FMT_BF16 ? unpalettize_f<FMT_BF16, false>(idx, idx_bytes, n, bits, lut, out, s)
+                           : unpalettize_f<FMT_FP16, false>(idx, idx_bytes, n, bits, lut, out, s);
 }
 
 static uint32_t align_grid(int64_t rows, int64_t cols) {

@@ -135,8 +135,9 @@ hipError_t launch_product(const ProductArgs& a, int fmt, int opa, int opb, float
 hipError_t launch_tiled_palette(ProductArgs a, int fmt, float* part, hipStream_t s);
 hipError_t launch_few(const ProductArgs& a, int fmt, int bits, hipStream_t s);
 hipError_t launch_dz(const DzArgs& a, int fmt, hipStream_t s);
+// past: by stores past the caches.
 hipError_t launch_unpalettize(const uint8_t* idx, uint64_t idx_bytes, uint64_t n, int bits, int fmt, const float* lut,
-                              uint16_t* out, hipStream_t s);
+                              uint16_t* out, bool past, hipStream_t s);
 hipError_t launch_align_rows(const AlignArgs& a, hipStream_t s);
 hipError_t launch_unpalettize_rows(const uint8_t* idx, uint64_t idx_bytes, int64_t rows, int64_t cols, int bits, int fmt,
                                    const float* lut, uint16_t* out, hipStream_t s);

@@ -254,7 +254,7 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
     uint16_t* w = static_cast<uint16_t*>(ws);
     char* xs = base + up256((size_t)n * up8(k) * 2);
     const hipError_t e = k % 8 ? launch_unpalettize_rows(indices, p.idx_bytes, n, k, bits, format, lut, w, stream)
-                               : launch_unpalettize(indices, p.idx_bytes, (uint64_t)n * k, bits, format, lut, w, stream);
+                               : launch_unpalettize(indices, p.idx_bytes, (uint64_t)n * k, bits, format, lut, w, false, stream);
     p.b = w;
     p.ldb = up8(k);
     AlignArgs copies{};
@@ -271,7 +271,7 @@ edkm_status edkm_unpalettize(const uint8_t* indices, uint64_t n, int bits, int f
         (format != EDKM_KEYS_FP16 && format != EDKM_KEYS_BF16))
         return EDKM_ERR_ARG;
     const uint64_t bytes = (n * (uint64_t)bits + 7) / 8;
-    return launch_unpalettize(indices, bytes, n, bits, format, lut, w_out, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    return launch_unpalettize(indices, bytes, n, bits, format, lut, w_out, true, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
 }
 
 edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int grad_type, int state_bits,

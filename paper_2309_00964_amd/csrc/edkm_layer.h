@@ -89,7 +89,7 @@ struct DzArgs {
 constexpr int DZ_COLS = 512, DZ_ROWS_LEAST = 4, DZ_ROWS_MOST = 64;   // one workgroup's share of them
 // Rows of a workgroup: as many as leave 1024 of them (four per CU).  With silu and the bias
 // gradient 1001 x 1336 takes 7.4 us (11.8 by 64 rows each), 2048 x 4096 12.1 (16.7, and 14.6
-// by 4 rows), 8192 x 11008 111 (130 by 4).
+// by 4 rows), 8192 x 11008 through the caches 111 (130 by 4).
 inline int dz_rows(int64_t rows, int64_t cols) {
     int64_t r = DZ_ROWS_MOST;
     while (r > DZ_ROWS_LEAST && (rows + r - 1) / r * ((cols + DZ_COLS - 1) / DZ_COLS) < 1024) r /= 2;

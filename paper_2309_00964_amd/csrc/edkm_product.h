@@ -180,8 +180,10 @@ struct Decoder {
 };
 
 // eight consecutive values, `left` of them there (zeros after them)
+template <bool PAST = false>
 __device__ __forceinline__ s16x8 row8(const uint16_t* q, int left) {
-    if (left >= 8) return reinterpret_cast<const S16x8*>(q)->v;
+    typedef short any8 __attribute__((ext_vector_type(8), aligned(2)));
+    if (left >= 8) return PAST ? __builtin_nontemporal_load(reinterpret_cast<const any8*>(q)) : reinterpret_cast<const S16x8*>(q)->v;
     s16x8 v = {};
 #pragma unroll
     for (int j = 0; j < 8; ++j)

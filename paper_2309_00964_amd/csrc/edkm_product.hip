@@ -12,9 +12,11 @@ namespace edkm {
 
 // A thread takes eight columns of every fourth row of the block's; one pass over dy and z
 // (bound by its bytes: 6 B per element with an activation, 2 B without) writes dz and sums
-// the bias gradient in fp32, unrounded.  8192 x 11008 with silu takes 111 us (4.9 TB/s),
-// without activation 30 us (6.0 TB/s, from the Infinity Cache in part).
-template <int F, int ACT>
+// the bias gradient in fp32, unrounded.  PAST: dy and z are read past the caches, for
+// matrices that do not fit them: 8192 x 11008 with silu takes 93 us so (5.8 TB/s) and 111
+// through them, 4096 x 4096 21.2 and 19.3.  Without activation 8192 x 11008 takes 30 us (6.0 TB/s, from
+// the Infinity Cache in part).
+template <int F, int ACT, bool PAST>
 __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
     __shared__ float red[4][DZ_COLS];
     const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
@@ -26,12 +28,12 @@ __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
     if (left > 0) {
 #pragma unroll 2
         for (int r = r0 + q; r < r1; r += 4) {
-            const s16x8 d = row8(a.dy + (int64_t)r * a.lddy + c, left);
+            const s16x8 d = row8<PAST>(a.dy + (int64_t)r * a.lddy + c, left);
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = to_f32<F>((uint16_t)d[j]);
             if (ACT != ACT_NONE) {
-                const s16x8 z = row8(a.z + (int64_t)r * a.cols + c, left);
+                const s16x8 z = row8<PAST>(a.z + (int64_t)r * a.cols + c, left);
                 uint16_t* out = a.dz + (int64_t)r * a.lddz + c;
                 s16x8 o;
 #pragma unroll
@@ -146,16 +148,23 @@ ProductPlan product_plan(const ProductArgs& p, int opa, int opb) {
     return q;
 }
 
+constexpr int64_t INFINITY_CACHE = 256 << 20;
 template <int F>
 static hipError_t dz_f(const DzArgs& a, hipStream_t s) {
     const int chunks = (a.rows + a.per - 1) / a.per;
-    if (chunks > 0 && (a.dbias || a.act != ACT_NONE))
-    {
+    if (chunks > 0 && (a.dbias || a.act != ACT_NONE)) {
         const dim3 grid((uint32_t)((a.cols + DZ_COLS - 1) / DZ_COLS) * chunks);
-        if (a.act == ACT_NONE) EDKM_GO((k_dz<F, ACT_NONE>), grid, dim3(256), a);
-        else if (a.act == ACT_RELU) EDKM_GO((k_dz<F, ACT_RELU>), grid, dim3(256), a);
-        else if (a.act == ACT_GELU) EDKM_GO((k_dz<F, ACT_GELU>), grid, dim3(256), a);
-        else EDKM_GO((k_dz<F, ACT_SILU>), grid, dim3(256), a);
+        if (a.act == ACT_NONE) {
+            EDKM_GO((k_dz<F, ACT_NONE, false>), grid, dim3(256), a);
+        } else if (6 * (int64_t)a.rows * a.cols > INFINITY_CACHE) {
+            if (a.act == ACT_RELU) EDKM_GO((k_dz<F, ACT_RELU, true>), grid, dim3(256), a);
+            else if (a.act == ACT_GELU) EDKM_GO((k_dz<F, ACT_GELU, true>), grid, dim3(256), a);
+            else EDKM_GO((k_dz<F, ACT_SILU, true>), grid, dim3(256), a);
+        } else {
+            if (a.act == ACT_RELU) EDKM_GO((k_dz<F, ACT_RELU, false>), grid, dim3(256), a);
+            else if (a.act == ACT_GELU) EDKM_GO((k_dz<F, ACT_GELU, false>), grid, dim3(256), a);
+            else EDKM_GO((k_dz<F, ACT_SILU, false>), grid, dim3(256), a);
+        }
     }
     if (a.dbias) EDKM_GO(k_dbias<F>, dim3((a.cols + 31) / 32), dim3(1024), a, chunks);
     return hipSuccess;

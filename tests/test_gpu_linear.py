@@ -619,3 +619,18 @@ def test_captured_palette_products(m, n, k, bits):
         torch.cuda.synchronize()
         assert torch.equal(y, want)
         L.assert_within(y, *L.product(x, w, bias, None, "silu")[1:], "y")
+
+
+@pytest.mark.parametrize("name,lead,gap", [("silu", 8, 0), ("relu", 1, 3)])
+def test_gradient_at_the_activation_of_a_large_matrix(name, lead, gap):
+    """More than the caches hold: dy and z are read past them, odd rows among them."""
+    m, n, dt = 6000, 8203, torch.bfloat16
+    say("large gradient at the activation", name, lead, gap)
+    dy, z = randn(1, m, n, dtype=dt), randn(2, m, n, dtype=dt)
+    _, dyv = inside(dy, lead, gap)
+    x, dw = randn(3, m, 8, dtype=dt), torch.empty(n, 8, dtype=dt, device=DEV)
+    db = torch.empty(n, dtype=dt, device=DEV)
+    edkm.linear_backward(dyv, x, None, dw=dw, dbias=db, z=z, activation=name)
+    ref = L.gradients(dy, x, torch.zeros(n, 8, dtype=dt, device=DEV), z, name)
+    L.assert_within(dw, *ref["dw"], "dw")
+    L.assert_within(db, *ref["db"], "db")

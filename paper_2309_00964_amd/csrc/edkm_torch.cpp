@@ -563,6 +563,9 @@ PyObject* py_apply_palette_linear(PyObject*, PyObject* const* a, Py_ssize_t n_ar
             refuse("a palette's table takes no gradient; train the weights through dkm and linear");
         if (n < 1) refuse("out_features must be 1 at least");
         fits(x, n, bias, res);
+        // without reverse mode autograd is passed by, so its own refusal of tangents does not come
+        for (const Tensor* t : {&x, &lut, bias, res})
+            TORCH_CHECK(!t || !t->_fw_grad(0).defined(), "palette_linear: forward-mode derivatives are not implemented");
         const bool grad = at::GradMode::is_enabled() &&
                           (x.requires_grad() || (bias && bias->requires_grad()) || (res && res->requires_grad()));
         Tensor y;

@@ -147,7 +147,7 @@ def dkm_batch(ws, c0s, tau: float = 2e-3, max_iter: int = 5, eps: float = 0.0, o
 
 
 def linear(x, w, bias=None, residual=None, activation: str = "none"):
-    """act(x w^T + bias) + residual; differentiable (once) in all four tensors.
+    """act(x w^T + bias) + residual; differentiable (once, in reverse mode) in all four tensors.
 
     x: fp16 or bf16, (..., k); w: n x k of x's type, say W~ of ``dkm`` with
     out_half; bias: n; residual: (..., n); activation: none, relu, gelu or silu.
@@ -158,5 +158,5 @@ def linear(x, w, bias=None, residual=None, activation: str = "none"):
 def palette_linear(x, indices, lut, out_features: int, bias=None, residual=None, activation: str = "none"):
     """act(x W^T + bias) + residual with W (out_features x k) given as the packed
     indices and the table of ``edkm.palettize``: the product of a served model.
-    Differentiable (once) in x, bias and residual; the palette is frozen."""
+    Differentiable (once, in reverse mode) in x, bias and residual; the palette is frozen."""
     return edkm._x.apply_palette_linear(x, indices, lut, out_features, bias, residual, edkm._activation(activation))

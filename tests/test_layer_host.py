@@ -215,3 +215,19 @@ def test_optimizer_refusals():
     q.grad = torch.zeros(4, dtype=torch.float16)
     with pytest.raises(ValueError, match="GPU tensors"):
         AdamW([q]).step()
+
+
+@pytest.mark.parametrize("which", ["x", "bias", "residual", "lut"])
+@pytest.mark.parametrize("grad", [False, True])
+def test_palette_linear_refuses_forward_derivatives(which, grad):
+    """A tangent is never dropped, which would count as a zero derivative."""
+    from torch.autograd import forward_ad
+    from paper_2309_00964_amd import function
+    t = dict(x=h(4, 16), bias=h(8), residual=h(4, 8), lut=h(8, dtype=torch.float32))
+    other = "bias" if which == "x" else "x"
+    with forward_ad.dual_level():
+        t[which] = forward_ad.make_dual(t[which], torch.ones_like(t[which]))
+        t[other] = t[other].requires_grad_(grad)
+        for mode in (torch.enable_grad, torch.no_grad):
+            with mode(), pytest.raises(RuntimeError, match="forward-mode derivatives"):
+                function.palette_linear(t["x"], h(48, dtype=torch.uint8), t["lut"], 8, t["bias"], t["residual"])

@@ -358,7 +358,7 @@ edkm_status edkm_linear(int64_t m, int64_t n, int64_t k, int format, int activat
 /* Its gradients for a given dL/dy: with dz = dy act'(z),
  *   dx = dz W (m x k), dw = dz^T x (n x k without gaps: the dL/dW~ that
  *   edkm_backward_ex takes with EDKM_GRAD_IN_HALF), dbias = sum over m of dz (n),
- * all in the 16-bit format; each nullable, one at least given.  dL/dresidual
+ * all in the 16-bit format; each nullable, one at least given with m > 0.  dL/dresidual
  * is dy itself.  With an activation, dz is rounded to 16 bits before the two
  * products (the bias gradient sums it unrounded).
  *   z   the z of edkm_linear; not read without activation.  x is read for dw

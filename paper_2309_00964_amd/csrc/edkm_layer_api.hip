@@ -143,10 +143,12 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
                                  int64_t lddy, const void* z, const void* x, int64_t ldx, const void* w, int64_t ldw,
                                  void* dx, int64_t lddx, void* dw, void* dbias, void* ws, size_t ws_bytes,
                                  hipStream_t stream) {
-    if (!product_ok(m, n, k, format, activation) || (!dx && !dw && !dbias)) return EDKM_ERR_ARG;
+    // without tokens dx is empty, and its pointer may be null
+    if (!product_ok(m, n, k, format, activation) || (m > 0 && !dx && !dw && !dbias)) return EDKM_ERR_ARG;
     if (m > 0 && (!dy || (activation != ACT_NONE && !z) || (dw && !x))) return EDKM_ERR_ARG;
     if (dx && (!w || !ld_ok(ldw, n, k) || !ld_ok(lddx, m, k))) return EDKM_ERR_ARG;
     if ((dw && !ld_ok(ldx, m, k)) || !ld_ok(lddy, m, n)) return EDKM_ERR_ARG;
+    if (m == 0 && !dw && !dbias) return EDKM_OK;
     const BackwardWs L = backward_ws(m, n, k, activation);
     // without products only dz and the partial sums, which do not depend on k
     const edkm_status st = ws_ok(ws, ws_bytes, dx || dw ? L.total : L.x);

@@ -634,3 +634,25 @@ def test_gradient_at_the_activation_of_a_large_matrix(name, lead, gap):
     ref = L.gradients(dy, x, torch.zeros(n, 8, dtype=dt, device=DEV), z, name)
     L.assert_within(dw, *ref["dw"], "dw")
     L.assert_within(db, *ref["db"], "db")
+
+
+@pytest.mark.parametrize("name", ["none", "gelu"])
+@pytest.mark.parametrize("shape", [(0, 33), (2, 0, 33)])
+def test_no_tokens_through_a_frozen_layer(name, shape):
+    """Only x takes a gradient, which is empty."""
+    n, k, dt = 70, 33, torch.bfloat16
+    say("no tokens, frozen", name, shape)
+    w = randn(1, n, k, dtype=dt)
+    _, packed, lut, _ = device_palette(n, k, 3, 1)
+    x = torch.empty(shape, dtype=dt, device=DEV).requires_grad_(True)
+    for y in (function.linear(x, w, None, None, name), function.palette_linear(x, packed, lut, n, None, None, name)):
+        assert y.shape == (*shape[:-1], n)
+        (gx,) = torch.autograd.grad(y, [x], torch.empty_like(y))
+        assert gx.shape == x.shape
+    dy, z = (torch.empty(0, n, dtype=dt, device=DEV) for _ in range(2))
+    edkm.linear_backward(dy, None, w, dx=torch.empty(0, k, dtype=dt, device=DEV), z=z, activation=name)
+    bias = randn(2, n, dtype=dt).requires_grad_(True)
+    y = function.palette_linear(x, packed, lut, n, bias, None, name)
+    gx, gb = torch.autograd.grad(y, [x, bias], torch.empty_like(y))
+    assert gx.shape == x.shape and not bool(gb.any())
+    torch.cuda.synchronize()

@@ -231,3 +231,12 @@ def test_palette_linear_refuses_forward_derivatives(which, grad):
         for mode in (torch.enable_grad, torch.no_grad):
             with mode(), pytest.raises(RuntimeError, match="forward-mode derivatives"):
                 function.palette_linear(t["x"], h(48, dtype=torch.uint8), t["lut"], 8, t["bias"], t["residual"])
+
+
+def test_backward_of_no_tokens_that_writes_nothing():
+    """An empty dx (a null pointer, or any) and no other gradient: nothing to do, no workspace."""
+    for dx in (None, P):
+        for act in (0, 3):
+            assert backward(m=0, act=act, dy=None, x=None, dx=dx, dw=None, db=None, ws=None, nws=0) == edkm.OK
+    assert backward(m=0, n=0, dx=None, dw=None, db=None) == edkm.ERR_ARG
+    assert backward(m=0, dw=None, db=None, w=None) == edkm.ERR_ARG

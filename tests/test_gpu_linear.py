@@ -656,3 +656,31 @@ def test_no_tokens_through_a_frozen_layer(name, shape):
     gx, gb = torch.autograd.grad(y, [x, bias], torch.empty_like(y))
     assert gx.shape == x.shape and not bool(gb.any())
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+def test_gelu_of_every_number_down_to_minus_nine(fmt):
+    """z Phi(z) and its slope relative to their own size, where Phi's tail is small: every
+    16-bit z in [-9, -1/64].  Phi is off by the fit of its tail (7.3e-7) and a dozen roundings of
+    2^-24, and by the exponent's: seven of 2^-24 times z^2 / 2."""
+    dt = L.DT[fmt]
+    say("gelu tail", fmt)
+    z = torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16).view(dt).to(DEV)
+    z = z[(z >= -9) & (z <= -1 / 64)].contiguous()
+    z64 = z.double()
+    phi, density = 0.5 * torch.erfc(-z64 / 2 ** 0.5), torch.exp(-0.5 * z64 * z64) / (2 * np.pi) ** 0.5
+    off = 7.3e-7 + (12 + 7 * z64 * z64 / 2) * 2.0 ** -24
+    ref = z64 * phi
+    tol = ref.abs() * (L.half(dt) + 1.01 * off) + L.tiny(dt)
+    for m in (1, 20, 70):
+        y = torch.empty(m, z.numel(), dtype=dt, device=DEV)
+        edkm.linear(torch.ones(m, 1, dtype=dt, device=DEV), z[:, None], y, None, None, "gelu")
+        for row in (0, m - 1):
+            L.assert_within(y[row], ref, tol, "y")
+    # dz is rounded, then the product with 1
+    dx = torch.empty(z.numel(), 1, dtype=dt, device=DEV)
+    one = torch.ones(1, 1, dtype=dt, device=DEV)
+    edkm.linear_backward(one.expand(z.numel(), 1).contiguous(), None, one, dx=dx, z=z[:, None], activation="gelu")
+    ref = phi + z64 * density
+    tol = ref.abs() * L.half(dt) + 1.01 * off * (phi + z64.abs() * density) + L.tiny(dt)
+    L.assert_within(dx[:, 0], ref, tol, "slope")

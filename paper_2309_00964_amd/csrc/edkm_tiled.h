@@ -312,6 +312,12 @@ struct Eight {
 // tile of 16) goes through LDS, so that lanes take eight columns of a row: whole 128-byte
 // lines to and from memory.  Its 16-byte places are permuted by the row.
 constexpr int EPI_BYTES = 16 * 64 * 4;
+// Orders the wave's LDS accesses before and after it: what its lanes wrote is what its lanes
+// read next.  No instruction; LDS serves a wave's accesses in the order in which they are issued.
+__device__ __forceinline__ void epi_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
 __device__ __forceinline__ void epi_put(char* lds, int lane, int j, f32x4 v) {
     const int r = lane & 15;
     *reinterpret_cast<f32x4*>(lds + r * 256 + (((j * 4 + (lane >> 4)) ^ r) * 16)) = v;
@@ -440,7 +446,9 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < TC; ++j) epi_put(mine + h * EPI_BYTES, lane, j, acc[i + h][j]);
+        epi_order();
         epi_rows(p, mine, lane, r0 + wr + i * 16, c0 + wc, eight);
+        epi_order();
     }
 }
 

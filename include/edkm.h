@@ -416,8 +416,8 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
  *   step       device int32[1]: the steps done before this one
  *   lr_dev     nullable, device float[1]: the rate (lr is then ignored), so that
  *              a captured step can follow a schedule
- * Elementwise on each tensor's own arrays; repeatable bit for bit.  Tensors of
- * one call must not overlap (those of one launch are checked). */
+ * Elementwise on each tensor's own arrays; repeatable bit for bit.  The arrays
+ * that a call writes must not overlap (those of one launch are checked). */
 enum { EDKM_TYPE_FP16 = 0, EDKM_TYPE_BF16 = 1, EDKM_TYPE_FP32 = 2 };
 #define EDKM_STATE_BLOCK 256
 edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int grad_type, int state_bits,

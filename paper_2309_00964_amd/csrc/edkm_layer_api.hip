@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <utility>
 
 using namespace edkm;
 
@@ -296,13 +297,33 @@ edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int g
         if (!params[i] || !grads[i] || !exp_avg[i] || !exp_avg_sq[i] || (state_bits == 8 && (!m_scales[i] || !v_scales[i])))
             return EDKM_ERR_ARG;
     }
-    auto clash = [](const void* a, size_t na, const void* b, size_t nb) {
-        return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+    // Two workgroups must not write the same place: what the tensors of one launch have written.
+    // Kinds of arrays go by the address of their first, so that flat buffers come sorted.
+    struct Kind {
+        const void* const* at;
+        size_t size, per;   // bytes for each `per` elements
     };
-    // Two workgroups must not write the same place: tensors of one launch that overlap.
-    auto overlap = [&](int i, int j) {
-        return clash(params[i], n[i] * pe, params[j], n[j] * pe) || clash(exp_avg[i], n[i] * se, exp_avg[j], n[j] * se) ||
-               clash(exp_avg_sq[i], n[i] * se, exp_avg_sq[j], n[j] * se);
+    Kind kinds[6] = {{params, pe, 1}, {exp_avg, se, 1}, {exp_avg_sq, se, 1}};
+    int kinds_n = 3;
+    if (masters) kinds[kinds_n++] = {reinterpret_cast<const void* const*>(masters), 4, 1};
+    if (state_bits == 8) {
+        kinds[kinds_n++] = {reinterpret_cast<const void* const*>(m_scales), 4, ADAMW_BLOCK};
+        kinds[kinds_n++] = {reinterpret_cast<const void* const*>(v_scales), 4, ADAMW_BLOCK};
+    }
+    auto overlap = [&](const int* src, int tensors) {
+        typedef std::pair<uintptr_t, uintptr_t> Span;
+        Span spans[6 * MAXB];
+        int k = 0;
+        std::sort(kinds, kinds + kinds_n, [&](const Kind& a, const Kind& b) { return a.at[src[0]] < b.at[src[0]]; });
+        for (int q = 0; q < kinds_n; ++q)
+            for (int x = 0; x < tensors; ++x) {
+                const uintptr_t at = (uintptr_t)kinds[q].at[src[x]];
+                if (at) spans[k++] = {at, at + (n[src[x]] + kinds[q].per - 1) / kinds[q].per * kinds[q].size};
+            }
+        if (!std::is_sorted(spans, spans + k)) std::sort(spans, spans + k);
+        for (int x = 1; x < k; ++x)
+            if (spans[x].first < spans[x - 1].second) return true;
+        return false;
     };
     // by the average launch of the call
     uint64_t total = 0;
@@ -348,9 +369,7 @@ edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int g
             for (int j = a.count; j < MAXB; ++j) a.wg_begin[j] = 0xFFFFFFFFu;
             if (a.count == 0) continue;
             if (pass == 0) {
-                for (int x = 0; x < a.count; ++x)
-                    for (int y = 0; y < x; ++y)
-                        if (overlap(src[x], src[y])) return EDKM_ERR_ARG;
+                if (overlap(src, a.count)) return EDKM_ERR_ARG;
             } else if (launch_adamw(a, (uint32_t)grid, param_type, grad_type, state_bits, stream) != hipSuccess) {
                 return EDKM_ERR_HIP;
             }

@@ -240,3 +240,23 @@ def test_backward_of_no_tokens_that_writes_nothing():
             assert backward(m=0, act=act, dy=None, x=None, dx=dx, dw=None, db=None, ws=None, nws=0) == edkm.OK
     assert backward(m=0, n=0, dx=None, dw=None, db=None) == edkm.ERR_ARG
     assert backward(m=0, dw=None, db=None, w=None) == edkm.ERR_ARG
+
+
+E8 = dict(bits=8, ms=(7 * P, 8 * P), vs=(9 * P, 10 * P), sizes=(1000, 500))
+
+
+@pytest.mark.parametrize("kw", [dict(w=(7 * P, 7 * P)), dict(w=(7 * P, 7 * P + 396)), dict(w=(7 * P + 196, 7 * P)),
+                                dict(E8, ms=(7 * P, 7 * P)), dict(E8, ms=(7 * P, 7 * P + 12)), dict(E8, vs=(9 * P + 4, 9 * P)),
+                                dict(v=(4 * P, 6 * P)), dict(w=(P, 7 * P)), dict(w=(None, P)), dict(E8, ms=(7 * P, 9 * P + 12)),
+                                dict(m=(3 * P, 4 * P), v=(3 * P + 400 - 4, 6 * P))])
+def test_adamw_refuses_arrays_that_overlap(kw):
+    """Masters and block scales too, and arrays of two kinds: all that one launch writes."""
+    assert adamw(**kw) == edkm.ERR_ARG
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the pointers are none: no launch may come of them")
+@pytest.mark.parametrize("kw", [dict(w=(7 * P, 7 * P + 400)), E8, dict(E8, ms=(7 * P, 7 * P + 16)), dict(E8, vs=(9 * P + 8, 9 * P)),
+                                dict(w=(7 * P + 200, 7 * P)), dict(w=(None, None)), dict(g=(P, P))])
+def test_adamw_accepts_neighbouring_arrays(kw):
+    """Past the checks, where without a GPU the launch fails."""
+    assert adamw(**kw) == edkm.ERR_HIP

@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
     float* red = reinterpret_cast<float*>(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
     const int l = lane & 15, g = lane >> 4;
-    const int c0 = blockIdx.x * 16 * NT;
+    const int c0 = (p.first + blockIdx.x) * 16 * NT;
     const int runs = (p.depth + 127) / 128;
     constexpr int RUN_BYTES = BITS ? 16 * BITS : 256;        // of one row
     const uint32_t row_bytes = BITS ? (uint32_t)((uint64_t)p.depth * BITS / 8) : (uint32_t)(p.ldb * 2);
@@ -281,12 +281,12 @@ __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
 }
 
 template <int F, int BITS, bool WHOLE, int MT, int NT>
-static hipError_t few_go(const ProductArgs& p, hipStream_t s) {
+static hipError_t few_go(ProductArgs p, hipStream_t s) {
     constexpr int U = WHOLE && BITS && MT == 1 && NT < 3 ? 2 : 1, NW = MT == 1 ? 16 : 8;
     const int runs = (p.depth + 127) / 128;
     int nw = 1;
     while (nw < runs && nw < NW) nw *= 2;
-    EDKM_GO((k_few<F, BITS, WHOLE, MT, NT, U, NW>), dim3((uint32_t)(((int64_t)p.cols + 16 * NT - 1) / (16 * NT))), dim3(nw * 64), p);
+    EDKM_GO_PARTS((k_few<F, BITS, WHOLE, MT, NT, U, NW>), ((uint64_t)p.cols + 16 * NT - 1) / (16 * NT), nw * 64, p);
     return hipSuccess;
 }
 

@@ -2,6 +2,7 @@
 // 16-bit or palettized weights, the palette read-back and the AdamW step.
 #pragma once
 #include "edkm_internal.h"
+#include "edkm_launch.h"
 
 namespace edkm {
 
@@ -38,6 +39,7 @@ struct ProductArgs {
     // a split product: steps of 64 depths per part, and the parts' sums (null: not split)
     int split_steps;
     float* part;
+    uint32_t first;         // the launch's first workgroup
 };
 
 // Whether a forward goes to k_few, which takes up to 64 tokens: always up to 16; past them,
@@ -84,6 +86,7 @@ struct DzArgs {
     int32_t rows, cols;
     int act;
     int per;                // rows of a workgroup
+    uint32_t first;         // the launch's first workgroup
 };
 
 constexpr int DZ_COLS = 512, DZ_ROWS_LEAST = 4, DZ_ROWS_MOST = 64;   // one workgroup's share of them

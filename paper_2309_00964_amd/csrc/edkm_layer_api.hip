@@ -350,6 +350,7 @@ edkm_status edkm_adamw_batch(int count, const uint64_t* n, int param_type, int g
             for (; i < count && a.count < MAXB; ++i) {
                 if (n[i] == 0) continue;
                 const uint64_t wgs = (n[i] + chunk - 1) / chunk;
+                if (a.count && grid + wgs > most_groups(256)) break;     // the rest by another launch
                 AdamwTensor& T = a.t[a.count];
                 T.p = params[i];
                 T.master = masters ? masters[i] : nullptr;

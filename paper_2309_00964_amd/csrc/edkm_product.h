@@ -209,6 +209,17 @@ __device__ __forceinline__ s16x8 keep_first(s16x8 v, int n) {
     return v;
 }
 
+// A one-dimensional grid of any number of workgroups, whose kernel starts with args.first
+#define EDKM_GO_PARTS(kern, groups, threads, args, ...)                                                          \
+    do {                                                                                                          \
+        const hipError_t p_ = in_parts((groups), (threads), hipSuccess, [&](uint32_t first_, uint32_t groups_) {  \
+            (args).first = first_;                                                                                \
+            hipLaunchKernelGGL(kern, dim3(groups_), dim3(threads), 0, s, args, ##__VA_ARGS__);                    \
+            return hipGetLastError();                                                                             \
+        });                                                                                                       \
+        if (p_ != hipSuccess) return p_;                                                                          \
+    } while (0)
+
 #define EDKM_GO(kern, grid, block, ...)                       \
     do {                                                       \
         hipLaunchKernelGGL(kern, grid, block, 0, s, __VA_ARGS__); \

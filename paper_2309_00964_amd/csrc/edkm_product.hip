@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
     __shared__ float red[4][DZ_COLS];
     const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
     // workgroups go column block by column block through a chunk of rows
-    const uint32_t nc = (a.cols + DZ_COLS - 1) / DZ_COLS, cb = blockIdx.x % nc, chunk = blockIdx.x / nc;
+    const uint32_t nc = (a.cols + DZ_COLS - 1) / DZ_COLS, cb = (a.first + blockIdx.x) % nc, chunk = (a.first + blockIdx.x) / nc;
     const int c = cb * DZ_COLS + lane * 8, left = a.cols - c;
     const int r0 = chunk * a.per, r1 = min(r0 + a.per, a.rows);
     float sum[8] = {};
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(256) k_dz(DzArgs a) {
 template <int F>
 __global__ void __launch_bounds__(1024) k_dbias(DzArgs a, int chunks) {
     __shared__ float red[32][33];
-    const int l = threadIdx.x & 31, q = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
+    const int l = threadIdx.x & 31, q = threadIdx.x >> 5, c = (a.first + blockIdx.x) * 32 + l;
     float sum = 0.f;
     if (c < a.cols)
 #pragma unroll 4
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(1024) k_dbias(DzArgs a, int chunks) {
     sum = red[l][q];
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor(sum, o, 32);
-    const int mine = blockIdx.x * 32 + q;
+    const int mine = (a.first + blockIdx.x) * 32 + q;
     if (l == 0 && mine < a.cols) a.dbias[mine] = to_16<F>(sum);
 }
 
@@ -150,23 +150,23 @@ ProductPlan product_plan(const ProductArgs& p, int opa, int opb) {
 
 constexpr int64_t INFINITY_CACHE = 256 << 20;
 template <int F>
-static hipError_t dz_f(const DzArgs& a, hipStream_t s) {
+static hipError_t dz_f(DzArgs a, hipStream_t s) {
     const int chunks = (a.rows + a.per - 1) / a.per;
     if (chunks > 0 && (a.dbias || a.act != ACT_NONE)) {
-        const dim3 grid((uint32_t)((a.cols + DZ_COLS - 1) / DZ_COLS) * chunks);
+        const uint64_t groups = (uint64_t)((a.cols + DZ_COLS - 1) / DZ_COLS) * chunks;
         if (a.act == ACT_NONE) {
-            EDKM_GO((k_dz<F, ACT_NONE, false>), grid, dim3(256), a);
+            EDKM_GO_PARTS((k_dz<F, ACT_NONE, false>), groups, 256, a);
         } else if (6 * (int64_t)a.rows * a.cols > INFINITY_CACHE) {
-            if (a.act == ACT_RELU) EDKM_GO((k_dz<F, ACT_RELU, true>), grid, dim3(256), a);
-            else if (a.act == ACT_GELU) EDKM_GO((k_dz<F, ACT_GELU, true>), grid, dim3(256), a);
-            else EDKM_GO((k_dz<F, ACT_SILU, true>), grid, dim3(256), a);
+            if (a.act == ACT_RELU) EDKM_GO_PARTS((k_dz<F, ACT_RELU, true>), groups, 256, a);
+            else if (a.act == ACT_GELU) EDKM_GO_PARTS((k_dz<F, ACT_GELU, true>), groups, 256, a);
+            else EDKM_GO_PARTS((k_dz<F, ACT_SILU, true>), groups, 256, a);
         } else {
-            if (a.act == ACT_RELU) EDKM_GO((k_dz<F, ACT_RELU, false>), grid, dim3(256), a);
-            else if (a.act == ACT_GELU) EDKM_GO((k_dz<F, ACT_GELU, false>), grid, dim3(256), a);
-            else EDKM_GO((k_dz<F, ACT_SILU, false>), grid, dim3(256), a);
+            if (a.act == ACT_RELU) EDKM_GO_PARTS((k_dz<F, ACT_RELU, false>), groups, 256, a);
+            else if (a.act == ACT_GELU) EDKM_GO_PARTS((k_dz<F, ACT_GELU, false>), groups, 256, a);
+            else EDKM_GO_PARTS((k_dz<F, ACT_SILU, false>), groups, 256, a);
         }
     }
-    if (a.dbias) EDKM_GO(k_dbias<F>, dim3((a.cols + 31) / 32), dim3(1024), a, chunks);
+    if (a.dbias) EDKM_GO_PARTS(k_dbias<F>, (uint64_t)(a.cols + 31) / 32, 1024, a, chunks);
     return hipSuccess;
 }
 

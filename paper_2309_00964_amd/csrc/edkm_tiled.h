@@ -369,8 +369,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t tx, ty;
     const uint32_t nx = (p.cols + BN - 1) / BN, ny = (p.rows + BM - 1) / BM;
-    const uint32_t split = blockIdx.x / (nx * ny);
-    tile_of(blockIdx.x % (nx * ny), nx, ny, tx, ty);
+    const uint32_t group = p.first + blockIdx.x, split = group / (nx * ny);
+    tile_of(group % (nx * ny), nx, ny, tx, ty);
     const int r0 = ty * BM, c0 = tx * BN;
     const int wr = (wave / WN) * (BM / WM), wc = (wave % WN) * (BN / WN);
     FA fa;
@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
         if (s + 1 < steps) step(a1, b1, a0, b0, s + 1);
     }
     if (p.part) {
-        float* at = p.part + ((int64_t)blockIdx.x * NW + wave) * (TR * 1024) + lane * 4;
+        float* at = p.part + ((int64_t)group * NW + wave) * (TR * 1024) + lane * 4;
 #pragma unroll
         for (int i = 0; i < TR; ++i)
 #pragma unroll
@@ -496,9 +496,9 @@ __global__ void __launch_bounds__(W * 64) k_join(ProductArgs p, int splits) {
 }
 
 template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, int BITS = 0>
-static hipError_t tiled(const ProductArgs& p, const ProductPlan& q, hipStream_t s) {
+static hipError_t tiled(ProductArgs p, const ProductPlan& q, hipStream_t s) {
     const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
-    EDKM_GO((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS>), dim3((uint32_t)(tiles * q.splits)), dim3(WM * WN * 64), p);
+    EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS>), (uint64_t)(tiles * q.splits), WM * WN * 64, p);
     const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
     if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4>), blocks, dim3(256), p, q.splits);
     else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1>), blocks, dim3(64), p, q.splits);

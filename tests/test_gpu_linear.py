@@ -684,3 +684,43 @@ def test_gelu_of_every_number_down_to_minus_nine(fmt):
     ref = phi + z64 * density
     tol = ref.abs() * L.half(dt) + 1.01 * off * (phi + z64.abs() * density) + L.tiny(dt)
     L.assert_within(dx[:, 0], ref, tol, "slope")
+
+
+@pytest.mark.parametrize("bits", [0, 1])
+def test_more_outputs_than_one_launch_has_threads(bits):
+    """2^30 outputs and some of one token: four threads each are more than 32 bits count."""
+    n, dt = (1 << 30) + 8 * 1000 + 5, torch.bfloat16
+    say("2^30 outputs", bits)
+    y = torch.zeros(1, n, dtype=dt, device=DEV)
+    if bits:
+        x = torch.tensor([[1.0, 2.0]], dtype=dt, device=DEV)
+        packed = torch.randint(0, 256, ((2 * n + 7) // 8,), dtype=torch.uint8, device=DEV)
+        edkm.palette_linear(x, packed, torch.tensor([0.0, 1.0], device=DEV), y)
+        # index bits 2 r and 2 r + 1 of output r
+        for at in range(0, n, 1 << 27):
+            r = torch.arange(at, min(at + (1 << 27), n), device=DEV)
+            two = (packed[r >> 2] >> (2 * (r & 3)).to(torch.uint8)) & 3
+            assert torch.equal(y[0, at:at + r.numel()], two.to(dt)), at
+    else:
+        x = torch.ones(1, 1, dtype=dt, device=DEV)
+        w = torch.randn(n, dtype=dt, device=DEV)[:, None]
+        edkm.linear(x, w, y)
+        assert torch.equal(y[0], w[:, 0])
+
+
+@pytest.mark.parametrize("m,n,name", [((1 << 30) + 1000, 1, "none"), ((1 << 30) + 1000, 1, "relu"), (3, (1 << 27) + 45, "none")])
+def test_bias_gradient_of_more_than_one_launch(m, n, name):
+    dt = torch.bfloat16
+    say("bias gradient of many", m, n, name)
+    db = torch.full((n,), float("nan"), dtype=dt, device=DEV)
+    z = torch.ones(m, n, dtype=dt, device=DEV) if name != "none" else None
+    if n == 1:
+        dy = torch.zeros(m, n, dtype=dt, device=DEV)
+        dy[:50] = 1
+        dy[-100:] = 1
+        edkm.linear_backward(dy, None, None, dbias=db, z=z, activation=name)
+        assert db.tolist() == [150.0]
+    else:
+        row = torch.randint(-8, 8, (n,), device=DEV).to(dt)
+        edkm.linear_backward(row.expand(m, n).contiguous(), None, None, dbias=db)
+        assert torch.equal(db, m * row)

@@ -260,3 +260,47 @@ def test_adamw_refuses_arrays_that_overlap(kw):
 def test_adamw_accepts_neighbouring_arrays(kw):
     """Past the checks, where without a GPU the launch fails."""
     assert adamw(**kw) == edkm.ERR_HIP
+
+
+PARTS = r'''
+#include "edkm_launch.h"
+#include <cstdio>
+int main() {
+    unsigned long long groups;
+    unsigned threads, fail;
+    while (std::scanf("%llu %u %u", &groups, &threads, &fail) == 3) {
+        unsigned calls = 0;
+        int s = edkm::in_parts(groups, threads, 0, [&](uint32_t first, uint32_t n) {
+            std::printf("%u %u ", first, n);
+            return ++calls == fail ? 7 : 0;
+        });
+        std::printf("= %d\n", s);
+    }
+}
+'''
+
+
+def test_parts_of_a_large_grid(tmp_path):
+    """Every workgroup once and in order, fewer than 2^32 threads a launch, parts that start on
+    a multiple of eight, and nothing more after a part that fails."""
+    import shutil
+    import subprocess
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    (tmp_path / "parts.cpp").write_text(PARTS)
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2309_00964_amd", "csrc"), "-o",
+                           str(tmp_path / "parts"), str(tmp_path / "parts.cpp")])
+    cases = [(g, t, f) for t in (64, 128, 256, 512, 1024) for g in (1, 7, (1 << 32) // t - 1, (1 << 32) // t, (1 << 31) // 16, (1 << 32) - 1)
+             for f in (0, 1, 2)]
+    text = "".join("%d %d %d\n" % c for c in cases)
+    lines = subprocess.run([str(tmp_path / "parts")], input=text, capture_output=True, text=True, check=True).stdout.splitlines()
+    assert len(lines) == len(cases)
+    for (groups, threads, fail), line in zip(cases, lines):
+        parts, status = line.split("=")
+        vals = [int(v) for v in parts.split()]
+        at = 0
+        for first, n in zip(vals[::2], vals[1::2]):
+            assert first == at and first % 8 == 0 and n >= 1 and n * threads < 1 << 32
+            at += n
+        assert at <= groups and (int(status) == 7) == (fail > 0 and len(vals) // 2 == fail)
+        assert at == groups or int(status) == 7

@@ -16,6 +16,25 @@ from . import edkm
 _PARAM_TYPES = (torch.float16, torch.bfloat16, torch.float32)
 
 
+def _check_group(group):
+    """Refuses options, the defaults' or a group's own, and parameters that a step cannot take."""
+    lr, betas = group["lr"], group["betas"]
+    if group["state_bits"] not in (8, 32):
+        raise ValueError("state_bits must be 8 or 32")
+    if isinstance(lr, torch.Tensor):
+        if lr.numel() != 1 or lr.dtype != torch.float32:
+            raise ValueError("a tensor lr must be one float32")
+    elif not 0 <= lr < float("inf"):
+        raise ValueError("lr must be finite and not negative")
+    if not (0 <= betas[0] < 1 and 0 <= betas[1] < 1):
+        raise ValueError("betas must be in [0, 1)")
+    if not 0 <= group["eps"] < float("inf") or not 0 <= group["weight_decay"] < float("inf"):
+        raise ValueError("eps and weight_decay must be finite and not negative")
+    for p in group["params"]:
+        if p.dtype not in _PARAM_TYPES:
+            raise ValueError("parameters must be fp16, bf16 or float32, not %s" % p.dtype)
+
+
 class AdamW(torch.optim.Optimizer):
     """AdamW with decoupled weight decay over fp16, bf16 and float32 parameters on a GPU.
 
@@ -31,25 +50,16 @@ class AdamW(torch.optim.Optimizer):
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32,
                  master_weights=False, seed=0):
-        if state_bits not in (8, 32):
-            raise ValueError("state_bits must be 8 or 32")
-        if isinstance(lr, torch.Tensor):
-            if lr.numel() != 1 or lr.dtype != torch.float32:
-                raise ValueError("a tensor lr must be one float32")
-        elif not 0 <= lr < float("inf"):
-            raise ValueError("lr must be finite and not negative")
-        if not (0 <= betas[0] < 1 and 0 <= betas[1] < 1):
-            raise ValueError("betas must be in [0, 1)")
-        if not 0 <= eps < float("inf") or not 0 <= weight_decay < float("inf"):
-            raise ValueError("eps and weight_decay must be finite and not negative")
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay, state_bits=state_bits,
                                       master_weights=bool(master_weights), seed=int(seed)))
 
     def add_param_group(self, group):
         super().add_param_group(group)
-        for p in self.param_groups[-1]["params"]:
-            if p.dtype not in _PARAM_TYPES:
-                raise ValueError("parameters must be fp16, bf16 or float32, not %s" % p.dtype)
+        try:
+            _check_group(self.param_groups[-1])
+        except Exception:
+            del self.param_groups[-1]
+            raise
 
     def _new_state(self, p, group, step):
         if not p.is_cuda or not p.is_contiguous():

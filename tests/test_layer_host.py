@@ -304,3 +304,20 @@ def test_parts_of_a_large_grid(tmp_path):
             at += n
         assert at <= groups and (int(status) == 7) == (fail > 0 and len(vals) // 2 == fail)
         assert at == groups or int(status) == 7
+
+
+@pytest.mark.parametrize("kw,what", [(dict(state_bits=16), "state_bits"), (dict(lr=-1.0), "lr"), (dict(lr=float("nan")), "lr"),
+                                     (dict(lr=torch.zeros(2)), "tensor lr"), (dict(lr=torch.zeros(1, dtype=torch.float64)), "tensor lr"),
+                                     (dict(betas=(0.9, 1.0)), "betas"), (dict(eps=float("inf")), "eps"), (dict(weight_decay=-1.0), "weight_decay"),
+                                     (dict(params=[torch.nn.Parameter(torch.zeros(4, dtype=torch.float64))]), "float64")])
+def test_optimizer_checks_a_groups_own_options(kw, what):
+    from paper_2309_00964_amd.optim import AdamW
+    group = lambda: dict(dict(params=[torch.nn.Parameter(torch.zeros(4))]), **kw)  # noqa: E731
+    with pytest.raises(ValueError, match=what):
+        AdamW([group()])
+    opt = AdamW([torch.nn.Parameter(torch.zeros(3))])
+    with pytest.raises(ValueError, match=what):
+        opt.add_param_group(group())
+    assert len(opt.param_groups) == 1          # the refused group is not kept
+    opt.add_param_group(dict(params=[torch.nn.Parameter(torch.zeros(4))], lr=torch.zeros(1), state_bits=8))
+    assert len(opt.param_groups) == 2

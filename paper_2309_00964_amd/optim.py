@@ -150,8 +150,14 @@ class AdamW(torch.optim.Optimizer):
 
     def load_state_dict(self, state_dict):
         """torch's, but with every state tensor in its own type (torch casts them to the
-        parameter's) and the counters shared as they were saved."""
+        parameter's), the counters shared as they were saved, and rates that are tensors on
+        their parameters' device."""
         super().load_state_dict(state_dict)
+        rates = {}
+        for group in self.param_groups:
+            if isinstance(group["lr"], torch.Tensor) and group["params"]:
+                lr, device = group["lr"], group["params"][0].device
+                group["lr"] = rates.setdefault((id(lr), device), lr.to(device))
         saved = state_dict["state"]
         ids = [i for group in state_dict["param_groups"] for i in group["params"]]
         params = [p for group in self.param_groups for p in group["params"]]

@@ -200,3 +200,28 @@ def test_training_step_of_clustered_layers(fmt):
         with torch.no_grad():
             out = palette_linear(x[:rows], packed, c0[0], hid, bias, None, "silu")
         L.assert_within(out, *L.product(x[:rows], w16, bias.detach(), None, "silu")[1:], "served")
+
+
+def test_a_checkpoint_on_the_host_with_its_rate_as_a_tensor():
+    """Loaded with every tensor on the CPU, the rate among them, the next step goes on as if it
+    had not been saved."""
+    import io
+    say("checkpoint on the host")
+    ps = params(9, torch.bfloat16)
+    a = AdamW(ps, lr=torch.full((1,), 1e-2, device=DEV), state_bits=8, master_weights=True)
+    grads(ps, 80)
+    a.step()
+    file = io.BytesIO()
+    torch.save(a.state_dict(), file)
+    file.seek(0)
+    qs = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    b = AdamW(qs, lr=1e-4, state_bits=8, master_weights=True)
+    b.load_state_dict(torch.load(file, map_location="cpu", weights_only=True))
+    assert b.param_groups[0]["lr"].device == qs[0].device
+    assert len({id(b.state[q]["step"]) for q in qs}) == 1          # one counter still
+    for opt, xs in ((a, ps), (b, qs)):
+        grads(xs, 81)
+        opt.step()
+    torch.cuda.synchronize()
+    for p, q in zip(ps, qs):
+        assert torch.equal(p, q) and int(b.state[q]["step"]) == 2

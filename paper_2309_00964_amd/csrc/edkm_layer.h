@@ -64,6 +64,8 @@ struct AlignArgs {
     AlignJob job[3];
 };
 
+constexpr int SPLIT_TILE = 128;    // the only tile whose depths are ever split
+
 // How a product is carried out.
 struct ProductPlan {
     int tile;               // 256 or 128 outputs square

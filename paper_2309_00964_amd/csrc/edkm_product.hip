@@ -119,7 +119,7 @@ static void shape_plan(int64_t rows, int64_t cols, int64_t depth, bool direct, P
     q.direct = direct;
     q.tile = direct && large_cost < cost ? 256 : 128;
     q.splits = 1;
-    if (q.tile == 128) {
+    if (q.tile == SPLIT_TILE) {
         auto time = [&](int64_t s) { return 26 * ((steps + s - 1) / s) + (s > 1 ? 94 + s * t : 0); };
         for (int s = 2; s <= std::min<int64_t>(64, 512 / t); ++s)
             if (time(s) < time(q.splits)) q.splits = s;

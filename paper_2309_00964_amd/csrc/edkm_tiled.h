@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
         step(a0, b0, a1, b1, s);
         if (s + 1 < steps) step(a1, b1, a0, b0, s + 1);
     }
-    if (p.part) {
+    if (BM == SPLIT_TILE && p.part) {
         float* at = p.part + ((int64_t)group * NW + wave) * (TR * 1024) + lane * 4;
 #pragma unroll
         for (int i = 0; i < TR; ++i)
@@ -499,9 +499,11 @@ template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, int BITS 
 static hipError_t tiled(ProductArgs p, const ProductPlan& q, hipStream_t s) {
     const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
     EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS>), (uint64_t)(tiles * q.splits), WM * WN * 64, p);
-    const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
-    if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4>), blocks, dim3(256), p, q.splits);
-    else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1>), blocks, dim3(64), p, q.splits);
+    if constexpr (B == SPLIT_TILE) {
+        const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
+        if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4>), blocks, dim3(256), p, q.splits);
+        else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1>), blocks, dim3(64), p, q.splits);
+    }
     return hipSuccess;
 }
 

@@ -76,13 +76,16 @@ BackwardWs backward_ws(int64_t m, int64_t n, int64_t k, int act) {
     return w;
 }
 
-// Has a matrix's rows copied to `to` if their length asks for it, and points there.
-void align_rows(AlignArgs& a, const uint16_t*& p, int64_t& ld, int64_t rows, int64_t cols, char* to) {
-    if (cols % 8 == 0 || rows == 0) return;
+// Has a matrix's rows copied to `to`, and points there.
+void copy_rows(AlignArgs& a, const uint16_t*& p, int64_t& ld, int64_t rows, int64_t cols, char* to) {
     uint16_t* out = reinterpret_cast<uint16_t*>(to);
     a.job[a.count++] = {p, ld, (int)rows, (int)cols, out};
     p = out;
     ld = up8(cols);
+}
+// The same, if their length asks for it.
+void align_rows(AlignArgs& a, const uint16_t*& p, int64_t& ld, int64_t rows, int64_t cols, char* to) {
+    if (cols % 8 && rows > 0) copy_rows(a, p, ld, rows, cols, to);
 }
 
 edkm_status ws_ok(const void* ws, size_t have, size_t need) {
@@ -209,15 +212,19 @@ edkm_status edkm_linear_backward(int64_t m, int64_t n, int64_t k, int format, in
 // takes 21.3 us for 65 tokens, 24.2 for 256, 33.2 for 512 and 58.4 for 1024; decoded first
 // by a launch of its own 26.9, 31.2, 38.5 and 59.2.  Past that the decoding that is done over
 // and over costs more: 81.0 against 77.8 at 512 x 11008 x 4096, 87.4 against 72.2 for 2048 tokens.
-static bool palette_fused(const ProductArgs& p) {
-    const int64_t tiles = ((int64_t)p.rows + 127) / 128 * (((int64_t)p.cols + 127) / 128);
-    return tiles <= 256 && p.depth % 8 == 0 && p.idx_bytes >= 4 && product_plan(p, OP_ROWS, OP_PALETTE).direct;
+// Tokens that cannot go to LDS directly are copied first (2 to 4 us).
+static bool palette_fused(int64_t m, int64_t n, int64_t k, int bits) {
+    const int64_t tiles = (m + 127) / 128 * ((n + 127) / 128);
+    return tiles <= 256 && k % 8 == 0 && k <= DIRECT_LD_MOST && n * k * bits > 24;
 }
 
 size_t edkm_palette_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int bits) {
     if (!product_ok(m, n, k, EDKM_KEYS_FP16, EDKM_ACT_NONE) || bits < 1 || bits > EDKM_MAX_BITS || few_tokens(m, k, true)) return 0;
-    // the decoded weights, in rows of whole 16-byte pieces; an aligned copy of x; a split's sums
-    return up256((size_t)n * up8(k) * 2) + aligned_bytes(m, k) + up256(product_part_bytes(m, n, k));
+    // an aligned copy of x and a split's sums; before them the weights, in rows of whole
+    // 16-byte pieces, where they are decoded first
+    const size_t parts = up256(product_part_bytes(m, n, k));
+    if (palette_fused(m, n, k, bits)) return up256((size_t)m * k * 2) + parts;
+    return up256((size_t)n * up8(k) * 2) + aligned_bytes(m, k) + parts;
 }
 
 edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int format, int activation, const void* x,
@@ -251,8 +258,13 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
     p.act = activation;
     if (few_tokens(m, k, true)) return launch_few(p, format, bits, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
     p.padded = 1;
-    if (palette_fused(p))
-        return launch_tiled_palette(p, format, static_cast<float*>(ws), stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    AlignArgs copies{};
+    if (palette_fused(m, n, k, bits)) {
+        if (!product_plan(p, OP_ROWS, OP_PALETTE).direct) copy_rows(copies, p.a, p.lda, m, k, static_cast<char*>(ws));
+        float* part = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)m * k * 2));
+        if (launch_align_rows(copies, stream) != hipSuccess) return EDKM_ERR_HIP;
+        return launch_tiled_palette(p, format, part, stream) == hipSuccess ? EDKM_OK : EDKM_ERR_HIP;
+    }
     char* base = static_cast<char*>(ws);
     uint16_t* w = static_cast<uint16_t*>(ws);
     char* xs = base + up256((size_t)n * up8(k) * 2);
@@ -260,7 +272,6 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
                                : launch_unpalettize(indices, p.idx_bytes, (uint64_t)n * k, bits, format, lut, w, false, stream);
     p.b = w;
     p.ldb = up8(k);
-    AlignArgs copies{};
     align_rows(copies, p.a, p.lda, m, k, xs);
     if (e != hipSuccess || launch_align_rows(copies, stream) != hipSuccess) return EDKM_ERR_HIP;
     return launch_product(p, format, OP_ROWS, OP_ROWS, reinterpret_cast<float*>(xs + aligned_bytes(m, k)), stream) == hipSuccess

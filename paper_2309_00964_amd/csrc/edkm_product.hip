@@ -142,7 +142,7 @@ size_t product_part_bytes(int64_t rows, int64_t cols, int64_t depth) {
 ProductPlan product_plan(const ProductArgs& p, int opa, int opb) {
     ProductPlan q{};
     auto whole = [&](const void* m, int64_t ld, int op) {
-        return ((uintptr_t)m & 15) == 0 && ld % 8 == 0 && ld <= (1 << 22) && (op == OP_DEPTH || p.depth % 8 == 0 || p.padded);
+        return ((uintptr_t)m & 15) == 0 && ld % 8 == 0 && ld <= DIRECT_LD_MOST && (op == OP_DEPTH || p.depth % 8 == 0 || p.padded);
     };
     shape_plan(p.rows, p.cols, p.depth, whole(p.a, p.lda, opa) && (opb == OP_PALETTE || whole(p.b, p.ldb, opb)), q);
     return q;

@@ -724,3 +724,20 @@ def test_bias_gradient_of_more_than_one_launch(m, n, name):
         row = torch.randint(-8, 8, (n,), device=DEV).to(dt)
         edkm.linear_backward(row.expand(m, n).contiguous(), None, None, dbias=db)
         assert torch.equal(db, m * row)
+
+
+@pytest.mark.parametrize("m,n,k,bits", [(65, 96, 4096, 3), (70, 130, 264, 1), (300, 257, 1000, 4), (40, 64, 16000, 2)])
+def test_palette_with_unaligned_tokens_equals_aligned_ones(m, n, k, bits):
+    """Tokens that start on any element take the same kernels by way of an aligned copy, within
+    the workspace's size."""
+    dt = torch.bfloat16
+    say("unaligned tokens", m, n, k, bits)
+    _, packed, lut, _ = device_palette(n, k, bits, bits)
+    x, want, y = randn(1, m, k, dtype=dt), *(torch.empty(m, n, dtype=dt, device=DEV) for _ in range(2))
+    edkm.palette_linear(x, packed, lut, want)
+    need = edkm.palette_linear_workspace_bytes(m, n, k, bits)
+    for lead, gap in ((1, 0), (1, 3), (8, 4)):
+        _, xv = inside(x, lead, gap)
+        buf = torch.full((need + 256,), 77, dtype=torch.uint8, device=DEV)
+        edkm.palette_linear(xv, packed, lut, y, workspace=buf[:need])
+        assert torch.equal(y, want) and bool((buf[need:] == 77).all())

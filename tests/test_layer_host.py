@@ -321,3 +321,11 @@ def test_optimizer_checks_a_groups_own_options(kw, what):
     assert len(opt.param_groups) == 1          # the refused group is not kept
     opt.add_param_group(dict(params=[torch.nn.Parameter(torch.zeros(4))], lr=torch.zeros(1), state_bits=8))
     assert len(opt.param_groups) == 2
+
+
+@pytest.mark.parametrize("m,n,k,bits", [(65, 4096, 4096, 3), (128, 4096, 4096, 3), (300, 4096, 4096, 4), (1024, 4096, 4096, 1)])
+def test_palette_workspace_holds_no_weights_that_are_decoded_on_the_way(m, n, k, bits):
+    """An aligned copy of x and a split's sums at most; the weights where they are decoded first."""
+    assert edkm.palette_linear_workspace_bytes(m, n, k, bits) <= 2 * m * k + edkm.linear_workspace_bytes(m, n, k)
+    assert edkm.palette_linear_workspace_bytes(4096, n, k, bits) >= 2 * n * k
+    assert edkm.palette_linear_workspace_bytes(m, n, k + 1, bits) >= 2 * n * (k + 1)

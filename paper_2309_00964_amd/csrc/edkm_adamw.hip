@@ -137,11 +137,11 @@ __device__ __forceinline__ uint32_t half_max(uint32_t x) {
 }
 
 // Eight elements per thread and pass, 32 lanes for the 256 elements of a scale.  Bound by
-// the bytes moved (10.06 B per bf16 element with 8-bit states, 22 with fp32 ones); the
-// arithmetic of the 8-bit form, about 60 slots per element, comes close to that.  The 202M
-// bf16 weights of a decoder layer take 374 to 381 us with 8-bit states (5.4 TB/s, half of the
-// reads from the Infinity Cache), 658 with fp32 masters, 924 with fp32 states (4.8 TB/s)
-// and 1199 with both.
+// the bytes moved (10.06 B per bf16 element with 8-bit states, 22 with fp32 ones) and, in the
+// 8-bit form, as much by its arithmetic, which keeps the vector units busy for 85% of the time
+// (14% with fp32 states).  The 202M bf16 weights of a decoder layer take 374 to 382 us with
+// 8-bit states (5.4 TB/s; an elementwise kernel that reads as much as it writes reaches 6.2),
+// 658 with fp32 masters, 924 with fp32 states (4.8 TB/s) and 1199 with both.
 template <int PT, int GT, bool S8>
 __global__ void __launch_bounds__(256) k_adamw(AdamwArgs a) {
 #pragma clang fp contract(off)

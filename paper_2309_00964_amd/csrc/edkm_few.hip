@@ -131,10 +131,13 @@ struct FewWeights {
 // runs of 128 and add their sums through LDS.  The MFMA takes the weights as its rows: lane
 // l holds row l mod 16, depths 32 (l / 16) + 8 j + 0 .. 7 of a run at its j-th step, so its
 // share of a palette's run is 4 b consecutive bytes.  A wave asks for its weights of U runs,
-// and for U more ahead, before it waits for anything, the table included.  Bound by the
-// weights' bytes where they are 16 bits; a palette's few bytes leave the vector instructions
-// as the bound (two a weight pair and its lookup), so addresses are one 32-bit offset per
-// row from a pointer that all lanes share.  A call among others takes, with 3 bits and 4096
+// and for U more ahead, before it waits for anything, the table included.  One
+// token's 16-bit weights are bound by their bytes.  With a palette it is the chain of a
+// workgroup's steps: with 11008 depths at 4 bits the vector units are busy for 29% of the time,
+// LDS for 19%, and the waves wait for loads and barriers for 59% of theirs, with one workgroup
+// of sixteen waves on a CU and five or six runs a wave.  Addresses are one 32-bit offset per row
+// from a pointer that all lanes share.  More tokens are bound by their way into the CUs, since every
+// workgroup reads all of them: 64 x 4096 are 512 KiB each, 12 bytes a clock.  A call among others takes, with 3 bits and 4096
 // depths, for 4096 outputs 5.1 us (1 token), 7.4 (16), 18.1 (64); for 11008 outputs 8.1
 // (2.1 TB/s of indices), 10.3 and 22.9; 16-bit weights of 11008 outputs 18.6 us (4.8 TB/s).
 template <int F, int BITS, bool WHOLE, int MT, int NT, int U, int NW>

@@ -352,10 +352,11 @@ __device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, 
 // 1940 TFLOP/s, and the loads alone take 60 to 75% of the whole, the same where all tiles read
 // the same addresses.  Hence the largest square tile that LDS holds twice (2 x 64 KiB), loads
 // that write LDS themselves, the next step's asked for before this one's products, and no
-// conflicts in LDS, which is busy 24% of the time.  bf16, forward, dx, dw: 8192^3 1227, 1285
-// and 1305 TFLOP/s, 4096^3 1220, 1253 and 1290, 8192 x 11008 x 4096 631, 573 and 595 us,
-// 2048 x 4096 x 4096 66, 64 and 58 us.  Four stages of 32 depths gave 1178 to 1285, loads
-// through registers 1060 to 1123.
+// conflicts in LDS, which is busy 22 to 26% of the time.  bf16, forward, dx, dw, after some
+// milliseconds of the same (the clocks settle): 8192^3 1340, 1330 and 1355 TFLOP/s, 4096^3 1305,
+// 1308 and 1358, 8192 x 11008 x 4096 600, 552 and 580 us, 2048 x 4096 x 4096 63, 62 and 56 us.
+// On a slower card, where 8192^3 ran at 1227, 1285 and 1305, four stages of 32 depths gave 1178
+// to 1285, loads through registers 1060 to 1123.
 // BITS: b is a palette's.
 template <int F, int OPA, int OPB, int BM, int BN, int WM, int WN, bool DIRECT, int BITS = 0>
 __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {

@@ -741,3 +741,21 @@ def test_palette_with_unaligned_tokens_equals_aligned_ones(m, n, k, bits):
         buf = torch.full((need + 256,), 77, dtype=torch.uint8, device=DEV)
         edkm.palette_linear(xv, packed, lut, y, workspace=buf[:need])
         assert torch.equal(y, want) and bool((buf[need:] == 77).all())
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+@pytest.mark.parametrize("name", ["relu", "gelu", "silu"])
+def test_activations_of_every_finite_number(fmt, name):
+    """Each finite 16-bit z through the epilogue: within 2e-5 of the value (1e-35 where that is less)
+    before the rounding, by the few tokens' kernel and the tiles."""
+    dt = L.DT[fmt]
+    say("activations", fmt, name)
+    z = torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16).view(dt).to(DEV)
+    z = z[z.isfinite()].contiguous()
+    z64 = z.double()
+    ref = {"relu": z64.clamp_min(0), "gelu": z64 * 0.5 * torch.erfc(-z64 / 2 ** 0.5), "silu": z64 / (1 + torch.exp(-z64))}[name]
+    off = 2e-5 * ref.abs() + 1e-35
+    for m in (1, 70):
+        y = torch.empty(m, z.numel(), dtype=dt, device=DEV)
+        edkm.linear(torch.ones(m, 1, dtype=dt, device=DEV), z[:, None], y, None, None, name)
+        L.assert_within(y[m - 1], ref, ref.abs() * L.half(dt) + off * (1 + L.half(dt)) + L.tiny(dt), name)

@@ -136,10 +136,11 @@ struct FewWeights {
 // workgroup's steps: with 11008 depths at 4 bits the vector units are busy for 29% of the time,
 // LDS for 19%, and the waves wait for loads and barriers for 59% of theirs, with one workgroup
 // of sixteen waves on a CU and five or six runs a wave.  Addresses are one 32-bit offset per row
-// from a pointer that all lanes share.  More tokens are bound by their way into the CUs, since every
-// workgroup reads all of them: 64 x 4096 are 512 KiB each, 12 bytes a clock.  A call among others takes, with 3 bits and 4096
-// depths, for 4096 outputs 5.1 us (1 token), 7.4 (16), 18.1 (64); for 11008 outputs 8.1
-// (2.1 TB/s of indices), 10.3 and 22.9; 16-bit weights of 11008 outputs 18.6 us (4.8 TB/s).
+// from a pointer that all lanes share.  More tokens are bound by their way into the CUs, since
+// every workgroup reads all of them: 64 x 4096 are 512 KiB each, 12 bytes a clock.  A call among
+// others takes, with 3 bits and 4096 depths, for 4096 outputs 5.1 us (1 token), 7.4 (16), 18.1
+// (64); for 11008 outputs 8.1 (2.1 TB/s of indices), 10.3 and 22.9; 16-bit weights of 11008
+// outputs 18.6 us (4.8 TB/s).
 template <int F, int BITS, bool WHOLE, int MT, int NT, int U, int NW>
 __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
     constexpr int ENTRIES = 1 << (2 * BITS);

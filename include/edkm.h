@@ -391,6 +391,81 @@ edkm_status edkm_palette_linear(int64_t m, int64_t n, int64_t k, int bits, int f
                                 const void* bias, const void* residual, int64_t ldr,
                                 void* y, int64_t ldy, void* z, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * A model's two ends and the step from one block to the next.  The conventions
+ * of the layer operators hold.  Token indices are EDKM_INDEX_INT32 or _INT64
+ * arrays of the device without gaps; an index outside the table or vocabulary
+ * (-1, -100, any) stands for no token. */
+enum { EDKM_INDEX_INT32 = 0, EDKM_INDEX_INT64 = 1 };
+
+/* Embedding: y_i = scale table[ids_i], a row of zeros for no token.
+ *   table  v x d, 16-bit;  y  m x d;  scale finite */
+edkm_status edkm_embedding(int64_t m, int64_t v, int64_t d, int format, int index_type, const void* ids,
+                           const void* table, int64_t ldt, float scale, void* y, int64_t ldy, hipStream_t stream);
+/* The same with the v x d table given as edkm_palettize packs it (rows may start
+ * inside a byte), v d <= EDKM_MAX_N; an entry is rounded to the format, then scaled. */
+edkm_status edkm_palette_embedding(int64_t m, int64_t v, int64_t d, int bits, int format, int index_type,
+                                   const void* ids, const uint8_t* indices, const float* lut, float scale,
+                                   void* y, int64_t ldy, hipStream_t stream);
+/* The table's gradient: dtable_t = scale (sum of dy_i over the i with ids_i = t), in an
+ * order that depends on ids and sizes only, rounded once.  With accumulate the
+ * sum is added to what dtable holds, and rows that no token names are neither
+ * read nor written; without it they become zeros. */
+size_t edkm_embedding_backward_workspace_bytes(int64_t m, int64_t v, int64_t d);
+edkm_status edkm_embedding_backward(int64_t m, int64_t v, int64_t d, int format, int index_type, const void* ids,
+                                    const void* dy, int64_t lddy, float scale, int accumulate,
+                                    void* dtable, int64_t lddt, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Step from one block to the next: h = r + scale gate N(u; post), y = N(h; w) with
+ * N(v; w) = v / sqrt(mean(v^2) + eps) w over each row.
+ *   r     m x n, the residual stream;  w  n
+ *   u     nullable, m x n, the block's output; without it h = r, h is not
+ *         written, and post and gate must be NULL
+ *   post  nullable, n: without it N(u; post) is u
+ *   gate  nullable, n values, or m x n with gate_rows = 1 (ldg then counts)
+ *   h     m x n (with u); may be r or u (same leading dimension);  y  m x n
+ * n is 1 .. 16384, eps a normal fp32 number above 0.  y is of h before its rounding.  Squares are
+ * summed in fp32: a row whose mean square is beyond its range is divided by Inf. */
+#define EDKM_NORM_MAX 16384
+edkm_status edkm_residual_norm(int64_t m, int64_t n, int format, const void* r, int64_t ldr, const void* u, int64_t ldu,
+                               const void* w, const void* post, const void* gate, int64_t ldg, int gate_rows,
+                               float scale, float eps, void* h, int64_t ldh, void* y, int64_t ldy, hipStream_t stream);
+/* Its gradients for given dL/dy and dL/dh (each nullable: 0).
+ *   r, u .. eps  as edkm_residual_norm had them (h is formed from them again)
+ *   dr     m x n;  du  m x n (with u);  dw, dpost  n;  dgate  n, or m x n without gaps;
+ *          each nullable, one at least given with m > 0.  With m = 0 the vectors become zeros.
+ *          dr may be dy, dh or r, du may be u (same leading dimension) */
+size_t edkm_residual_norm_backward_workspace_bytes(int64_t m, int64_t n);
+edkm_status edkm_residual_norm_backward(int64_t m, int64_t n, int format, const void* dy, int64_t lddy,
+                                        const void* dh, int64_t lddh, const void* r, int64_t ldr,
+                                        const void* u, int64_t ldu, const void* w, const void* post,
+                                        const void* gate, int64_t ldg, int gate_rows, float scale, float eps,
+                                        void* dr, int64_t lddr, void* du, int64_t lddu, void* dw, void* dpost,
+                                        void* dgate, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Softmax cross entropy of the product z = x W^T (m x n, n words) against target words:
+ *   l_i = log(sum_j exp z_ij) - z_{i, targets_i};  0 for no target
+ * z is never in memory.
+ *   reduction  EDKM_REDUCE_NONE: loss is float[m], l; _SUM: float[1]; _MEAN: float[1], over
+ *              the rows with a target (0 if there are none)
+ *   lse        float[m]: log(sum_j exp z_ij), for the backward (nullable) */
+enum { EDKM_REDUCE_NONE = 0, EDKM_REDUCE_SUM = 1, EDKM_REDUCE_MEAN = 2 };
+size_t edkm_linear_cross_entropy_workspace_bytes(int64_t m, int64_t n, int64_t k);
+edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int format, int index_type, int reduction,
+                                      const void* x, int64_t ldx, const void* w, int64_t ldw, const void* targets,
+                                      float* loss, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+/* Its gradients for a given dL/dloss (device float[m], or float[1] with a reduction): with
+ * g_i = dL/dl_i and dz_ij = g_i (exp(z_ij - lse_i) - [j = targets_i]),
+ *   dx = dz W (m x k),  dw = dz^T x (n x k without gaps), in the 16-bit format; one may be NULL.
+ * z is formed again, some thousand words at a time, and dz is rounded to 16 bits on the way
+ * into the two products, as a share of 2^15 times the largest |g_i| (in fp16 a token whose
+ * |g_i| is below 2^-14 of that keeps fewer digits). */
+size_t edkm_linear_cross_entropy_backward_workspace_bytes(int64_t m, int64_t n, int64_t k);
+edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, int format, int index_type, int reduction,
+                                               const float* dloss, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                               const void* targets, const float* lse, void* dx, int64_t lddx, void* dw,
+                                               void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* One AdamW step over `count` tensors, one launch per EDKM_LAUNCH_GROUP of them:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)

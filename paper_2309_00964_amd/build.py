@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 # their own, and the layer and optimizer operators', which all builds share.
 SOURCES = [os.path.join(CSRC, f) for f in ("edkm_kernels.hip", "edkm_api.hip")]
 LAYER_SOURCES = [os.path.join(CSRC, f) for f in ("edkm_product.hip", "edkm_product_palette.hip", "edkm_few.hip", "edkm_adamw.hip",
-                                                      "edkm_layer_api.hip")]
+                                                      "edkm_layer_api.hip", "edkm_embedding.hip", "edkm_norm.hip", "edkm_loss.hip",
+                                                      "edkm_loss_products.hip", "edkm_model_api.hip")]
 OUT = os.path.join(HERE, "libedkm.so")
 # Diagnostics build: the same library with per-block timeline stamps
 # (-DEDKM_BLOCK_STAMPS, include/edkm_stamps.h); load it with EDKM_LIBRARY.

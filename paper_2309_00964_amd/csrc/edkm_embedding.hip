@@ -1,0 +1,405 @@
+// Embedding for gfx950 (MI355X): rows of a 16-bit or palettized table by token, and the
+// table's gradient, summed over tokens that are sorted by their row.
+
+#include "edkm_model.h"
+#include "edkm_product.h"
+
+namespace edkm {
+
+// The row of token i, or v for no token.
+template <int IDX>
+__device__ __forceinline__ uint32_t row_of(const void* ids, int64_t i, uint32_t v) {
+    if (IDX == IDX_64) {
+        const uint64_t t = static_cast<const uint64_t*>(ids)[i];     // negative: beyond any table
+        return t < v ? (uint32_t)t : v;
+    }
+    const uint32_t t = static_cast<const uint32_t*>(ids)[i];
+    return t < v ? t : v;
+}
+
+// stores the first `left` of eight values
+__device__ __forceinline__ void store8(uint16_t* q, s16x8 v, int left) {
+    if (left >= 8) {
+        reinterpret_cast<S16x8*>(q)->v = v;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < left) q[j] = (uint16_t)v[j];
+}
+
+// ----------------------------------------------------------------------------
+// lookup
+
+// A thread takes eight columns of one token after another; a workgroup `rows` tokens.  Bound
+// by the bytes of the rows read and written.
+template <int F, int IDX, int BITS>
+__global__ void __launch_bounds__(256) k_embed(EmbedArgs a) {
+    Decoder<F> dec;
+    if constexpr (BITS != 0) dec.init(a.lut, BITS);
+    const uint32_t pieces = (a.d + 7) / 8;
+    const int64_t i0 = (int64_t)(a.first + blockIdx.x) * a.rows;
+    const uint32_t rows = (uint32_t)min((int64_t)a.rows, a.m - i0);
+    for (uint32_t l = threadIdx.x; l < rows * pieces; l += 256) {
+        const uint32_t r = l / pieces, c = (l - r * pieces) * 8;
+        const int left = (int)min(a.d - c, 8u);
+        const uint32_t t = row_of<IDX>(a.ids, i0 + r, a.v);
+        s16x8 v = {};
+        if (t < a.v) {
+            if constexpr (BITS != 0)
+                v = dec.eight(load_idx8(a.idx, a.idx_bytes, (uint64_t)t * a.d + c, BITS), BITS);
+            else
+                v = row8(a.table + (int64_t)t * a.ldt + c, left);
+            if (a.scale != 1.f)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = (short)to_16<F>(to_f32<F>((uint16_t)v[j]) * a.scale);
+        }
+        store8(a.y + (i0 + r) * a.ldy + c, v, left);
+    }
+}
+
+template <int F, int IDX>
+static hipError_t embed_fi(EmbedArgs a, int bits, hipStream_t s) {
+    const uint32_t pieces = (a.d + 7) / 8;
+    a.rows = pieces >= 1024 ? 1 : 1024 / pieces;
+    const uint64_t groups = (uint64_t)((a.m + a.rows - 1) / a.rows);
+    switch (bits) {
+    case 0: EDKM_GO_PARTS((k_embed<F, IDX, 0>), groups, 256, a); break;
+    case 1: EDKM_GO_PARTS((k_embed<F, IDX, 1>), groups, 256, a); break;
+    case 2: EDKM_GO_PARTS((k_embed<F, IDX, 2>), groups, 256, a); break;
+    case 3: EDKM_GO_PARTS((k_embed<F, IDX, 3>), groups, 256, a); break;
+    default: EDKM_GO_PARTS((k_embed<F, IDX, 4>), groups, 256, a); break;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_embed(EmbedArgs a, int fmt, int index_type, int bits, hipStream_t s) {
+    if (fmt == FMT_BF16) return index_type == IDX_64 ? embed_fi<FMT_BF16, IDX_64>(a, bits, s) : embed_fi<FMT_BF16, IDX_32>(a, bits, s);
+    return index_type == IDX_64 ? embed_fi<FMT_FP16, IDX_64>(a, bits, s) : embed_fi<FMT_FP16, IDX_32>(a, bits, s);
+}
+
+// ----------------------------------------------------------------------------
+// tokens by row
+
+// A token's place among the sorted is the number of tokens of lower rows, and of its own row
+// before it.  A workgroup counts for 32 tokens, eight threads to a token, against all tokens
+// in LDS: no pass waits for another, and nothing depends on an order of arrival.
+template <int IDX>
+__global__ void __launch_bounds__(256) k_rank(SortArgs a) {
+    __shared__ __attribute__((aligned(16))) uint32_t all[RANK_MOST];
+    __shared__ uint32_t count[8][RANK_TOKENS];
+    const uint32_t m4 = (a.m + 3) & ~3u;
+    for (uint32_t j = threadIdx.x; j < m4; j += 256) all[j] = j < a.m ? row_of<IDX>(a.ids, j, a.v) : 0xFFFFFFFFu;
+    __syncthreads();
+    const uint32_t mine = threadIdx.x & (RANK_TOKENS - 1), q = threadIdx.x / RANK_TOKENS;
+    const uint32_t i0 = blockIdx.x * RANK_TOKENS, i = i0 + mine;
+    const uint32_t key = i < a.m ? all[i] : 0;
+    const uint4* four = reinterpret_cast<const uint4*>(all);
+    uint32_t n = 0;
+    // tokens before the workgroup's: also those of the same row; after them: lower rows only
+    for (uint32_t j = q; j < i0 / 4; j += 8) {
+        const uint4 o = four[j];
+        n += (o.x <= key) + (o.y <= key) + (o.z <= key) + (o.w <= key);
+    }
+    for (uint32_t j = i0 / 4 + RANK_TOKENS / 4 + q; j < m4 / 4; j += 8) {
+        const uint4 o = four[j];
+        n += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
+    }
+    for (uint32_t j = i0 + q; j < min(i0 + RANK_TOKENS, a.m); j += 8) n += all[j] < key || (all[j] == key && j < i);
+    count[q][mine] = n;
+    __syncthreads();
+    if (threadIdx.x < RANK_TOKENS && i < a.m) {
+        uint32_t at = 0;
+#pragma unroll
+        for (int p = 0; p < 8; ++p) at += count[p][mine];
+        a.key[at] = key;
+        a.pos[at] = i;
+    }
+}
+
+// A pass over one digit of the rows, for more tokens: how many of each digit value a
+// workgroup's tokens have ...
+template <int IDX>
+__global__ void __launch_bounds__(256) k_digits(SortArgs a) {
+    __shared__ uint32_t bins[1 << DIGIT_BITS];
+    for (uint32_t d = threadIdx.x; d < a.digits; d += 256) bins[d] = 0;
+    __syncthreads();
+    const uint32_t i0 = blockIdx.x * a.per, i1 = min(i0 + a.per, a.m);
+    for (uint32_t i = i0 + threadIdx.x; i < i1; i += 256) {
+        const uint32_t key = a.key_in ? a.key_in[i] : row_of<IDX>(a.ids, i, a.v);
+        atomicAdd(&bins[(key >> a.shift) & (a.digits - 1)], 1u);
+    }
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < a.digits; d += 256) a.counts[(uint64_t)blockIdx.x * a.digits + d] = bins[d];
+}
+
+// orders a wave's LDS accesses before and after it
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// ... and where they go: behind all lower digits, the same digit in workgroups before this
+// one, in waves before this one, and in lanes before this one.  A wave takes its quarter of
+// the tokens 64 at a time, in order; the lanes of a digit find each other by a ballot for
+// each of its bits.
+template <int IDX>
+__global__ void __launch_bounds__(256) k_place(SortArgs a) {
+    constexpr int MOST = 1 << DIGIT_BITS;
+    __shared__ uint32_t next[4][MOST];      // per wave: the next place of a digit
+    __shared__ uint32_t scan[4];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const uint32_t share = a.per / 4, i0 = blockIdx.x * a.per + w * share, i1 = min(i0 + share, a.m);
+    for (uint32_t d = tid; d < 4 * MOST; d += 256) (&next[0][0])[d] = 0;
+    __syncthreads();
+    for (uint32_t i = i0 + lane; i < i1; i += 64) {
+        const uint32_t key = a.key_in ? a.key_in[i] : row_of<IDX>(a.ids, i, a.v);
+        atomicAdd(&next[w][(key >> a.shift) & (a.digits - 1)], 1u);
+    }
+    // thread t sums digits t D .. t D + D - 1: all workgroups', and those before this one
+    const uint32_t D = (a.digits + 255) / 256;
+    uint32_t before[MOST / 256] = {}, total[MOST / 256] = {};
+    for (uint32_t g = 0; g < a.groups; ++g)
+#pragma unroll
+        for (uint32_t k = 0; k < MOST / 256; ++k)
+            if (k < D && tid * D + k < a.digits) {
+                const uint32_t c = a.counts[(uint64_t)g * a.digits + tid * D + k];
+                total[k] += c;
+                before[k] += g < blockIdx.x ? c : 0;
+            }
+    uint32_t sum = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < MOST / 256; ++k) sum += total[k];
+    uint32_t run = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const uint32_t up = __shfl_up(run, o);
+        if ((int)lane >= o) run += up;
+    }
+    if (lane == 63) scan[w] = run;
+    __syncthreads();
+    uint32_t base = run - sum;
+    for (uint32_t q = 0; q < w; ++q) base += scan[q];
+#pragma unroll
+    for (uint32_t k = 0; k < MOST / 256; ++k)
+        if (k < D && tid * D + k < a.digits) {
+            uint32_t at = base + before[k];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t c = next[q][tid * D + k];
+                next[q][tid * D + k] = at;
+                at += c;
+            }
+            base += total[k];
+        }
+    __syncthreads();
+    for (uint32_t i = i0; i < i1; i += 64) {
+        const bool live = i + lane < i1;
+        uint32_t key = 0, pos = i + lane;
+        if (live) {
+            key = a.key_in ? a.key_in[pos] : row_of<IDX>(a.ids, pos, a.v);
+            if (a.pos_in) pos = a.pos_in[pos];
+        }
+        const uint32_t digit = (key >> a.shift) & (a.digits - 1);
+        uint64_t same = __ballot(live);
+        for (uint32_t b = 1; b < a.digits; b *= 2) {
+            const uint64_t set = __ballot((digit & b) != 0);
+            same &= (digit & b) ? set : ~set;
+        }
+        if (live) {
+            const uint32_t at = next[w][digit] + __popcll(same & ((1ull << lane) - 1));
+            a.key[at] = key;
+            a.pos[at] = pos;
+        }
+        wave_order();
+        if (live && (same >> lane) == 1) next[w][digit] += __popcll(same);    // the digit's last lane
+        wave_order();
+    }
+}
+
+template <int IDX>
+static hipError_t sort_i(SortArgs a, uint32_t* key, uint32_t* pos, uint32_t* spare, hipStream_t s) {
+    const SortPlan q = sort_plan(a.m, a.v);
+    a.key = key;
+    a.pos = pos;
+    if (q.passes == 0) {
+        EDKM_GO(k_rank<IDX>, dim3((a.m + RANK_TOKENS - 1) / RANK_TOKENS), dim3(256), a);
+        return hipSuccess;
+    }
+    a.per = q.per;
+    a.groups = q.groups;
+    a.digits = 1u << q.width;
+    // the last pass writes key and pos, those before it in turn
+    for (int p = 0; p < q.passes; ++p) {
+        const bool last = (q.passes - 1 - p) % 2 == 0;
+        a.key = last ? key : spare;
+        a.pos = last ? pos : spare + a.m;
+        a.shift = p * q.width;
+        EDKM_GO(k_digits<IDX>, dim3(a.groups), dim3(256), a);
+        EDKM_GO(k_place<IDX>, dim3(a.groups), dim3(256), a);
+        a.key_in = a.key;
+        a.pos_in = a.pos;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_sort(const void* ids, int index_type, int64_t m, int64_t v, uint32_t* key, uint32_t* pos, uint32_t* spare,
+                       uint32_t* counts, hipStream_t s) {
+    SortArgs a{};
+    a.ids = ids;
+    a.counts = counts;
+    a.m = (uint32_t)m;
+    a.v = (uint32_t)v;
+    return index_type == IDX_64 ? sort_i<IDX_64>(a, key, pos, spare, s) : sort_i<IDX_32>(a, key, pos, spare, s);
+}
+
+// ----------------------------------------------------------------------------
+// the table's gradient
+
+template <int F>
+__device__ __forceinline__ void write_row(const EmbedGradArgs& a, uint32_t t, uint32_t c, const float (&sum)[8]) {
+    uint16_t* q = a.dt + (int64_t)t * a.lddt + c;
+    const int left = (int)min(a.d - c, 8u);
+    s16x8 o;
+    if (a.accumulate) {
+        const s16x8 old = row8(q, left);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = (short)to_16<F>(fmaf(a.scale, sum[j], to_f32<F>((uint16_t)old[j])));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = (short)to_16<F>(a.scale * sum[j]);
+    }
+    store8(q, o, left);
+}
+
+// The first sorted place whose row is not below t.
+__device__ __forceinline__ uint32_t lower(const uint32_t* key, uint32_t m, uint32_t t) {
+    uint32_t lo = 0, hi = m;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (key[mid] < t) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// The sorted tokens are cut into chunks of `per`; a thread sums eight columns of a chunk's
+// tokens, row by row.  A row whose tokens lie in one chunk is written; what a chunk has of
+// others goes to part: place 0 for a row that began in an earlier chunk, place 1 for one
+// that begins here and goes on.  Long rows are thereby shared by many threads, and every sum
+// has one order.  Workgroups after those write zeros to the rows of no token.
+template <int F>
+__global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
+    const uint32_t group = a.first + blockIdx.x, pieces = (a.d + 7) / 8;
+    if (group >= a.chunk_groups) {
+        __shared__ uint32_t at[ZERO_ROWS + 1];
+        const uint32_t t0 = (group - a.chunk_groups) * ZERO_ROWS, rows = min((uint32_t)ZERO_ROWS, a.v - t0);
+        if (threadIdx.x <= rows) at[threadIdx.x] = lower(a.key, a.m, t0 + threadIdx.x);
+        __syncthreads();
+        uint32_t T = 256;       // threads to a row
+        while (T > 8 && T / 2 >= pieces) T /= 2;
+        for (uint32_t r = threadIdx.x / T; r < rows; r += 256 / T) {
+            if (at[r] != at[r + 1]) continue;
+            uint16_t* q = a.dt + (int64_t)(t0 + r) * a.lddt;
+            for (uint64_t c = threadIdx.x % T * 8; c < a.d; c += T * 8) store8(q + c, s16x8{}, (int)min(a.d - (uint32_t)c, 8u));
+        }
+        return;
+    }
+    const uint64_t id = (uint64_t)group * 256 + threadIdx.x;
+    const uint32_t chunk = (uint32_t)(id / pieces), c = (uint32_t)(id - (uint64_t)chunk * pieces) * 8;
+    if (chunk >= a.chunks) return;
+    const uint32_t j0 = chunk * a.per, j1 = min(j0 + a.per, a.m);
+    const int left = (int)min(a.d - c, 8u);
+    const uint64_t wide = (uint64_t)pieces * 8;
+    const uint32_t before = chunk ? a.key[j0 - 1] : 0xFFFFFFFFu, after = j1 < a.m ? a.key[j1] : 0xFFFFFFFFu;
+    uint32_t row = a.key[j0];
+    float sum[8] = {};
+    auto part = [&](int place) {
+        float* q = a.part + ((uint64_t)chunk * 2 + place) * wide + c;
+        reinterpret_cast<f32x4*>(q)[0] = f32x4{sum[0], sum[1], sum[2], sum[3]};
+        reinterpret_cast<f32x4*>(q)[1] = f32x4{sum[4], sum[5], sum[6], sum[7]};
+    };
+    constexpr int U = 8;
+    for (uint32_t j = j0; j < j1; j += U) {
+        s16x8 v[U];
+        uint32_t key[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            key[u] = j + u < j1 ? a.key[j + u] : a.v;
+            v[u] = key[u] < a.v ? row8(a.dy + (int64_t)a.pos[j + u] * a.lddy + c, left) : s16x8{};
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (j + u >= j1) break;
+            if (key[u] != row) {
+                if (row < a.v) {
+                    if (row == before) part(0);
+                    else write_row<F>(a, row, c, sum);
+                }
+                row = key[u];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += to_f32<F>((uint16_t)v[u][e]);
+        }
+    }
+    if (row >= a.v) return;
+    if (row == before) part(0);
+    else if (row == after) part(1);
+    else write_row<F>(a, row, c, sum);
+}
+
+// Adds the parts of the rows that go on past their first chunk.
+template <int F>
+__global__ void __launch_bounds__(256) k_embed_join(EmbedGradArgs a) {
+    const uint32_t pieces = (a.d + 7) / 8;
+    const uint64_t id = (uint64_t)(a.first + blockIdx.x) * 256 + threadIdx.x;
+    const uint32_t chunk = (uint32_t)(id / pieces), c = (uint32_t)(id - (uint64_t)chunk * pieces) * 8;
+    if (chunk + 1 >= a.chunks) return;
+    const uint32_t j0 = chunk * a.per, row = a.key[j0 + a.per - 1];
+    if (row >= a.v || a.key[j0 + a.per] != row || (chunk && a.key[j0 - 1] == row && a.key[j0] == row)) return;
+    const uint64_t wide = (uint64_t)pieces * 8;
+    const float* q = a.part + (uint64_t)chunk * 2 * wide + c;
+    f32x4 lo = reinterpret_cast<const f32x4*>(q + wide)[0], hi = reinterpret_cast<const f32x4*>(q + wide)[1];
+    constexpr int U = 8;
+    bool on = true;
+    for (uint32_t k = chunk + 1; on && k < a.chunks; k += U) {
+        f32x4 l[U], h[U];
+        uint32_t key[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t e = min(k + u, a.chunks - 1);
+            const float* p = a.part + (uint64_t)e * 2 * wide + c;
+            key[u] = k + u < a.chunks ? a.key[e * a.per] : 0xFFFFFFFFu;
+            l[u] = reinterpret_cast<const f32x4*>(p)[0];
+            h[u] = reinterpret_cast<const f32x4*>(p)[1];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            on = on && key[u] == row;
+            if (on) {
+                lo += l[u];
+                hi += h[u];
+            }
+        }
+    }
+    const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    write_row<F>(a, row, c, sum);
+}
+
+template <int F>
+static hipError_t grad_f(EmbedGradArgs a, hipStream_t s) {
+    const uint64_t threads = (uint64_t)a.chunks * ((a.d + 7) / 8);
+    const uint64_t sums = (threads + 255) / 256, zeros = a.accumulate ? 0 : ((uint64_t)a.v + ZERO_ROWS - 1) / ZERO_ROWS;
+    a.chunk_groups = (uint32_t)sums;
+    EDKM_GO_PARTS(k_embed_grad<F>, sums + zeros, 256, a);
+    if (a.chunks > 1) EDKM_GO_PARTS(k_embed_join<F>, sums, 256, a);
+    return hipSuccess;
+}
+
+hipError_t launch_embed_grad(EmbedGradArgs a, int fmt, hipStream_t s) {
+    return fmt == FMT_BF16 ? grad_f<FMT_BF16>(a, s) : grad_f<FMT_FP16>(a, s);
+}
+
+}  // namespace edkm

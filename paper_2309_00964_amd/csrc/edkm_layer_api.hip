@@ -2,7 +2,7 @@
 // the launches of each call.  Every check runs on the host before any HIP call.
 
 #include "../../include/edkm.h"
-#include "edkm_layer.h"
+#include "edkm_checks.h"
 
 #include <algorithm>
 #include <cmath>
@@ -18,33 +18,7 @@ static_assert(EDKM_ACT_NONE == ACT_NONE && EDKM_ACT_RELU == ACT_RELU && EDKM_ACT
 static_assert(EDKM_TYPE_FP16 == PT_FP16 && EDKM_TYPE_BF16 == PT_BF16 && EDKM_TYPE_FP32 == PT_FP32, "types");
 static_assert(EDKM_STATE_BLOCK == ADAMW_BLOCK, "8-bit state blocks");
 
-constexpr int64_t DIM_MAX = 0x7FFFFFFF - 1024;   // sizes are 32-bit in the kernels, tile ends included
-
-constexpr int64_t MATRIX_MAX = (int64_t)1 << 40;     // elements of a matrix: its tiles are numbered in 32 bits
-
-bool size_ok(int64_t v, int64_t least) { return v >= least && v <= DIM_MAX; }
-
-bool product_ok(int64_t m, int64_t n, int64_t k, int format, int act) {
-    return size_ok(m, 0) && size_ok(n, 1) && size_ok(k, 1) && std::max(m, k) <= MATRIX_MAX / n && m <= MATRIX_MAX / k && (format == EDKM_KEYS_FP16 || format == EDKM_KEYS_BF16) &&
-           act >= 0 && act < ACT_COUNT;
-}
-
-// Leading dimension of a matrix with `rows` rows of `cols`: any for a single row, which
-// then gets one that the kernels can work with.
-bool ld_ok(int64_t& ld, int64_t rows, int64_t cols) {
-    if (rows <= 1) ld = (cols + 7) & ~(int64_t)7;
-    return ld >= cols && ld < (int64_t)1 << 40;
-}
-
-size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
-
 int64_t dz_chunks(int64_t m, int64_t n) { return (m + dz_rows(m, n) - 1) / dz_rows(m, n); }
-
-int64_t up8(int64_t v) { return (v + 7) & ~(int64_t)7; }
-
-// Rows whose length is no multiple of eight cannot be loaded by 16-byte pieces: a product
-// first copies them to rows that can.
-size_t aligned_bytes(int64_t rows, int64_t cols) { return cols % 8 ? up256((size_t)rows * up8(cols) * 2) : 0; }
 
 // Workspace of a forward: aligned copies of x and w, then a split product's sums.
 struct ForwardWs {
@@ -74,23 +48,6 @@ BackwardWs backward_ws(int64_t m, int64_t n, int64_t k, int act) {
     w.split = w.w + aligned_bytes(n, k);
     w.total = w.split + up256(std::max(m ? product_part_bytes(m, k, n) : 0, product_part_bytes(n, k, m)));
     return w;
-}
-
-// Has a matrix's rows copied to `to`, and points there.
-void copy_rows(AlignArgs& a, const uint16_t*& p, int64_t& ld, int64_t rows, int64_t cols, char* to) {
-    uint16_t* out = reinterpret_cast<uint16_t*>(to);
-    a.job[a.count++] = {p, ld, (int)rows, (int)cols, out};
-    p = out;
-    ld = up8(cols);
-}
-// The same, if their length asks for it.
-void align_rows(AlignArgs& a, const uint16_t*& p, int64_t& ld, int64_t rows, int64_t cols, char* to) {
-    if (cols % 8 && rows > 0) copy_rows(a, p, ld, rows, cols, to);
-}
-
-edkm_status ws_ok(const void* ws, size_t have, size_t need) {
-    if (need == 0) return EDKM_OK;
-    return !ws || have < need || ((uintptr_t)ws & 255u) ? EDKM_ERR_WORKSPACE : EDKM_OK;
 }
 
 }  // namespace

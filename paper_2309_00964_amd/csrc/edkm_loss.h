@@ -1,0 +1,152 @@
+// Device code of the cross entropy: what becomes of a product's sums.
+#pragma once
+#include "edkm_model.h"
+#include "edkm_tiled.h"
+
+namespace edkm {
+
+// What only the device knows: how many tokens have a target.  They are the rows of z and of
+// dx, and the depths of dw.
+struct LossBegin {
+    typedef LossArgs Args;
+    __device__ __forceinline__ static bool begin(LossArgs& p) {
+        const int count = *p.rows_of.count;
+        if (p.dynamic == 2) {
+            p.depth = count;
+            if (p.all && count == p.m) {
+                p.b = p.all;
+                p.ldb = p.ld_all;
+            }
+            return true;
+        }
+        if (p.all && count == p.m) {
+            p.a = p.all;
+            p.lda = p.ld_all;
+        }
+        p.rows = min(p.rows, count - p.base);
+        p.a += (int64_t)p.base * p.lda;
+        return p.rows > 0;
+    }
+};
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+
+// The largest of a row's 64 logits and the sum of e^(z - largest), and the target's logit.
+// A row's logits lie in the four lanes r, r + 16, r + 32 and r + 48.
+struct LossStats : LossBegin {
+    __device__ __forceinline__ static void block(const LossArgs& p, char*, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
+        if (r0 >= p.rows || c0 >= p.cols) return;
+        const int row = r0 + (lane & 15), c = c0 + (lane >> 4) * 4;
+        const float none = -__builtin_inff();
+        if (row < p.rows) {
+            const int t = p.rows_of.word[p.base + row] - c;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (t == j * 16 + e) p.rows_of.value[p.base + row] = acc[j][e];
+        }
+        if (c0 + 64 > p.cols)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + j * 16 + e >= p.cols) acc[j][e] = none;
+        float top = none;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[j][e]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float from = top == none ? 0.f : top;      // all -Inf: the sum is 0, or NaN if one is
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += exp_of(acc[j][e] - from);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 16 && row < p.rows) p.stats[(int64_t)(c0 / 64) * p.stat_rows + row] = make_float2(top, sum);
+    }
+};
+
+// Stores a 16 x 64 block as 16-bit values, whole lines at a time; `to` gives a row's place.
+// Columns from p.cols on up to `wide` become zeros.
+template <int F, class To>
+__device__ __forceinline__ void store_block(const LossArgs& p, char* lds, int lane, int r0, int c0, const f32x4 (&acc)[4], int wide, To to) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) epi_put(lds, lane, j, acc[j]);
+    epi_order();
+    const int c = c0 + (lane & 7) * 8;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = i * 8 + (lane >> 3), q = (lane & 7) * 2;
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + r * 256 + ((q ^ r) * 16));
+        const f32x4 hi = *reinterpret_cast<const f32x4*>(lds + r * 256 + (((q + 1) ^ r) * 16));
+        if (r0 + r >= p.rows || c >= wide) continue;
+        const float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        s16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < p.cols ? (short)to_16<F>(f[e]) : (short)0;
+        uint16_t* out = to(r0 + r) + c;
+        if (c + 8 <= wide) {
+            reinterpret_cast<S16x8*>(out)->v = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < wide) out[e] = (uint16_t)v[e];
+        }
+    }
+    epi_order();
+}
+
+// dz = factor (e^(z - lse) - [word is the target]), rounded to 16 bits because the matrix
+// units take it so in both products; the factor is the token's share of 2^15 times the largest
+// |dL/dl|, so that fp16 holds probabilities down to 2^-30 (2^-39 with fewer digits).
+template <int F>
+struct LossDz : LossBegin {
+    __device__ __forceinline__ static void block(const LossArgs& p, char* lds, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
+        const int wide = (p.cols + 7) & ~7;
+        if (r0 >= p.rows || c0 >= wide) return;
+        const int row = min(r0 + (lane & 15), p.rows - 1), t = p.rows_of.word[row] - p.col0 - c0 - (lane >> 4) * 4;
+        const float lse = p.lse[p.rows_of.row[row]], factor = p.rows_of.value[row];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j][e] = factor * (exp_of(acc[j][e] - lse) - (t == j * 16 + e ? 1.f : 0.f));
+        store_block<F>(p, lds, lane, r0, c0, acc, wide, [&](int r) { return p.out + (int64_t)r * p.ldo; });
+    }
+};
+
+// dx or dw: the sums of one launch, or with those of the launches before, times alpha.
+template <int F>
+struct LossSum : LossBegin {
+    __device__ __forceinline__ static void block(const LossArgs& p, char* lds, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t place) {
+        if (r0 >= p.rows || c0 >= p.cols) return;
+        float* at = p.accum + place * 1024 + lane * 4;
+        if (!p.begins)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] += *reinterpret_cast<const f32x4*>(at + j * 256);
+        if (!p.ends) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(at + j * 256) = acc[j];
+            return;
+        }
+        const float alpha = *p.rows_of.alpha;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j][e] *= alpha;
+        store_block<F>(p, lds, lane, r0, c0, acc, p.cols,
+                       [&](int r) { return p.out + (int64_t)(p.scatter ? p.rows_of.row[r] : r) * p.ldo; });
+    }
+};
+
+template <int F, int OPA, int OPB, class E>
+static hipError_t loss_tiled(const LossArgs& p, const ProductPlan& q, hipStream_t s) {
+    if (q.tile == 256) return tiled<F, OPA, OPB, 256, 2, 4, true, 0, E>(p, q, s);
+    return q.direct ? tiled<F, OPA, OPB, 128, 2, 2, true, 0, E>(p, q, s) : tiled<F, OPA, OPB, 128, 2, 2, false, 0, E>(p, q, s);
+}
+
+}  // namespace edkm

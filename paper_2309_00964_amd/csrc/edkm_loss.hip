@@ -1,0 +1,195 @@
+// Softmax cross entropy of a product with a vocabulary, for gfx950 (MI355X): the logits'
+// tiles end as their rows' statistics, or as the gradient at the logits, and are never in
+// memory themselves.
+
+#include "edkm_loss.h"
+
+namespace edkm {
+
+// ----------------------------------------------------------------------------
+// tokens with a target
+
+template <int IDX>
+__device__ __forceinline__ int word_of(const void* targets, int64_t i, int64_t n) {
+    if (IDX == IDX_64) {
+        const uint64_t t = static_cast<const uint64_t*>(targets)[i];
+        return t < (uint64_t)n ? (int)t : -1;
+    }
+    const uint32_t t = static_cast<const uint32_t*>(targets)[i];
+    return t < (uint64_t)n ? (int)t : -1;
+}
+
+// One workgroup lists the tokens with a target in order, for a backward those whose loss has a
+// gradient; a backward's factors follow, once their largest is known.  What the products
+// read has no row of any other token, so whatever those hold (NaN, Inf) reaches no gradient.
+template <int IDX>
+__global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
+    __shared__ int waves[2][16];
+    __shared__ float tops[16];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int base = 0, turn = 0;
+    float top = 0.f;
+    for (int64_t i0 = 0; i0 < a.m; i0 += 1024, turn ^= 1) {
+        const int64_t i = i0 + threadIdx.x;
+        int t = i < a.m ? word_of<IDX>(a.targets, i, a.n) : -1;
+        float g = 1.f;
+        if (a.dloss && t >= 0) g = a.dloss[a.reduction == RED_NONE ? i : 0];
+        if (g == 0.f) t = -1;
+        const uint64_t there = __ballot(t >= 0);
+        if (lane == 0) waves[turn][w] = __popcll(there);
+        __syncthreads();
+        int at = base;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const int c = waves[turn][q];
+            at += q < w ? c : 0;
+            base += c;
+        }
+        if (t >= 0) {
+            at += __popcll(there & ((1ull << lane) - 1));
+            a.r.row[at] = (int)i;
+            a.r.word[at] = t;
+            if (a.dloss) {
+                a.r.slot[i] = at;
+                a.r.value[at] = g;
+                top = fmaxf(top, fabsf(g));
+            }
+        } else if (i < a.m) {
+            if (a.dloss) a.r.slot[i] = -1;
+            if (a.loss && a.reduction == RED_NONE) a.loss[i] = 0.f;
+            if (a.lse) a.lse[i] = 0.f;
+        }
+    }
+    if (threadIdx.x == 0) a.r.count[0] = base;
+    if (!a.dloss) return;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) tops[w] = top;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 16; ++q) top = fmaxf(top, tops[q]);
+    for (int i = threadIdx.x; i < base; i += 1024) a.r.value[i] = a.r.value[i] / top * 32768.f;
+    if (threadIdx.x == 0) *a.r.alpha = top * (1.f / 32768.f) / (a.reduction == RED_MEAN ? (float)max(base, 1) : 1.f);
+}
+
+hipError_t launch_pick(const PickArgs& a, int index_type, hipStream_t s) {
+    if (index_type == IDX_64) EDKM_GO(k_pick<IDX_64>, dim3(1), dim3(1024), a);
+    else EDKM_GO(k_pick<IDX_32>, dim3(1), dim3(1024), a);
+    return hipSuccess;
+}
+
+// A row to a group of threads: 256 where rows are long.
+__global__ void __launch_bounds__(256) k_gather(GatherArgs a, int threads) {
+    const int count = *a.r.count;
+    const int64_t i = (int64_t)(a.first + blockIdx.x) * (256 / threads) + threadIdx.x / threads;
+    if (i >= a.m) return;
+    if (i < count && (a.always || count < a.m)) {
+        const uint16_t* from = a.x + (int64_t)a.r.row[i] * a.ldx;
+        uint16_t* to = a.out + i * a.ldo;
+        for (int64_t c = threadIdx.x % threads * 8; c < a.k; c += threads * 8)
+            *reinterpret_cast<s16x8*>(to + c) = row8(from + c, a.k - (int)c);
+    }
+    if (a.zero && a.r.slot[i] < 0) {
+        uint16_t* to = a.zero + i * a.ldz;
+        for (int64_t c = threadIdx.x % threads * 8; c < a.k; c += threads * 8) {
+            if (c + 8 <= a.k) {
+                reinterpret_cast<S16x8*>(to + c)->v = s16x8{};
+            } else {
+                for (int64_t e = c; e < a.k; ++e) to[e] = 0;
+            }
+        }
+    }
+}
+
+hipError_t launch_gather(GatherArgs a, hipStream_t s) {
+    int threads = 8;
+    while (threads < 256 && threads * 8 < a.k) threads *= 2;
+    const int rows = 256 / threads;
+    EDKM_GO_PARTS(k_gather, (uint64_t)((a.m + rows - 1) / rows), 256, a, threads);
+    return hipSuccess;
+}
+
+// ----------------------------------------------------------------------------
+// statistics of the blocks of 64 words to losses
+
+// Sixteen rows per workgroup, 64 threads to a row.
+__global__ void __launch_bounds__(1024) k_loss_end(LossEndArgs a) {
+    __shared__ float2 part[16][17];
+    const int rows = min(a.rows, *a.r.count - a.base);
+    const int row = blockIdx.x * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if ((int)blockIdx.x * 16 >= rows) return;
+    const float none = -__builtin_inff();
+    float top = none, sum = 0.f;
+    auto add = [&](float t, float s) {
+        const float m = fmaxf(top, t), from = m == none ? 0.f : m;
+        sum = sum * exp_of(top - from) + s * exp_of(t - from);
+        top = m;
+    };
+    if (row < rows)
+        for (int b = q; b < a.blocks; b += 64) {
+            const float2 v = a.stats[(int64_t)b * a.stat_rows + row];
+            add(v.x, v.y);
+        }
+#pragma unroll
+    for (int o = 16; o < 64; o *= 2) {
+        const float t = __shfl_xor(top, o), s = __shfl_xor(sum, o);
+        add(t, s);
+    }
+    if (lane < 16) part[w][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (threadIdx.x >= 16 || row >= rows) return;
+    top = none;
+    sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < 16; ++p) add(part[p][lane].x, part[p][lane].y);
+    const float l = logf(sum), loss = (top - a.r.value[a.base + row]) + l;
+    const int i = a.r.row[a.base + row];
+    if (a.reduction == RED_NONE) a.loss[i] = loss;
+    else a.r.value[a.base + row] = loss;
+    if (a.lse) a.lse[i] = top + l;
+}
+
+hipError_t launch_loss_end(const LossEndArgs& a, hipStream_t s) {
+    EDKM_GO(k_loss_end, dim3((a.rows + 15) / 16), dim3(1024), a);
+    return hipSuccess;
+}
+
+__global__ void __launch_bounds__(1024) k_loss_reduce(LossEndArgs a) {
+    __shared__ float waves[16];
+    const int count = *a.r.count;
+    // many tokens: a thread's long sum keeps what its additions round off
+    float sum = 0.f, lost = 0.f;
+    for (int i = threadIdx.x; i < count; i += 1024) {
+        const float v = a.r.value[i], t = sum + v, z = t - sum;
+        lost += (sum - (t - z)) + (v - z);
+        sum = t;
+    }
+    sum += __builtin_isfinite(lost) ? lost : 0.f;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x) return;
+    sum = 0.f;
+    for (int q = 0; q < 16; ++q) sum += waves[q];
+    a.loss[0] = a.reduction == RED_MEAN ? sum / (float)max(count, 1) : sum;
+}
+
+hipError_t launch_loss_reduce(const LossEndArgs& a, hipStream_t s) {
+    EDKM_GO(k_loss_reduce, dim3(1), dim3(1024), a);
+    return hipSuccess;
+}
+
+// ----------------------------------------------------------------------------
+// the products with the vocabulary
+
+hipError_t launch_loss_stats(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s) {
+    return fmt == FMT_BF16 ? loss_tiled<FMT_BF16, OP_ROWS, OP_ROWS, LossStats>(a, q, s)
+                           : loss_tiled<FMT_FP16, OP_ROWS, OP_ROWS, LossStats>(a, q, s);
+}
+hipError_t launch_loss_dz(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s) {
+    return fmt == FMT_BF16 ? loss_tiled<FMT_BF16, OP_ROWS, OP_ROWS, LossDz<FMT_BF16>>(a, q, s)
+                           : loss_tiled<FMT_FP16, OP_ROWS, OP_ROWS, LossDz<FMT_FP16>>(a, q, s);
+}
+
+}  // namespace edkm

@@ -1,0 +1,204 @@
+// Internal declarations of the operators at a model's ends and between its blocks: the
+// embedding, the norms around a block and the cross entropy of a product.
+#pragma once
+#include "edkm_layer.h"
+
+namespace edkm {
+
+enum IndexType : int { IDX_32 = 0, IDX_64 = 1 };
+
+// ----------------------------------------------------------------------------
+// embedding
+
+struct EmbedArgs {
+    uint32_t first;         // the launch's first workgroup
+    const void* ids;
+    const uint16_t* table;
+    int64_t ldt;
+    const uint8_t* idx;     // a palette's
+    const float* lut;
+    uint64_t idx_bytes;
+    uint16_t* y;
+    int64_t ldy;
+    int64_t m;
+    uint32_t v, d;
+    uint32_t rows;          // tokens of a workgroup
+    float scale;
+};
+
+// Tokens sorted by their row of the table, in order within a row (no token: row v, last).
+struct SortArgs {
+    uint32_t first;
+    const void* ids;
+    const uint32_t *key_in, *pos_in;    // the pass before's; null: the ids
+    uint32_t *key, *pos;
+    uint32_t* counts;       // [groups][digits]
+    uint32_t m, v, per, groups, shift, digits;
+};
+
+struct EmbedGradArgs {
+    uint32_t first;
+    const uint32_t *key, *pos;
+    const uint16_t* dy;
+    int64_t lddy;
+    uint16_t* dt;
+    int64_t lddt;
+    float* part;            // [chunks][2][up8(d)]
+    uint32_t m, v, d, per, chunks;
+    uint32_t chunk_groups;  // workgroups that sum; those after them write the rows of no token
+    float scale;
+    int accumulate;
+};
+
+// Tokens that one launch ranks by comparing all with all (256 workgroups of 32, 67M
+// comparisons), and that a digit's pass takes for a workgroup, at least.
+constexpr int64_t RANK_MOST = 8192;
+constexpr int RANK_TOKENS = 32, PLACE_LEAST = 1024, PLACE_GROUPS = 512, DIGIT_BITS = 10;
+// Tokens of a chunk that one thread sums for its eight columns, and rows that one workgroup
+// looks up to write those of no token.
+constexpr int CHUNK_LEAST = 16, CHUNKS_MOST = 2048, ZERO_ROWS = 32;
+
+struct SortPlan {
+    int passes, width;      // digits' number and bits; 0 passes: ranked
+    uint32_t per, groups;
+};
+inline SortPlan sort_plan(int64_t m, int64_t v) {
+    SortPlan q{};
+    if (m <= RANK_MOST) return q;
+    int bits = 1;
+    while (v >> bits) ++bits;           // keys are 0 .. v
+    q.passes = (bits + DIGIT_BITS - 1) / DIGIT_BITS;
+    q.width = (bits + q.passes - 1) / q.passes;
+    int64_t per = (m + PLACE_GROUPS - 1) / PLACE_GROUPS;
+    if (per < PLACE_LEAST) per = PLACE_LEAST;
+    q.per = (uint32_t)((per + 255) / 256 * 256);
+    q.groups = (uint32_t)((m + q.per - 1) / q.per);
+    return q;
+}
+inline uint32_t chunk_tokens(int64_t m) {
+    const int64_t per = (m + CHUNKS_MOST - 1) / CHUNKS_MOST;
+    return (uint32_t)(per < CHUNK_LEAST ? CHUNK_LEAST : per);
+}
+
+hipError_t launch_embed(EmbedArgs a, int fmt, int index_type, int bits, hipStream_t s);
+// key/pos: the sorted tokens' arrays; spare: two more of m, between passes
+hipError_t launch_sort(const void* ids, int index_type, int64_t m, int64_t v, uint32_t* key, uint32_t* pos, uint32_t* spare,
+                       uint32_t* counts, hipStream_t s);
+hipError_t launch_embed_grad(EmbedGradArgs a, int fmt, hipStream_t s);
+
+// ----------------------------------------------------------------------------
+// norms
+
+struct NormArgs {
+    uint32_t first;
+    const uint16_t *r, *u, *w, *post, *gate;
+    int64_t ldr, ldu, ldg;
+    int gate_rows;
+    float scale, eps;
+    uint16_t *h, *y;
+    int64_t ldh, ldy;
+    int64_t m;
+    int n;
+    // backward
+    const uint16_t *dy, *dh;
+    int64_t lddy, lddh;
+    uint16_t *dr, *du, *dw, *dpost, *dgate;
+    int64_t lddr, lddu;
+    float* part;            // [groups][3][n]
+    uint32_t groups;
+};
+uint32_t norm_groups(int64_t m, int64_t n);      // workgroups of a backward
+hipError_t launch_norm(NormArgs a, int fmt, hipStream_t s);
+hipError_t launch_norm_backward(NormArgs a, int fmt, hipStream_t s);
+
+// ----------------------------------------------------------------------------
+// cross entropy of a product
+
+enum Reduction : int { RED_NONE = 0, RED_SUM = 1, RED_MEAN = 2, RED_COUNT = 3 };
+
+// What the tokens with a target (in a backward: and a gradient other than 0) have, in order and without gaps.
+struct LossRows {
+    int32_t* count;         // [2]: how many there are
+    float* alpha;           // backward: what dz is a share of
+    int32_t* row;           // [m] the token
+    int32_t* word;          // [m] its target
+    int32_t* slot;          // [m] backward: a token's place among them, -1 for none
+    float* value;           // [m] forward: its target's logit, then its loss; backward: dz's factor
+};
+
+struct PickArgs {
+    const void* targets;
+    int64_t m, n;
+    int reduction;
+    LossRows r;
+    float *loss, *lse;      // forward: zeros for tokens without a target
+    const float* dloss;     // backward
+};
+
+// x's rows of those tokens, one after another with zeros up to ldo; nothing if all tokens
+// have a target and x can be used as it is.  zero: rows of tokens without a target to clear.
+struct GatherArgs {
+    uint32_t first;
+    LossRows r;
+    const uint16_t* x;
+    int64_t ldx;
+    uint16_t* out;
+    int64_t ldo;
+    int64_t m;
+    int k;
+    int always;
+    uint16_t* zero;
+    int64_t ldz;
+};
+
+struct LossArgs : ProductArgs {
+    int splits;
+    LossRows rows_of;
+    const uint16_t* all;    // x itself, where it can be used; else null
+    int64_t ld_all;
+    int32_t m, base;        // tokens in all; the first row of this launch
+    int dynamic;            // what the count of tokens is here: 1 the rows, 2 the depths
+    // statistics: per 64 words and row the largest logit and the sum of exponentials
+    float2* stats;
+    int32_t stat_rows;
+    int32_t col0;           // the first word of this launch
+    const float* lse;
+    // sums over several launches
+    float* accum;
+    int begins, ends, scatter;
+};
+
+struct LossEndArgs {
+    LossRows r;
+    const float2* stats;
+    int32_t stat_rows, blocks, base, rows;
+    int reduction;
+    float *loss, *lse;
+};
+
+enum LossProduct : int { LOSS_STATS = 0, LOSS_DZ = 1, LOSS_SUM = 2 };
+hipError_t launch_pick(const PickArgs& a, int index_type, hipStream_t s);
+hipError_t launch_gather(GatherArgs a, hipStream_t s);
+hipError_t launch_loss_stats(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s);
+hipError_t launch_loss_dz(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s);
+hipError_t launch_loss_sum(const LossArgs& a, int fmt, int opa, const ProductPlan& q, hipStream_t s);
+hipError_t launch_loss_end(const LossEndArgs& a, hipStream_t s);
+hipError_t launch_loss_reduce(const LossEndArgs& a, hipStream_t s);
+
+// Words of a piece of the vocabulary whose dz is held at a time: as many as keep it within the
+// Infinity Cache, which the two products that read it then hit; 2048 at least.
+constexpr int64_t DZ_BYTES = 256 << 20, DZ_LEAST = 2048;
+inline int64_t loss_piece(int64_t m, int64_t n) {
+    int64_t p = DZ_BYTES / (2 * (m > 0 ? m : 1));
+    if (p < DZ_LEAST) p = DZ_LEAST;
+    if (p >= n) return n;
+    const int64_t pieces = (n + p - 1) / p;
+    return (((n + pieces - 1) / pieces) + 255) / 256 * 256;
+}
+// Tokens of a forward's launch: as many as keep the statistics within 256 MiB, 256 at least.
+inline int64_t loss_rows(int64_t m, int64_t n) {
+    const int64_t blocks = (n + 63) / 64, r = (256 << 20) / (blocks * 8) / 256 * 256;
+    return m < 256 || m < r ? m : r < 256 ? 256 : r;
+}
+
+}  // namespace edkm

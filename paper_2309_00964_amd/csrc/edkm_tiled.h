@@ -322,6 +322,10 @@ __device__ __forceinline__ void epi_put(char* lds, int lane, int j, f32x4 v) {
     const int r = lane & 15;
     *reinterpret_cast<f32x4*>(lds + r * 256 + (((j * 4 + (lane >> 4)) ^ r) * 16)) = v;
 }
+__device__ __forceinline__ f32x4 epi_get(const char* lds, int lane, int j) {
+    const int r = lane & 15;
+    return *reinterpret_cast<const f32x4*>(lds + r * 256 + (((j * 4 + (lane >> 4)) ^ r) * 16));
+}
 // Finishes two such blocks.
 template <int F, bool PLAIN>
 __device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, int lane, int r0, int c0, Eight<F, PLAIN>& e) {
@@ -358,8 +362,21 @@ __device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, 
 // On a slower card, where 8192^3 ran at 1227, 1285 and 1305, four stages of 32 depths gave 1178
 // to 1285, loads through registers 1060 to 1123.
 // BITS: b is a palette's.
-template <int F, int OPA, int OPB, int BM, int BN, int WM, int WN, bool DIRECT, int BITS = 0>
-__global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
+// E: what becomes of the sums where that is not the epilogue above: E::Args, a ProductArgs, are
+// the kernel's; E::begin sets what only the device knows, and says whether there is anything to
+// do; E::block takes a wave's 16 x 64 sums as the MFMA leaves them.
+template <class E>
+struct ArgsOf {
+    typedef typename E::Args type;
+};
+template <>
+struct ArgsOf<void> {
+    typedef ProductArgs type;
+};
+template <int F, int OPA, int OPB, int BM, int BN, int WM, int WN, bool DIRECT, int BITS = 0, class E = void>
+__global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(typename ArgsOf<E>::type p) {
+    if constexpr (!std::is_void_v<E>)
+        if (!E::begin(p)) return;
     constexpr int NW = WM * WN, TR = BM / WM / 16, TC = BN / WN / 16;
     static_assert(TC == 4 && TR % 4 == 0, "a wave's columns are those of the epilogue");
     typedef Feed<OPA, BM, NW, DIRECT> FA;
@@ -371,6 +388,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
     uint32_t tx, ty;
     const uint32_t nx = (p.cols + BN - 1) / BN, ny = (p.rows + BM - 1) / BM;
     const uint32_t group = p.first + blockIdx.x, split = group / (nx * ny);
+    if constexpr (!std::is_void_v<E>)
+        if (split >= (uint32_t)p.splits) return;     // a grid for more rows than there are
     tile_of(group % (nx * ny), nx, ny, tx, ty);
     const int r0 = ty * BM, c0 = tx * BN;
     const int wr = (wave / WN) * (BM / WM), wc = (wave % WN) * (BN / WN);
@@ -438,6 +457,11 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
     }
     // each wave has two blocks of LDS: in a0/a1 the first half of the waves, in b0/b1 the others
     char* mine = (wave < NW / 2 ? a0 : b0) + (wave % (NW / 2)) * 2 * EPI_BYTES;
+    if constexpr (!std::is_void_v<E>) {
+#pragma unroll
+        for (int i = 0; i < TR; ++i) E::block(p, mine, lane, r0 + wr + i * 16, c0 + wc, acc[i], ((int64_t)group * NW + wave) * TR + i);
+        return;
+    }
     Eight<F, OPB == OP_DEPTH> eight;
     eight.init(p, c0 + wc + (lane & 7) * 8);
     static_assert(NW / 2 * 2 * EPI_BYTES <= (FA::T::BYTES < FB::T::BYTES ? FA::T::BYTES : FB::T::BYTES), "");
@@ -458,14 +482,18 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(ProductArgs p) {
 // bytes for few splits, where one wave is best (512 x 4096 x 4096 in four parts: 29.8 us with
 // the product, 30.3 by four waves), and by the chain of loads for many (128 x 128 x 32768 in
 // 64: 20.0 us, 14.3 by four).
-template <int F, int BM, int BN, int WM, int WN, bool PLAIN, int W>
-__global__ void __launch_bounds__(W * 64) k_join(ProductArgs p, int splits) {
+template <int F, int BM, int BN, int WM, int WN, bool PLAIN, int W, class E = void>
+__global__ void __launch_bounds__(W * 64) k_join(typename ArgsOf<E>::type p, int splits) {
+    if constexpr (!std::is_void_v<E>)
+        if (!E::begin(p)) return;
     constexpr int NW = WM * WN, TR = BM / WM / 16;
     __shared__ __attribute__((aligned(16))) char lds[W][EPI_BYTES];
     const uint32_t nx = (p.cols + BN - 1) / BN, ny = (p.rows + BM - 1) / BM;
     const uint32_t w = blockIdx.x / (NW * TR);
     const int wave = blockIdx.x / TR % NW, i = blockIdx.x % TR, lane = threadIdx.x & 63, share = threadIdx.x >> 6;
     uint32_t tx, ty;
+    if constexpr (!std::is_void_v<E>)
+        if (w >= nx * ny) return;
     tile_of(w, nx, ny, tx, ty);
     const int r0 = ty * BM + wave / WN * (BM / WM) + i * 16, c0 = tx * BN + wave % WN * 64;
     if (r0 >= p.rows || c0 >= p.cols) return;
@@ -480,6 +508,24 @@ __global__ void __launch_bounds__(W * 64) k_join(ProductArgs p, int splits) {
     for (int s = share * per; s < end; ++s)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] += *reinterpret_cast<const f32x4*>(at + s * stride + j * 256);
+    if constexpr (!std::is_void_v<E>) {
+        if (W > 1) {
+            // the waves' shares, by the first wave
+#pragma unroll
+            for (int j = 0; j < 4; ++j) epi_put(lds[share], lane, j, acc[j]);
+            __syncthreads();
+            if (share) return;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                acc[j] = f32x4{};
+#pragma unroll
+                for (int q = 0; q < W; ++q) acc[j] += epi_get(lds[q], lane, j);
+            }
+            epi_order();
+        }
+        E::block(p, lds[0], lane, r0, c0, acc, ((int64_t)w * NW + wave) * TR + i);
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) epi_put(lds[share], lane, j, acc[j]);
     __syncthreads();
@@ -496,14 +542,14 @@ __global__ void __launch_bounds__(W * 64) k_join(ProductArgs p, int splits) {
     }
 }
 
-template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, int BITS = 0>
-static hipError_t tiled(ProductArgs p, const ProductPlan& q, hipStream_t s) {
+template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, int BITS = 0, class E = void>
+static hipError_t tiled(typename ArgsOf<E>::type p, const ProductPlan& q, hipStream_t s) {
     const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
-    EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS>), (uint64_t)(tiles * q.splits), WM * WN * 64, p);
+    EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS, E>), (uint64_t)(tiles * q.splits), WM * WN * 64, p);
     if constexpr (B == SPLIT_TILE) {
         const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
-        if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4>), blocks, dim3(256), p, q.splits);
-        else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1>), blocks, dim3(64), p, q.splits);
+        if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4, E>), blocks, dim3(256), p, q.splits);
+        else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1, E>), blocks, dim3(64), p, q.splits);
     }
     return hipSuccess;
 }

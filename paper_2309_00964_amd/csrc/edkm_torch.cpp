@@ -11,6 +11,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/edkm.h"
@@ -35,6 +36,17 @@ struct Library {
     decltype(&edkm_palette_linear) palette;
     decltype(&edkm_unpalettize) unpalettize;
     decltype(&edkm_adamw_batch) adamw;
+    decltype(&edkm_embedding) embedding;
+    decltype(&edkm_palette_embedding) palette_embedding;
+    decltype(&edkm_embedding_backward_workspace_bytes) embedding_ws;
+    decltype(&edkm_embedding_backward) embedding_backward;
+    decltype(&edkm_residual_norm) norm;
+    decltype(&edkm_residual_norm_backward_workspace_bytes) norm_ws;
+    decltype(&edkm_residual_norm_backward) norm_backward;
+    decltype(&edkm_linear_cross_entropy_workspace_bytes) loss_ws;
+    decltype(&edkm_linear_cross_entropy) loss;
+    decltype(&edkm_linear_cross_entropy_backward_workspace_bytes) loss_backward_ws;
+    decltype(&edkm_linear_cross_entropy_backward) loss_backward;
     decltype(&edkm_status_str) status;
 } lib;
 
@@ -213,6 +225,154 @@ void do_unpalettize(const Tensor& idx, const Tensor& lut, const Tensor& w, const
           "unpalettize");
 }
 
+// Tokens or targets: int32 or int64, without gaps.
+struct Index {
+    const void* p;
+    int type;
+};
+Index index_of(const Tensor& t, int64_t count, const Tensor& ref, const char* name) {
+    if (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong) refuse("%s must be int32 or int64, not %s", name, type_name(t.scalar_type()));
+    if (t.device() != ref.device()) refuse("%s must be on %s", name, ref.device().str().c_str());
+    if (t.numel() != count || !t.is_contiguous()) refuse("%s must hold %lld contiguous indices", name, (long long)count);
+    return {t.data_ptr(), t.scalar_type() == at::kLong ? EDKM_INDEX_INT64 : EDKM_INDEX_INT32};
+}
+float* floats(const Tensor* t, int64_t count, const Tensor& ref, const char* name) {
+    if (!t) return nullptr;
+    if (t->scalar_type() != at::kFloat || t->device() != ref.device() || t->numel() != count || !t->is_contiguous())
+        refuse("%s must hold %lld contiguous float32 values on %s", name, (long long)count, ref.device().str().c_str());
+    return (float*)t->data_ptr();
+}
+
+void do_embedding(const Tensor& ids, const Tensor& table, const Tensor& y, double scale, const hipStream_t* given) {
+    const int fmt = format_of(table, "table");
+    if (table.dim() != 2) refuse("table must be a matrix");
+    const int64_t m = ids.numel(), v = table.size(0), d = table.size(1);
+    const Matrix mt = matrix(table, v, d, table, "table"), my = matrix(y, m, d, table, "y");
+    const Index ix = index_of(ids, m, table, "ids");
+    on_gpu(table, "table");
+    c10::OptionalDeviceGuard guard(table.device());
+    check(lib.embedding(m, v, d, fmt, ix.type, ix.p, mt.p, mt.ld, (float)scale, my.p, my.ld, stream_of(table, given)), "embedding");
+}
+
+void do_palette_embedding(const Tensor& ids, const Tensor& idx, const Tensor& lut, int64_t v, const Tensor& y, double scale,
+                          const hipStream_t* given) {
+    const int fmt = format_of(y, "y");
+    if (y.dim() != 2) refuse("y must be a matrix");
+    const int64_t m = ids.numel(), d = y.size(1);
+    const Matrix my = matrix(y, m, d, y, "y");
+    const Index ix = index_of(ids, m, y, "ids");
+    if (v < 1 || d < 1) refuse("a palette's table has one row and one column at least");
+    if (d > (int64_t)EDKM_MAX_N / v) refuse("a palette holds at most %llu weights", (unsigned long long)EDKM_MAX_N);
+    const int bits = palette_bits(idx, lut, v * d, y);
+    on_gpu(y, "y");
+    c10::OptionalDeviceGuard guard(y.device());
+    check(lib.palette_embedding(m, v, d, bits, fmt, ix.type, ix.p, (const uint8_t*)idx.data_ptr(), (const float*)lut.data_ptr(), (float)scale,
+                                my.p, my.ld, stream_of(y, given)),
+          "palette_embedding");
+}
+
+void do_embedding_backward(const Tensor& ids, const Tensor& dy, const Tensor& dt, double scale, bool accumulate, const Tensor* ws,
+                           const hipStream_t* given) {
+    const int fmt = format_of(dy, "dy");
+    if (dt.dim() != 2) refuse("dtable must be a matrix");
+    const int64_t m = ids.numel(), v = dt.size(0), d = dt.size(1);
+    const Matrix mt = matrix(dt, v, d, dy, "dtable"), my = matrix(dy, m, d, dy, "dy");
+    const Index ix = index_of(ids, m, dy, "ids");
+    on_gpu(dy, "dy");
+    c10::OptionalDeviceGuard guard(dy.device());
+    Scratch s(ws, lib.embedding_ws(m, v, d), dy, given);
+    check(lib.embedding_backward(m, v, d, fmt, ix.type, ix.p, my.p, my.ld, (float)scale, accumulate, mt.p, mt.ld, s.p, s.bytes,
+                                 stream_of(dy, given)),
+          "embedding_backward");
+}
+
+// A gate: n values, or a value for each of m x n.
+struct Gate {
+    Matrix m;
+    int rows = 0;
+};
+Gate gate_of(const Tensor* gate, int64_t m, int64_t n, const Tensor& ref) {
+    Gate g;
+    if (!gate) return g;
+    if (gate->dim() == 1) {
+        g.m.p = vec(gate, n, ref, "gate");
+    } else {
+        g.m = matrix(*gate, m, n, ref, "gate");
+        g.rows = 1;
+    }
+    return g;
+}
+
+void do_norm(const Tensor& r, const Tensor& w, const Tensor& y, const Tensor* h, const Tensor* u, const Tensor* post, const Tensor* gate,
+             double scale, double eps, const hipStream_t* given) {
+    const int fmt = format_of(r, "residual");
+    if (r.dim() != 2) refuse("residual must be a matrix");
+    const int64_t m = r.size(0), n = r.size(1);
+    if (!u && (post || gate || h)) refuse("post_weight, gate and h belong to a block's output");
+    if (u && !h) refuse("a block's output needs h");
+    const Matrix mr = matrix(r, m, n, r, "residual"), my = matrix(y, m, n, r, "y"), mh = matrix(h, m, n, r, "h"), mu = matrix(u, m, n, r, "block");
+    const void *pw = vec(&w, n, r, "weight"), *pp = vec(post, n, r, "post_weight");
+    const Gate g = gate_of(gate, m, n, r);
+    on_gpu(r, "residual");
+    c10::OptionalDeviceGuard guard(r.device());
+    check(lib.norm(m, n, fmt, mr.p, mr.ld, mu.p, mu.ld, pw, pp, g.m.p, g.m.ld, g.rows, (float)scale, (float)eps, mh.p, mh.ld, my.p, my.ld,
+                   stream_of(r, given)),
+          "residual_norm");
+}
+
+void do_norm_backward(const Tensor* dy, const Tensor* dh, const Tensor& r, const Tensor* u, const Tensor& w, const Tensor* post,
+                      const Tensor* gate, double scale, double eps, const Tensor* dr, const Tensor* du, const Tensor* dw, const Tensor* dpost,
+                      const Tensor* dgate, const Tensor* ws, const hipStream_t* given) {
+    const int fmt = format_of(r, "residual");
+    if (r.dim() != 2) refuse("residual must be a matrix");
+    const int64_t m = r.size(0), n = r.size(1);
+    if (!u && (post || gate || du)) refuse("post_weight, gate and dblock belong to a block's output");
+    if ((dpost && !post) || (dgate && !gate)) refuse("a gradient of what is not given");
+    const Matrix mr = matrix(r, m, n, r, "residual"), mdy = matrix(dy, m, n, r, "dy"), mdh = matrix(dh, m, n, r, "dh"), mu = matrix(u, m, n, r, "block"),
+                 mdr = matrix(dr, m, n, r, "dresidual"), mdu = matrix(du, m, n, r, "dblock");
+    const void *pw = vec(&w, n, r, "weight"), *pp = vec(post, n, r, "post_weight");
+    const Gate g = gate_of(gate, m, n, r);
+    void *pdw = vec(dw, n, r, "dweight"), *pdp = vec(dpost, n, r, "dpost_weight"), *pdg = vec(dgate, g.rows ? m * n : n, r, "dgate");
+    on_gpu(r, "residual");
+    c10::OptionalDeviceGuard guard(r.device());
+    Scratch s(ws, lib.norm_ws(m, n), r, given);
+    check(lib.norm_backward(m, n, fmt, mdy.p, mdy.ld, mdh.p, mdh.ld, mr.p, mr.ld, mu.p, mu.ld, pw, pp, g.m.p, g.m.ld, g.rows, (float)scale,
+                            (float)eps, mdr.p, mdr.ld, mdu.p, mdu.ld, pdw, pdp, pdg, s.p, s.bytes, stream_of(r, given)),
+          "residual_norm_backward");
+}
+
+void do_loss(const Tensor& x, const Tensor& w, const Tensor& targets, const Tensor& loss, const Tensor* lse, int reduction, const Tensor* ws,
+             const hipStream_t* given) {
+    const int fmt = format_of(x, "x");
+    if (x.dim() != 2 || w.dim() != 2) refuse("x and w must be matrices");
+    const int64_t m = x.size(0), k = x.size(1), n = w.size(0);
+    const Matrix mx = matrix(x, m, k, x, "x"), mw = matrix(w, n, k, x, "w");
+    const Index ix = index_of(targets, m, x, "targets");
+    float *pl = floats(&loss, reduction == EDKM_REDUCE_NONE ? m : 1, x, "loss"), *pe = floats(lse, m, x, "lse");
+    on_gpu(x, "x");
+    c10::OptionalDeviceGuard guard(x.device());
+    Scratch s(ws, lib.loss_ws(m, n, k), x, given);
+    check(lib.loss(m, n, k, fmt, ix.type, reduction, mx.p, mx.ld, mw.p, mw.ld, ix.p, pl, pe, s.p, s.bytes, stream_of(x, given)),
+          "linear_cross_entropy");
+}
+
+void do_loss_backward(const Tensor& dloss, const Tensor& x, const Tensor& w, const Tensor& targets, const Tensor& lse, const Tensor* dx,
+                      const Tensor* dw, int reduction, const Tensor* ws, const hipStream_t* given) {
+    const int fmt = format_of(x, "x");
+    if (x.dim() != 2 || w.dim() != 2) refuse("x and w must be matrices");
+    const int64_t m = x.size(0), k = x.size(1), n = w.size(0);
+    const Matrix mx = matrix(x, m, k, x, "x"), mw = matrix(w, n, k, x, "w"), mdx = matrix(dx, m, k, x, "dx");
+    const Index ix = index_of(targets, m, x, "targets");
+    float *pg = floats(&dloss, reduction == EDKM_REDUCE_NONE ? m : 1, x, "dloss"), *pe = floats(&lse, m, x, "lse");
+    void* pdw = vec(dw, n * k, x, "dw");
+    on_gpu(x, "x");
+    c10::OptionalDeviceGuard guard(x.device());
+    Scratch s(ws, lib.loss_backward_ws(m, n, k), x, given);
+    check(lib.loss_backward(m, n, k, fmt, ix.type, reduction, pg, mx.p, mx.ld, mw.p, mw.ld, ix.p, pe, mdx.p, mdx.ld, pdw, s.p, s.bytes,
+                            stream_of(x, given)),
+          "linear_cross_entropy_backward");
+}
+
 // ---------------------------------------------------------------------------
 // differentiable forms
 
@@ -259,12 +419,12 @@ using torch::autograd::Variable;
 using torch::autograd::variable_list;
 
 // A gradient that cannot be differentiated again says so when that is tried.
-void once(variable_list& g) {
+void once(variable_list& g, const char* why = "the product's gradients cannot be differentiated again") {
     if (!at::GradMode::is_enabled()) return;
     variable_list there;
     for (auto& t : g)
         if (t.defined()) there.push_back(t.detach().requires_grad_(true));
-    auto node = std::make_shared<torch::autograd::DelayedError>("the product's gradients cannot be differentiated again", (int)there.size());
+    auto node = std::make_shared<torch::autograd::DelayedError>(why, (int)there.size());
     node->set_next_edges(torch::autograd::collect_next_edges(there));
     there = node->apply(std::move(there));
     size_t i = 0;
@@ -367,6 +527,135 @@ struct PaletteFunction : torch::autograd::Function<PaletteFunction> {
         }
         once(out);
         if (need & 4) out[2] = grads[0];
+        return out;
+    }
+};
+
+Tensor as_rows(const Tensor& t, int64_t n) { return t.dim() == 2 ? t : t.view({-1, n}); }
+
+struct EmbeddingFunction : torch::autograd::Function<EmbeddingFunction> {
+    static Variable forward(AutogradContext* ctx, const Tensor& table, const Tensor& ids, double scale) {
+        at::AutoDispatchBelowADInplaceOrView below;
+        const int64_t d = table.size(1);
+        auto shape = ids.sizes().vec();
+        shape.push_back(d);
+        Tensor y = at::empty(shape, table.options());
+        do_embedding(ids.contiguous(), rows_of(table, d), y.dim() == 2 ? y : y.view({ids.numel(), d}), scale, nullptr);
+        ctx->save_for_backward({ids});
+        ctx->saved_data["v"] = table.size(0);
+        ctx->saved_data["d"] = d;
+        ctx->saved_data["scale"] = scale;
+        return y;
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        variable_list out(3);
+        if (!grads[0].defined()) return out;
+        const auto saved = ctx->get_saved_variables();
+        const int64_t v = ctx->saved_data["v"].toInt(), d = ctx->saved_data["d"].toInt();
+        {
+            at::AutoDispatchBelowADInplaceOrView below;
+            const Tensor ids = saved[0].contiguous();
+            Tensor dy = grads[0];
+            dy = dy.dim() == 2 ? rows_of(dy, d) : rows_of(dy.reshape({ids.numel(), d}), d);
+            out[0] = at::empty({v, d}, dy.options());
+            do_embedding_backward(ids, dy, out[0], ctx->saved_data["scale"].toDouble(), false, nullptr, nullptr);
+        }
+        once(out, "the embedding's gradient cannot be differentiated again");
+        return out;
+    }
+};
+
+struct LossFunction : torch::autograd::Function<LossFunction> {
+    static Variable forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Tensor& targets, int64_t reduction) {
+        at::AutoDispatchBelowADInplaceOrView below;
+        const int64_t k = x.size(-1);
+        const Tensor x2 = rows_of(x, k), w2 = rows_of(w, k);
+        const auto o = x.options().dtype(at::kFloat);
+        Tensor loss = reduction == EDKM_REDUCE_NONE ? at::empty(targets.sizes(), o) : at::empty({}, o), lse = at::empty({x2.size(0)}, o);
+        do_loss(x2, w2, targets.contiguous(), loss, &lse, (int)reduction, nullptr, nullptr);
+        ctx->save_for_backward({x, w, targets, lse});
+        ctx->saved_data["reduction"] = reduction;
+        return loss;
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        variable_list out(4);
+        if (!grads[0].defined()) return out;
+        const auto saved = ctx->get_saved_variables();
+        const Tensor &x = saved[0], &w = saved[1];
+        const int64_t k = x.size(-1);
+        {
+            at::AutoDispatchBelowADInplaceOrView below;
+            Tensor dx;
+            if (ctx->needs_input_grad(0)) {
+                out[0] = at::empty(x.sizes(), x.options());
+                dx = as_rows(out[0], k);
+            }
+            if (ctx->needs_input_grad(1)) out[1] = at::empty(w.sizes(), w.options());
+            if (dx.defined() || out[1].defined())
+                do_loss_backward(grads[0].contiguous(), rows_of(x, k), rows_of(w, k), saved[2].contiguous(), saved[3], dx.defined() ? &dx : nullptr,
+                                 out[1].defined() ? &out[1] : nullptr, (int)ctx->saved_data["reduction"].toInt(), nullptr, nullptr);
+        }
+        once(out, "the cross entropy's gradients cannot be differentiated again");
+        return out;
+    }
+};
+
+// h and y, or y alone without a block's output.
+struct NormFunction : torch::autograd::Function<NormFunction> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& r, const Tensor& w, const Maybe& u, const Maybe& post, const Maybe& gate,
+                                 double scale, double eps) {
+        at::AutoDispatchBelowADInplaceOrView below;
+        const int64_t n = r.size(-1);
+        const Tensor r2 = rows_of(r, n), w1 = w.contiguous();
+        Tensor y = at::empty(r.sizes(), r.options()), h, h2, u2, p1, g2;
+        if (u) {
+            h = at::empty(r.sizes(), r.options());
+            h2 = as_rows(h, n);
+            u2 = rows_of(*u, n);
+        }
+        if (post) p1 = post->contiguous();
+        if (gate) g2 = gate->dim() == 1 && r.dim() > 1 ? gate->contiguous() : gate_rows(*gate, n);
+        do_norm(r2, w1, as_rows(y, n), h.defined() ? &h2 : nullptr, u ? &u2 : nullptr, post ? &p1 : nullptr, gate ? &g2 : nullptr, scale, eps,
+                nullptr);
+        ctx->save_for_backward({r, w, u ? *u : Tensor(), post ? *post : Tensor(), gate ? *gate : Tensor()});
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["eps"] = eps;
+        ctx->set_materialize_grads(false);
+        return u ? variable_list{h, y} : variable_list{y};
+    }
+    // a single row's gate may be a vector; more rows' is one for each
+    static Tensor gate_rows(const Tensor& gate, int64_t n) { return gate.dim() == 1 ? gate.contiguous() : rows_of(gate, n); }
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        variable_list out(7);
+        const auto saved = ctx->get_saved_variables();
+        const Tensor &r = saved[0], &w = saved[1], &u = saved[2], &post = saved[3], &gate = saved[4];
+        const Tensor& gy = grads.back();
+        const Tensor gh = u.defined() ? grads[0] : Tensor();
+        if (!gy.defined() && !gh.defined()) return out;
+        const int64_t n = r.size(-1);
+        {
+            at::AutoDispatchBelowADInplaceOrView below;
+            Tensor dy, dh, u2, p1, g2, dr, du;
+            if (gy.defined()) dy = rows_of(gy, n);
+            if (gh.defined()) dh = rows_of(gh, n);
+            if (u.defined()) u2 = rows_of(u, n);
+            if (post.defined()) p1 = post.contiguous();
+            if (gate.defined()) g2 = gate_rows(gate, n);
+            const Tensor* in[] = {&r, &w, &u, &post, &gate};
+            bool any = false;
+            for (int i = 0, edge = 0; i < 5; ++i)      // autograd numbers the tensors that were given
+                if (in[i]->defined() && ctx->needs_input_grad(edge++)) {
+                    out[i] = at::empty(in[i]->sizes(), in[i]->options().memory_format(at::MemoryFormat::Contiguous));
+                    any = true;
+                }
+            if (!any) return out;
+            if (out[0].defined()) dr = as_rows(out[0], n);
+            if (out[2].defined()) du = as_rows(out[2], n);
+            auto at_ = [](const Tensor& t) { return t.defined() ? &t : nullptr; };
+            do_norm_backward(at_(dy), at_(dh), rows_of(r, n), at_(u2), w.contiguous(), at_(p1), at_(g2), ctx->saved_data["scale"].toDouble(),
+                             ctx->saved_data["eps"].toDouble(), at_(dr), at_(du), at_(out[1]), at_(out[3]), at_(out[4]), nullptr, nullptr);
+        }
+        once(out, "the norm's gradients cannot be differentiated again");
         return out;
     }
 };
@@ -489,6 +778,17 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
         lib.palette = (decltype(lib.palette))at("edkm_palette_linear");
         lib.unpalettize = (decltype(lib.unpalettize))at("edkm_unpalettize");
         lib.adamw = (decltype(lib.adamw))at("edkm_adamw_batch");
+        lib.embedding = (decltype(lib.embedding))at("edkm_embedding");
+        lib.palette_embedding = (decltype(lib.palette_embedding))at("edkm_palette_embedding");
+        lib.embedding_ws = (decltype(lib.embedding_ws))at("edkm_embedding_backward_workspace_bytes");
+        lib.embedding_backward = (decltype(lib.embedding_backward))at("edkm_embedding_backward");
+        lib.norm = (decltype(lib.norm))at("edkm_residual_norm");
+        lib.norm_ws = (decltype(lib.norm_ws))at("edkm_residual_norm_backward_workspace_bytes");
+        lib.norm_backward = (decltype(lib.norm_backward))at("edkm_residual_norm_backward");
+        lib.loss_ws = (decltype(lib.loss_ws))at("edkm_linear_cross_entropy_workspace_bytes");
+        lib.loss = (decltype(lib.loss))at("edkm_linear_cross_entropy");
+        lib.loss_backward_ws = (decltype(lib.loss_backward_ws))at("edkm_linear_cross_entropy_backward_workspace_bytes");
+        lib.loss_backward = (decltype(lib.loss_backward))at("edkm_linear_cross_entropy_backward");
         lib.status = (decltype(lib.status))at("edkm_status_str");
         Py_INCREF(a[1]);
         Py_XSETREF(error_type, a[1]);
@@ -655,7 +955,165 @@ PyObject* py_adamw_batch(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// embedding(ids, table, y, scale, stream)
+PyObject* py_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 5, [&]() -> PyObject* {
+        do_embedding(tensor(a[0], "ids"), tensor(a[1], "table"), tensor(a[2], "y"), number(a[3]), Given(a[4]).get());
+        Py_RETURN_NONE;
+    });
+}
+
+// palette_embedding(ids, indices, lut, rows, y, scale, stream)
+PyObject* py_palette_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 7, [&]() -> PyObject* {
+        do_palette_embedding(tensor(a[0], "ids"), tensor(a[1], "indices"), tensor(a[2], "lut"), integer(a[3]), tensor(a[4], "y"), number(a[5]),
+                             Given(a[6]).get());
+        Py_RETURN_NONE;
+    });
+}
+
+// embedding_backward(ids, dy, dtable, scale, accumulate, workspace, stream)
+PyObject* py_embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 7, [&]() -> PyObject* {
+        do_embedding_backward(tensor(a[0], "ids"), tensor(a[1], "dy"), tensor(a[2], "dtable"), number(a[3]), integer(a[4]) != 0,
+                              maybe(a[5], "workspace"), Given(a[6]).get());
+        Py_RETURN_NONE;
+    });
+}
+
+// residual_norm(residual, weight, y, h, block, post_weight, gate, scale, eps, stream)
+PyObject* py_residual_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&]() -> PyObject* {
+        do_norm(tensor(a[0], "residual"), tensor(a[1], "weight"), tensor(a[2], "y"), maybe(a[3], "h"), maybe(a[4], "block"),
+                maybe(a[5], "post_weight"), maybe(a[6], "gate"), number(a[7]), number(a[8]), Given(a[9]).get());
+        Py_RETURN_NONE;
+    });
+}
+
+// residual_norm_backward(dy, dh, residual, block, weight, post_weight, gate, scale, eps, dresidual, dblock, dweight, dpost_weight,
+//                        dgate, workspace, stream)
+PyObject* py_residual_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 16, [&]() -> PyObject* {
+        do_norm_backward(maybe(a[0], "dy"), maybe(a[1], "dh"), tensor(a[2], "residual"), maybe(a[3], "block"), tensor(a[4], "weight"),
+                         maybe(a[5], "post_weight"), maybe(a[6], "gate"), number(a[7]), number(a[8]), maybe(a[9], "dresidual"),
+                         maybe(a[10], "dblock"), maybe(a[11], "dweight"), maybe(a[12], "dpost_weight"), maybe(a[13], "dgate"),
+                         maybe(a[14], "workspace"), Given(a[15]).get());
+        Py_RETURN_NONE;
+    });
+}
+
+// linear_cross_entropy(x, w, targets, loss, lse, reduction, workspace, stream)
+PyObject* py_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&]() -> PyObject* {
+        do_loss(tensor(a[0], "x"), tensor(a[1], "w"), tensor(a[2], "targets"), tensor(a[3], "loss"), maybe(a[4], "lse"), (int)integer(a[5]),
+                maybe(a[6], "workspace"), Given(a[7]).get());
+        Py_RETURN_NONE;
+    });
+}
+
+// linear_cross_entropy_backward(dloss, x, w, targets, lse, dx, dw, reduction, workspace, stream)
+PyObject* py_loss_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&]() -> PyObject* {
+        do_loss_backward(tensor(a[0], "dloss"), tensor(a[1], "x"), tensor(a[2], "w"), tensor(a[3], "targets"), tensor(a[4], "lse"),
+                         maybe(a[5], "dx"), maybe(a[6], "dw"), (int)integer(a[7]), maybe(a[8], "workspace"), Given(a[9]).get());
+        Py_RETURN_NONE;
+    });
+}
+
+// apply_embedding(ids, table, scale) -> y
+PyObject* py_apply_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 3, [&]() -> PyObject* {
+        const Tensor &ids = tensor(a[0], "ids"), &table = tensor(a[1], "table");
+        format_of(table, "table");
+        if (table.dim() != 2) refuse("table must be a matrix");
+        index_of(ids.contiguous(), ids.numel(), table, "ids");
+        on_gpu(table, "table");
+        return THPVariable_Wrap(EmbeddingFunction::apply(table, ids, number(a[2])));
+    });
+}
+
+// apply_palette_embedding(ids, indices, lut, rows, columns, scale, dtype) -> y
+PyObject* py_apply_palette_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 7, [&]() -> PyObject* {
+        const Tensor &ids = tensor(a[0], "ids"), &idx = tensor(a[1], "indices"), &lut = tensor(a[2], "lut");
+        const int64_t v = integer(a[3]), d = integer(a[4]);
+        const double scale = number(a[5]);
+        if (!THPDtype_Check(a[6])) refuse("dtype must be a torch type");
+        const at::ScalarType type = ((THPDtype*)a[6])->scalar_type;
+        if (type != at::kHalf && type != at::kBFloat16) refuse("dtype must be fp16 or bf16, not %s", type_name(type));
+        if (lut.requires_grad() && at::GradMode::is_enabled())
+            refuse("a palette's table takes no gradient; train the weights through dkm and embedding");
+        TORCH_CHECK(!lut._fw_grad(0).defined(), "palette_embedding: forward-mode derivatives are not implemented");
+        if (v < 1 || d < 1) refuse("a palette's table has one row and one column at least");
+        on_gpu(lut, "lut");
+        at::AutoDispatchBelowADInplaceOrView below;
+        auto shape = ids.sizes().vec();
+        shape.push_back(d);
+        Tensor y = at::empty(shape, lut.options().dtype(type));
+        do_palette_embedding(ids.contiguous(), idx, lut, v, y.dim() == 2 ? y : y.view({ids.numel(), d}), scale, nullptr);
+        return THPVariable_Wrap(y);
+    });
+}
+
+// apply_norm(residual, weight, block, post_weight, gate, scale, eps) -> y, or (h, y) with a block
+PyObject* py_apply_norm(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded(n_args, 7, [&]() -> PyObject* {
+        const Tensor &r = tensor(a[0], "residual"), &w = tensor(a[1], "weight");
+        const Tensor *u = maybe(a[2], "block"), *post = maybe(a[3], "post_weight"), *gate = maybe(a[4], "gate");
+        format_of(r, "residual");
+        if (r.dim() < 1) refuse("residual needs a last dimension");
+        const int64_t n = r.size(-1);
+        like(w, r, "weight");
+        if (w.dim() != 1 || w.size(0) != n) refuse("weight must hold %lld elements", (long long)n);
+        if (u) {
+            like(*u, r, "block");
+            if (u->sizes() != r.sizes()) refuse("block must have the residual's shape");
+        }
+        if (post && (post->dim() != 1 || post->size(0) != n)) refuse("post_weight must hold %lld elements", (long long)n);
+        if (post) like(*post, r, "post_weight");
+        if (gate && !(gate->dim() == 1 && gate->size(0) == n) && gate->sizes() != r.sizes())
+            refuse("gate must hold %lld elements or have the residual's shape", (long long)n);
+        if (gate) like(*gate, r, "gate");
+        on_gpu(r, "residual");
+        auto may = [](const Tensor* t) { return t ? Maybe(*t) : Maybe(); };
+        const variable_list o = NormFunction::apply(r, w, may(u), may(post), may(gate), number(a[5]), number(a[6]));
+        if (o.size() == 1) return THPVariable_Wrap(o[0]);
+        PyObject *h = THPVariable_Wrap(o[0]), *y = THPVariable_Wrap(o[1]);
+        PyObject* t = h && y ? PyTuple_Pack(2, h, y) : nullptr;
+        Py_XDECREF(h);
+        Py_XDECREF(y);
+        return t;
+    });
+}
+
+// apply_loss(x, w, targets, reduction) -> loss
+PyObject* py_apply_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 4, [&]() -> PyObject* {
+        const Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "w"), &targets = tensor(a[2], "targets");
+        format_of(x, "x");
+        if (x.dim() < 1 || w.dim() != 2 || x.size(-1) != w.size(1)) refuse("w must be n x k for x of (..., k)");
+        like(w, x, "w");
+        bool ok = targets.dim() + 1 == x.dim();
+        for (int64_t i = 0; ok && i < targets.dim(); ++i) ok = targets.size(i) == x.size(i);
+        if (!ok) refuse("targets must have x's shape without its last dimension");
+        index_of(targets.contiguous(), targets.numel(), x, "targets");
+        on_gpu(x, "x");
+        return THPVariable_Wrap(LossFunction::apply(x, w, targets, integer(a[3])));
+    });
+}
+
 PyMethodDef methods[] = {
+    {"embedding", (PyCFunction)(void*)py_embedding, METH_FASTCALL, nullptr},
+    {"palette_embedding", (PyCFunction)(void*)py_palette_embedding, METH_FASTCALL, nullptr},
+    {"embedding_backward", (PyCFunction)(void*)py_embedding_backward, METH_FASTCALL, nullptr},
+    {"residual_norm", (PyCFunction)(void*)py_residual_norm, METH_FASTCALL, nullptr},
+    {"residual_norm_backward", (PyCFunction)(void*)py_residual_norm_backward, METH_FASTCALL, nullptr},
+    {"linear_cross_entropy", (PyCFunction)(void*)py_loss, METH_FASTCALL, nullptr},
+    {"linear_cross_entropy_backward", (PyCFunction)(void*)py_loss_backward, METH_FASTCALL, nullptr},
+    {"apply_embedding", (PyCFunction)(void*)py_apply_embedding, METH_FASTCALL, nullptr},
+    {"apply_palette_embedding", (PyCFunction)(void*)py_apply_palette_embedding, METH_FASTCALL, nullptr},
+    {"apply_norm", (PyCFunction)(void*)py_apply_norm, METH_FASTCALL, nullptr},
+    {"apply_loss", (PyCFunction)(void*)py_apply_loss, METH_FASTCALL, nullptr},
     {"bind", (PyCFunction)(void*)py_bind, METH_FASTCALL, nullptr},
     {"linear", (PyCFunction)(void*)py_linear, METH_FASTCALL, nullptr},
     {"linear_backward", (PyCFunction)(void*)py_linear_backward, METH_FASTCALL, nullptr},

@@ -110,6 +110,20 @@ _SIGS = {
                                    _P, _sz, _P]),
     "edkm_adamw_batch": (_i32, [_i32, _P, _i32, _i32, _i32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _f64, _f64, _f64,
                                 _f64, _f64, _u32, _P]),
+    "edkm_embedding": (_i32, [_i64, _i64, _i64, _i32, _i32, _P, _P, _i64, _f32, _P, _i64, _P]),
+    "edkm_palette_embedding": (_i32, [_i64, _i64, _i64, _i32, _i32, _i32, _P, _P, _P, _f32, _P, _i64, _P]),
+    "edkm_embedding_backward_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "edkm_embedding_backward": (_i32, [_i64, _i64, _i64, _i32, _i32, _P, _P, _i64, _f32, _i32, _P, _i64, _P, _sz, _P]),
+    "edkm_residual_norm": (_i32, [_i64, _i64, _i32, _P, _i64, _P, _i64, _P, _P, _P, _i64, _i32, _f32, _f32, _P, _i64, _P, _i64,
+                                  _P]),
+    "edkm_residual_norm_backward_workspace_bytes": (_sz, [_i64, _i64]),
+    "edkm_residual_norm_backward": (_i32, [_i64, _i64, _i32, _P, _i64, _P, _i64, _P, _i64, _P, _i64, _P, _P, _P, _i64, _i32, _f32,
+                                           _f32, _P, _i64, _P, _i64, _P, _P, _P, _P, _sz, _P]),
+    "edkm_linear_cross_entropy_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "edkm_linear_cross_entropy": (_i32, [_i64, _i64, _i64, _i32, _i32, _i32, _P, _i64, _P, _i64, _P, _P, _P, _P, _sz, _P]),
+    "edkm_linear_cross_entropy_backward_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "edkm_linear_cross_entropy_backward": (_i32, [_i64, _i64, _i64, _i32, _i32, _i32, _P, _P, _i64, _P, _i64, _P, _P, _P, _i64, _P,
+                                                  _P, _sz, _P]),
     "edkm_plan_set_pass_events": (_i32, [_PLAN, _i32, _P, _P]),
     "edkm_plan_hip_error": (_i32, [_PLAN, ctypes.POINTER(_i32), ctypes.POINTER(ctypes.c_char_p),
                                    ctypes.POINTER(ctypes.c_char_p)]),
@@ -502,3 +516,88 @@ def adamw_batch(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1: float = 0
     ``v_scales``; ``seed`` then varies their rounding noise."""
     _x.adamw_batch(params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1, beta2, eps, weight_decay, masters, m_scales, v_scales,
                    int(seed), _given(stream))
+
+
+# ---------------------------------------------------------------------------
+# a model's two ends and the step from one block to the next
+
+REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
+INDEX_INT32, INDEX_INT64 = 0, 1
+NORM_MAX = 16384           # EDKM_NORM_MAX: values of a row
+
+
+def _reduction(name):
+    try:
+        return REDUCTIONS[name]
+    except (KeyError, TypeError):
+        raise ValueError("reduction must be one of %s" % sorted(REDUCTIONS)) from None
+
+
+def embedding_backward_workspace_bytes(m: int, v: int, d: int) -> int:
+    return int(_lib.edkm_embedding_backward_workspace_bytes(int(m), int(v), int(d)))
+
+
+def residual_norm_backward_workspace_bytes(m: int, n: int) -> int:
+    return int(_lib.edkm_residual_norm_backward_workspace_bytes(int(m), int(n)))
+
+
+def linear_cross_entropy_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(_lib.edkm_linear_cross_entropy_workspace_bytes(int(m), int(n), int(k)))
+
+
+def linear_cross_entropy_backward_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(_lib.edkm_linear_cross_entropy_backward_workspace_bytes(int(m), int(n), int(k)))
+
+
+def embedding(ids, table, y, scale: float = 1.0, stream=None) -> None:
+    """y_i = scale table[ids_i] for int32 or int64 ``ids`` (m of any shape), a 16-bit
+    table (v x d) and y (m x d), whose rows may lie apart.  An id outside 0 .. v - 1
+    stands for no token: a row of zeros."""
+    _x.embedding(ids, table, y, scale, _given(stream))
+
+
+def palette_embedding(ids, indices, lut, num_embeddings: int, y, scale: float = 1.0, stream=None) -> None:
+    """embedding with the table (num_embeddings x d) given as palettize's indices and table."""
+    _x.palette_embedding(ids, indices, lut, num_embeddings, y, scale, _given(stream))
+
+
+def embedding_backward(ids, dy, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None) -> None:
+    """The table's gradient: dtable_t = scale (sum of dy_i over the i with ids_i = t), or with
+    ``accumulate`` that much more (rows of no token are then left alone).  Without
+    ``workspace`` one is taken from torch's allocator, as in linear."""
+    _x.embedding_backward(ids, dy, dtable, scale, int(bool(accumulate)), workspace, _given(stream))
+
+
+def residual_norm(residual, weight, y, h=None, block=None, post_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6,
+                  stream=None) -> None:
+    """h = residual + scale gate N(block; post_weight) and y = N(h; weight) over the rows of
+    16-bit matrices (m x n), N(v; w) = v / sqrt(mean(v^2) + eps) w.  ``gate`` holds n values
+    or m x n; without ``post_weight`` the block's output is added as it is, and without
+    ``block`` y is N(residual; weight).  h may be the residual or the block's output."""
+    _x.residual_norm(residual, weight, y, h, block, post_weight, gate, scale, eps, _given(stream))
+
+
+def residual_norm_backward(dy, dh, residual, weight, block=None, post_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6,
+                           dresidual=None, dblock=None, dweight=None, dpost_weight=None, dgate=None, workspace=None,
+                           stream=None) -> None:
+    """residual_norm's gradients for dL/dy and dL/dh (either may be None) into those outputs
+    that are given; the other tensors are those that residual_norm had (h is formed from
+    them again)."""
+    _x.residual_norm_backward(dy, dh, residual, block, weight, post_weight, gate, scale, eps, dresidual, dblock, dweight, dpost_weight, dgate,
+                              workspace, _given(stream))
+
+
+def linear_cross_entropy(x, w, targets, loss, lse=None, reduction: str = "none", workspace=None, stream=None) -> None:
+    """Softmax cross entropy of x w^T (x: m x k, w: n x k, 16-bit) against int32 or int64
+    ``targets``, without the m x n logits in memory.  ``loss`` is float32: m values, or one
+    with reduction "sum" or "mean"; a target outside 0 .. n - 1 stands for none, has loss 0
+    and does not count in the mean (0 over none).  ``lse`` (float32, m) receives
+    log(sum(exp(logits))) of the rows with a target, for linear_cross_entropy_backward."""
+    _x.linear_cross_entropy(x, w, targets, loss, lse, _reduction(reduction), workspace, _given(stream))
+
+
+def linear_cross_entropy_backward(dloss, x, w, targets, lse, dx=None, dw=None, reduction: str = "none", workspace=None,
+                                  stream=None) -> None:
+    """The gradients of x and w for dL/dloss (float32, as ``loss`` of the forward) into dx
+    (m x k) and dw (n x k, contiguous), one at least."""
+    _x.linear_cross_entropy_backward(dloss, x, w, targets, lse, dx, dw, _reduction(reduction), workspace, _given(stream))

@@ -160,3 +160,45 @@ def palette_linear(x, indices, lut, out_features: int, bias=None, residual=None,
     indices and the table of ``edkm.palettize``: the product of a served model.
     Differentiable (once, in reverse mode) in x, bias and residual; the palette is frozen."""
     return edkm._x.apply_palette_linear(x, indices, lut, out_features, bias, residual, edkm._activation(activation))
+
+
+def embedding(ids, table, scale: float = 1.0):
+    """scale table[ids]; differentiable (once, in reverse mode) in the table.
+
+    ids: int32 or int64, any shape; one outside 0 .. v - 1 (-1, -100) stands for no token: a
+    row of zeros and no gradient.  table: v x d, fp16 or bf16, say W~ of ``dkm`` with
+    out_half.  The gradient sums each row's tokens in fp32 in one order, rounded once."""
+    return edkm._x.apply_embedding(ids, table, scale)
+
+
+def palette_embedding(ids, indices, lut, num_embeddings: int, embedding_dim: int, scale: float = 1.0, dtype=torch.bfloat16):
+    """embedding with the table given as the packed indices and the table of
+    ``edkm.palettize``: the lookup of a served model.  No gradient."""
+    return edkm._x.apply_palette_embedding(ids, indices, lut, num_embeddings, embedding_dim, scale, dtype)
+
+
+def rms_norm(x, weight, eps: float = 1e-6):
+    """x / sqrt(mean(x^2) + eps) weight over the last dimension; differentiable (once, in
+    reverse mode) in both.  fp16 or bf16; sums in fp32."""
+    return edkm._x.apply_norm(x, weight, None, None, None, 1.0, eps)
+
+
+def residual_norm(residual, block, weight, post_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6):
+    """The step from one block to the next: h = residual + scale gate N(block; post_weight),
+    y = N(h; weight) -> (h, y), in one pass; differentiable (once, in reverse mode) in all tensors.
+
+    residual, block: (..., n), fp16 or bf16; weight, post_weight: n; gate: n, or (..., n).
+    Without post_weight the block's output is added as it is.  The backward keeps residual and block."""
+    return edkm._x.apply_norm(residual, weight, block, post_weight, gate, scale, eps)
+
+
+def linear_cross_entropy(x, w, targets, reduction: str = "mean"):
+    """Softmax cross entropy of the logits x w^T against target words, which are never in
+    memory; differentiable (once, in reverse mode) in x and w.
+
+    x: fp16 or bf16, (..., k); w: n x k of x's type, say W~ of ``dkm`` with out_half;
+    targets: int32 or int64, (...), one outside 0 .. n - 1 (-100) stands for none: loss 0, no
+    gradient, not counted.  reduction: mean over the counted tokens (0 if there are none),
+    sum, or none (a loss for each token).  The loss is float32.  The backward keeps x, w and
+    a number per token, and forms the logits again."""
+    return edkm._x.apply_loss(x, w, targets, edkm._reduction(reduction))

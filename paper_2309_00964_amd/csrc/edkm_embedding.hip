@@ -31,30 +31,43 @@ __device__ __forceinline__ void store8(uint16_t* q, s16x8 v, int left) {
 // ----------------------------------------------------------------------------
 // lookup
 
-// A thread takes eight columns of one token after another; a workgroup `rows` tokens.  Bound
+// A thread takes eight columns of four tokens at a time; a workgroup `rows` tokens.  Bound
 // by the bytes of the rows read and written.
-template <int F, int IDX, int BITS>
+template <int F, int IDX, int BITS, bool TINY>
 __global__ void __launch_bounds__(256) k_embed(EmbedArgs a) {
+    constexpr int U = BITS ? 1 : 4;
     Decoder<F> dec;
     if constexpr (BITS != 0) dec.init(a.lut, BITS);
     const uint32_t pieces = (a.d + 7) / 8;
+    const bool ragged = a.d % 8 != 0;
     const int64_t i0 = (int64_t)(a.first + blockIdx.x) * a.rows;
-    const uint32_t rows = (uint32_t)min((int64_t)a.rows, a.m - i0);
-    for (uint32_t l = threadIdx.x; l < rows * pieces; l += 256) {
-        const uint32_t r = l / pieces, c = (l - r * pieces) * 8;
-        const int left = (int)min(a.d - c, 8u);
-        const uint32_t t = row_of<IDX>(a.ids, i0 + r, a.v);
-        s16x8 v = {};
-        if (t < a.v) {
-            if constexpr (BITS != 0)
-                v = dec.eight(load_idx8(a.idx, a.idx_bytes, (uint64_t)t * a.d + c, BITS), BITS);
-            else
-                v = row8(a.table + (int64_t)t * a.ldt + c, left);
+    const uint32_t rows = (uint32_t)min((int64_t)a.rows, a.m - i0), total = rows * pieces;
+    for (uint32_t l0 = threadIdx.x; l0 < total; l0 += 256 * U) {
+        uint32_t r[U], c[U], t[U];
+        s16x8 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t l = min(l0 + u * 256, total - 1);
+            r[u] = l / pieces;
+            c[u] = (l - r[u] * pieces) * 8;
+            t[u] = row_of<IDX>(a.ids, i0 + r[u], a.v);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t at = t[u] < a.v ? t[u] : 0;
+            if constexpr (BITS != 0) v[u] = dec.eight(load_idx8(a.idx, a.idx_bytes, (uint64_t)at * a.d + c[u], BITS), BITS);
+            else v[u] = ask8<TINY>(a.table + (int64_t)at * a.ldt, (int)c[u], (int)a.d);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int left = (int)min(a.d - c[u], 8u);
+            if constexpr (BITS == 0) v[u] = had8<TINY>(v[u], left, ragged);
             if (a.scale != 1.f)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = (short)to_16<F>(to_f32<F>((uint16_t)v[j]) * a.scale);
+                for (int j = 0; j < 8; ++j) v[u][j] = (short)to_16<F>(to_f32<F>((uint16_t)v[u][j]) * a.scale);
+            if (t[u] >= a.v) v[u] = s16x8{};
+            if (l0 + u * 256 < total) store8(a.y + (i0 + r[u]) * a.ldy + c[u], v[u], left);
         }
-        store8(a.y + (i0 + r) * a.ldy + c, v, left);
     }
 }
 
@@ -64,11 +77,14 @@ static hipError_t embed_fi(EmbedArgs a, int bits, hipStream_t s) {
     a.rows = pieces >= 1024 ? 1 : 1024 / pieces;
     const uint64_t groups = (uint64_t)((a.m + a.rows - 1) / a.rows);
     switch (bits) {
-    case 0: EDKM_GO_PARTS((k_embed<F, IDX, 0>), groups, 256, a); break;
-    case 1: EDKM_GO_PARTS((k_embed<F, IDX, 1>), groups, 256, a); break;
-    case 2: EDKM_GO_PARTS((k_embed<F, IDX, 2>), groups, 256, a); break;
-    case 3: EDKM_GO_PARTS((k_embed<F, IDX, 3>), groups, 256, a); break;
-    default: EDKM_GO_PARTS((k_embed<F, IDX, 4>), groups, 256, a); break;
+    case 0:
+        if (a.d < 8) EDKM_GO_PARTS((k_embed<F, IDX, 0, true>), groups, 256, a);
+        else EDKM_GO_PARTS((k_embed<F, IDX, 0, false>), groups, 256, a);
+        break;
+    case 1: EDKM_GO_PARTS((k_embed<F, IDX, 1, false>), groups, 256, a); break;
+    case 2: EDKM_GO_PARTS((k_embed<F, IDX, 2, false>), groups, 256, a); break;
+    case 3: EDKM_GO_PARTS((k_embed<F, IDX, 3, false>), groups, 256, a); break;
+    default: EDKM_GO_PARTS((k_embed<F, IDX, 4, false>), groups, 256, a); break;
     }
     return hipSuccess;
 }
@@ -82,14 +98,19 @@ hipError_t launch_embed(EmbedArgs a, int fmt, int index_type, int bits, hipStrea
 // tokens by row
 
 // A token's place among the sorted is the number of tokens of lower rows, and of its own row
-// before it.  A workgroup counts for 32 tokens, eight threads to a token, against all tokens
+// before it.  A workgroup counts for 32 tokens, 32 threads to a token, against all tokens
 // in LDS: no pass waits for another, and nothing depends on an order of arrival.
 template <int IDX>
-__global__ void __launch_bounds__(256) k_rank(SortArgs a) {
+__global__ void __launch_bounds__(1024) k_rank(SortArgs a) {
+    constexpr int T = 1024 / RANK_TOKENS;
     __shared__ __attribute__((aligned(16))) uint32_t all[RANK_MOST];
-    __shared__ uint32_t count[8][RANK_TOKENS];
+    __shared__ uint32_t count[T][RANK_TOKENS];
     const uint32_t m4 = (a.m + 3) & ~3u;
-    for (uint32_t j = threadIdx.x; j < m4; j += 256) all[j] = j < a.m ? row_of<IDX>(a.ids, j, a.v) : 0xFFFFFFFFu;
+#pragma unroll
+    for (uint32_t k = 0; k < RANK_MOST / 1024; ++k) {
+        const uint32_t j = k * 1024 + threadIdx.x;
+        if (j < m4) all[j] = j < a.m ? row_of<IDX>(a.ids, j, a.v) : 0xFFFFFFFFu;
+    }
     __syncthreads();
     const uint32_t mine = threadIdx.x & (RANK_TOKENS - 1), q = threadIdx.x / RANK_TOKENS;
     const uint32_t i0 = blockIdx.x * RANK_TOKENS, i = i0 + mine;
@@ -97,21 +118,23 @@ __global__ void __launch_bounds__(256) k_rank(SortArgs a) {
     const uint4* four = reinterpret_cast<const uint4*>(all);
     uint32_t n = 0;
     // tokens before the workgroup's: also those of the same row; after them: lower rows only
-    for (uint32_t j = q; j < i0 / 4; j += 8) {
+#pragma unroll 8
+    for (uint32_t j = q; j < i0 / 4; j += T) {
         const uint4 o = four[j];
         n += (o.x <= key) + (o.y <= key) + (o.z <= key) + (o.w <= key);
     }
-    for (uint32_t j = i0 / 4 + RANK_TOKENS / 4 + q; j < m4 / 4; j += 8) {
+#pragma unroll 8
+    for (uint32_t j = i0 / 4 + RANK_TOKENS / 4 + q; j < m4 / 4; j += T) {
         const uint4 o = four[j];
         n += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
     }
-    for (uint32_t j = i0 + q; j < min(i0 + RANK_TOKENS, a.m); j += 8) n += all[j] < key || (all[j] == key && j < i);
+    if (i0 + q < a.m) n += all[i0 + q] < key || (all[i0 + q] == key && q < mine);
     count[q][mine] = n;
     __syncthreads();
     if (threadIdx.x < RANK_TOKENS && i < a.m) {
         uint32_t at = 0;
 #pragma unroll
-        for (int p = 0; p < 8; ++p) at += count[p][mine];
+        for (int p = 0; p < T; ++p) at += count[p][mine];
         a.key[at] = key;
         a.pos[at] = i;
     }
@@ -159,6 +182,7 @@ __global__ void __launch_bounds__(256) k_place(SortArgs a) {
     // thread t sums digits t D .. t D + D - 1: all workgroups', and those before this one
     const uint32_t D = (a.digits + 255) / 256;
     uint32_t before[MOST / 256] = {}, total[MOST / 256] = {};
+#pragma unroll 8
     for (uint32_t g = 0; g < a.groups; ++g)
 #pragma unroll
         for (uint32_t k = 0; k < MOST / 256; ++k)
@@ -223,7 +247,7 @@ static hipError_t sort_i(SortArgs a, uint32_t* key, uint32_t* pos, uint32_t* spa
     a.key = key;
     a.pos = pos;
     if (q.passes == 0) {
-        EDKM_GO(k_rank<IDX>, dim3((a.m + RANK_TOKENS - 1) / RANK_TOKENS), dim3(256), a);
+        EDKM_GO(k_rank<IDX>, dim3((a.m + RANK_TOKENS - 1) / RANK_TOKENS), dim3(1024), a);
         return hipSuccess;
     }
     a.per = q.per;
@@ -288,7 +312,7 @@ __device__ __forceinline__ uint32_t lower(const uint32_t* key, uint32_t m, uint3
 // others goes to part: place 0 for a row that began in an earlier chunk, place 1 for one
 // that begins here and goes on.  Long rows are thereby shared by many threads, and every sum
 // has one order.  Workgroups after those write zeros to the rows of no token.
-template <int F>
+template <int F, bool TINY>
 __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
     const uint32_t group = a.first + blockIdx.x, pieces = (a.d + 7) / 8;
     if (group >= a.chunk_groups) {
@@ -320,17 +344,22 @@ __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
         reinterpret_cast<f32x4*>(q)[1] = f32x4{sum[4], sum[5], sum[6], sum[7]};
     };
     constexpr int U = 8;
-    for (uint32_t j = j0; j < j1; j += U) {
+    const bool ragged = a.d % 8 != 0;
+    for (uint32_t j = j0; j < j1 && row < a.v; j += U) {
         s16x8 v[U];
-        uint32_t key[U];
+        uint32_t key[U], pos[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            key[u] = j + u < j1 ? a.key[j + u] : a.v;
-            v[u] = key[u] < a.v ? row8(a.dy + (int64_t)a.pos[j + u] * a.lddy + c, left) : s16x8{};
+            const uint32_t at = min(j + u, j1 - 1);
+            key[u] = a.key[at];
+            pos[u] = a.pos[at];
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = ask8<TINY>(a.dy + (int64_t)pos[u] * a.lddy, (int)c, (int)a.d);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (j + u >= j1) break;
+            if (ragged) v[u] = had8<TINY>(v[u], left, true);
             if (key[u] != row) {
                 if (row < a.v) {
                     if (row == before) part(0);
@@ -393,7 +422,8 @@ static hipError_t grad_f(EmbedGradArgs a, hipStream_t s) {
     const uint64_t threads = (uint64_t)a.chunks * ((a.d + 7) / 8);
     const uint64_t sums = (threads + 255) / 256, zeros = a.accumulate ? 0 : ((uint64_t)a.v + ZERO_ROWS - 1) / ZERO_ROWS;
     a.chunk_groups = (uint32_t)sums;
-    EDKM_GO_PARTS(k_embed_grad<F>, sums + zeros, 256, a);
+    if (a.d < 8) EDKM_GO_PARTS((k_embed_grad<F, true>), sums + zeros, 256, a);
+    else EDKM_GO_PARTS((k_embed_grad<F, false>), sums + zeros, 256, a);
     if (a.chunks > 1) EDKM_GO_PARTS(k_embed_join<F>, sums, 256, a);
     return hipSuccess;
 }

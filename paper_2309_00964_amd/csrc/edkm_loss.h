@@ -34,12 +34,19 @@ __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f
 // The largest of a row's 64 logits and the sum of e^(z - largest), and the target's logit.
 // A row's logits lie in the four lanes r, r + 16, r + 32 and r + 48.
 struct LossStats : LossBegin {
-    __device__ __forceinline__ static void block(const LossArgs& p, char*, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
+  template <int TR>
+  struct End {
+    int word[TR];
+    __device__ __forceinline__ void init(const LossArgs& p, int lane, int r) {
+#pragma unroll
+        for (int i = 0; i < TR; ++i) word[i] = p.rows_of.word[p.base + min(r + i * 16 + (lane & 15), p.rows - 1)];
+    }
+    __device__ __forceinline__ void block(const LossArgs& p, int i, char*, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
         if (r0 >= p.rows || c0 >= p.cols) return;
         const int row = r0 + (lane & 15), c = c0 + (lane >> 4) * 4;
         const float none = -__builtin_inff();
         if (row < p.rows) {
-            const int t = p.rows_of.word[p.base + row] - c;
+            const int t = word[i] - c;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -69,9 +76,11 @@ struct LossStats : LossBegin {
         sum += __shfl_xor(sum, 32);
         if (lane < 16 && row < p.rows) p.stats[(int64_t)(c0 / 64) * p.stat_rows + row] = make_float2(top, sum);
     }
+  };
 };
 
-// Stores a 16 x 64 block as 16-bit values, whole lines at a time; `to` gives a row's place.
+// Stores a 16 x 64 block as 16-bit values, whole lines at a time; `to` gives the place of the
+// lane's first (row lane / 8) and second (eight rows on) row.
 // Columns from p.cols on up to `wide` become zeros.
 template <int F, class To>
 __device__ __forceinline__ void store_block(const LossArgs& p, char* lds, int lane, int r0, int c0, const f32x4 (&acc)[4], int wide, To to) {
@@ -89,7 +98,7 @@ __device__ __forceinline__ void store_block(const LossArgs& p, char* lds, int la
         s16x8 v;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = c + e < p.cols ? (short)to_16<F>(f[e]) : (short)0;
-        uint16_t* out = to(r0 + r) + c;
+        uint16_t* out = to(i) + c;
         if (c + 8 <= wide) {
             reinterpret_cast<S16x8*>(out)->v = v;
         } else {
@@ -106,23 +115,50 @@ __device__ __forceinline__ void store_block(const LossArgs& p, char* lds, int la
 // |dL/dl|, so that fp16 holds probabilities down to 2^-30 (2^-39 with fewer digits).
 template <int F>
 struct LossDz : LossBegin {
-    __device__ __forceinline__ static void block(const LossArgs& p, char* lds, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
+  template <int TR>
+  struct End {
+    int word[TR];
+    float lse[TR], factor[TR];
+    __device__ __forceinline__ void init(const LossArgs& p, int lane, int r) {
+#pragma unroll
+        for (int i = 0; i < TR; ++i) {
+            const int row = min(r + i * 16 + (lane & 15), p.rows - 1);
+            word[i] = p.rows_of.word[row];
+            factor[i] = p.rows_of.value[row];
+            lse[i] = p.lse[p.rows_of.row[row]];
+        }
+    }
+    __device__ __forceinline__ void block(const LossArgs& p, int i, char* lds, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
         const int wide = (p.cols + 7) & ~7;
         if (r0 >= p.rows || c0 >= wide) return;
-        const int row = min(r0 + (lane & 15), p.rows - 1), t = p.rows_of.word[row] - p.col0 - c0 - (lane >> 4) * 4;
-        const float lse = p.lse[p.rows_of.row[row]], factor = p.rows_of.value[row];
+        const int t = word[i] - p.col0 - c0 - (lane >> 4) * 4;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[j][e] = factor * (exp_of(acc[j][e] - lse) - (t == j * 16 + e ? 1.f : 0.f));
-        store_block<F>(p, lds, lane, r0, c0, acc, wide, [&](int r) { return p.out + (int64_t)r * p.ldo; });
+            for (int e = 0; e < 4; ++e) acc[j][e] = factor[i] * (exp_of(acc[j][e] - lse[i]) - (t == j * 16 + e ? 1.f : 0.f));
+        store_block<F>(p, lds, lane, r0, c0, acc, wide, [&](int q) { return p.out + (int64_t)(r0 + (lane >> 3) + q * 8) * p.ldo; });
     }
+  };
 };
 
 // dx or dw: the sums of one launch, or with those of the launches before, times alpha.
 template <int F>
 struct LossSum : LossBegin {
-    __device__ __forceinline__ static void block(const LossArgs& p, char* lds, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t place) {
+  template <int TR>
+  struct End {
+    int row[TR][2];         // where the lane's two rows of a block go
+    float alpha;
+    __device__ __forceinline__ void init(const LossArgs& p, int lane, int r) {
+        alpha = *p.rows_of.alpha;
+#pragma unroll
+        for (int i = 0; i < TR; ++i)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                row[i][q] = min(r + i * 16 + q * 8 + (lane >> 3), p.rows - 1);
+                if (p.scatter) row[i][q] = p.rows_of.row[row[i][q]];
+            }
+    }
+    __device__ __forceinline__ void block(const LossArgs& p, int i, char* lds, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t place) {
         if (r0 >= p.rows || c0 >= p.cols) return;
         float* at = p.accum + place * 1024 + lane * 4;
         if (!p.begins)
@@ -133,14 +169,13 @@ struct LossSum : LossBegin {
             for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(at + j * 256) = acc[j];
             return;
         }
-        const float alpha = *p.rows_of.alpha;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[j][e] *= alpha;
-        store_block<F>(p, lds, lane, r0, c0, acc, p.cols,
-                       [&](int r) { return p.out + (int64_t)(p.scatter ? p.rows_of.row[r] : r) * p.ldo; });
+        store_block<F>(p, lds, lane, r0, c0, acc, p.cols, [&](int q) { return p.out + (int64_t)row[i][q] * p.ldo; });
     }
+  };
 };
 
 template <int F, int OPA, int OPB, class E>

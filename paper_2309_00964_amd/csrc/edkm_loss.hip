@@ -22,6 +22,7 @@ __device__ __forceinline__ int word_of(const void* targets, int64_t i, int64_t n
 // One workgroup lists the tokens with a target in order, for a backward those whose loss has a
 // gradient; a backward's factors follow, once their largest is known.  What the products
 // read has no row of any other token, so whatever those hold (NaN, Inf) reaches no gradient.
+constexpr int PICK = 8;      // tokens of a thread at a time
 template <int IDX>
 __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
     __shared__ int waves[2][16];
@@ -29,35 +30,51 @@ __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     int base = 0, turn = 0;
     float top = 0.f;
-    for (int64_t i0 = 0; i0 < a.m; i0 += 1024, turn ^= 1) {
-        const int64_t i = i0 + threadIdx.x;
-        int t = i < a.m ? word_of<IDX>(a.targets, i, a.n) : -1;
-        float g = 1.f;
-        if (a.dloss && t >= 0) g = a.dloss[a.reduction == RED_NONE ? i : 0];
-        if (g == 0.f) t = -1;
-        const uint64_t there = __ballot(t >= 0);
-        if (lane == 0) waves[turn][w] = __popcll(there);
+    for (int64_t i0 = 0; i0 < a.m; i0 += 1024 * PICK, turn ^= 1) {
+        const int64_t i = i0 + threadIdx.x * PICK;
+        int t[PICK], mine = 0;
+        float g[PICK];
+#pragma unroll
+        for (int e = 0; e < PICK; ++e) {
+            t[e] = i + e < a.m ? word_of<IDX>(a.targets, i + e, a.n) : -1;
+            g[e] = a.dloss && i + e < a.m ? a.dloss[a.reduction == RED_NONE ? i + e : 0] : 1.f;
+        }
+#pragma unroll
+        for (int e = 0; e < PICK; ++e) {
+            if (g[e] == 0.f) t[e] = -1;
+            mine += t[e] >= 0;
+        }
+        int run = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int up = __shfl_up(run, o);
+            if (lane >= o) run += up;
+        }
+        if (lane == 63) waves[turn][w] = run;
         __syncthreads();
-        int at = base;
+        int at = base + run - mine;
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
             const int c = waves[turn][q];
             at += q < w ? c : 0;
             base += c;
         }
-        if (t >= 0) {
-            at += __popcll(there & ((1ull << lane) - 1));
-            a.r.row[at] = (int)i;
-            a.r.word[at] = t;
-            if (a.dloss) {
-                a.r.slot[i] = at;
-                a.r.value[at] = g;
-                top = fmaxf(top, fabsf(g));
+#pragma unroll
+        for (int e = 0; e < PICK; ++e) {
+            if (i + e >= a.m) break;
+            if (a.dloss) a.r.slot[i + e] = t[e] >= 0 ? at : -1;
+            if (t[e] >= 0) {
+                a.r.row[at] = (int)(i + e);
+                a.r.word[at] = t[e];
+                if (a.dloss) {
+                    a.r.value[at] = g[e];
+                    top = fmaxf(top, fabsf(g[e]));
+                }
+                ++at;
+            } else {
+                if (a.loss && a.reduction == RED_NONE) a.loss[i + e] = 0.f;
+                if (a.lse) a.lse[i + e] = 0.f;
             }
-        } else if (i < a.m) {
-            if (a.dloss) a.r.slot[i] = -1;
-            if (a.loss && a.reduction == RED_NONE) a.loss[i] = 0.f;
-            if (a.lse) a.lse[i] = 0.f;
         }
     }
     if (threadIdx.x == 0) a.r.count[0] = base;

@@ -104,7 +104,7 @@ struct NormArgs {
     int64_t lddy, lddh;
     uint16_t *dr, *du, *dw, *dpost, *dgate;
     int64_t lddr, lddu;
-    float* part;            // [groups][3][n]
+    float* part;            // [groups][2][n]
     uint32_t groups;
 };
 uint32_t norm_groups(int64_t m, int64_t n);      // workgroups of a backward

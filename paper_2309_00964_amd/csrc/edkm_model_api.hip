@@ -261,7 +261,7 @@ edkm_status edkm_residual_norm(int64_t m, int64_t n, int format, const void* r, 
 
 size_t edkm_residual_norm_backward_workspace_bytes(int64_t m, int64_t n) {
     if (!norm_ok(m, n, EDKM_KEYS_FP16, 1.f, 1.f) || m == 0) return 0;
-    return up256((size_t)norm_groups(m, n) * 3 * n * 4);
+    return up256((size_t)norm_groups(m, n) * 2 * n * 4);
 }
 
 edkm_status edkm_residual_norm_backward(int64_t m, int64_t n, int format, const void* dy, int64_t lddy, const void* dh, int64_t lddh,

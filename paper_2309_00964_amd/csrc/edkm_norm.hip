@@ -9,21 +9,37 @@
 
 namespace edkm {
 
+// The sum of a wave's values, by moves between lanes of a row of sixteen and from row to row.
+template <int MOVE, int ROWS>
+__device__ __forceinline__ float moved(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), MOVE, ROWS, 0xF, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v += moved<0x111, 0xF>(v);      // row_shr:1, 2, 4, 8: the last lane of a row has its sum
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);      // row_bcast:15 and 31: the last lane has all rows'
+    v += moved<0x143, 0xC>(v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
 // L threads share a row, each with I pieces of eight columns.
 template <int L>
 struct Row {
-    static constexpr int THREADS = L < 256 ? 256 : L;
+    static constexpr int THREADS = L == 64 ? 256 : L;
     static constexpr int ROWS = THREADS / L;      // of a workgroup, side by side
     static constexpr int WAVES = L / 64;
+
+    // The workgroup's row, the same for a wave: its addresses are scalars.
+    __device__ __forceinline__ static uint32_t mine() { return ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / L); }
 
     // Sums of a row's K values over its threads.  Sums that follow one another take different
     // places in LDS, so that one barrier each is enough.
     template <int K>
     __device__ __forceinline__ static void sum(float (&v)[K], float (*lds)[16], int place) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int o = 32; o; o >>= 1) v[k] += __shfl_xor(v[k], o);
+        for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
         if constexpr (WAVES > 1) {
             static_assert(WAVES <= 16 && K <= 3, "places");
             const int w = threadIdx.x >> 6;
@@ -60,18 +76,34 @@ __device__ __forceinline__ void put8(uint16_t* q, const float (&f)[8], int left)
         if (j < left) q[j] = (uint16_t)v[j];
 }
 
+// Keeps a vector's values as they are: without it the compiler converts them once before the
+// loop over the rows and holds twice the registers (170 against 110 in k_norm_grad).
+__device__ __forceinline__ void packed(s16x8& v) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    u32x4 b = __builtin_bit_cast(u32x4, v);
+    asm volatile("" : "+v"(b));
+    v = __builtin_bit_cast(s16x8, b);
+}
+
+template <int F>
+__device__ __forceinline__ s16x8 ones() {
+    const short o = F == FMT_BF16 ? 0x3F80 : 0x3C00;
+    return s16x8{o, o, o, o, o, o, o, o};
+}
+
 __device__ __forceinline__ float over_root(float sum, const NormArgs& a) {
     return __builtin_amdgcn_rsqf(fmaf(sum, 1.0f / (float)a.n, a.eps));
 }
 
 // A row lies in its threads' registers from its loads to its stores; the vectors stay there
 // from row to row.  Bound by its bytes: r, u (and a gate's) read, h and y written, once.
-template <int F, int L, int I, bool BLOCK>
+template <int F, int L, int I, bool BLOCK, bool TINY>
 __global__ void __launch_bounds__(Row<L>::THREADS) k_norm(NormArgs a) {
     typedef Row<L> R;
+    const bool ragged = a.n % 8 != 0;
     __shared__ float lds[6][16];
     const int l = threadIdx.x % L;
-    s16x8 w[I], post[I], gate[I];
+    s16x8 w[I], post[I] = {}, gate[I] = {};
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         const int c = (i * L + l) * 8;
@@ -79,20 +111,27 @@ __global__ void __launch_bounds__(Row<L>::THREADS) k_norm(NormArgs a) {
         if (BLOCK && a.post) post[i] = row8(a.post + c, a.n - c);
         if (BLOCK && a.gate && !a.gate_rows) gate[i] = row8(a.gate + c, a.n - c);
     }
-    for (int64_t r = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / L; r < a.m; r += (int64_t)gridDim.x * R::ROWS) {
+    for (int64_t r = (int64_t)blockIdx.x * R::ROWS + R::mine(); r < a.m; r += (int64_t)gridDim.x * R::ROWS) {
         float h[I][8];
+        s16x8 nr[I], nu[BLOCK ? I : 1], ng[BLOCK ? I : 1];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int c = (i * L + l) * 8;
-            floats<F>(row8(a.r + r * a.ldr + c, a.n - c), h[i]);
+            nr[i] = ask8<TINY>(a.r + r * a.ldr, c, a.n);
+            if constexpr (BLOCK) {
+                nu[i] = ask8<TINY>(a.u + r * a.ldu, c, a.n);
+                if (a.gate_rows) ng[i] = ask8<TINY>(a.gate + r * a.ldg, c, a.n);
+            }
         }
-        if (BLOCK) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) floats<F>(had8<TINY>(nr[i], a.n - (i * L + l) * 8, ragged), h[i]);
+        if constexpr (BLOCK) {
             float b[I][8], ss[1] = {0.f};
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int c = (i * L + l) * 8;
-                floats<F>(row8(a.u + r * a.ldu + c, a.n - c), b[i]);
-                if (a.gate_rows) gate[i] = row8(a.gate + r * a.ldg + c, a.n - c);
+                floats<F>(had8<TINY>(nu[i], a.n - c, ragged), b[i]);
+                if (a.gate_rows) gate[i] = had8<TINY>(ng[i], a.n - c, ragged);
             }
             if (a.post) {
 #pragma unroll
@@ -140,37 +179,73 @@ __global__ void __launch_bounds__(Row<L>::THREADS) k_norm(NormArgs a) {
 // The gradients, a row in registers as above: dh' = dh + s (g - hn mean(g hn)) with g = dy w,
 // hn = s h; then the block's share of it through gate and norm.  h is formed again from r and u,
 // which costs no more bytes than reading it and keeps it unrounded.  A thread adds up its
-// columns' shares of the vectors' gradients in fp32 over its rows; k_norm_join adds the threads'.
-template <int F, int L, int I, bool BLOCK>
-__global__ void __launch_bounds__(Row<L>::THREADS) k_norm_grad(NormArgs a) {
+// columns' shares of the vectors' gradients in fp32 over its rows, and k_norm_join the threads':
+// dy hn for dw, and one sum for both others, since of scale gate dh' un (dpost) and
+// scale dh' un post (a vector gate's) all but dh' un is the column's.
+template <int F, int L, int I, bool BLOCK, bool TINY>
+__global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
     typedef Row<L> R;
+    const bool ragged = a.n % 8 != 0;
+    constexpr bool AHEAD = I == 1;      // registers for the next row's loads beside this one's work
     __shared__ float lds[9][16];
     const int l = threadIdx.x % L;
     const float per = 1.0f / (float)a.n;
-    float sw[I][8] = {}, sp[BLOCK ? I : 1][8] = {}, sg[BLOCK ? I : 1][8] = {};
-    const uint32_t group = blockIdx.x * R::ROWS + threadIdx.x / L;
-    s16x8 w[I], post[I], gate[I];
+    float sw[I][8] = {}, sb[BLOCK ? I : 1][8] = {};
+    const uint32_t group = blockIdx.x * R::ROWS + R::mine();
+    s16x8 w[I], post[I] = {}, gate[I] = {};
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         const int c = (i * L + l) * 8;
         w[i] = row8(a.w + c, a.n - c);
-        if (BLOCK && a.post) post[i] = row8(a.post + c, a.n - c);
-        if (BLOCK && a.gate && !a.gate_rows) gate[i] = row8(a.gate + c, a.n - c);
+        // a norm or a gate that is not there is one of ones
+        if (BLOCK) post[i] = a.post ? row8(a.post + c, a.n - c) : ones<F>();
+        if (BLOCK && !a.gate_rows) gate[i] = a.gate ? row8(a.gate + c, a.n - c) : ones<F>();
     }
+    s16x8 nr[I], ndy[I], ndh[I], nu[BLOCK ? I : 1];      // the next row
+    auto ask = [&](int64_t r) {
+        // where a gradient is not given any row is loaded, and taken as zeros
+        const uint16_t *x = a.r + r * a.ldr, *y = a.dy ? a.dy + r * a.lddy : x, *z = a.dh ? a.dh + r * a.lddh : x;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int c = (i * L + l) * 8;
+            nr[i] = ask8<TINY>(x, c, a.n);
+            ndy[i] = ask8<TINY>(y, c, a.n);
+            ndh[i] = ask8<TINY>(z, c, a.n);
+            if constexpr (BLOCK) nu[i] = ask8<TINY>(a.u + r * a.ldu, c, a.n);
+        }
+    };
+    s16x8 u[I];
+    auto again = [&] {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            packed(w[i]);
+            packed(post[i]);
+            packed(gate[i]);
+            if (BLOCK) packed(u[i]);
+        }
+    };
+    if (AHEAD && group < a.m) ask(group);
     for (int64_t r = group; r < a.m; r += a.groups) {
-        s16x8 u[I];
+        if (!AHEAD) ask(r);
         float dy[I][8], d[I][8], h[I][8], su = 1.f;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int c = (i * L + l) * 8, left = a.n - c;
-            floats<F>(row8(a.r + r * a.ldr + c, left), h[i]);
-            floats<F>(a.dy ? row8(a.dy + r * a.lddy + c, left) : s16x8{}, dy[i]);
-            floats<F>(a.dh ? row8(a.dh + r * a.lddh + c, left) : s16x8{}, d[i]);
-            if (BLOCK) {
-                u[i] = row8(a.u + r * a.ldu + c, left);
-                if (a.gate_rows) gate[i] = row8(a.gate + r * a.ldg + c, left);
-            }
+            if constexpr (BLOCK)
+                if (a.gate_rows) gate[i] = had8<TINY>(ask8<TINY>(a.gate + r * a.ldg, c, a.n), left, ragged);
+            floats<F>(had8<TINY>(nr[i], left, ragged), h[i]);
+            floats<F>(had8<TINY>(ndy[i], a.dy ? left : 0, ragged), dy[i]);
+            floats<F>(had8<TINY>(ndh[i], a.dh ? left : 0, ragged), d[i]);
+            if (TINY && !a.dy)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dy[i][j] = 0.f;
+            if (TINY && !a.dh)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[i][j] = 0.f;
+            if constexpr (BLOCK) u[i] = had8<TINY>(nu[i], left, ragged);
         }
+        if (AHEAD && r + a.groups < a.m) ask(r + a.groups);
+        again();
         if (BLOCK) {
             if (a.post) {
                 float s[1] = {0.f};
@@ -183,13 +258,13 @@ __global__ void __launch_bounds__(Row<L>::THREADS) k_norm_grad(NormArgs a) {
                     }
                 R::sum(s, lds, 0);
                 su = over_root(s[0], a);
+                again();
             }
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float g = a.gate ? a.scale * to_f32<F>((uint16_t)gate[i][j]) : a.scale;
-                    const float p = a.post ? su * to_f32<F>((uint16_t)post[i][j]) : 1.f;
+                    const float g = a.scale * to_f32<F>((uint16_t)gate[i][j]), p = su * to_f32<F>((uint16_t)post[i][j]);
                     h[i][j] = fmaf(g, to_f32<F>((uint16_t)u[i][j]) * p, h[i][j]);
                 }
         }
@@ -202,6 +277,7 @@ __global__ void __launch_bounds__(Row<L>::THREADS) k_norm_grad(NormArgs a) {
                 s[1] = fmaf(dy[i][j] * to_f32<F>((uint16_t)w[i][j]), h[i][j], s[1]);
             }
         R::sum(s, lds, 1);
+        again();
         const float sh = over_root(s[0], a), mean = s[1] * sh * per;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
@@ -217,35 +293,34 @@ __global__ void __launch_bounds__(Row<L>::THREADS) k_norm_grad(NormArgs a) {
                 // h's registers take the gate's gradient from here on, d's the block's
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float un = to_f32<F>((uint16_t)u[i][j]) * su, q = a.scale * d[i][j];
-                    const float p = a.post ? to_f32<F>((uint16_t)post[i][j]) : 1.f;
-                    const float g = a.gate ? to_f32<F>((uint16_t)gate[i][j]) : 1.f;
-                    h[i][j] = q * un * p;
-                    sg[i][j] += h[i][j];
-                    sp[i][j] = fmaf(q * g, un, sp[i][j]);
-                    d[i][j] = q * g * p;
+                    const float un = to_f32<F>((uint16_t)u[i][j]) * su, p = a.scale * to_f32<F>((uint16_t)post[i][j]);
+                    const float g = to_f32<F>((uint16_t)gate[i][j]);
+                    h[i][j] = d[i][j] * un;
+                    sb[i][j] = fmaf(h[i][j], a.gate_rows ? g : 1.f, sb[i][j]);
+                    h[i][j] *= p;
+                    d[i][j] *= g * p;
                     s2[0] = fmaf(d[i][j], un, s2[0]);
                 }
                 if (a.dgate && a.gate_rows) put8<F>(a.dgate + r * a.n + c, h[i], a.n - c);
             }
         }
+        again();
         if (BLOCK && a.post) R::sum(s2, lds, 2);
         else if (R::WAVES > 1) __syncthreads();      // place 1 is free for the next row
         if (BLOCK && a.du) {
-            const float mean2 = s2[0] * per;
+            const float mean2 = a.post ? s2[0] * per : 0.f;
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int c = (i * L + l) * 8;
-                if (a.post)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) d[i][j] = su * fmaf(-to_f32<F>((uint16_t)u[i][j]) * su, mean2, d[i][j]);
+                for (int j = 0; j < 8; ++j) d[i][j] = su * fmaf(-to_f32<F>((uint16_t)u[i][j]) * su, mean2, d[i][j]);
                 put8<F>(a.du + r * a.lddu + c, d[i], a.n - c);
             }
         }
     }
     if (group >= a.groups) return;
     auto keep = [&](int k, const float (&v)[8], int c) {
-        float* q = a.part + ((int64_t)group * 3 + k) * a.n + c;
+        float* q = a.part + ((int64_t)group * 2 + k) * a.n + c;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (c + j < a.n) q[j] = v[j];
@@ -254,10 +329,8 @@ __global__ void __launch_bounds__(Row<L>::THREADS) k_norm_grad(NormArgs a) {
     for (int i = 0; i < I; ++i) {
         const int c = (i * L + l) * 8;
         if (a.dw) keep(0, sw[i], c);
-        if constexpr (BLOCK) {
-            if (a.dpost) keep(1, sp[i], c);
-            if (a.dgate && !a.gate_rows) keep(2, sg[i], c);
-        }
+        if constexpr (BLOCK)
+            if (a.dpost || (a.dgate && !a.gate_rows)) keep(1, sb[i], c);
     }
 }
 
@@ -266,26 +339,43 @@ template <int F>
 __global__ void __launch_bounds__(1024) k_norm_join(NormArgs a) {
     __shared__ float red[32][33];
     const int k = blockIdx.y;
-    uint16_t* out = k == 0 ? a.dw : k == 1 ? a.dpost : a.gate_rows ? nullptr : a.dgate;
-    if (!out) return;
+    uint16_t *gate = a.gate_rows ? nullptr : a.dgate, *post = a.dpost;
+    if (k == 0 ? !a.dw : !gate && !post) return;
     const int l = threadIdx.x & 31, q = threadIdx.x >> 5, c = blockIdx.x * 32 + l;
     float sum = 0.f;
     if (c < a.n)
 #pragma unroll 4
-        for (uint32_t i = q; i < a.groups; i += 32) sum += a.part[((int64_t)i * 3 + k) * a.n + c];
+        for (uint32_t i = q; i < a.groups; i += 32) sum += a.part[((int64_t)i * 2 + k) * a.n + c];
     red[q][l] = sum;
     __syncthreads();
     sum = red[l][q];
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor(sum, o, 32);
     const int mine = blockIdx.x * 32 + q;
-    if (l == 0 && mine < a.n) out[mine] = to_16<F>(sum);
+    if (l || mine >= a.n) return;
+    if (k == 0) {
+        a.dw[mine] = to_16<F>(sum);
+        return;
+    }
+    sum *= a.scale;
+    if (post) post[mine] = to_16<F>(a.gate && !a.gate_rows ? sum * to_f32<F>(a.gate[mine]) : sum);
+    if (gate) gate[mine] = to_16<F>(a.post ? sum * to_f32<F>(a.post[mine]) : sum);
 }
 
 // ----------------------------------------------------------------------------
 // launches
 
-// Threads and pieces of a row by its length.
+// Threads and pieces of a row by its length, forward and backward (whose sums over the rows
+// take three registers a column).
+template <class Go>
+static hipError_t by_length_back(int64_t n, Go go) {
+    if (n <= 512) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+    if (n <= 1024) return go(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
+    if (n <= 2048) return go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+    if (n <= 4096) return go(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{});
+    if (n <= 8192) return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+    return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+}
 template <class Go>
 static hipError_t by_length(int64_t n, Go go) {
     if (n <= 512) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
@@ -295,11 +385,10 @@ static hipError_t by_length(int64_t n, Go go) {
     if (n <= 8192) return go(std::integral_constant<int, 512>{}, std::integral_constant<int, 2>{});
     return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
 }
-static int row_threads(int64_t n) { return n <= 1024 ? 64 : n <= 4096 ? 256 : n <= 8192 ? 512 : 1024; }
 
+// Rows that a backward has in work: two workgroups a CU for the longest.
 uint32_t norm_groups(int64_t m, int64_t n) {
-    const int64_t side = row_threads(n) == 64 ? 4 : 1;
-    return (uint32_t)std::min<int64_t>(m, 512 * side);
+    return (uint32_t)std::min<int64_t>(m, n <= 512 ? 2048 : n <= 1024 ? 2048 : n <= 2048 ? 1024 : n <= 4096 ? 512 : 256);
 }
 
 template <int F>
@@ -307,8 +396,14 @@ static hipError_t norm_f(const NormArgs& a, hipStream_t s) {
     return by_length(a.n, [&](auto L, auto I) -> hipError_t {
         constexpr int l = decltype(L)::value, i = decltype(I)::value;
         const dim3 grid((uint32_t)std::min<int64_t>((a.m + Row<l>::ROWS - 1) / Row<l>::ROWS, 2048)), block(Row<l>::THREADS);
-        if (a.u) EDKM_GO((k_norm<F, l, i, true>), grid, block, a);
-        else EDKM_GO((k_norm<F, l, i, false>), grid, block, a);
+        if (l == 64 && i == 1 && a.n < 8) {
+            if (a.u) EDKM_GO((k_norm<F, 64, 1, true, true>), grid, block, a);
+            else EDKM_GO((k_norm<F, 64, 1, false, true>), grid, block, a);
+        } else if (a.u) {
+            EDKM_GO((k_norm<F, l, i, true, false>), grid, block, a);
+        } else {
+            EDKM_GO((k_norm<F, l, i, false, false>), grid, block, a);
+        }
         return hipSuccess;
     });
 }
@@ -316,16 +411,22 @@ static hipError_t norm_f(const NormArgs& a, hipStream_t s) {
 template <int F>
 static hipError_t grad_f(const NormArgs& a, hipStream_t s) {
     if (a.m > 0) {
-        const hipError_t e = by_length(a.n, [&](auto L, auto I) -> hipError_t {
+        const hipError_t e = by_length_back(a.n, [&](auto L, auto I) -> hipError_t {
             constexpr int l = decltype(L)::value, i = decltype(I)::value;
             const dim3 grid((a.groups + Row<l>::ROWS - 1) / Row<l>::ROWS), block(Row<l>::THREADS);
-            if (a.u) EDKM_GO((k_norm_grad<F, l, i, true>), grid, block, a);
-            else EDKM_GO((k_norm_grad<F, l, i, false>), grid, block, a);
+            if (l == 64 && i == 1 && a.n < 8) {
+                if (a.u) EDKM_GO((k_norm_grad<F, 64, 1, true, true>), grid, block, a);
+                else EDKM_GO((k_norm_grad<F, 64, 1, false, true>), grid, block, a);
+            } else if (a.u) {
+                EDKM_GO((k_norm_grad<F, l, i, true, false>), grid, block, a);
+            } else {
+                EDKM_GO((k_norm_grad<F, l, i, false, false>), grid, block, a);
+            }
             return hipSuccess;
         });
         if (e != hipSuccess) return e;
     }
-    if (a.dw || a.dpost || (a.dgate && !a.gate_rows)) EDKM_GO(k_norm_join<F>, dim3((a.n + 31) / 32, 3), dim3(1024), a);
+    if (a.dw || a.dpost || (a.dgate && !a.gate_rows)) EDKM_GO(k_norm_join<F>, dim3((a.n + 31) / 32, 2), dim3(1024), a);
     return hipSuccess;
 }
 

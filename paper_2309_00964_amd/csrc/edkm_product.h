@@ -201,6 +201,37 @@ __device__ __forceinline__ s16x8 row8(const uint16_t* q, int left) {
     return v;
 }
 
+// Eight columns of a row of `n` from column c on, in two steps, so that no branch stands
+// between one load and the next (the copies at its end would wait for the load): ask8 loads
+// the row's last eight where fewer are left, had8 moves them into place with zeros after them.
+// For rows of eight columns at least; a TINY one is read column by column.
+template <bool TINY = false>
+__device__ __forceinline__ s16x8 ask8(const uint16_t* row, int c, int n) {
+    if (TINY) return row8(row + c, n - c);
+    return reinterpret_cast<const S16x8*>(row + min(c, n - 8))->v;
+}
+// ragged: n is no multiple of eight (the same for all lanes)
+template <bool TINY = false>
+__device__ __forceinline__ s16x8 had8(s16x8 v, int left, bool ragged) {
+    if (TINY) return v;
+    if (!ragged) return left > 0 ? v : s16x8{};
+    typedef __attribute__((ext_vector_type(2))) uint64_t u64x2;
+    u64x2 q = __builtin_bit_cast(u64x2, v);
+    int s = 8 - left;
+    if (s >= 4) {
+        q[0] = q[1];
+        q[1] = 0;
+        s -= 4;
+    }
+    if (s >= 4) {
+        q[0] = 0;
+    } else if (s > 0) {
+        q[0] = (q[0] >> (16 * s)) | (q[1] << (64 - 16 * s));
+        q[1] >>= 16 * s;
+    }
+    return __builtin_bit_cast(s16x8, q);
+}
+
 // the first `n` of eight values, zeros after them
 __device__ __forceinline__ s16x8 keep_first(s16x8 v, int n) {
 #pragma unroll

@@ -364,7 +364,8 @@ __device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, 
 // BITS: b is a palette's.
 // E: what becomes of the sums where that is not the epilogue above: E::Args, a ProductArgs, are
 // the kernel's; E::begin sets what only the device knows, and says whether there is anything to
-// do; E::block takes a wave's 16 x 64 sums as the MFMA leaves them.
+// do; an E is made for a wave's rows before the sums are, so that what it reads is there by
+// then, and its block takes 16 x 64 sums as the MFMA leaves them.
 template <class E>
 struct ArgsOf {
     typedef typename E::Args type;
@@ -372,6 +373,17 @@ struct ArgsOf {
 template <>
 struct ArgsOf<void> {
     typedef ProductArgs type;
+};
+template <class E, int TR>
+struct EndOf {
+    typedef typename E::template End<TR> type;
+};
+template <int TR>
+struct EndOf<void, TR> {
+    typedef void type;
+};
+struct NoEnd {
+    __device__ __forceinline__ void init(const ProductArgs&, int, int) {}
 };
 template <int F, int OPA, int OPB, int BM, int BN, int WM, int WN, bool DIRECT, int BITS = 0, class E = void>
 __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(typename ArgsOf<E>::type p) {
@@ -405,6 +417,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(typename ArgsOf<E>::t
     } else {
         fb.init(p.b, p.ldb, c0, p.cols, p.depth, wave, lane);
     }
+    std::conditional_t<std::is_void_v<E>, NoEnd, typename EndOf<E, TR>::type> end;
+    end.init(p, lane, r0 + wr);
     typename FA::T ta;
     typename FB::T tb;
     ta.init(wr, lane);
@@ -459,7 +473,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(typename ArgsOf<E>::t
     char* mine = (wave < NW / 2 ? a0 : b0) + (wave % (NW / 2)) * 2 * EPI_BYTES;
     if constexpr (!std::is_void_v<E>) {
 #pragma unroll
-        for (int i = 0; i < TR; ++i) E::block(p, mine, lane, r0 + wr + i * 16, c0 + wc, acc[i], ((int64_t)group * NW + wave) * TR + i);
+        for (int i = 0; i < TR; ++i) end.block(p, i, mine, lane, r0 + wr + i * 16, c0 + wc, acc[i], ((int64_t)group * NW + wave) * TR + i);
         return;
     }
     Eight<F, OPB == OP_DEPTH> eight;
@@ -509,6 +523,8 @@ __global__ void __launch_bounds__(W * 64) k_join(typename ArgsOf<E>::type p, int
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] += *reinterpret_cast<const f32x4*>(at + s * stride + j * 256);
     if constexpr (!std::is_void_v<E>) {
+        typename EndOf<E, 1>::type end;
+        end.init(p, lane, r0);
         if (W > 1) {
             // the waves' shares, by the first wave
 #pragma unroll
@@ -523,7 +539,7 @@ __global__ void __launch_bounds__(W * 64) k_join(typename ArgsOf<E>::type p, int
             }
             epi_order();
         }
-        E::block(p, lds[0], lane, r0, c0, acc, ((int64_t)w * NW + wave) * TR + i);
+        end.block(p, 0, lds[0], lane, r0, c0, acc, ((int64_t)w * NW + wave) * TR + i);
         return;
     }
 #pragma unroll

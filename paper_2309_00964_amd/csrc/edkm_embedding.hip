@@ -18,9 +18,12 @@ __device__ __forceinline__ uint32_t row_of(const void* ids, int64_t i, uint32_t 
 }
 
 // stores the first `left` of eight values
+template <bool PAST = false>
 __device__ __forceinline__ void store8(uint16_t* q, s16x8 v, int left) {
     if (left >= 8) {
-        reinterpret_cast<S16x8*>(q)->v = v;
+        typedef short any8 __attribute__((ext_vector_type(8), aligned(2)));
+        if (PAST) __builtin_nontemporal_store(v, reinterpret_cast<any8*>(q));
+        else reinterpret_cast<S16x8*>(q)->v = v;
         return;
     }
 #pragma unroll
@@ -140,6 +143,13 @@ __global__ void __launch_bounds__(1024) k_rank(SortArgs a) {
     }
 }
 
+// A token's row, in the order that the pass before left.
+template <int IDX>
+__device__ __forceinline__ uint32_t key_of(const SortArgs& a, uint32_t i) {
+    return a.key_in ? a.key_in[i] : row_of<IDX>(a.ids, i, a.v);
+}
+constexpr int KEYS = 4;     // of a thread, loaded side by side
+
 // A pass over one digit of the rows, for more tokens: how many of each digit value a
 // workgroup's tokens have ...
 template <int IDX>
@@ -148,9 +158,13 @@ __global__ void __launch_bounds__(256) k_digits(SortArgs a) {
     for (uint32_t d = threadIdx.x; d < a.digits; d += 256) bins[d] = 0;
     __syncthreads();
     const uint32_t i0 = blockIdx.x * a.per, i1 = min(i0 + a.per, a.m);
-    for (uint32_t i = i0 + threadIdx.x; i < i1; i += 256) {
-        const uint32_t key = a.key_in ? a.key_in[i] : row_of<IDX>(a.ids, i, a.v);
-        atomicAdd(&bins[(key >> a.shift) & (a.digits - 1)], 1u);
+    for (uint32_t i = i0 + threadIdx.x; i < i1; i += 256 * KEYS) {
+        uint32_t key[KEYS];
+#pragma unroll
+        for (int k = 0; k < KEYS; ++k) key[k] = key_of<IDX>(a, min(i + k * 256, i1 - 1));
+#pragma unroll
+        for (int k = 0; k < KEYS; ++k)
+            if (i + k * 256 < i1) atomicAdd(&bins[(key[k] >> a.shift) & (a.digits - 1)], 1u);
     }
     __syncthreads();
     for (uint32_t d = threadIdx.x; d < a.digits; d += 256) a.counts[(uint64_t)blockIdx.x * a.digits + d] = bins[d];
@@ -175,69 +189,79 @@ __global__ void __launch_bounds__(256) k_place(SortArgs a) {
     const uint32_t share = a.per / 4, i0 = blockIdx.x * a.per + w * share, i1 = min(i0 + share, a.m);
     for (uint32_t d = tid; d < 4 * MOST; d += 256) (&next[0][0])[d] = 0;
     __syncthreads();
-    for (uint32_t i = i0 + lane; i < i1; i += 64) {
-        const uint32_t key = a.key_in ? a.key_in[i] : row_of<IDX>(a.ids, i, a.v);
-        atomicAdd(&next[w][(key >> a.shift) & (a.digits - 1)], 1u);
-    }
-    // thread t sums digits t D .. t D + D - 1: all workgroups', and those before this one
-    const uint32_t D = (a.digits + 255) / 256;
-    uint32_t before[MOST / 256] = {}, total[MOST / 256] = {};
-#pragma unroll 8
-    for (uint32_t g = 0; g < a.groups; ++g)
+    for (uint32_t i = i0 + lane; i < i1; i += 64 * KEYS) {
+        uint32_t key[KEYS];
 #pragma unroll
-        for (uint32_t k = 0; k < MOST / 256; ++k)
-            if (k < D && tid * D + k < a.digits) {
-                const uint32_t c = a.counts[(uint64_t)g * a.digits + tid * D + k];
-                total[k] += c;
-                before[k] += g < blockIdx.x ? c : 0;
+        for (int k = 0; k < KEYS; ++k) key[k] = key_of<IDX>(a, min(i + k * 64, i1 - 1));
+#pragma unroll
+        for (int k = 0; k < KEYS; ++k)
+            if (i + k * 64 < i1) atomicAdd(&next[w][(key[k] >> a.shift) & (a.digits - 1)], 1u);
+    }
+    // a thread sums every 256th digit: all workgroups', and those before this one
+    uint32_t below = 0;
+    for (uint32_t d0 = 0; d0 < a.digits; d0 += 256) {
+        const uint32_t d = d0 + tid, at = min(d, a.digits - 1);
+        uint32_t before = 0, total = 0;
+        for (uint32_t g = 0; g < a.groups; g += 16) {
+            uint32_t c[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) c[k] = a.counts[(uint64_t)min(g + k, a.groups - 1) * a.digits + at];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                total += g + k < a.groups ? c[k] : 0;
+                before += g + k < blockIdx.x ? c[k] : 0;
             }
-    uint32_t sum = 0;
+        }
+        if (d >= a.digits) total = 0;
+        uint32_t run = total;
 #pragma unroll
-    for (uint32_t k = 0; k < MOST / 256; ++k) sum += total[k];
-    uint32_t run = sum;
+        for (int o = 1; o < 64; o *= 2) {
+            const uint32_t up = __shfl_up(run, o);
+            if ((int)lane >= o) run += up;
+        }
+        if (lane == 63) scan[w] = run;
+        __syncthreads();       // also: the waves' counts are there
+        uint32_t start = below + run - total + before;
 #pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const uint32_t up = __shfl_up(run, o);
-        if ((int)lane >= o) run += up;
-    }
-    if (lane == 63) scan[w] = run;
-    __syncthreads();
-    uint32_t base = run - sum;
-    for (uint32_t q = 0; q < w; ++q) base += scan[q];
-#pragma unroll
-    for (uint32_t k = 0; k < MOST / 256; ++k)
-        if (k < D && tid * D + k < a.digits) {
-            uint32_t at = base + before[k];
+        for (uint32_t q = 0; q < 4; ++q) {
+            start += q < w ? scan[q] : 0;
+            below += scan[q];
+        }
+        if (d < a.digits)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t c = next[q][tid * D + k];
-                next[q][tid * D + k] = at;
-                at += c;
+                const uint32_t c = next[q][d];
+                next[q][d] = start;
+                start += c;
             }
-            base += total[k];
+        __syncthreads();
+    }
+    for (uint32_t i = i0; i < i1; i += 64 * KEYS) {
+        uint32_t key[KEYS], pos[KEYS];
+#pragma unroll
+        for (int k = 0; k < KEYS; ++k) {
+            const uint32_t at = min(i + k * 64 + lane, i1 - 1);
+            key[k] = key_of<IDX>(a, at);
+            pos[k] = a.pos_in ? a.pos_in[at] : at;
         }
-    __syncthreads();
-    for (uint32_t i = i0; i < i1; i += 64) {
-        const bool live = i + lane < i1;
-        uint32_t key = 0, pos = i + lane;
-        if (live) {
-            key = a.key_in ? a.key_in[pos] : row_of<IDX>(a.ids, pos, a.v);
-            if (a.pos_in) pos = a.pos_in[pos];
+#pragma unroll
+        for (int k = 0; k < KEYS; ++k) {
+            const bool live = i + k * 64 + lane < i1;
+            const uint32_t digit = (key[k] >> a.shift) & (a.digits - 1);
+            uint64_t same = __ballot(live);
+            for (uint32_t b = 1; b < a.digits; b *= 2) {
+                const uint64_t set = __ballot((digit & b) != 0);
+                same &= (digit & b) ? set : ~set;
+            }
+            if (live) {
+                const uint32_t at = next[w][digit] + __popcll(same & ((1ull << lane) - 1));
+                a.key[at] = key[k];
+                a.pos[at] = pos[k];
+            }
+            wave_order();
+            if (live && (same >> lane) == 1) next[w][digit] += __popcll(same);    // the digit's last lane
+            wave_order();
         }
-        const uint32_t digit = (key >> a.shift) & (a.digits - 1);
-        uint64_t same = __ballot(live);
-        for (uint32_t b = 1; b < a.digits; b *= 2) {
-            const uint64_t set = __ballot((digit & b) != 0);
-            same &= (digit & b) ? set : ~set;
-        }
-        if (live) {
-            const uint32_t at = next[w][digit] + __popcll(same & ((1ull << lane) - 1));
-            a.key[at] = key;
-            a.pos[at] = pos;
-        }
-        wave_order();
-        if (live && (same >> lane) == 1) next[w][digit] += __popcll(same);    // the digit's last lane
-        wave_order();
     }
 }
 
@@ -311,7 +335,9 @@ __device__ __forceinline__ uint32_t lower(const uint32_t* key, uint32_t m, uint3
 // tokens, row by row.  A row whose tokens lie in one chunk is written; what a chunk has of
 // others goes to part: place 0 for a row that began in an earlier chunk, place 1 for one
 // that begins here and goes on.  Long rows are thereby shared by many threads, and every sum
-// has one order.  Workgroups after those write zeros to the rows of no token.
+// has one order.  dy is read past the caches, as it is read once (65536 x 1024 tokens' 36 us, 48
+// through them).  Workgroups after those write zeros to the rows of no token, past the caches if the
+// table would fill them (8192 tokens of 32000 x 4096: 57 us, 65 through them).
 template <int F, bool TINY>
 __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
     const uint32_t group = a.first + blockIdx.x, pieces = (a.d + 7) / 8;
@@ -325,7 +351,10 @@ __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
         for (uint32_t r = threadIdx.x / T; r < rows; r += 256 / T) {
             if (at[r] != at[r + 1]) continue;
             uint16_t* q = a.dt + (int64_t)(t0 + r) * a.lddt;
-            for (uint64_t c = threadIdx.x % T * 8; c < a.d; c += T * 8) store8(q + c, s16x8{}, (int)min(a.d - (uint32_t)c, 8u));
+            for (uint64_t c = threadIdx.x % T * 8; c < a.d; c += T * 8) {
+                if (a.past) store8<true>(q + c, s16x8{}, (int)min(a.d - (uint32_t)c, 8u));
+                else store8(q + c, s16x8{}, (int)min(a.d - (uint32_t)c, 8u));
+            }
         }
         return;
     }
@@ -355,7 +384,7 @@ __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
             pos[u] = a.pos[at];
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = ask8<TINY>(a.dy + (int64_t)pos[u] * a.lddy, (int)c, (int)a.d);
+        for (int u = 0; u < U; ++u) v[u] = ask8<TINY, true>(a.dy + (int64_t)pos[u] * a.lddy, (int)c, (int)a.d);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (j + u >= j1) break;
@@ -379,28 +408,30 @@ __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
     else write_row<F>(a, row, c, sum);
 }
 
-// Adds the parts of the rows that go on past their first chunk.
+// Adds the parts of the rows that go on past their first chunk: four threads for eight
+// columns, each every fourth of the chunks, whose sums are then added in order.  (By sixteen,
+// 17 us for 65536 tokens x 1024 where most rows have two parts; by four, 9.)
 template <int F>
 __global__ void __launch_bounds__(256) k_embed_join(EmbedGradArgs a) {
-    const uint32_t pieces = (a.d + 7) / 8;
-    const uint64_t id = (uint64_t)(a.first + blockIdx.x) * 256 + threadIdx.x;
-    const uint32_t chunk = (uint32_t)(id / pieces), c = (uint32_t)(id - (uint64_t)chunk * pieces) * 8;
-    if (chunk + 1 >= a.chunks) return;
+    __shared__ f32x4 sums[2][4][64];
+    const uint32_t pieces = (a.d + 7) / 8, blocks = (pieces + 63) / 64, group = a.first + blockIdx.x;
+    const uint32_t chunk = group / blocks, piece = group % blocks * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
     const uint32_t j0 = chunk * a.per, row = a.key[j0 + a.per - 1];
     if (row >= a.v || a.key[j0 + a.per] != row || (chunk && a.key[j0 - 1] == row && a.key[j0] == row)) return;
     const uint64_t wide = (uint64_t)pieces * 8;
-    const float* q = a.part + (uint64_t)chunk * 2 * wide + c;
-    f32x4 lo = reinterpret_cast<const f32x4*>(q + wide)[0], hi = reinterpret_cast<const f32x4*>(q + wide)[1];
+    const uint32_t c = min(piece, pieces - 1) * 8;
+    f32x4 lo = {}, hi = {};
     constexpr int U = 8;
     bool on = true;
-    for (uint32_t k = chunk + 1; on && k < a.chunks; k += U) {
+    // part 1 of the first chunk, part 0 of those after it
+    for (uint32_t k = chunk + q; on && k < a.chunks; k += 4 * U) {
         f32x4 l[U], h[U];
         uint32_t key[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t e = min(k + u, a.chunks - 1);
-            const float* p = a.part + (uint64_t)e * 2 * wide + c;
-            key[u] = k + u < a.chunks ? a.key[e * a.per] : 0xFFFFFFFFu;
+            const uint32_t e = min(k + 4 * u, a.chunks - 1);
+            const float* p = a.part + ((uint64_t)e * 2 + (e == chunk)) * wide + c;
+            key[u] = k + 4 * u == chunk ? row : k + 4 * u < a.chunks ? a.key[e * a.per] : 0xFFFFFFFFu;
             l[u] = reinterpret_cast<const f32x4*>(p)[0];
             h[u] = reinterpret_cast<const f32x4*>(p)[1];
         }
@@ -413,6 +444,15 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradArgs a) {
             }
         }
     }
+    sums[0][q][threadIdx.x & 63] = lo;
+    sums[1][q][threadIdx.x & 63] = hi;
+    __syncthreads();
+    if (q || piece >= pieces) return;
+#pragma unroll
+    for (int p = 1; p < 4; ++p) {
+        lo += sums[0][p][threadIdx.x];
+        hi += sums[1][p][threadIdx.x];
+    }
     const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     write_row<F>(a, row, c, sum);
 }
@@ -422,9 +462,10 @@ static hipError_t grad_f(EmbedGradArgs a, hipStream_t s) {
     const uint64_t threads = (uint64_t)a.chunks * ((a.d + 7) / 8);
     const uint64_t sums = (threads + 255) / 256, zeros = a.accumulate ? 0 : ((uint64_t)a.v + ZERO_ROWS - 1) / ZERO_ROWS;
     a.chunk_groups = (uint32_t)sums;
+    a.past = (int64_t)a.v * a.d * 2 > INFINITY_CACHE / 2;
     if (a.d < 8) EDKM_GO_PARTS((k_embed_grad<F, true>), sums + zeros, 256, a);
     else EDKM_GO_PARTS((k_embed_grad<F, false>), sums + zeros, 256, a);
-    if (a.chunks > 1) EDKM_GO_PARTS(k_embed_join<F>, sums, 256, a);
+    if (a.chunks > 1) EDKM_GO_PARTS(k_embed_join<F>, (uint64_t)(a.chunks - 1) * (((a.d + 7) / 8 + 63) / 64), 256, a);
     return hipSuccess;
 }
 

@@ -64,6 +64,7 @@ struct AlignArgs {
     AlignJob job[3];
 };
 
+constexpr int64_t INFINITY_CACHE = 256 << 20;
 constexpr int64_t DIRECT_LD_MOST = 1 << 22;    // of operands that go to LDS directly: a tile's offsets fit 32 bits
 constexpr int SPLIT_TILE = 128;    // the only tile whose depths are ever split
 

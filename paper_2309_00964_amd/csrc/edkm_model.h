@@ -47,7 +47,7 @@ struct EmbedGradArgs {
     uint32_t m, v, d, per, chunks;
     uint32_t chunk_groups;  // workgroups that sum; those after them write the rows of no token
     float scale;
-    int accumulate;
+    int accumulate, past;
 };
 
 // Tokens that one launch ranks by comparing all with all (256 workgroups of 32, 67M

@@ -62,13 +62,15 @@ __device__ __forceinline__ void floats(s16x8 v, float (&f)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = to_f32<F>((uint16_t)v[j]);
 }
-template <int F>
+template <int F, bool PAST = false>
 __device__ __forceinline__ void put8(uint16_t* q, const float (&f)[8], int left) {
     s16x8 v;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (short)to_16<F>(f[j]);
     if (left >= 8) {
-        reinterpret_cast<S16x8*>(q)->v = v;
+        typedef short any8 __attribute__((ext_vector_type(8), aligned(2)));
+        if (PAST) __builtin_nontemporal_store(v, reinterpret_cast<any8*>(q));
+        else reinterpret_cast<S16x8*>(q)->v = v;
         return;
     }
 #pragma unroll
@@ -181,8 +183,9 @@ __global__ void __launch_bounds__(Row<L>::THREADS) k_norm(NormArgs a) {
 // which costs no more bytes than reading it and keeps it unrounded.  A thread adds up its
 // columns' shares of the vectors' gradients in fp32 over its rows, and k_norm_join the threads':
 // dy hn for dw, and one sum for both others, since of scale gate dh' un (dpost) and
-// scale dh' un post (a vector gate's) all but dh' un is the column's.
-template <int F, int L, int I, bool BLOCK, bool TINY>
+// scale dh' un post (a vector gate's) all but dh' un is the column's.  PAST: rows are read and
+// written past the caches, where they do not fit them.
+template <int F, int L, int I, bool BLOCK, bool TINY, bool PAST>
 __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
     typedef Row<L> R;
     const bool ragged = a.n % 8 != 0;
@@ -208,10 +211,10 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int c = (i * L + l) * 8;
-            nr[i] = ask8<TINY>(x, c, a.n);
-            ndy[i] = ask8<TINY>(y, c, a.n);
-            ndh[i] = ask8<TINY>(z, c, a.n);
-            if constexpr (BLOCK) nu[i] = ask8<TINY>(a.u + r * a.ldu, c, a.n);
+            nr[i] = ask8<TINY, PAST>(x, c, a.n);
+            ndy[i] = ask8<TINY, PAST>(y, c, a.n);
+            ndh[i] = ask8<TINY, PAST>(z, c, a.n);
+            if constexpr (BLOCK) nu[i] = ask8<TINY, PAST>(a.u + r * a.ldu, c, a.n);
         }
     };
     s16x8 u[I];
@@ -288,7 +291,7 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
                 d[i][j] = fmaf(sh, fmaf(-hn, mean, dy[i][j] * to_f32<F>((uint16_t)w[i][j])), d[i][j]);
                 sw[i][j] = fmaf(dy[i][j], hn, sw[i][j]);
             }
-            if (a.dr) put8<F>(a.dr + r * a.lddr + c, d[i], a.n - c);
+            if (a.dr) put8<F, PAST>(a.dr + r * a.lddr + c, d[i], a.n - c);
             if (BLOCK) {
                 // h's registers take the gate's gradient from here on, d's the block's
 #pragma unroll
@@ -314,7 +317,7 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
                 const int c = (i * L + l) * 8;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[i][j] = su * fmaf(-to_f32<F>((uint16_t)u[i][j]) * su, mean2, d[i][j]);
-                put8<F>(a.du + r * a.lddu + c, d[i], a.n - c);
+                put8<F, PAST>(a.du + r * a.lddu + c, d[i], a.n - c);
             }
         }
     }
@@ -415,12 +418,14 @@ static hipError_t grad_f(const NormArgs& a, hipStream_t s) {
             constexpr int l = decltype(L)::value, i = decltype(I)::value;
             const dim3 grid((a.groups + Row<l>::ROWS - 1) / Row<l>::ROWS), block(Row<l>::THREADS);
             if (l == 64 && i == 1 && a.n < 8) {
-                if (a.u) EDKM_GO((k_norm_grad<F, 64, 1, true, true>), grid, block, a);
-                else EDKM_GO((k_norm_grad<F, 64, 1, false, true>), grid, block, a);
-            } else if (a.u) {
-                EDKM_GO((k_norm_grad<F, l, i, true, false>), grid, block, a);
+                if (a.u) EDKM_GO((k_norm_grad<F, 64, 1, true, true, false>), grid, block, a);
+                else EDKM_GO((k_norm_grad<F, 64, 1, false, true, false>), grid, block, a);
+            } else if (12 * a.m * a.n > INFINITY_CACHE) {
+                if (a.u) EDKM_GO((k_norm_grad<F, l, i, true, false, true>), grid, block, a);
+                else EDKM_GO((k_norm_grad<F, l, i, false, false, true>), grid, block, a);
             } else {
-                EDKM_GO((k_norm_grad<F, l, i, false, false>), grid, block, a);
+                if (a.u) EDKM_GO((k_norm_grad<F, l, i, true, false, false>), grid, block, a);
+                else EDKM_GO((k_norm_grad<F, l, i, false, false, false>), grid, block, a);
             }
             return hipSuccess;
         });

@@ -205,10 +205,12 @@ __device__ __forceinline__ s16x8 row8(const uint16_t* q, int left) {
 // between one load and the next (the copies at its end would wait for the load): ask8 loads
 // the row's last eight where fewer are left, had8 moves them into place with zeros after them.
 // For rows of eight columns at least; a TINY one is read column by column.
-template <bool TINY = false>
+template <bool TINY = false, bool PAST = false>
 __device__ __forceinline__ s16x8 ask8(const uint16_t* row, int c, int n) {
+    typedef short any8 __attribute__((ext_vector_type(8), aligned(2)));
     if (TINY) return row8(row + c, n - c);
-    return reinterpret_cast<const S16x8*>(row + min(c, n - 8))->v;
+    return PAST ? __builtin_nontemporal_load(reinterpret_cast<const any8*>(row + min(c, n - 8)))
+                : reinterpret_cast<const S16x8*>(row + min(c, n - 8))->v;
 }
 // ragged: n is no multiple of eight (the same for all lanes)
 template <bool TINY = false>

@@ -151,7 +151,6 @@ ProductPlan product_plan(const ProductArgs& p, int opa, int opb) {
     return q;
 }
 
-constexpr int64_t INFINITY_CACHE = 256 << 20;
 template <int F>
 static hipError_t dz_f(DzArgs a, hipStream_t s) {
     const int chunks = (a.rows + a.per - 1) / a.per;

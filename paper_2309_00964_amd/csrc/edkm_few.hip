@@ -1,7 +1,7 @@
 // Products of few tokens with 16-bit or palettized weights, and the 16-bit weights of a
 // palette, for gfx950 (MI355X).
 
-#include "edkm_product.h"
+#include "edkm_loss.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -141,8 +141,9 @@ struct FewWeights {
 // others takes, with 3 bits and 4096 depths, for 4096 outputs 5.1 us (1 token), 7.4 (16), 18.1
 // (64); for 11008 outputs 8.1 (2.1 TB/s of indices), 10.3 and 22.9; 16-bit weights of 11008
 // outputs 18.6 us (4.8 TB/s).
-template <int F, int BITS, bool WHOLE, int MT, int NT, int U, int NW>
-__global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
+// E: what becomes of the sums where that is not the epilogue; its row16 takes sixteen of a row.
+template <int F, int BITS, bool WHOLE, int MT, int NT, int U, int NW, class E = void>
+__global__ void __launch_bounds__(NW * 64) k_few(typename ArgsOf<E>::type p) {
     constexpr int ENTRIES = 1 << (2 * BITS);
     constexpr int TABLE = BITS ? ENTRIES * PAIR_BANKS : 0, SUMS = NW * MT * NT * 256;
     // the table, and after the last lookup the waves' sums
@@ -275,6 +276,10 @@ __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
         float z = 0.f;
         for (int w = 0; w < nw; ++w) z += red[w * MT * NT * 256 + at];
         const int col = c0 + n;
+        if constexpr (!std::is_void_v<E>) {
+            E::row16(p, r, col, z);
+            continue;
+        }
         if (col >= p.cols) continue;
         if (p.bias) z += to_f32<F>(p.bias[col]);
         if (p.z) p.z[(int64_t)r * p.cols + col] = keep_z<F>(z);
@@ -284,13 +289,13 @@ __global__ void __launch_bounds__(NW * 64) k_few(ProductArgs p) {
     }
 }
 
-template <int F, int BITS, bool WHOLE, int MT, int NT>
-static hipError_t few_go(ProductArgs p, hipStream_t s) {
+template <int F, int BITS, bool WHOLE, int MT, int NT, class E = void>
+static hipError_t few_go(typename ArgsOf<E>::type p, hipStream_t s) {
     constexpr int U = WHOLE && BITS && MT == 1 && NT < 3 ? 2 : 1, NW = MT == 1 ? 16 : 8;
     const int runs = (p.depth + 127) / 128;
     int nw = 1;
     while (nw < runs && nw < NW) nw *= 2;
-    EDKM_GO_PARTS((k_few<F, BITS, WHOLE, MT, NT, U, NW>), ((uint64_t)p.cols + 16 * NT - 1) / (16 * NT), nw * 64, p);
+    EDKM_GO_PARTS((k_few<F, BITS, WHOLE, MT, NT, U, NW, E>), ((uint64_t)p.cols + 16 * NT - 1) / (16 * NT), nw * 64, p);
     return hipSuccess;
 }
 
@@ -319,11 +324,15 @@ static hipError_t few_bits(const ProductArgs& p, hipStream_t s) {
     return p.rows <= 32 ? few_rows<F, BITS, WHOLE, 2>(p, s) : few_rows<F, BITS, WHOLE, 4>(p, s);
 }
 
-template <int F>
-static hipError_t few(const ProductArgs& p, int bits, hipStream_t s) {
+static bool few_whole(const ProductArgs& p, int bits) {
     // 32-bit offsets: 64 rows of at most 2^25 bytes
     const bool x16 = ((uintptr_t)p.a & 15) == 0 && p.lda % 8 == 0 && p.depth % 32 == 0 && p.lda < (1 << 24) && p.ldb < (1 << 24);
-    const bool whole = x16 && (bits ? ((uintptr_t)p.idx & 3) == 0 : ((uintptr_t)p.b & 15) == 0 && p.ldb % 8 == 0);
+    return x16 && (bits ? ((uintptr_t)p.idx & 3) == 0 : ((uintptr_t)p.b & 15) == 0 && p.ldb % 8 == 0);
+}
+
+template <int F>
+static hipError_t few(const ProductArgs& p, int bits, hipStream_t s) {
+    const bool whole = few_whole(p, bits);
     switch (bits) {
     case 1: return whole ? few_bits<F, 1, true>(p, s) : few_bits<F, 1, false>(p, s);
     case 2: return whole ? few_bits<F, 2, true>(p, s) : few_bits<F, 2, false>(p, s);
@@ -335,6 +344,12 @@ static hipError_t few(const ProductArgs& p, int bits, hipStream_t s) {
 
 hipError_t launch_few(const ProductArgs& p, int fmt, int bits, hipStream_t s) {
     return fmt == FMT_BF16 ? few<FMT_BF16>(p, bits, s) : few<FMT_FP16>(p, bits, s);
+}
+
+hipError_t launch_few_loss(const LossArgs& p, int fmt, hipStream_t s) {
+    const bool whole = few_whole(p, 0);
+    if (fmt == FMT_BF16) return whole ? few_go<FMT_BF16, 0, true, 1, 1, LossStats>(p, s) : few_go<FMT_BF16, 0, false, 1, 1, LossStats>(p, s);
+    return whole ? few_go<FMT_FP16, 0, true, 1, 1, LossStats>(p, s) : few_go<FMT_FP16, 0, false, 1, 1, LossStats>(p, s);
 }
 
 template <int F, bool PAST>

@@ -5,11 +5,25 @@
 
 namespace edkm {
 
+template <int IDX>
+__device__ __forceinline__ int word_of(const void* targets, int64_t i, int64_t n) {
+    if (IDX == IDX_64) {
+        const uint64_t t = static_cast<const uint64_t*>(targets)[i];
+        return t < (uint64_t)n ? (int)t : -1;
+    }
+    const uint32_t t = static_cast<const uint32_t*>(targets)[i];
+    return t < (uint64_t)n ? (int)t : -1;
+}
+__device__ __forceinline__ int word_of(const void* targets, int index_type, int64_t i, int64_t n) {
+    return index_type == IDX_64 ? word_of<IDX_64>(targets, i, n) : word_of<IDX_32>(targets, i, n);
+}
+
 // What only the device knows: how many tokens have a target.  They are the rows of z and of
 // dx, and the depths of dw.
 struct LossBegin {
     typedef LossArgs Args;
     __device__ __forceinline__ static bool begin(LossArgs& p) {
+        if (p.dynamic == 0) return true;
         const int count = *p.rows_of.count;
         if (p.dynamic == 2) {
             p.depth = count;
@@ -25,33 +39,73 @@ struct LossBegin {
         }
         p.rows = min(p.rows, count - p.base);
         p.a += (int64_t)p.base * p.lda;
-        return p.rows > 0;
+        if (p.rows <= 0) return false;
+        if (p.groups) {
+            // as many parts of the depths as the launch has workgroups for, now that the tiles are known
+            const int tiles = ((p.rows + p.tile - 1) / p.tile) * ((p.cols + p.tile - 1) / p.tile), steps = (p.depth + 63) / 64;
+            const int parts = max(1, min(p.groups / tiles, steps / PART_STEPS));
+            p.split_steps = (steps + parts - 1) / parts;
+            p.splits = (steps + p.split_steps - 1) / p.split_steps;
+            if (p.splits == 1) p.part = nullptr;
+        }
+        return true;
     }
 };
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+// e^(z - from), `by` being from's product with log2 e
+__device__ __forceinline__ float exp_from(float z, float by) { return __builtin_amdgcn_exp2f(fmaf(z, 1.4426950408889634f, -by)); }
+
+// The lanes r, r + 16, r + 32 and r + 48 together, by exchanges of rows of sixteen lanes.
+template <class Op>
+__device__ __forceinline__ float four_rows(float v, Op op) {
+    const uint32_t a = __float_as_uint(v);
+    const auto s = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    const uint32_t b = __float_as_uint(op(__uint_as_float(s[0]), __uint_as_float(s[1])));
+    const auto t = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return op(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
 
 // The largest of a row's 64 logits and the sum of e^(z - largest), and the target's logit.
 // A row's logits lie in the four lanes r, r + 16, r + 32 and r + 48.
 struct LossStats : LossBegin {
+  // sixteen logits of a row in as many lanes
+  __device__ __forceinline__ static void row16(const LossArgs& p, int row, int col, float z) {
+    const float none = -__builtin_inff();
+    if (col == word_of(p.targets, p.index_type, row, p.cols)) p.rows_of.value[row] = z;
+    if (col >= p.cols) z = none;
+    float top = z;
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+    float sum = exp_of(z - (top == none ? 0.f : top));
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) sum += __shfl_xor(sum, o);
+    if (col % 16 == 0) p.stats[(int64_t)(col / 16) * p.stat_rows + row] = make_float2(top, sum);
+  }
   template <int TR>
   struct End {
     int word[TR];
     __device__ __forceinline__ void init(const LossArgs& p, int lane, int r) {
 #pragma unroll
-        for (int i = 0; i < TR; ++i) word[i] = p.rows_of.word[p.base + min(r + i * 16 + (lane & 15), p.rows - 1)];
+        for (int i = 0; i < TR; ++i) {
+            const int row = p.base + min(r + i * 16 + (lane & 15), p.rows - 1);
+            word[i] = p.targets ? word_of(p.targets, p.index_type, row, p.cols) : p.rows_of.word[row];
+        }
     }
     __device__ __forceinline__ void block(const LossArgs& p, int i, char*, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
         if (r0 >= p.rows || c0 >= p.cols) return;
         const int row = r0 + (lane & 15), c = c0 + (lane >> 4) * 4;
         const float none = -__builtin_inff();
-        if (row < p.rows) {
-            const int t = word[i] - c;
+        // few blocks have a row's target
+        const uint32_t t = (uint32_t)(word[i] - c);
+        if (__ballot(t < 52)) {
+            float z = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (t == j * 16 + e) p.rows_of.value[p.base + row] = acc[j][e];
+                    if (t == j * 16u + e) z = acc[j][e];
+            if (t < 52 && (t & 15) < 4 && row < p.rows) p.rows_of.value[p.base + row] = z;
         }
         if (c0 + 64 > p.cols)
 #pragma unroll
@@ -64,16 +118,14 @@ struct LossStats : LossBegin {
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[j][e]);
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float from = top == none ? 0.f : top;      // all -Inf: the sum is 0, or NaN if one is
+        top = four_rows(top, [](float a, float b) { return fmaxf(a, b); });
+        const float by = (top == none ? 0.f : top) * 1.4426950408889634f;      // all -Inf: the sum is 0, or NaN if one is
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += exp_of(acc[j][e] - from);
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
+            for (int e = 0; e < 4; ++e) sum += exp_from(acc[j][e], by);
+        sum = four_rows(sum, [](float a, float b) { return a + b; });
         if (lane < 16 && row < p.rows) p.stats[(int64_t)(c0 / 64) * p.stat_rows + row] = make_float2(top, sum);
     }
   };
@@ -131,11 +183,17 @@ struct LossDz : LossBegin {
     __device__ __forceinline__ void block(const LossArgs& p, int i, char* lds, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
         const int wide = (p.cols + 7) & ~7;
         if (r0 >= p.rows || c0 >= wide) return;
-        const int t = word[i] - p.col0 - c0 - (lane >> 4) * 4;
+        const uint32_t t = (uint32_t)(word[i] - p.col0 - c0 - (lane >> 4) * 4);
+        const bool any = __ballot(t < 52) != 0;      // few blocks have a row's target
+        const float by = lse[i] * 1.4426950408889634f;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[j][e] = factor[i] * (exp_of(acc[j][e] - lse[i]) - (t == j * 16 + e ? 1.f : 0.f));
+            for (int e = 0; e < 4; ++e) {
+                float share = exp_from(acc[j][e], by);
+                if (any) share -= t == j * 16u + e ? 1.f : 0.f;
+                acc[j][e] = factor[i] * share;
+            }
         store_block<F>(p, lds, lane, r0, c0, acc, wide, [&](int q) { return p.out + (int64_t)(r0 + (lane >> 3) + q * 8) * p.ldo; });
     }
   };
@@ -178,8 +236,23 @@ struct LossSum : LossBegin {
   };
 };
 
+// A launch that finds its splits by itself, and the join of as many rows of blocks as there can be.
+template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, class E>
+static hipError_t split_tiled(LossArgs p, hipStream_t s) {
+    EDKM_GO((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, 0, E>), dim3(p.groups), dim3(WM * WN * 64), p);
+    const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
+    const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
+    if (p.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, true, 4, E>), blocks, dim3(256), p, 0);
+    else EDKM_GO((k_join<F, B, B, WM, WN, true, 1, E>), blocks, dim3(64), p, 0);
+    return hipSuccess;
+}
+
 template <int F, int OPA, int OPB, class E>
 static hipError_t loss_tiled(const LossArgs& p, const ProductPlan& q, hipStream_t s) {
+    if (p.groups) {
+        if (q.tile == 256) return split_tiled<F, OPA, OPB, 256, 2, 4, true, E>(p, s);
+        return q.direct ? split_tiled<F, OPA, OPB, 128, 2, 2, true, E>(p, s) : split_tiled<F, OPA, OPB, 128, 2, 2, false, E>(p, s);
+    }
     if (q.tile == 256) return tiled<F, OPA, OPB, 256, 2, 4, true, 0, E>(p, q, s);
     return q.direct ? tiled<F, OPA, OPB, 128, 2, 2, true, 0, E>(p, q, s) : tiled<F, OPA, OPB, 128, 2, 2, false, 0, E>(p, q, s);
 }

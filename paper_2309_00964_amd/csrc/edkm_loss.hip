@@ -9,16 +9,6 @@ namespace edkm {
 // ----------------------------------------------------------------------------
 // tokens with a target
 
-template <int IDX>
-__device__ __forceinline__ int word_of(const void* targets, int64_t i, int64_t n) {
-    if (IDX == IDX_64) {
-        const uint64_t t = static_cast<const uint64_t*>(targets)[i];
-        return t < (uint64_t)n ? (int)t : -1;
-    }
-    const uint32_t t = static_cast<const uint32_t*>(targets)[i];
-    return t < (uint64_t)n ? (int)t : -1;
-}
-
 // One workgroup lists the tokens with a target in order, for a backward those whose loss has a
 // gradient; a backward's factors follow, once their largest is known.  What the products
 // read has no row of any other token, so whatever those hold (NaN, Inf) reaches no gradient.
@@ -129,12 +119,13 @@ hipError_t launch_gather(GatherArgs a, hipStream_t s) {
 // ----------------------------------------------------------------------------
 // statistics of the blocks of 64 words to losses
 
-// Sixteen rows per workgroup, 64 threads to a row.
+// R rows per workgroup: sixteen, or one where there are few tokens.
+template <int R>
 __global__ void __launch_bounds__(1024) k_loss_end(LossEndArgs a) {
-    __shared__ float2 part[16][17];
-    const int rows = min(a.rows, *a.r.count - a.base);
-    const int row = blockIdx.x * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if ((int)blockIdx.x * 16 >= rows) return;
+    __shared__ float2 part[16][R];
+    const int rows = a.targets ? a.rows : min(a.rows, *a.r.count - a.base);
+    const int row = blockIdx.x * R + threadIdx.x % R, q = threadIdx.x / R, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if ((int)blockIdx.x * R >= rows) return;
     const float none = -__builtin_inff();
     float top = none, sum = 0.f;
     auto add = [&](float t, float s) {
@@ -142,41 +133,61 @@ __global__ void __launch_bounds__(1024) k_loss_end(LossEndArgs a) {
         sum = sum * exp_of(top - from) + s * exp_of(t - from);
         top = m;
     };
-    if (row < rows)
-        for (int b = q; b < a.blocks; b += 64) {
-            const float2 v = a.stats[(int64_t)b * a.stat_rows + row];
-            add(v.x, v.y);
-        }
+    constexpr int U = 8, STEP = 1024 / R;
+    const int at = min(row, rows - 1);
+    for (int b = q; b < a.blocks; b += STEP * U) {
+        float2 v[U];
 #pragma unroll
-    for (int o = 16; o < 64; o *= 2) {
+        for (int u = 0; u < U; ++u) v[u] = a.stats[(int64_t)min(b + u * STEP, a.blocks - 1) * a.stat_rows + at];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (b + u * STEP < a.blocks) add(v[u].x, v[u].y);
+    }
+#pragma unroll
+    for (int o = R; o < 64; o *= 2) {
         const float t = __shfl_xor(top, o), s = __shfl_xor(sum, o);
         add(t, s);
     }
-    if (lane < 16) part[w][lane] = make_float2(top, sum);
+    if (lane < R) part[w][lane] = make_float2(top, sum);
     __syncthreads();
-    if (threadIdx.x >= 16 || row >= rows) return;
+    if (threadIdx.x >= R || row >= rows) return;
     top = none;
     sum = 0.f;
 #pragma unroll
     for (int p = 0; p < 16; ++p) add(part[p][lane].x, part[p][lane].y);
-    const float l = logf(sum), loss = (top - a.r.value[a.base + row]) + l;
-    const int i = a.r.row[a.base + row];
+    const bool there = !a.targets || word_of(a.targets, a.index_type, a.base + row, a.words) >= 0;
+    const float l = logf(sum), loss = there ? (top - a.r.value[a.base + row]) + l : 0.f;
+    const int i = a.targets ? a.base + row : a.r.row[a.base + row];
     if (a.reduction == RED_NONE) a.loss[i] = loss;
     else a.r.value[a.base + row] = loss;
-    if (a.lse) a.lse[i] = top + l;
+    if (a.lse) a.lse[i] = there ? top + l : 0.f;
 }
 
 hipError_t launch_loss_end(const LossEndArgs& a, hipStream_t s) {
-    EDKM_GO(k_loss_end, dim3((a.rows + 15) / 16), dim3(1024), a);
+    if (a.rows <= 64) EDKM_GO(k_loss_end<1>, dim3(a.rows), dim3(1024), a);
+    else EDKM_GO(k_loss_end<16>, dim3((a.rows + 15) / 16), dim3(1024), a);
     return hipSuccess;
 }
 
 __global__ void __launch_bounds__(1024) k_loss_reduce(LossEndArgs a) {
     __shared__ float waves[16];
-    const int count = *a.r.count;
+    int count;
+    if (a.targets) {
+        // no list: every token's loss is there, 0 for one without a target
+        __shared__ int counts[16];
+        const bool there = (int)threadIdx.x < a.rows && word_of(a.targets, a.index_type, threadIdx.x, a.words) >= 0;
+        const int mine = __popcll(__ballot(there));
+        if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = mine;
+        __syncthreads();
+        count = 0;
+        for (int q = 0; q < 16; ++q) count += counts[q];
+    } else {
+        count = *a.r.count;
+    }
+    const int there = a.targets ? a.rows : count;
     // many tokens: a thread's long sum keeps what its additions round off
     float sum = 0.f, lost = 0.f;
-    for (int i = threadIdx.x; i < count; i += 1024) {
+    for (int i = threadIdx.x; i < there; i += 1024) {
         const float v = a.r.value[i], t = sum + v, z = t - sum;
         lost += (sum - (t - z)) + (v - z);
         sum = t;

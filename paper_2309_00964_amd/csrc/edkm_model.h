@@ -3,6 +3,8 @@
 #pragma once
 #include "edkm_layer.h"
 
+#include <algorithm>
+
 namespace edkm {
 
 enum IndexType : int { IDX_32 = 0, IDX_64 = 1 };
@@ -153,11 +155,14 @@ struct GatherArgs {
 
 struct LossArgs : ProductArgs {
     int splits;
+    int groups, tile;       // workgroups of a launch that finds its splits by itself, and its tile; or 0
     LossRows rows_of;
     const uint16_t* all;    // x itself, where it can be used; else null
     int64_t ld_all;
     int32_t m, base;        // tokens in all; the first row of this launch
-    int dynamic;            // what the count of tokens is here: 1 the rows, 2 the depths
+    int dynamic;            // what the count of tokens is here: 1 the rows, 2 the depths, 0 nothing (no list)
+    const void* targets;    // without a list
+    int index_type;
     // statistics: per 64 words and row the largest logit and the sum of exponentials
     float2* stats;
     int32_t stat_rows;
@@ -173,6 +178,9 @@ struct LossEndArgs {
     const float2* stats;
     int32_t stat_rows, blocks, base, rows;
     int reduction;
+    const void* targets;    // without a list of tokens
+    int index_type;
+    int64_t words;
     float *loss, *lse;
 };
 
@@ -182,8 +190,40 @@ hipError_t launch_gather(GatherArgs a, hipStream_t s);
 hipError_t launch_loss_stats(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s);
 hipError_t launch_loss_dz(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s);
 hipError_t launch_loss_sum(const LossArgs& a, int fmt, int opa, const ProductPlan& q, hipStream_t s);
+hipError_t launch_few_loss(const LossArgs& a, int fmt, hipStream_t s);
 hipError_t launch_loss_end(const LossEndArgs& a, hipStream_t s);
 hipError_t launch_loss_reduce(const LossEndArgs& a, hipStream_t s);
+
+// dx sums over thousands of words for tokens whose number only the device knows.  Where they
+// make fewer tiles than the launch has workgroups (one of 256 on a CU, two of 128), the depths are
+// split among them.  A tile of 256 takes 1.5 times a step's time of two of 128 on a CU, a part its
+// way to memory and back: 1536 of 2048 tokens x 2048 over 65536 words 516 us by tiles of 128 in two
+// parts, 382 by tiles of 256 in five.  A part has eight steps at least
+// (1001 x 777 over 1003 words: two parts 15 us, eight 18).
+struct SumPlan {
+    ProductPlan q;
+    int groups;             // 0: not split
+};
+constexpr int PART_STEPS = 8;
+constexpr int64_t SUM_PART_BYTES = (int64_t)256 * 256 * 256 * 4;
+inline SumPlan sum_plan(int64_t rows, int64_t cols, int64_t depth, bool direct) {
+    const int64_t steps = (depth + 63) / 64;
+    auto cost = [&](int64_t tile, int64_t most, double step) {
+        const int64_t t = ((rows + tile - 1) / tile) * ((cols + tile - 1) / tile);
+        const int64_t parts = t < most ? std::max<int64_t>(1, std::min(most / t, steps / PART_STEPS)) : 1;
+        const double rounds = parts > 1 ? 1 : (double)((t + most - 1) / most);
+        return rounds * step * (double)((steps + parts - 1) / parts) + (parts > 1 ? 4 + (double)(t * parts * tile * tile) * 8 / 5e6 : 0);
+    };
+    SumPlan p{};
+    p.q.direct = direct;
+    p.q.tile = direct && cost(256, 256, 1.5) < cost(128, 512, 1.0) ? 256 : 128;
+    const int64_t most = p.q.tile == 256 ? 256 : 512, t = ((rows + p.q.tile - 1) / p.q.tile) * ((cols + p.q.tile - 1) / p.q.tile);
+    const int64_t parts = t < most ? std::max<int64_t>(1, std::min(most / t, steps / PART_STEPS)) : 1;
+    p.q.split_steps = (int)((steps + parts - 1) / parts);
+    p.q.splits = (int)((steps + p.q.split_steps - 1) / p.q.split_steps);
+    p.groups = t < most && steps >= 2 * PART_STEPS ? (int)most : 0;
+    return p;
+}
 
 // Words of a piece of the vocabulary whose dz is held at a time: as many as keep it within the
 // Infinity Cache, which the two products that read it then hit; 2048 at least.
@@ -195,6 +235,12 @@ inline int64_t loss_piece(int64_t m, int64_t n) {
     const int64_t pieces = (n + p - 1) / p;
     return (((n + pieces - 1) / pieces) + 255) / 256 * 256;
 }
+// Tokens up to which a forward makes no list of those with a target: it would be two launches
+// (9 us; 512 x 32000 x 4096 takes 131 us without, 140 with), and leaving out a quarter of the tokens
+// pays from about as many on.  And up to which each workgroup takes sixteen words for all tokens,
+// which is bound by the words' bytes (32000 x 4096: 1 token 52 us, 5.0 TB/s, 16 tokens 72; by the
+// tiles 83 and 84).
+constexpr int64_t LIST_LEAST = 1024, LOSS_FEW = 16;
 // Tokens of a forward's launch: as many as keep the statistics within 256 MiB, 256 at least.
 inline int64_t loss_rows(int64_t m, int64_t n) {
     const int64_t blocks = (n + 63) / 64, r = (256 << 20) / (blocks * 8) / 256 * 256;

@@ -81,7 +81,7 @@ LossWs loss_ws(int64_t m, int64_t n, int64_t k) {
     L.w = L.rows.total;
     L.stats = L.w + aligned_bytes(n, k);
     const int64_t rows = loss_rows(m, n);
-    L.split = L.stats + up256((size_t)((n + 63) / 64) * rows * 8);
+    L.split = L.stats + up256((size_t)(m <= LOSS_FEW ? (n + 15) / 16 : (n + 63) / 64) * rows * 8);
     size_t parts = 0;
     if (m > 0) {
         parts = product_part_bytes(rows, n, k);
@@ -109,7 +109,9 @@ LossBackWs loss_back_ws(int64_t m, int64_t n, int64_t k) {
     size_t parts = product_part_bytes(L.piece, k, m);
     if (last) parts = std::max(parts, product_part_bytes(last, k, m));
     if (m > 0) {
-        parts = std::max({parts, product_part_bytes(m, L.piece, k), product_part_bytes(m, k, L.piece)});
+        parts = std::max(parts, product_part_bytes(m, L.piece, k));
+        const SumPlan x = sum_plan(m, k, L.piece, true), y = sum_plan(m, k, L.piece, false);
+        if (x.groups || y.groups) parts = std::max(parts, (size_t)SUM_PART_BYTES);
         if (last) parts = std::max(parts, product_part_bytes(m, last, k));
     }
     L.total = L.split + up256(parts);
@@ -335,45 +337,65 @@ edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int forma
     pick.lse = lse;
     uint16_t* xs = reinterpret_cast<uint16_t*>(base + L.rows.x);
     AlignArgs copies{};
-    if (m > 0) align_rows(copies, pw, ldw, n, k, base + L.w);
-    if (begin_loss(pick, index_type, px, ldx, k, xs, nullptr, 0, copies, stream) != hipSuccess) return EDKM_ERR_HIP;
+    const bool list = m > LIST_LEAST || m == 0, few = m > 0 && m <= LOSS_FEW;
+    if (m > 0 && !few) align_rows(copies, pw, ldw, n, k, base + L.w);
+    if (list) {
+        if (begin_loss(pick, index_type, px, ldx, k, xs, nullptr, 0, copies, stream) != hipSuccess) return EDKM_ERR_HIP;
+    } else {
+        if (!few && !whole(px, ldx, k)) copy_rows(copies, px, ldx, m, k, reinterpret_cast<char*>(xs));
+        if (launch_align_rows(copies, stream) != hipSuccess) return EDKM_ERR_HIP;
+    }
     const int64_t most = loss_rows(m, n);
     LossEndArgs end{};
     end.r = pick.r;
     end.stats = reinterpret_cast<float2*>(base + L.stats);
-    end.blocks = (int32_t)((n + 63) / 64);
+    end.blocks = (int32_t)(few ? (n + 15) / 16 : (n + 63) / 64);
     end.reduction = reduction;
     end.loss = loss;
     end.lse = lse;
+    end.targets = list ? nullptr : targets;
+    end.index_type = index_type;
+    end.words = n;
     for (int64_t at = 0; at < m; at += most) {
         const int64_t rows = std::min(most, m - at);
         LossArgs p{};
-        p.a = xs;
-        p.lda = up8(k);
+        p.a = list ? xs : px;
+        p.lda = list ? up8(k) : ldx;
         p.b = pw;
         p.ldb = ldw;
         p.rows = (int32_t)rows;
         p.cols = (int32_t)n;
         p.depth = (int32_t)k;
         p.padded = 1;
-        const ProductPlan q = product_plan(p, OP_ROWS, OP_ROWS);
-        p.split_steps = q.split_steps;
-        p.splits = q.splits;
-        p.part = q.splits > 1 ? reinterpret_cast<float*>(base + L.split) : nullptr;
         p.rows_of = pick.r;
-        p.all = whole(x, ldx, k) ? px : nullptr;
-        p.ld_all = ldx;
         p.m = (int32_t)m;
-        p.base = (int32_t)at;
-        p.dynamic = 1;
+        p.targets = end.targets;
+        p.index_type = index_type;
         p.stats = reinterpret_cast<float2*>(base + L.stats);
         p.stat_rows = (int32_t)rows;
-        if (launch_loss_stats(p, format, q, stream) != hipSuccess) return EDKM_ERR_HIP;
+        if (few) {
+            if (launch_few_loss(p, format, stream) != hipSuccess) return EDKM_ERR_HIP;
+        } else {
+            const ProductPlan q = product_plan(p, OP_ROWS, OP_ROWS);
+            p.split_steps = q.split_steps;
+            p.splits = q.splits;
+            p.part = q.splits > 1 ? reinterpret_cast<float*>(base + L.split) : nullptr;
+            if (list) {
+                p.all = whole(x, ldx, k) ? px : nullptr;
+                p.ld_all = ldx;
+                p.dynamic = 1;
+            } else {
+                p.a += at * p.lda;
+            }
+            p.base = (int32_t)at;
+            if (launch_loss_stats(p, format, q, stream) != hipSuccess) return EDKM_ERR_HIP;
+        }
         end.stat_rows = (int32_t)rows;
         end.base = (int32_t)at;
         end.rows = (int32_t)rows;
         if (launch_loss_end(end, stream) != hipSuccess) return EDKM_ERR_HIP;
     }
+    end.rows = (int32_t)m;
     return reduction == RED_NONE ? EDKM_OK : done(launch_loss_reduce(end, stream));
 }
 
@@ -408,7 +430,7 @@ edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, 
         return EDKM_ERR_HIP;
     float* parts = reinterpret_cast<float*>(base + L.split);
     const uint16_t* all = m > 0 && whole(x, ldx, k) ? px : nullptr;
-    ProductPlan qx{};
+    SumPlan qx{};
     for (int64_t c0 = 0; c0 < n; c0 += L.piece) {
         const int64_t words = std::min(L.piece, n - c0), ldz = up8(L.piece);
         LossArgs p{};
@@ -445,21 +467,25 @@ edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, 
         if (dx && m > 0) {
             p.cols = (int32_t)k;
             p.depth = (int32_t)words;
-            if (c0 == 0) qx = product_plan(p, OP_ROWS, OP_DEPTH);     // the same for every piece
-            plan(qx);
+            if (c0 == 0) qx = sum_plan(m, k, words, product_plan(p, OP_ROWS, OP_DEPTH).direct);     // the same for every piece
+            plan(qx.q);
+            p.groups = qx.groups;
+            p.tile = qx.q.tile;
+            if (qx.groups) p.part = parts;
             p.accum = reinterpret_cast<float*>(base + L.accum);
             p.begins = c0 == 0;
             p.ends = c0 + words == n;
             p.scatter = 1;
             p.out = static_cast<uint16_t*>(dx);
             p.ldo = lddx;
-            if (launch_loss_sum(p, format, OP_ROWS, qx, stream) != hipSuccess) return EDKM_ERR_HIP;
+            if (launch_loss_sum(p, format, OP_ROWS, qx.q, stream) != hipSuccess) return EDKM_ERR_HIP;
         }
         if (dw) {
             p.b = xs;
             p.ldb = up8(k);
             p.all = all;
             p.ld_all = ldx;
+            p.groups = 0;
             p.rows = (int32_t)words;
             p.cols = (int32_t)k;
             p.depth = (int32_t)m;

@@ -242,6 +242,16 @@ __device__ __forceinline__ s16x8 keep_first(s16x8 v, int n) {
     return v;
 }
 
+// The arguments of a product whose sums E takes, or of one with the epilogue above (void).
+template <class E>
+struct ArgsOf {
+    typedef typename E::Args type;
+};
+template <>
+struct ArgsOf<void> {
+    typedef ProductArgs type;
+};
+
 // A one-dimensional grid of any number of workgroups, whose kernel starts with args.first
 #define EDKM_GO_PARTS(kern, groups, threads, args, ...)                                                          \
     do {                                                                                                          \

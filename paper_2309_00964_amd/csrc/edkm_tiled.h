@@ -366,14 +366,6 @@ __device__ __forceinline__ void epi_rows(const ProductArgs& p, const char* lds, 
 // the kernel's; E::begin sets what only the device knows, and says whether there is anything to
 // do; an E is made for a wave's rows before the sums are, so that what it reads is there by
 // then, and its block takes 16 x 64 sums as the MFMA leaves them.
-template <class E>
-struct ArgsOf {
-    typedef typename E::Args type;
-};
-template <>
-struct ArgsOf<void> {
-    typedef ProductArgs type;
-};
 template <class E, int TR>
 struct EndOf {
     typedef typename E::template End<TR> type;
@@ -461,7 +453,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(typename ArgsOf<E>::t
         step(a0, b0, a1, b1, s);
         if (s + 1 < steps) step(a1, b1, a0, b0, s + 1);
     }
-    if (BM == SPLIT_TILE && p.part) {
+    if ((BM == SPLIT_TILE || !std::is_void_v<E>) && p.part) {
         float* at = p.part + ((int64_t)group * NW + wave) * (TR * 1024) + lane * 4;
 #pragma unroll
         for (int i = 0; i < TR; ++i)
@@ -498,8 +490,10 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(typename ArgsOf<E>::t
 // 64: 20.0 us, 14.3 by four).
 template <int F, int BM, int BN, int WM, int WN, bool PLAIN, int W, class E = void>
 __global__ void __launch_bounds__(W * 64) k_join(typename ArgsOf<E>::type p, int splits) {
-    if constexpr (!std::is_void_v<E>)
-        if (!E::begin(p)) return;
+    if constexpr (!std::is_void_v<E>) {
+        if (!E::begin(p) || p.splits == 1) return;
+        splits = p.splits;
+    }
     constexpr int NW = WM * WN, TR = BM / WM / 16;
     __shared__ __attribute__((aligned(16))) char lds[W][EPI_BYTES];
     const uint32_t nx = (p.cols + BN - 1) / BN, ny = (p.rows + BM - 1) / BM;
@@ -562,7 +556,7 @@ template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, int BITS 
 static hipError_t tiled(typename ArgsOf<E>::type p, const ProductPlan& q, hipStream_t s) {
     const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
     EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS, E>), (uint64_t)(tiles * q.splits), WM * WN * 64, p);
-    if constexpr (B == SPLIT_TILE) {
+    if constexpr (B == SPLIT_TILE || !std::is_void_v<E>) {
         const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
         if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4, E>), blocks, dim3(256), p, q.splits);
         else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1, E>), blocks, dim3(64), p, q.splits);

@@ -23,7 +23,7 @@ __device__ __forceinline__ int word_of(const void* targets, int index_type, int6
 struct LossBegin {
     typedef LossArgs Args;
     __device__ __forceinline__ static bool begin(LossArgs& p) {
-        if (p.dynamic == 0) return true;
+        if (p.dynamic == 0) return split(p);
         const int count = *p.rows_of.count;
         if (p.dynamic == 2) {
             p.depth = count;
@@ -31,7 +31,7 @@ struct LossBegin {
                 p.b = p.all;
                 p.ldb = p.ld_all;
             }
-            return true;
+            return split(p);
         }
         if (p.all && count == p.m) {
             p.a = p.all;
@@ -39,13 +39,15 @@ struct LossBegin {
         }
         p.rows = min(p.rows, count - p.base);
         p.a += (int64_t)p.base * p.lda;
-        if (p.rows <= 0) return false;
+        return p.rows > 0 && split(p);
+    }
+    // as many parts of the depths as the launch has workgroups for, now that the tiles are known
+    __device__ __forceinline__ static bool split(LossArgs& p) {
         if (p.groups) {
-            // as many parts of the depths as the launch has workgroups for, now that the tiles are known
             const int tiles = ((p.rows + p.tile - 1) / p.tile) * ((p.cols + p.tile - 1) / p.tile), steps = (p.depth + 63) / 64;
             const int parts = max(1, min(p.groups / tiles, steps / PART_STEPS));
-            p.split_steps = (steps + parts - 1) / parts;
-            p.splits = (steps + p.split_steps - 1) / p.split_steps;
+            p.split_steps = max(1, (steps + parts - 1) / parts);
+            p.splits = max(1, (steps + p.split_steps - 1) / p.split_steps);
             if (p.splits == 1) p.part = nullptr;
         }
         return true;
@@ -236,11 +238,96 @@ struct LossSum : LossBegin {
   };
 };
 
-// A launch that finds its splits by itself, and the join of as many rows of blocks as there can be.
-template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, class E>
-static hipError_t split_tiled(LossArgs p, hipStream_t s) {
-    EDKM_GO((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, 0, E>), dim3(p.groups), dim3(WM * WN * 64), p);
+// The same product by tiles of 64 x 64, four steps of 64 depths in LDS and three of them on their
+// way, for sizes that make too few larger tiles: there a step takes as long as its loads' way
+// from memory, which the steps ahead hide, and twice to four times the CUs have a tile.  A wave
+// takes 16 rows.  Every wave waits for its own loads of a step and then for the other waves,
+// asks for the step three ahead (into the buffer that all have read one step ago) and multiplies.
+// 1001 x 1003 x 777 with its statistics takes 12 us so, and 19 by tiles of 128 two steps deep.
+constexpr int SMALL_WAVES = 4;
+template <int F, int OPA, int OPB, class E>
+__global__ void __launch_bounds__(SMALL_WAVES * 64, 2) k_small(LossArgs p) {
+    if (!E::begin(p)) return;
+    typedef Feed<OPA, SMALL, SMALL_WAVES, true> FA;
+    typedef Feed<OPB, SMALL, SMALL_WAVES, true> FB;
+    constexpr int BYTES = FA::T::BYTES;
+    static_assert(FA::T::PER == 2 && FB::T::PER == 2, "eight loads in two steps");
+    static_assert(SMALL_WAVES * EPI_BYTES <= 2 * BYTES, "the epilogue's blocks fit");
+    // separate arrays, so that the compiler knows the loads of one buffer apart from the reads of another
+    __shared__ __attribute__((aligned(1024))) char a0[BYTES], a1[BYTES], a2[BYTES], a3[BYTES], b0[BYTES], b1[BYTES], b2[BYTES], b3[BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t nx = (p.cols + SMALL - 1) / SMALL, ny = (p.rows + SMALL - 1) / SMALL;
+    const uint32_t group = p.first + blockIdx.x, split = group / (nx * ny);
+    if (split >= (uint32_t)p.splits) return;
+    uint32_t tx, ty;
+    tile_of(group % (nx * ny), nx, ny, tx, ty);
+    const int r0 = ty * SMALL, c0 = tx * SMALL;
+    FA fa;
+    FB fb;
+    fa.init(p.a, p.lda, r0, p.rows, p.depth, wave, lane);
+    fb.init(p.b, p.ldb, c0, p.cols, p.depth, wave, lane);
+    typename E::template End<1> end;
+    end.init(p, lane, r0 + wave * 16);
+    typename FA::T ta;
+    typename FB::T tb;
+    ta.init(wave * 16, lane);
+    tb.init(0, lane);
+    f32x4 acc[4] = {};
+    const int first = split * p.split_steps, steps = min(first + p.split_steps, (p.depth + 63) / 64);
+    // past the last step too, so that as many loads are on their way in every step: they read nothing and write zeros
+    auto ask = [&](char* a, char* b, int s) {
+        fa.start(a, s * 64);
+        fb.start(b, s * 64);
+    };
+    auto step = [&](const char* a, const char* b, char* an, char* bn, int s) {
+        asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");      // its loads of this step, its reads of the last
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        ask(an, bn, s + 3);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const s16x8 va = ta.frag(a, 0, ks);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = mfma16<F>(tb.frag(b, j, ks), va, acc[j]);
+        }
+    };
+    ask(a0, b0, first);
+    ask(a1, b1, first + 1);
+    ask(a2, b2, first + 2);
+    for (int s = first; s < steps; s += 4) {
+        step(a0, b0, a3, b3, s);
+        if (s + 1 < steps) step(a1, b1, a0, b0, s + 1);
+        if (s + 2 < steps) step(a2, b2, a1, b1, s + 2);
+        if (s + 3 < steps) step(a3, b3, a2, b2, s + 3);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();       // every load has arrived, and every wave has read
+    if (p.part) {
+        float* at = p.part + ((int64_t)group * SMALL_WAVES + wave) * 1024 + lane * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(at + j * 256) = acc[j];
+        return;
+    }
+    char* mine = (wave < 2 ? a0 : b0) + (wave & 1) * EPI_BYTES;
+    end.block(p, 0, mine, lane, r0 + wave * 16, c0, acc, (int64_t)group * SMALL_WAVES + wave);
+}
+
+template <int F, int OPA, int OPB, int B, bool DIRECT, class E>
+static hipError_t loss_go(LossArgs p, uint64_t groups, hipStream_t s) {
+    if constexpr (B == SMALL) EDKM_GO_PARTS((k_small<F, OPA, OPB, E>), groups, SMALL_WAVES * 64, p);
+    else if constexpr (B == 128) EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, 2, 2, DIRECT, 0, E>), groups, 256, p);
+    else EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, 2, 4, DIRECT, 0, E>), groups, 512, p);
+    return hipSuccess;
+}
+
+// With p.groups the launch finds its splits by itself (LossBegin), and there is a join of as
+// many blocks as there can be; else every tile takes all depths.
+template <int F, int OPA, int OPB, int B, bool DIRECT, class E>
+static hipError_t loss_launch(const LossArgs& p, hipStream_t s) {
+    constexpr int WM = B == SMALL ? 4 : 2, WN = B == SMALL ? 1 : B == 128 ? 2 : 4;
     const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
+    const hipError_t e = loss_go<F, OPA, OPB, B, DIRECT, E>(p, p.groups ? p.groups : tiles, s);
+    if (e != hipSuccess || !p.groups) return e;
     const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
     if (p.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, true, 4, E>), blocks, dim3(256), p, 0);
     else EDKM_GO((k_join<F, B, B, WM, WN, true, 1, E>), blocks, dim3(64), p, 0);
@@ -248,13 +335,10 @@ static hipError_t split_tiled(LossArgs p, hipStream_t s) {
 }
 
 template <int F, int OPA, int OPB, class E>
-static hipError_t loss_tiled(const LossArgs& p, const ProductPlan& q, hipStream_t s) {
-    if (p.groups) {
-        if (q.tile == 256) return split_tiled<F, OPA, OPB, 256, 2, 4, true, E>(p, s);
-        return q.direct ? split_tiled<F, OPA, OPB, 128, 2, 2, true, E>(p, s) : split_tiled<F, OPA, OPB, 128, 2, 2, false, E>(p, s);
-    }
-    if (q.tile == 256) return tiled<F, OPA, OPB, 256, 2, 4, true, 0, E>(p, q, s);
-    return q.direct ? tiled<F, OPA, OPB, 128, 2, 2, true, 0, E>(p, q, s) : tiled<F, OPA, OPB, 128, 2, 2, false, 0, E>(p, q, s);
+static hipError_t loss_tiled(const LossArgs& p, const LossPlan& q, hipStream_t s) {
+    if (q.tile == 256) return loss_launch<F, OPA, OPB, 256, true, E>(p, s);
+    if (q.tile == SMALL) return loss_launch<F, OPA, OPB, SMALL, true, E>(p, s);
+    return q.direct ? loss_launch<F, OPA, OPB, 128, true, E>(p, s) : loss_launch<F, OPA, OPB, 128, false, E>(p, s);
 }
 
 }  // namespace edkm

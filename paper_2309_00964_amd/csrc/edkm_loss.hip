@@ -4,6 +4,8 @@
 
 #include "edkm_loss.h"
 
+#include <algorithm>
+
 namespace edkm {
 
 // ----------------------------------------------------------------------------
@@ -211,11 +213,52 @@ hipError_t launch_loss_reduce(const LossEndArgs& a, hipStream_t s) {
 // ----------------------------------------------------------------------------
 // the products with the vocabulary
 
-hipError_t launch_loss_stats(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s) {
+// By the time of the launch's rounds over the CUs, in us: a round's steps, one CU's workgroups side
+// by side, and what a tile costs beside them (its first loads, its end).  Splitting the depths
+// adds a launch and the parts' way to memory and back.  Measured for 256, 128 and 64: 4096 x 4096 x 4096
+// 114, 132 and 217; 200 x 32000 x 4096 95, 77 and 120; 1001 x 1003 x 777 32, 19 and 12; 90 x 5000 x 704 20,
+// 11 and 7; dw of 64 tokens x 512 and 32000 words 14, 14 and 25; dx of 1536 of 2048 tokens x 2048 over 65536
+// words 382 by 256 in five parts, 526 by 128 in two.
+LossPlan loss_plan(int64_t rows, int64_t cols, int64_t depth, bool direct) {
+    const int64_t steps = std::max<int64_t>(1, (depth + 63) / 64);
+    LossPlan best{};
+    best.direct = direct;
+    double least = 0;
+    auto consider = [&](int tile, int64_t most, double alone, double full, double beside) {
+        const int64_t t = ((rows + tile - 1) / tile) * ((cols + tile - 1) / tile);
+        const int64_t many = t < most ? std::max<int64_t>(1, std::min(most / t, steps / PART_STEPS)) : 1;
+        for (const int64_t want : {(int64_t)1, many}) {
+            const int64_t each = (steps + want - 1) / want, parts = (steps + each - 1) / each, all = t * parts;
+            const double cost = (double)((all + most - 1) / most) * ((double)each * (all <= 256 ? alone : full) + beside) +
+                                (parts > 1 ? 4 + (double)all * tile * tile * 8 / 5e6 : 0);
+            if (best.tile && cost >= least) continue;
+            least = cost;
+            best.tile = tile;
+            best.splits = (int)parts;
+            best.split_steps = (int)each;
+            best.groups = parts > 1 ? (int)most : 0;
+        }
+    };
+    consider(128, 512, 0.77, 1.0, 4);
+    if (direct) consider(SMALL, 512, 0.3, 0.39, 2.5);
+    if (direct) consider(256, 256, 1.6, 1.6, 7);
+    return best;
+}
+
+size_t loss_part_bytes(int64_t rows, int64_t cols, int64_t depth) {
+    size_t most = 0;
+    for (const bool direct : {false, true}) {
+        const LossPlan q = loss_plan(rows, cols, depth, direct);
+        if (q.groups) most = std::max(most, (size_t)q.groups * q.tile * q.tile * 4);
+    }
+    return most;
+}
+
+hipError_t launch_loss_stats(const LossArgs& a, int fmt, const LossPlan& q, hipStream_t s) {
     return fmt == FMT_BF16 ? loss_tiled<FMT_BF16, OP_ROWS, OP_ROWS, LossStats>(a, q, s)
                            : loss_tiled<FMT_FP16, OP_ROWS, OP_ROWS, LossStats>(a, q, s);
 }
-hipError_t launch_loss_dz(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s) {
+hipError_t launch_loss_dz(const LossArgs& a, int fmt, const LossPlan& q, hipStream_t s) {
     return fmt == FMT_BF16 ? loss_tiled<FMT_BF16, OP_ROWS, OP_ROWS, LossDz<FMT_BF16>>(a, q, s)
                            : loss_tiled<FMT_FP16, OP_ROWS, OP_ROWS, LossDz<FMT_FP16>>(a, q, s);
 }

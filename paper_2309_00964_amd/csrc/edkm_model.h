@@ -153,6 +153,18 @@ struct GatherArgs {
     int64_t ldz;
 };
 
+// How one of a loss's products is carried out.
+struct LossPlan {
+    int tile;               // outputs square: 256, 128 or SMALL
+    int splits, split_steps;
+    int groups;             // workgroups of a launch that splits the depths among them; 0: a workgroup to a tile
+    bool direct;
+};
+constexpr int SMALL = 64, PART_STEPS = 8;
+LossPlan loss_plan(int64_t rows, int64_t cols, int64_t depth, bool direct);
+// Bytes of the parts' sums, whatever the operands' alignment.
+size_t loss_part_bytes(int64_t rows, int64_t cols, int64_t depth);
+
 struct LossArgs : ProductArgs {
     int splits;
     int groups, tile;       // workgroups of a launch that finds its splits by itself, and its tile; or 0
@@ -184,46 +196,14 @@ struct LossEndArgs {
     float *loss, *lse;
 };
 
-enum LossProduct : int { LOSS_STATS = 0, LOSS_DZ = 1, LOSS_SUM = 2 };
 hipError_t launch_pick(const PickArgs& a, int index_type, hipStream_t s);
 hipError_t launch_gather(GatherArgs a, hipStream_t s);
-hipError_t launch_loss_stats(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s);
-hipError_t launch_loss_dz(const LossArgs& a, int fmt, const ProductPlan& q, hipStream_t s);
-hipError_t launch_loss_sum(const LossArgs& a, int fmt, int opa, const ProductPlan& q, hipStream_t s);
+hipError_t launch_loss_stats(const LossArgs& a, int fmt, const LossPlan& q, hipStream_t s);
+hipError_t launch_loss_dz(const LossArgs& a, int fmt, const LossPlan& q, hipStream_t s);
+hipError_t launch_loss_sum(const LossArgs& a, int fmt, int opa, const LossPlan& q, hipStream_t s);
 hipError_t launch_few_loss(const LossArgs& a, int fmt, hipStream_t s);
 hipError_t launch_loss_end(const LossEndArgs& a, hipStream_t s);
 hipError_t launch_loss_reduce(const LossEndArgs& a, hipStream_t s);
-
-// dx sums over thousands of words for tokens whose number only the device knows.  Where they
-// make fewer tiles than the launch has workgroups (one of 256 on a CU, two of 128), the depths are
-// split among them.  A tile of 256 takes 1.5 times a step's time of two of 128 on a CU, a part its
-// way to memory and back: 1536 of 2048 tokens x 2048 over 65536 words 516 us by tiles of 128 in two
-// parts, 382 by tiles of 256 in five.  A part has eight steps at least
-// (1001 x 777 over 1003 words: two parts 15 us, eight 18).
-struct SumPlan {
-    ProductPlan q;
-    int groups;             // 0: not split
-};
-constexpr int PART_STEPS = 8;
-constexpr int64_t SUM_PART_BYTES = (int64_t)256 * 256 * 256 * 4;
-inline SumPlan sum_plan(int64_t rows, int64_t cols, int64_t depth, bool direct) {
-    const int64_t steps = (depth + 63) / 64;
-    auto cost = [&](int64_t tile, int64_t most, double step) {
-        const int64_t t = ((rows + tile - 1) / tile) * ((cols + tile - 1) / tile);
-        const int64_t parts = t < most ? std::max<int64_t>(1, std::min(most / t, steps / PART_STEPS)) : 1;
-        const double rounds = parts > 1 ? 1 : (double)((t + most - 1) / most);
-        return rounds * step * (double)((steps + parts - 1) / parts) + (parts > 1 ? 4 + (double)(t * parts * tile * tile) * 8 / 5e6 : 0);
-    };
-    SumPlan p{};
-    p.q.direct = direct;
-    p.q.tile = direct && cost(256, 256, 1.5) < cost(128, 512, 1.0) ? 256 : 128;
-    const int64_t most = p.q.tile == 256 ? 256 : 512, t = ((rows + p.q.tile - 1) / p.q.tile) * ((cols + p.q.tile - 1) / p.q.tile);
-    const int64_t parts = t < most ? std::max<int64_t>(1, std::min(most / t, steps / PART_STEPS)) : 1;
-    p.q.split_steps = (int)((steps + parts - 1) / parts);
-    p.q.splits = (int)((steps + p.q.split_steps - 1) / p.q.split_steps);
-    p.groups = t < most && steps >= 2 * PART_STEPS ? (int)most : 0;
-    return p;
-}
 
 // Words of a piece of the vocabulary whose dz is held at a time: as many as keep it within the
 // Infinity Cache, which the two products that read it then hit; 2048 at least.

@@ -84,8 +84,8 @@ LossWs loss_ws(int64_t m, int64_t n, int64_t k) {
     L.split = L.stats + up256((size_t)(m <= LOSS_FEW ? (n + 15) / 16 : (n + 63) / 64) * rows * 8);
     size_t parts = 0;
     if (m > 0) {
-        parts = product_part_bytes(rows, n, k);
-        if (m % rows) parts = std::max(parts, product_part_bytes(m % rows, n, k));
+        parts = loss_part_bytes(rows, n, k);
+        if (m % rows) parts = std::max(parts, loss_part_bytes(m % rows, n, k));
     }
     L.total = L.split + up256(parts);
     return L;
@@ -106,13 +106,12 @@ LossBackWs loss_back_ws(int64_t m, int64_t n, int64_t k) {
     L.accum = L.dz + up256((size_t)m * up8(L.piece) * 2);
     // tiles of either size
     L.split = L.accum + (L.piece < n ? up256((size_t)((m + 255) / 256 * 256) * ((k + 255) / 256 * 256) * 4) : 0);
-    size_t parts = product_part_bytes(L.piece, k, m);
-    if (last) parts = std::max(parts, product_part_bytes(last, k, m));
+    size_t parts = loss_part_bytes(L.piece, k, m);
+    if (last) parts = std::max(parts, loss_part_bytes(last, k, m));
     if (m > 0) {
-        parts = std::max(parts, product_part_bytes(m, L.piece, k));
-        const SumPlan x = sum_plan(m, k, L.piece, true), y = sum_plan(m, k, L.piece, false);
-        if (x.groups || y.groups) parts = std::max(parts, (size_t)SUM_PART_BYTES);
-        if (last) parts = std::max(parts, product_part_bytes(m, last, k));
+        parts = std::max(parts, loss_part_bytes(m, L.piece, k));
+        parts = std::max(parts, loss_part_bytes(m, k, L.piece));
+        if (last) parts = std::max(parts, loss_part_bytes(m, last, k));
     }
     L.total = L.split + up256(parts);
     return L;
@@ -125,6 +124,19 @@ bool loss_ok(int64_t m, int64_t n, int64_t k, int format, int index_type, int re
 // Rows that a product can take as they are.
 bool whole(const void* p, int64_t ld, int64_t k) {
     return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld <= DIRECT_LD_MOST && k % 8 == 0;
+}
+
+void set_plan(LossArgs& p, const LossPlan& q, float* parts) {
+    p.split_steps = q.split_steps;
+    p.splits = q.groups ? q.splits : 1;
+    p.groups = q.groups;
+    p.tile = q.tile;
+    p.part = q.groups ? parts : nullptr;
+}
+LossPlan planned(LossArgs& p, int opa, int opb, float* parts) {
+    const LossPlan q = loss_plan(p.rows, p.cols, p.depth, product_plan(p, opa, opb).direct);
+    set_plan(p, q, parts);
+    return q;
 }
 
 // The launches that a loss's forward and backward begin with: the list of tokens, their rows
@@ -376,10 +388,7 @@ edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int forma
         if (few) {
             if (launch_few_loss(p, format, stream) != hipSuccess) return EDKM_ERR_HIP;
         } else {
-            const ProductPlan q = product_plan(p, OP_ROWS, OP_ROWS);
-            p.split_steps = q.split_steps;
-            p.splits = q.splits;
-            p.part = q.splits > 1 ? reinterpret_cast<float*>(base + L.split) : nullptr;
+            const LossPlan q = planned(p, OP_ROWS, OP_ROWS, reinterpret_cast<float*>(base + L.split));
             if (list) {
                 p.all = whole(x, ldx, k) ? px : nullptr;
                 p.ld_all = ldx;
@@ -430,18 +439,13 @@ edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, 
         return EDKM_ERR_HIP;
     float* parts = reinterpret_cast<float*>(base + L.split);
     const uint16_t* all = m > 0 && whole(x, ldx, k) ? px : nullptr;
-    SumPlan qx{};
+    LossPlan qx{};
     for (int64_t c0 = 0; c0 < n; c0 += L.piece) {
         const int64_t words = std::min(L.piece, n - c0), ldz = up8(L.piece);
         LossArgs p{};
         p.rows_of = pick.r;
         p.m = (int32_t)m;
         p.padded = 1;
-        auto plan = [&](const ProductPlan& q) {
-            p.split_steps = q.split_steps;
-            p.splits = q.splits;
-            p.part = q.splits > 1 ? parts : nullptr;
-        };
         if (m > 0) {
             p.a = xs;
             p.lda = up8(k);
@@ -457,8 +461,7 @@ edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, 
             p.lse = lse;
             p.out = dz;
             p.ldo = ldz;
-            const ProductPlan q = product_plan(p, OP_ROWS, OP_ROWS);
-            plan(q);
+            const LossPlan q = planned(p, OP_ROWS, OP_ROWS, parts);
             if (launch_loss_dz(p, format, q, stream) != hipSuccess) return EDKM_ERR_HIP;
         }
         p.a = dz;
@@ -467,25 +470,22 @@ edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, 
         if (dx && m > 0) {
             p.cols = (int32_t)k;
             p.depth = (int32_t)words;
-            if (c0 == 0) qx = sum_plan(m, k, words, product_plan(p, OP_ROWS, OP_DEPTH).direct);     // the same for every piece
-            plan(qx.q);
-            p.groups = qx.groups;
-            p.tile = qx.q.tile;
-            if (qx.groups) p.part = parts;
+            // the same for every piece, whose sums are added tile by tile
+            if (c0 == 0) qx = planned(p, OP_ROWS, OP_DEPTH, parts);
+            else set_plan(p, qx, parts);
             p.accum = reinterpret_cast<float*>(base + L.accum);
             p.begins = c0 == 0;
             p.ends = c0 + words == n;
             p.scatter = 1;
             p.out = static_cast<uint16_t*>(dx);
             p.ldo = lddx;
-            if (launch_loss_sum(p, format, OP_ROWS, qx.q, stream) != hipSuccess) return EDKM_ERR_HIP;
+            if (launch_loss_sum(p, format, OP_ROWS, qx, stream) != hipSuccess) return EDKM_ERR_HIP;
         }
         if (dw) {
             p.b = xs;
             p.ldb = up8(k);
             p.all = all;
             p.ld_all = ldx;
-            p.groups = 0;
             p.rows = (int32_t)words;
             p.cols = (int32_t)k;
             p.depth = (int32_t)m;
@@ -494,8 +494,7 @@ edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, 
             p.scatter = 0;
             p.out = static_cast<uint16_t*>(dw) + c0 * k;
             p.ldo = k;
-            const ProductPlan q = product_plan(p, OP_DEPTH, OP_DEPTH);
-            plan(q);
+            const LossPlan q = planned(p, OP_DEPTH, OP_DEPTH, parts);
             if (launch_loss_sum(p, format, OP_DEPTH, q, stream) != hipSuccess) return EDKM_ERR_HIP;
         }
     }

@@ -87,6 +87,17 @@ hipError_t launch_pick(const PickArgs& a, int index_type, hipStream_t s) {
     return hipSuccess;
 }
 
+// Zeros into a row, by `threads` threads of which this is the t-th.
+__device__ __forceinline__ void clear_row(uint16_t* to, int k, int t, int threads) {
+    for (int64_t c = t * 8; c < k; c += threads * 8) {
+        if (c + 8 <= k) {
+            reinterpret_cast<S16x8*>(to + c)->v = s16x8{};
+        } else {
+            for (int64_t e = c; e < k; ++e) to[e] = 0;
+        }
+    }
+}
+
 // A row to a group of threads: 256 where rows are long.
 __global__ void __launch_bounds__(256) k_gather(GatherArgs a, int threads) {
     const int count = *a.r.count;
@@ -98,16 +109,7 @@ __global__ void __launch_bounds__(256) k_gather(GatherArgs a, int threads) {
         for (int64_t c = threadIdx.x % threads * 8; c < a.k; c += threads * 8)
             *reinterpret_cast<s16x8*>(to + c) = row8(from + c, a.k - (int)c);
     }
-    if (a.zero && a.r.slot[i] < 0) {
-        uint16_t* to = a.zero + i * a.ldz;
-        for (int64_t c = threadIdx.x % threads * 8; c < a.k; c += threads * 8) {
-            if (c + 8 <= a.k) {
-                reinterpret_cast<S16x8*>(to + c)->v = s16x8{};
-            } else {
-                for (int64_t e = c; e < a.k; ++e) to[e] = 0;
-            }
-        }
-    }
+    if (a.zero && a.r.slot[i] < 0) clear_row(a.zero + i * a.ldz, a.k, threadIdx.x % threads, threads);
 }
 
 hipError_t launch_gather(GatherArgs a, hipStream_t s) {
@@ -115,6 +117,71 @@ hipError_t launch_gather(GatherArgs a, hipStream_t s) {
     while (threads < 256 && threads * 8 < a.k) threads *= 2;
     const int rows = 256 / threads;
     EDKM_GO_PARTS(k_gather, (uint64_t)((a.m + rows - 1) / rows), 256, a, threads);
+    return hipSuccess;
+}
+
+// Both for up to 1024 tokens in one launch: every workgroup makes the list, which the first one
+// writes, and then has a share of x's rows, of dx's to clear and of w's to copy, a wave to a row.
+// (A launch less and one for w's rows less: 4 us of GPU time each, and 3 of the host's.)
+template <int IDX>
+__global__ void __launch_bounds__(1024) k_pick_gather(PickArgs a, GatherArgs g, AlignJob w) {
+    __shared__ int waves[16], rows[1024];
+    __shared__ float tops[16];
+    const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, i = threadIdx.x;
+    int t = i < a.m ? word_of<IDX>(a.targets, i, a.n) : -1;
+    const float grad = i < a.m ? a.dloss[a.reduction == RED_NONE ? i : 0] : 0.f;
+    if (grad == 0.f) t = -1;
+    const uint64_t there = __ballot(t >= 0);
+    float top = t >= 0 ? fabsf(grad) : 0.f;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) {
+        waves[q] = __popcll(there);
+        tops[q] = top;
+    }
+    __syncthreads();
+    int at = __popcll(there & ((1ull << lane) - 1)), count = 0;
+#pragma unroll
+    for (int p = 0; p < 16; ++p) {
+        at += p < q ? waves[p] : 0;
+        count += waves[p];
+        top = fmaxf(top, tops[p]);
+    }
+    if (t >= 0) rows[at] = i;
+    if (blockIdx.x == 0) {
+        if (i < a.m) a.r.slot[i] = t >= 0 ? at : -1;
+        if (t >= 0) {
+            a.r.row[at] = i;
+            a.r.word[at] = t;
+            a.r.value[at] = grad / top * 32768.f;
+        }
+        if (i == 0) {
+            a.r.count[0] = count;
+            *a.r.alpha = top * (1.f / 32768.f) / (a.reduction == RED_MEAN ? (float)max(count, 1) : 1.f);
+        }
+    }
+    // slot[] of this workgroup's own making: rows of dx without a token are those that are not in the list
+    __shared__ unsigned char has[1024];
+    has[i] = t >= 0;
+    __syncthreads();
+    const bool copy = g.always || count < a.m;
+    const int step = gridDim.x * 16, first = blockIdx.x * 16 + q;
+    for (int r = first; r < a.m; r += step) {
+        if (copy && r < count) {
+            const uint16_t* from = g.x + (int64_t)rows[r] * g.ldx;
+            for (int c = lane * 8; c < g.k; c += 512) *reinterpret_cast<s16x8*>(g.out + r * g.ldo + c) = row8(from + c, g.k - c);
+        }
+        if (g.zero && !has[r]) clear_row(g.zero + r * g.ldz, g.k, lane, 64);
+    }
+    for (int r = first; r < w.rows; r += step)
+        for (int c = lane * 8; c < w.cols; c += 512)
+            *reinterpret_cast<s16x8*>(w.out + (int64_t)r * ((w.cols + 7) & ~7) + c) = row8(w.m + (int64_t)r * w.ld + c, w.cols - c);
+}
+
+hipError_t launch_pick_gather(const PickArgs& a, const GatherArgs& g, const AlignJob& w, int index_type, hipStream_t s) {
+    const dim3 grid((uint32_t)std::min<int64_t>(512, (std::max<int64_t>(a.m, w.rows) + 15) / 16));
+    if (index_type == IDX_64) EDKM_GO(k_pick_gather<IDX_64>, grid, dim3(1024), a, g, w);
+    else EDKM_GO(k_pick_gather<IDX_32>, grid, dim3(1024), a, g, w);
     return hipSuccess;
 }
 

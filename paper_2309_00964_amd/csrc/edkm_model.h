@@ -198,6 +198,8 @@ struct LossEndArgs {
 
 hipError_t launch_pick(const PickArgs& a, int index_type, hipStream_t s);
 hipError_t launch_gather(GatherArgs a, hipStream_t s);
+// A backward's two and the copy of w's rows (w.rows 0: none) in one, for up to LIST_LEAST tokens.
+hipError_t launch_pick_gather(const PickArgs& a, const GatherArgs& g, const AlignJob& w, int index_type, hipStream_t s);
 hipError_t launch_loss_stats(const LossArgs& a, int fmt, const LossPlan& q, hipStream_t s);
 hipError_t launch_loss_dz(const LossArgs& a, int fmt, const LossPlan& q, hipStream_t s);
 hipError_t launch_loss_sum(const LossArgs& a, int fmt, int opa, const LossPlan& q, hipStream_t s);

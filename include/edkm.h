@@ -448,7 +448,9 @@ edkm_status edkm_residual_norm_backward(int64_t m, int64_t n, int format, const 
  * z is never in memory.
  *   reduction  EDKM_REDUCE_NONE: loss is float[m], l; _SUM: float[1]; _MEAN: float[1], over
  *              the rows with a target (0 if there are none)
- *   lse        float[m]: log(sum_j exp z_ij), for the backward (nullable) */
+ *   lse        nullable, float[m], for the backward: log(sum_j exp z_ij) of the rows with a
+ *              target, 0 for the others
+ * Rows without a target reach no other row's result, whatever they hold. */
 enum { EDKM_REDUCE_NONE = 0, EDKM_REDUCE_SUM = 1, EDKM_REDUCE_MEAN = 2 };
 size_t edkm_linear_cross_entropy_workspace_bytes(int64_t m, int64_t n, int64_t k);
 edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int format, int index_type, int reduction,
@@ -457,9 +459,10 @@ edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int forma
 /* Its gradients for a given dL/dloss (device float[m], or float[1] with a reduction): with
  * g_i = dL/dl_i and dz_ij = g_i (exp(z_ij - lse_i) - [j = targets_i]),
  *   dx = dz W (m x k),  dw = dz^T x (n x k without gaps), in the 16-bit format; one may be NULL.
+ * Rows without a target or with g_i = 0 have dx_i = 0 and no part in dw, whatever they hold.
  * z is formed again, some thousand words at a time, and dz is rounded to 16 bits on the way
- * into the two products, as a share of 2^15 times the largest |g_i| (in fp16 a token whose
- * |g_i| is below 2^-14 of that keeps fewer digits). */
+ * into the two products, as g_i's share of the largest |g_i| times 2^15 (in fp16 a token whose
+ * |g_i| is below 2^-14 of the largest keeps fewer digits). */
 size_t edkm_linear_cross_entropy_backward_workspace_bytes(int64_t m, int64_t n, int64_t k);
 edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, int format, int index_type, int reduction,
                                                const float* dloss, const void* x, int64_t ldx, const void* w, int64_t ldw,

@@ -166,7 +166,7 @@ __device__ __forceinline__ void store_block(const LossArgs& p, char* lds, int la
 
 // dz = factor (e^(z - lse) - [word is the target]), rounded to 16 bits because the matrix
 // units take it so in both products; the factor is the token's share of 2^15 times the largest
-// |dL/dl|, so that fp16 holds probabilities down to 2^-30 (2^-39 with fewer digits).
+// |dL/dl|, so that fp16 holds probabilities down to 2^-29 (2^-39 with fewer digits).
 template <int F>
 struct LossDz : LossBegin {
   template <int TR>

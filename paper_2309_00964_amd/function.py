@@ -17,7 +17,11 @@ activation and residual in its epilogue and its gradients from the library:
 dL/dW~ in 16 bits, as the clustering's backward reads it.  ``palette_linear`` is
 the same product with an exported palette in W's place.
 
-Each call makes its own plans (about 40 MiB of workspace per matrix through
+``embedding`` and ``palette_embedding`` look a model's tokens up, ``rms_norm`` and
+``residual_norm`` stand before and between its blocks, and ``linear_cross_entropy`` is
+its loss, without the logits in memory.
+
+Each call of ``dkm`` makes its own plans (about 40 MiB of workspace per matrix through
 torch's allocator), kept with the autograd graph until the backward has run,
 so two clustered layers in one graph never share state.
 """

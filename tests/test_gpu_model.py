@@ -293,7 +293,33 @@ def test_cross_entropy(fmt, m, n, k, reduction):
     assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
 
 
-@pytest.mark.parametrize("m,n,k,lead,gap", [(70, 200, 96, 1, 3), (70, 200, 96, 8, 8), (70, 201, 97, 3, 0), (300, 520, 136, 8, 4)])
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(16, 500, 300), (17, 500, 300), (1024, 300, 72), (1025, 300, 72), (40, 1000, 4096), (1300, 2100, 264),
+                                   (2048, 4100, 512), (1100, 16640, 1032), (2000, 16384, 2048), (4096, 1000, 128), (64, 40000, 96)])
+def test_cross_entropy_by_every_plan(fmt, m, n, k):
+    """Sizes on both sides of each choice: few tokens and the list's length, tiles of 64, 128 and
+    256, with the depths of one of the products split and not."""
+    dt = L.DT[fmt]
+    say("loss plans", fmt, m, n, k)
+    x, w = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt, scale=2 * k ** -0.5)
+    targets = tokens(3, m, n)
+    loss, lse = torch.empty(1, device=DEV), torch.full((m,), float("nan"), device=DEV)
+    edkm.linear_cross_entropy(x, w, targets, loss, lse, "mean")
+    ref, tol, rl, tl = M.cross_entropy(x, w, targets, "mean")
+    L.assert_within(loss, ref.view(1), tol.view(1), "loss")
+    L.assert_within(lse, rl, tl, "lse")
+    each = torch.empty(m, device=DEV)
+    edkm.linear_cross_entropy(x, w, targets, each)
+    ref, tol, _, _ = M.cross_entropy(x, w, targets, "none")
+    L.assert_within(each, ref, tol, "losses")
+    dloss, dx, dw = torch.full((1,), 512.0, device=DEV), torch.full_like(x, float("nan")), torch.full_like(w, float("nan"))
+    edkm.linear_cross_entropy_backward(dloss, x, w, targets, lse, dx, dw, "mean")
+    for key, (ref, tol) in M.cross_entropy_grads(dloss, x, w, targets, "mean").items():
+        L.assert_within({"dx": dx, "dw": dw}[key], ref, tol, key)
+
+
+@pytest.mark.parametrize("m,n,k,lead,gap", [(70, 200, 96, 1, 3), (70, 200, 96, 8, 8), (70, 201, 97, 3, 0), (300, 520, 136, 8, 4),
+                                            (40, 1000, 4096, 1, 3), (9, 300, 264, 1, 3)])
 def test_cross_entropy_views_in_nan_buffers(m, n, k, lead, gap):
     dt = torch.bfloat16
     say("loss views", m, n, k, lead, gap)
@@ -388,7 +414,7 @@ def test_large_and_infinite_logits():
     L.assert_within(loss, ref, tol, "loss with -Inf")
 
 
-def test_pieces_of_the_vocabulary_and_of_the_tokens(monkeypatch):
+def test_pieces_of_the_vocabulary_and_of_the_tokens():
     """Sizes of which the gradient takes several pieces and the forward several launches."""
     dt, m, n, k = torch.bfloat16, 33000, 9001, 40
     say("pieces", m, n, k)

@@ -88,10 +88,17 @@ struct LossStats : LossBegin {
   struct End {
     int word[TR];
     __device__ __forceinline__ void init(const LossArgs& p, int lane, int r) {
+        // one kind of load to a loop: a choice inside it would wait for one load after the other
+        auto row = [&](int i) { return p.base + min(r + i * 16 + (lane & 15), p.rows - 1); };
+        if (!p.targets) {
 #pragma unroll
-        for (int i = 0; i < TR; ++i) {
-            const int row = p.base + min(r + i * 16 + (lane & 15), p.rows - 1);
-            word[i] = p.targets ? word_of(p.targets, p.index_type, row, p.cols) : p.rows_of.word[row];
+            for (int i = 0; i < TR; ++i) word[i] = p.rows_of.word[row(i)];
+        } else if (p.index_type == IDX_64) {
+#pragma unroll
+            for (int i = 0; i < TR; ++i) word[i] = word_of<IDX_64>(p.targets, row(i), p.cols);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TR; ++i) word[i] = word_of<IDX_32>(p.targets, row(i), p.cols);
         }
     }
     __device__ __forceinline__ void block(const LossArgs& p, int i, char*, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t) {
@@ -213,10 +220,12 @@ struct LossSum : LossBegin {
 #pragma unroll
         for (int i = 0; i < TR; ++i)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                row[i][q] = min(r + i * 16 + q * 8 + (lane >> 3), p.rows - 1);
-                if (p.scatter) row[i][q] = p.rows_of.row[row[i][q]];
-            }
+            for (int q = 0; q < 2; ++q) row[i][q] = min(r + i * 16 + q * 8 + (lane >> 3), p.rows - 1);
+        if (p.scatter)
+#pragma unroll
+            for (int i = 0; i < TR; ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) row[i][q] = p.rows_of.row[row[i][q]];
     }
     __device__ __forceinline__ void block(const LossArgs& p, int i, char* lds, int lane, int r0, int c0, f32x4 (&acc)[4], int64_t place) {
         if (r0 >= p.rows || c0 >= p.cols) return;

@@ -430,10 +430,13 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_tiled(typename ArgsOf<E>::t
             for (int j = 0; j < TC; ++j) vb[j] = tb.frag(b, j, ks);
 #pragma unroll
             for (int i = 0; i < TR; ++i) va[i] = ta.frag(a, i, ks);
+            // the SIMD's wave that multiplies before the one that reads (8192 x 32000 x 4096: 1672 -> 1635 us)
+            if (!std::is_void_v<E>) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < TR; ++i)
 #pragma unroll
                 for (int j = 0; j < TC; ++j) acc[i][j] = mfma16<F>(vb[j], va[i], acc[i][j]);
+            if (!std::is_void_v<E>) __builtin_amdgcn_s_setprio(0);
             if (BITS && ks == 0 && s + 1 < steps) fb.finish(bn, (s + 1) * 64);
         }
         if (s + 1 < steps) {

@@ -53,12 +53,17 @@ struct EmbedGradArgs {
 };
 
 // Tokens that one launch ranks by comparing all with all (256 workgroups of 32, 67M
-// comparisons), and that a digit's pass takes for a workgroup, at least.
+// comparisons: 10 us; 8000 tokens' gradient added to 32000 x 256 24.0 us, by digits 32.3), and that a
+// digit's pass takes for a workgroup, at least.
 constexpr int64_t RANK_MOST = 8192;
 constexpr int RANK_TOKENS = 32, PLACE_LEAST = 1024, PLACE_GROUPS = 512, DIGIT_BITS = 10;
-// Tokens of a chunk that one thread sums for its eight columns, and rows that one workgroup
-// looks up to write those of no token.
-constexpr int CHUNK_LEAST = 16, CHUNKS_MOST = 2048, ZERO_ROWS = 32;
+// Tokens of a chunk that one thread sums for its eight columns: eight, so that there are threads
+// enough, or sixteen where there are anyway and fewer parts are joined (gradients added to a table, us
+// by 8 and by 16: 1000 x 4096 15.1 and 18.5, 3000 x 4096 24.6 and 27.3, 8000 x 256 20.9 and 24.0;
+// 8192 tokens of 32000 x 4096 104.8 and 100.0); more than that for 2048 chunks at most.  And rows that one
+// workgroup looks up to write those of no token.
+constexpr int CHUNK_LEAST = 8, CHUNK_MANY = 16, CHUNKS_MOST = 2048, ZERO_ROWS = 32;
+constexpr int64_t CHUNK_ELEMENTS = 1 << 24;
 
 struct SortPlan {
     int passes, width;      // digits' number and bits; 0 passes: ranked
@@ -77,9 +82,9 @@ inline SortPlan sort_plan(int64_t m, int64_t v) {
     q.groups = (uint32_t)((m + q.per - 1) / q.per);
     return q;
 }
-inline uint32_t chunk_tokens(int64_t m) {
-    const int64_t per = (m + CHUNKS_MOST - 1) / CHUNKS_MOST;
-    return (uint32_t)(per < CHUNK_LEAST ? CHUNK_LEAST : per);
+inline uint32_t chunk_tokens(int64_t m, int64_t d) {
+    const int64_t per = (m + CHUNKS_MOST - 1) / CHUNKS_MOST, least = m * d > CHUNK_ELEMENTS ? CHUNK_MANY : CHUNK_LEAST;
+    return (uint32_t)(per < least ? least : per);
 }
 
 hipError_t launch_embed(EmbedArgs a, int fmt, int index_type, int bits, hipStream_t s);
@@ -207,9 +212,10 @@ hipError_t launch_few_loss(const LossArgs& a, int fmt, hipStream_t s);
 hipError_t launch_loss_end(const LossEndArgs& a, hipStream_t s);
 hipError_t launch_loss_reduce(const LossEndArgs& a, hipStream_t s);
 
-// Words of a piece of the vocabulary whose dz is held at a time: as many as keep it within the
-// Infinity Cache, which the two products that read it then hit; 2048 at least.
-constexpr int64_t DZ_BYTES = 256 << 20, DZ_LEAST = 2048;
+// Words of a piece of the vocabulary whose dz is held at a time: as many as keep it within half
+// the Infinity Cache, which the two products that read it then hit; 2048 at least.  8192 x 32000 x 4096
+// with gradients takes 6925 us by 64 MiB, 6740 by 128, 6860 by 256 and 7000 by 512.
+constexpr int64_t DZ_BYTES = 128 << 20, DZ_LEAST = 2048;
 inline int64_t loss_piece(int64_t m, int64_t n) {
     int64_t p = DZ_BYTES / (2 * (m > 0 ? m : 1));
     if (p < DZ_LEAST) p = DZ_LEAST;

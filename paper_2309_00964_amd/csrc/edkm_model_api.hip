@@ -32,7 +32,7 @@ struct EmbedWs {
 EmbedWs embed_ws(int64_t m, int64_t v, int64_t d) {
     EmbedWs w;
     const SortPlan q = sort_plan(m, v);
-    w.per = chunk_tokens(m);
+    w.per = chunk_tokens(m, d);
     w.chunks = (uint32_t)((m + w.per - 1) / w.per);
     w.pos = up256((size_t)m * 4);
     w.spare = w.pos + up256((size_t)m * 4);

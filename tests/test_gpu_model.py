@@ -157,6 +157,21 @@ def test_embedding_past_32_bits():
     assert float(table.view(-1)[:: 4099].float().abs().sum().isnan()) == 0.0
 
 
+def test_embedding_of_no_tokens():
+    say("embedding of nothing")
+    dt = torch.bfloat16
+    ids, table = torch.empty(0, dtype=torch.int64, device=DEV), randn(1, 70, 40, dtype=dt).requires_grad_()
+    y = function.embedding(ids, table)
+    assert y.shape == (0, 40)
+    g, = torch.autograd.grad(y, table, torch.empty_like(y))
+    assert not bool(g.any())
+    old = randn(2, 70, 40, dtype=dt)
+    more = old.clone()
+    edkm.embedding_backward(ids, torch.empty(0, 40, dtype=dt, device=DEV), more, accumulate=True)
+    assert torch.equal(old, more)
+    assert function.embedding(torch.empty(2, 0, 3, dtype=torch.int32, device=DEV), table).shape == (2, 0, 3, 40)
+
+
 # ---------------------------------------------------------------------------
 # norms
 
@@ -435,6 +450,35 @@ def test_pieces_of_the_vocabulary_and_of_the_tokens():
         gw, ew = gw + g["dw"][0], ew + g["dw"][1]      # the bounds of a sum are at most the bounds' sum
     assert abs(float(loss) - float(total / count)) <= 1e-5 * float(total / count)
     L.assert_within(dw, gw, ew + gw.abs() * L.half(dt), "dw")
+
+
+@pytest.mark.parametrize("m", [3, 40])
+def test_cross_entropy_past_32_bits(m):
+    """A vocabulary's weights and their gradient of more than 2^32 bytes; words at both ends."""
+    dt, n, k = torch.bfloat16, 70001, 32768
+    say("loss past 32 bits", m)
+    x = randn(1, m, k, dtype=dt)
+    w = torch.empty(n, k, dtype=dt, device=DEV)
+    for a in range(0, n, 10000):
+        w[a:a + 10000] = randn(a + 7, min(10000, n - a), k, dtype=dt, scale=0.01)
+    targets = torch.randint(0, n, (m,), device=DEV)
+    targets[:3] = torch.tensor([n - 1, 0, 66000])
+    z = torch.cat([x.double() @ w[a:a + 4000].double().t() for a in range(0, n, 4000)], 1)
+    want = torch.logsumexp(z, 1) - z.gather(1, targets[:, None])[:, 0]
+    loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    edkm.linear_cross_entropy(x, w, targets, loss, lse)
+    # a logit is off by less than (k + 2) 2^-23 times its terms' magnitudes, about k 0.8 0.008
+    assert float((loss.double() - want).abs().max()) <= 2 * (k + 2) * 2.0 ** -23 * k * 0.0064
+    dw, dx = torch.empty_like(w), torch.empty_like(x)
+    edkm.linear_cross_entropy_backward(torch.ones(m, device=DEV), x, w, targets, lse, dx, dw)
+    dz = torch.softmax(z, 1)
+    dz[torch.arange(m, device=DEV), targets] -= 1
+    rows = torch.tensor([0, 1, 32767, 65535, 65536, 66000, n - 2, n - 1], device=DEV)
+    ref, mag = dz[:, rows].t() @ x.double(), dz[:, rows].abs().t() @ x.double().abs()
+    # dz's rounding and its own fp32 error (its logit's, relative), and the sum's and its rounding
+    bound = mag * (L.half(dt) * 2 + 2 * (k + 2) * 2.0 ** -23 * k * 0.0064) + ref.abs() * L.half(dt) + 1e-30
+    L.assert_within(dw[rows], ref, bound, "dw")
+    assert bool(dx.isfinite().all()) and bool(dw[::997].isfinite().all())
 
 
 # ---------------------------------------------------------------------------

@@ -203,7 +203,7 @@ struct LossEndArgs {
 
 hipError_t launch_pick(const PickArgs& a, int index_type, hipStream_t s);
 hipError_t launch_gather(GatherArgs a, hipStream_t s);
-// A backward's two and the copy of w's rows (w.rows 0: none) in one, for up to LIST_LEAST tokens.
+// The two and the copy of w's rows (w.rows 0: none) in one, for 1 to ONE_LIST tokens (slot is not written).
 hipError_t launch_pick_gather(const PickArgs& a, const GatherArgs& g, const AlignJob& w, int index_type, hipStream_t s);
 hipError_t launch_loss_stats(const LossArgs& a, int fmt, const LossPlan& q, hipStream_t s);
 hipError_t launch_loss_dz(const LossArgs& a, int fmt, const LossPlan& q, hipStream_t s);
@@ -228,7 +228,7 @@ inline int64_t loss_piece(int64_t m, int64_t n) {
 // pays from about as many on.  And up to which each workgroup takes sixteen words for all tokens,
 // which is bound by the words' bytes (32000 x 4096: 1 token 52 us, 5.0 TB/s, 16 tokens 72; by the
 // tiles 83 and 84).
-constexpr int64_t LIST_LEAST = 1024, LOSS_FEW = 16;
+constexpr int64_t LIST_LEAST = 1024, LOSS_FEW = 16, ONE_LIST = 8192;
 // Tokens of a forward's launch: as many as keep the statistics within 256 MiB, 256 at least.
 inline int64_t loss_rows(int64_t m, int64_t n) {
     const int64_t blocks = (n + 63) / 64, r = (256 << 20) / (blocks * 8) / 256 * 256;

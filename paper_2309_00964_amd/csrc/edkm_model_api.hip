@@ -12,7 +12,6 @@ using namespace edkm;
 namespace {
 
 static_assert(EDKM_INDEX_INT32 == IDX_32 && EDKM_INDEX_INT64 == IDX_64, "index types");
-static_assert(LIST_LEAST == 1024, "a thread for each token of a short list");
 static_assert(EDKM_REDUCE_NONE == RED_NONE && EDKM_REDUCE_SUM == RED_SUM && EDKM_REDUCE_MEAN == RED_MEAN, "reductions");
 
 bool format_ok(int format) { return format == EDKM_KEYS_FP16 || format == EDKM_KEYS_BF16; }
@@ -155,7 +154,7 @@ hipError_t begin_loss(const PickArgs& pick, int index_type, const uint16_t* x, i
     g.always = !whole(x, ldx, k);
     g.zero = zero;
     g.ldz = ldz;
-    if (pick.dloss && pick.m > 0 && pick.m <= LIST_LEAST) return launch_pick_gather(pick, g, copies.count ? copies.job[0] : AlignJob{}, index_type, s);
+    if (pick.m > 0 && pick.m <= ONE_LIST) return launch_pick_gather(pick, g, copies.count ? copies.job[0] : AlignJob{}, index_type, s);
     hipError_t e = launch_pick(pick, index_type, s);
     if (e == hipSuccess && pick.m > 0) e = launch_gather(g, s);
     return e == hipSuccess ? launch_align_rows(copies, s) : e;

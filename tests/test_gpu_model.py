@@ -310,7 +310,7 @@ def test_cross_entropy(fmt, m, n, k, reduction):
 
 @pytest.mark.parametrize("fmt", ["fp16", "bf16"])
 @pytest.mark.parametrize("m,n,k", [(16, 500, 300), (17, 500, 300), (1024, 300, 72), (1025, 300, 72), (40, 1000, 4096), (1300, 2100, 264),
-                                   (2048, 4100, 512), (1100, 16640, 1032), (2000, 16384, 2048), (4096, 1000, 128), (64, 40000, 96)])
+                                   (2048, 4100, 512), (1100, 16640, 1032), (2000, 16384, 2048), (4096, 1000, 128), (64, 40000, 96), (8192, 200, 40), (8193, 200, 40)])
 def test_cross_entropy_by_every_plan(fmt, m, n, k):
     """Sizes on both sides of each choice: few tokens and the list's length, tiles of 64, 128 and
     256, with the depths of one of the products split and not."""

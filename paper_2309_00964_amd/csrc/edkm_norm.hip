@@ -79,7 +79,7 @@ __device__ __forceinline__ void put8(uint16_t* q, const float (&f)[8], int left)
 }
 
 // Keeps a vector's values as they are: without it the compiler converts them once before the
-// loop over the rows and holds twice the registers (170 against 110 in k_norm_grad).
+// loop over the rows and holds twice the registers (170 against 117 in k_norm_grad).
 __device__ __forceinline__ void packed(s16x8& v) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
     u32x4 b = __builtin_bit_cast(u32x4, v);
@@ -98,7 +98,8 @@ __device__ __forceinline__ float over_root(float sum, const NormArgs& a) {
 }
 
 // A row lies in its threads' registers from its loads to its stores; the vectors stay there
-// from row to row.  Bound by its bytes: r, u (and a gate's) read, h and y written, once.
+// from row to row.  Bound by its bytes: r, u (and a gate's) read, h and y written, once: 8192 x 4096
+// takes 45 us (6.0 TB/s), one row 3.2.
 template <int F, int L, int I, bool BLOCK, bool TINY>
 __global__ void __launch_bounds__(Row<L>::THREADS) k_norm(NormArgs a) {
     typedef Row<L> R;
@@ -183,13 +184,17 @@ __global__ void __launch_bounds__(Row<L>::THREADS) k_norm(NormArgs a) {
 // which costs no more bytes than reading it and keeps it unrounded.  A thread adds up its
 // columns' shares of the vectors' gradients in fp32 over its rows, and k_norm_join the threads':
 // dy hn for dw, and one sum for both others, since of scale gate dh' un (dpost) and
-// scale dh' un post (a vector gate's) all but dh' un is the column's.  PAST: rows are read and
-// written past the caches, where they do not fit them.
+// scale dh' un post (a vector gate's) all but dh' un is the column's.  Bound by its bytes and by
+// the row's three sums, which wait for one another: 8192 x 4096 with all gradients takes 80 us (5.0
+// TB/s), 67 without norm and gate of the block; from 4097 columns on a CU has one workgroup (8192 x
+// 8192 177 us, 4.5 TB/s).  PAST: rows are read and written past the caches, where they do not fit
+// them (8192 x 4096 90 us through them).
 template <int F, int L, int I, bool BLOCK, bool TINY, bool PAST>
 __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
     typedef Row<L> R;
     const bool ragged = a.n % 8 != 0;
-    constexpr bool AHEAD = I == 1;      // registers for the next row's loads beside this one's work
+    // registers for the next row's loads beside this one's work, and for h between its sums
+    constexpr bool AHEAD = I == 1;
     __shared__ float lds[9][16];
     const int l = threadIdx.x % L;
     const float per = 1.0f / (float)a.n;
@@ -207,107 +212,106 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
     s16x8 nr[I], ndy[I], ndh[I], nu[BLOCK ? I : 1];      // the next row
     auto ask = [&](int64_t r) {
         // where a gradient is not given any row is loaded, and taken as zeros
-        const uint16_t *x = a.r + r * a.ldr, *y = a.dy ? a.dy + r * a.lddy : x, *z = a.dh ? a.dh + r * a.lddh : x;
+        const uint16_t *pr = a.r + r * a.ldr, *py = a.dy ? a.dy + r * a.lddy : pr, *ph = a.dh ? a.dh + r * a.lddh : pr;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int c = (i * L + l) * 8;
-            nr[i] = ask8<TINY, PAST>(x, c, a.n);
-            ndy[i] = ask8<TINY, PAST>(y, c, a.n);
-            ndh[i] = ask8<TINY, PAST>(z, c, a.n);
+            nr[i] = ask8<TINY, PAST>(pr, c, a.n);
+            ndy[i] = ask8<TINY, PAST>(py, c, a.n);
+            ndh[i] = ask8<TINY, PAST>(ph, c, a.n);
             if constexpr (BLOCK) nu[i] = ask8<TINY, PAST>(a.u + r * a.ldu, c, a.n);
         }
     };
-    s16x8 u[I];
+    // the row's own: values are taken from 16 bits again for each of its three sums, which leaves
+    // the registers for the rows to come
+    s16x8 x[I], y[I], z[I], u[I];
     auto again = [&] {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
+            packed(x[i]);
+            packed(y[i]);
+            packed(z[i]);
             packed(w[i]);
-            packed(post[i]);
-            packed(gate[i]);
-            if (BLOCK) packed(u[i]);
+            if (BLOCK) {
+                packed(u[i]);
+                packed(post[i]);
+                packed(gate[i]);
+            }
         }
     };
     if (AHEAD && group < a.m) ask(group);
     for (int64_t r = group; r < a.m; r += a.groups) {
         if (!AHEAD) ask(r);
-        float dy[I][8], d[I][8], h[I][8], su = 1.f;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int c = (i * L + l) * 8, left = a.n - c;
             if constexpr (BLOCK)
                 if (a.gate_rows) gate[i] = had8<TINY>(ask8<TINY>(a.gate + r * a.ldg, c, a.n), left, ragged);
-            floats<F>(had8<TINY>(nr[i], left, ragged), h[i]);
-            floats<F>(had8<TINY>(ndy[i], a.dy ? left : 0, ragged), dy[i]);
-            floats<F>(had8<TINY>(ndh[i], a.dh ? left : 0, ragged), d[i]);
-            if (TINY && !a.dy)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) dy[i][j] = 0.f;
-            if (TINY && !a.dh)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[i][j] = 0.f;
+            x[i] = had8<TINY>(nr[i], left, ragged);
+            y[i] = a.dy ? had8<TINY>(ndy[i], left, ragged) : s16x8{};
+            z[i] = a.dh ? had8<TINY>(ndh[i], left, ragged) : s16x8{};
             if constexpr (BLOCK) u[i] = had8<TINY>(nu[i], left, ragged);
         }
         if (AHEAD && r + a.groups < a.m) ask(r + a.groups);
         again();
-        if (BLOCK) {
-            if (a.post) {
-                float s[1] = {0.f};
-#pragma unroll
-                for (int i = 0; i < I; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float uv = to_f32<F>((uint16_t)u[i][j]);
-                        s[0] = fmaf(uv, uv, s[0]);
-                    }
-                R::sum(s, lds, 0);
-                su = over_root(s[0], a);
-                again();
-            }
+        float su = 1.f;
+        if (BLOCK && a.post) {
+            float s[1] = {0.f};
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float g = a.scale * to_f32<F>((uint16_t)gate[i][j]), p = su * to_f32<F>((uint16_t)post[i][j]);
-                    h[i][j] = fmaf(g, to_f32<F>((uint16_t)u[i][j]) * p, h[i][j]);
+                    const float uv = to_f32<F>((uint16_t)u[i][j]);
+                    s[0] = fmaf(uv, uv, s[0]);
                 }
+            R::sum(s, lds, 0);
+            su = over_root(s[0], a);
+            again();
         }
-        float s[2] = {0.f, 0.f}, s2[1] = {0.f};
+        // h, as the forward had it
+        auto formed = [&](int i, int j) {
+            const float v = to_f32<F>((uint16_t)x[i][j]);
+            if (!BLOCK) return v;
+            const float g = a.scale * to_f32<F>((uint16_t)gate[i][j]), p = su * to_f32<F>((uint16_t)post[i][j]);
+            return fmaf(g, to_f32<F>((uint16_t)u[i][j]) * p, v);
+        };
+        float s[2] = {0.f, 0.f}, s2[1] = {0.f}, h[AHEAD ? I : 1][8];
 #pragma unroll
-        for (int i = 0; i < I; ++i)
+        for (int i = 0; i < I; ++i) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                s[0] = fmaf(h[i][j], h[i][j], s[0]);
-                s[1] = fmaf(dy[i][j] * to_f32<F>((uint16_t)w[i][j]), h[i][j], s[1]);
+                const float v = formed(i, j);
+                if (AHEAD) h[i][j] = v;
+                s[0] = fmaf(v, v, s[0]);
+                s[1] = fmaf(to_f32<F>((uint16_t)y[i][j]) * to_f32<F>((uint16_t)w[i][j]), v, s[1]);
             }
+        }
         R::sum(s, lds, 1);
         again();
         const float sh = over_root(s[0], a), mean = s[1] * sh * per;
+        float q[BLOCK ? I : 1][8];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int c = (i * L + l) * 8;
+            float d[8], dg[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float hn = h[i][j] * sh;
-                d[i][j] = fmaf(sh, fmaf(-hn, mean, dy[i][j] * to_f32<F>((uint16_t)w[i][j])), d[i][j]);
-                sw[i][j] = fmaf(dy[i][j], hn, sw[i][j]);
-            }
-            if (a.dr) put8<F, PAST>(a.dr + r * a.lddr + c, d[i], a.n - c);
-            if (BLOCK) {
-                // h's registers take the gate's gradient from here on, d's the block's
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                const float hn = (AHEAD ? h[i][j] : formed(i, j)) * sh, dy = to_f32<F>((uint16_t)y[i][j]);
+                d[j] = fmaf(sh, fmaf(-hn, mean, dy * to_f32<F>((uint16_t)w[i][j])), to_f32<F>((uint16_t)z[i][j]));
+                sw[i][j] = fmaf(dy, hn, sw[i][j]);
+                if constexpr (BLOCK) {
                     const float un = to_f32<F>((uint16_t)u[i][j]) * su, p = a.scale * to_f32<F>((uint16_t)post[i][j]);
                     const float g = to_f32<F>((uint16_t)gate[i][j]);
-                    h[i][j] = d[i][j] * un;
-                    sb[i][j] = fmaf(h[i][j], a.gate_rows ? g : 1.f, sb[i][j]);
-                    h[i][j] *= p;
-                    d[i][j] *= g * p;
-                    s2[0] = fmaf(d[i][j], un, s2[0]);
+                    dg[j] = d[j] * un;
+                    sb[i][j] = fmaf(dg[j], a.gate_rows ? g : 1.f, sb[i][j]);
+                    dg[j] *= p;
+                    q[i][j] = d[j] * (g * p);
+                    s2[0] = fmaf(q[i][j], un, s2[0]);
                 }
-                if (a.dgate && a.gate_rows) put8<F>(a.dgate + r * a.n + c, h[i], a.n - c);
             }
+            if (a.dr) put8<F, PAST>(a.dr + r * a.lddr + c, d, a.n - c);
+            if (BLOCK && a.dgate && a.gate_rows) put8<F>(a.dgate + r * a.n + c, dg, a.n - c);
         }
-        again();
         if (BLOCK && a.post) R::sum(s2, lds, 2);
         else if (R::WAVES > 1) __syncthreads();      // place 1 is free for the next row
         if (BLOCK && a.du) {
@@ -315,9 +319,10 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int c = (i * L + l) * 8;
+                packed(u[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[i][j] = su * fmaf(-to_f32<F>((uint16_t)u[i][j]) * su, mean2, d[i][j]);
-                put8<F, PAST>(a.du + r * a.lddu + c, d[i], a.n - c);
+                for (int j = 0; j < 8; ++j) q[i][j] = su * fmaf(-to_f32<F>((uint16_t)u[i][j]) * su, mean2, q[i][j]);
+                put8<F, PAST>(a.du + r * a.lddu + c, q[i], a.n - c);
             }
         }
     }

@@ -245,11 +245,26 @@ __global__ void __launch_bounds__(1024) k_loss_end(LossEndArgs a) {
     }
     if (lane < R) part[w][lane] = make_float2(top, sum);
     __syncthreads();
-    if (threadIdx.x >= R || row >= rows) return;
+    if (threadIdx.x >= R || (row >= rows && !a.whole)) return;
     top = none;
     sum = 0.f;
 #pragma unroll
     for (int p = 0; p < 16; ++p) add(part[p][lane].x, part[p][lane].y);
+    if (a.whole) {
+        // the only workgroup: the sum over its rows too
+        const bool there = row < rows && word_of(a.targets, a.index_type, row, a.words) >= 0;
+        const float l = logf(sum);
+        float total = there ? (top - a.r.value[row]) + l : 0.f;
+        int count = there;
+        if (row < rows && a.lse) a.lse[row] = there ? top + l : 0.f;
+#pragma unroll
+        for (int o = 1; o < R; o *= 2) {
+            total += __shfl_xor(total, o);
+            count += __shfl_xor(count, o);
+        }
+        if (threadIdx.x == 0) a.loss[0] = a.reduction == RED_MEAN ? total / (float)max(count, 1) : total;
+        return;
+    }
     const bool there = !a.targets || word_of(a.targets, a.index_type, a.base + row, a.words) >= 0;
     const float l = logf(sum), loss = there ? (top - a.r.value[a.base + row]) + l : 0.f;
     const int i = a.targets ? a.base + row : a.r.row[a.base + row];
@@ -259,7 +274,8 @@ __global__ void __launch_bounds__(1024) k_loss_end(LossEndArgs a) {
 }
 
 hipError_t launch_loss_end(const LossEndArgs& a, hipStream_t s) {
-    if (a.rows <= 64) EDKM_GO(k_loss_end<1>, dim3(a.rows), dim3(1024), a);
+    if (a.whole) EDKM_GO(k_loss_end<16>, dim3(1), dim3(1024), a);
+    else if (a.rows <= 64) EDKM_GO(k_loss_end<1>, dim3(a.rows), dim3(1024), a);
     else EDKM_GO(k_loss_end<16>, dim3((a.rows + 15) / 16), dim3(1024), a);
     return hipSuccess;
 }

@@ -198,6 +198,7 @@ struct LossEndArgs {
     const void* targets;    // without a list of tokens
     int index_type;
     int64_t words;
+    int whole;              // one workgroup has all rows, and sums them up
     float *loss, *lse;
 };
 

@@ -12,6 +12,7 @@ using namespace edkm;
 namespace {
 
 static_assert(EDKM_INDEX_INT32 == IDX_32 && EDKM_INDEX_INT64 == IDX_64, "index types");
+static_assert(LOSS_FEW <= 16, "a workgroup has the rows of a few tokens");
 static_assert(EDKM_REDUCE_NONE == RED_NONE && EDKM_REDUCE_SUM == RED_SUM && EDKM_REDUCE_MEAN == RED_MEAN, "reductions");
 
 bool format_ok(int format) { return format == EDKM_KEYS_FP16 || format == EDKM_KEYS_BF16; }
@@ -367,6 +368,7 @@ edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int forma
     end.targets = list ? nullptr : targets;
     end.index_type = index_type;
     end.words = n;
+    end.whole = few && reduction != RED_NONE;
     for (int64_t at = 0; at < m; at += most) {
         const int64_t rows = std::min(most, m - at);
         LossArgs p{};
@@ -404,7 +406,7 @@ edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int forma
         if (launch_loss_end(end, stream) != hipSuccess) return EDKM_ERR_HIP;
     }
     end.rows = (int32_t)m;
-    return reduction == RED_NONE ? EDKM_OK : done(launch_loss_reduce(end, stream));
+    return reduction == RED_NONE || end.whole ? EDKM_OK : done(launch_loss_reduce(end, stream));
 }
 
 size_t edkm_linear_cross_entropy_backward_workspace_bytes(int64_t m, int64_t n, int64_t k) {

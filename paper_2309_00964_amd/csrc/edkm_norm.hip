@@ -24,22 +24,40 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
+// The same of sixteen lanes, in all of them, and of a row of lanes and the next one's.
+__device__ __forceinline__ float row_sum(float v) {
+    v += moved<0xB1, 0xF>(v);       // lanes in pairs, pairs in fours, fours and eights mirrored
+    v += moved<0x4E, 0xF>(v);
+    v += moved<0x141, 0xF>(v);
+    return v + moved<0x140, 0xF>(v);
+}
+__device__ __forceinline__ float two_rows(float v) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+__device__ __forceinline__ float two_halves(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
 // L threads share a row, each with I pieces of eight columns.
 template <int L>
 struct Row {
-    static constexpr int THREADS = L == 64 ? 256 : L;
+    static constexpr int THREADS = L <= 64 ? 256 : L;
     static constexpr int ROWS = THREADS / L;      // of a workgroup, side by side
     static constexpr int WAVES = L / 64;
 
-    // The workgroup's row, the same for a wave: its addresses are scalars.
-    __device__ __forceinline__ static uint32_t mine() { return ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / L); }
+    // The thread's row among its workgroup's; where it is the same for a wave its addresses are scalars.
+    __device__ __forceinline__ static uint32_t mine() {
+        return ROWS == 1 ? 0 : L == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : threadIdx.x / L;
+    }
 
     // Sums of a row's K values over its threads.  Sums that follow one another take different
     // places in LDS, so that one barrier each is enough.
     template <int K>
     __device__ __forceinline__ static void sum(float (&v)[K], float (*lds)[16], int place) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
+        for (int k = 0; k < K; ++k) v[k] = L == 16 ? row_sum(v[k]) : L == 32 ? two_rows(row_sum(v[k])) : wave_sum(v[k]);
         if constexpr (WAVES > 1) {
             static_assert(WAVES <= 16 && K <= 3, "places");
             const int w = threadIdx.x >> 6;
@@ -199,7 +217,7 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
     const int l = threadIdx.x % L;
     const float per = 1.0f / (float)a.n;
     float sw[I][8] = {}, sb[BLOCK ? I : 1][8] = {};
-    const uint32_t group = blockIdx.x * R::ROWS + R::mine();
+    const uint32_t group = blockIdx.x * R::ROWS + R::mine(), stride = L < 64 ? gridDim.x * R::ROWS : a.groups;
     s16x8 w[I], post[I] = {}, gate[I] = {};
 #pragma unroll
     for (int i = 0; i < I; ++i) {
@@ -240,7 +258,7 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
         }
     };
     if (AHEAD && group < a.m) ask(group);
-    for (int64_t r = group; r < a.m; r += a.groups) {
+    for (int64_t r = group; r < a.m; r += stride) {
         if (!AHEAD) ask(r);
 #pragma unroll
         for (int i = 0; i < I; ++i) {
@@ -252,7 +270,7 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
             z[i] = a.dh ? had8<TINY>(ndh[i], left, ragged) : s16x8{};
             if constexpr (BLOCK) u[i] = had8<TINY>(nu[i], left, ragged);
         }
-        if (AHEAD && r + a.groups < a.m) ask(r + a.groups);
+        if (AHEAD && r + stride < a.m) ask(r + stride);
         again();
         float su = 1.f;
         if (BLOCK && a.post) {
@@ -326,9 +344,21 @@ __global__ void __launch_bounds__(Row<L>::THREADS, 4) k_norm_grad(NormArgs a) {
             }
         }
     }
-    if (group >= a.groups) return;
+    // a wave's rows make one part
+    uint32_t at = group;
+    if (L < 64) {
+        at = blockIdx.x * 4 + (threadIdx.x >> 6);
+        auto all = [](float v) { return two_halves(L == 16 ? two_rows(v) : v); };
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            sw[0][j] = all(sw[0][j]);
+            if (BLOCK) sb[0][j] = all(sb[0][j]);
+        }
+        if ((threadIdx.x & 63) >= L) return;
+    }
+    if (at >= a.groups) return;
     auto keep = [&](int k, const float (&v)[8], int c) {
-        float* q = a.part + ((int64_t)group * 2 + k) * a.n + c;
+        float* q = a.part + ((int64_t)at * 2 + k) * a.n + c;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (c + j < a.n) q[j] = v[j];
@@ -374,9 +404,12 @@ __global__ void __launch_bounds__(1024) k_norm_join(NormArgs a) {
 // launches
 
 // Threads and pieces of a row by its length, forward and backward (whose sums over the rows
-// take three registers a column).
+// take two registers a column).  Narrow rows, a head's say, lie side by side in a wave: 65536 x 256 with
+// a gate for each value takes 27 and 51 us, by a wave to a row 31 and 96.
 template <class Go>
 static hipError_t by_length_back(int64_t n, Go go) {
+    if (n <= 128) return go(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+    if (n <= 256) return go(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
     if (n <= 512) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
     if (n <= 1024) return go(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
     if (n <= 2048) return go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
@@ -386,6 +419,8 @@ static hipError_t by_length_back(int64_t n, Go go) {
 }
 template <class Go>
 static hipError_t by_length(int64_t n, Go go) {
+    if (n <= 128) return go(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+    if (n <= 256) return go(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
     if (n <= 512) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
     if (n <= 1024) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
     if (n <= 2048) return go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
@@ -394,8 +429,13 @@ static hipError_t by_length(int64_t n, Go go) {
     return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
 }
 
-// Rows that a backward has in work: two workgroups a CU for the longest.
+// Parts of a backward's sums: one for each row that is in work (two workgroups a CU, or one of the
+// longest rows), or for each wave of narrow rows.
 uint32_t norm_groups(int64_t m, int64_t n) {
+    if (n <= 256) {
+        const int64_t rows = n <= 128 ? Row<16>::ROWS : Row<32>::ROWS;
+        return (uint32_t)std::min<int64_t>((m + rows - 1) / rows, 512) * 4;
+    }
     return (uint32_t)std::min<int64_t>(m, n <= 512 ? 2048 : n <= 1024 ? 2048 : n <= 2048 ? 1024 : n <= 4096 ? 512 : 256);
 }
 
@@ -404,9 +444,9 @@ static hipError_t norm_f(const NormArgs& a, hipStream_t s) {
     return by_length(a.n, [&](auto L, auto I) -> hipError_t {
         constexpr int l = decltype(L)::value, i = decltype(I)::value;
         const dim3 grid((uint32_t)std::min<int64_t>((a.m + Row<l>::ROWS - 1) / Row<l>::ROWS, 2048)), block(Row<l>::THREADS);
-        if (l == 64 && i == 1 && a.n < 8) {
-            if (a.u) EDKM_GO((k_norm<F, 64, 1, true, true>), grid, block, a);
-            else EDKM_GO((k_norm<F, 64, 1, false, true>), grid, block, a);
+        if (l == 16 && a.n < 8) {
+            if (a.u) EDKM_GO((k_norm<F, 16, 1, true, true>), grid, block, a);
+            else EDKM_GO((k_norm<F, 16, 1, false, true>), grid, block, a);
         } else if (a.u) {
             EDKM_GO((k_norm<F, l, i, true, false>), grid, block, a);
         } else {
@@ -421,10 +461,11 @@ static hipError_t grad_f(const NormArgs& a, hipStream_t s) {
     if (a.m > 0) {
         const hipError_t e = by_length_back(a.n, [&](auto L, auto I) -> hipError_t {
             constexpr int l = decltype(L)::value, i = decltype(I)::value;
-            const dim3 grid((a.groups + Row<l>::ROWS - 1) / Row<l>::ROWS), block(Row<l>::THREADS);
-            if (l == 64 && i == 1 && a.n < 8) {
-                if (a.u) EDKM_GO((k_norm_grad<F, 64, 1, true, true, false>), grid, block, a);
-                else EDKM_GO((k_norm_grad<F, 64, 1, false, true, false>), grid, block, a);
+            const int rows = l < 64 ? 4 : Row<l>::ROWS;      // parts of a workgroup
+            const dim3 grid((a.groups + rows - 1) / rows), block(Row<l>::THREADS);
+            if (l == 16 && a.n < 8) {
+                if (a.u) EDKM_GO((k_norm_grad<F, 16, 1, true, true, false>), grid, block, a);
+                else EDKM_GO((k_norm_grad<F, 16, 1, false, true, false>), grid, block, a);
             } else if (12 * a.m * a.n > INFINITY_CACHE) {
                 if (a.u) EDKM_GO((k_norm_grad<F, l, i, true, false, true>), grid, block, a);
                 else EDKM_GO((k_norm_grad<F, l, i, false, false, true>), grid, block, a);

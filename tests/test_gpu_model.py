@@ -178,7 +178,7 @@ def test_embedding_of_no_tokens():
 NORM = [(1, 1), (1, 4096), (3, 7), (5, 64), (2, 511), (130, 512), (70, 513), (9, 1024), (33, 1025), (300, 1333), (40, 2049), (17, 4097),
         (6, 8192), (5, 8193), (3, 16384), (700, 256), (2500, 72),
         # more rows than a backward's workgroups
-        (4200, 500), (2100, 600), (1100, 1101), (600, 2104), (300, 4203), (270, 8200)]
+        (9000, 100), (8200, 65), (5000, 200), (4200, 500), (2100, 600), (1100, 1101), (600, 2104), (300, 4203), (270, 8200)]
 
 
 @pytest.mark.parametrize("fmt", ["fp16", "bf16"])

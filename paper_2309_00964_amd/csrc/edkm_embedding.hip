@@ -18,12 +18,9 @@ __device__ __forceinline__ uint32_t row_of(const void* ids, int64_t i, uint32_t 
 }
 
 // stores the first `left` of eight values
-template <bool PAST = false>
 __device__ __forceinline__ void store8(uint16_t* q, s16x8 v, int left) {
     if (left >= 8) {
-        typedef short any8 __attribute__((ext_vector_type(8), aligned(2)));
-        if (PAST) __builtin_nontemporal_store(v, reinterpret_cast<any8*>(q));
-        else reinterpret_cast<S16x8*>(q)->v = v;
+        reinterpret_cast<S16x8*>(q)->v = v;
         return;
     }
 #pragma unroll
@@ -320,6 +317,19 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs& a, uint32_t t, ui
     store8(q, o, left);
 }
 
+// Zeros into n elements from q on, by a workgroup: whole 16-byte places of memory, and the few
+// elements before and after them.
+__device__ __forceinline__ void clear_span(uint16_t* q, int64_t n, bool past) {
+    const int64_t head = min((int64_t)((16 - ((uintptr_t)q & 15)) & 15) / 2, n), body = (n - head) / 8, tail = n - head - body * 8;
+    if (threadIdx.x < head) q[threadIdx.x] = 0;
+    if (threadIdx.x < tail) q[head + body * 8 + threadIdx.x] = 0;
+    s16x8* w = reinterpret_cast<s16x8*>(q + head);
+    if (past)
+        for (int64_t i = threadIdx.x; i < body; i += 256) __builtin_nontemporal_store(s16x8{}, w + i);
+    else
+        for (int64_t i = threadIdx.x; i < body; i += 256) w[i] = s16x8{};
+}
+
 // The first sorted place whose row is not below t.
 __device__ __forceinline__ uint32_t lower(const uint32_t* key, uint32_t m, uint32_t t) {
     uint32_t lo = 0, hi = m;
@@ -342,19 +352,47 @@ template <int F, bool TINY>
 __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
     const uint32_t group = a.first + blockIdx.x, pieces = (a.d + 7) / 8;
     if (group >= a.chunk_groups) {
-        __shared__ uint32_t at[ZERO_ROWS + 1];
-        const uint32_t t0 = (group - a.chunk_groups) * ZERO_ROWS, rows = min((uint32_t)ZERO_ROWS, a.v - t0);
-        if (threadIdx.x <= rows) at[threadIdx.x] = lower(a.key, a.m, t0 + threadIdx.x);
+        __shared__ uint32_t at[ZERO_MOST + 1];
+        const uint32_t t0 = (group - a.chunk_groups) * a.zero_rows, rows = min(a.zero_rows, a.v - t0);
+        for (uint32_t r = threadIdx.x; r <= rows; r += 256) at[r] = lower(a.key, a.m, t0 + r);
         __syncthreads();
+        if (a.lddt == (int64_t)a.d && a.zero_rows == ZERO_MOST) {
+            // short rows without gaps: by the 16-byte places of memory, a thread looking up whose each is
+            uint16_t* q = a.dt + (int64_t)t0 * a.d;
+            const int n = (int)(rows * a.d), off = (int)(((uintptr_t)q & 15) / 2);
+            for (int i = threadIdx.x * 8 - off; i < n; i += 2048) {
+                const uint32_t f = (uint32_t)max(i, 0) / a.d, l = (uint32_t)min(i + 7, n - 1) / a.d;
+                bool all = i >= 0 && i + 8 <= n;
+                for (uint32_t r = f; r <= l; ++r) all = all && at[r] == at[r + 1];
+                if (all) {
+                    *reinterpret_cast<s16x8*>(q + i) = s16x8{};
+                } else {
+                    for (int e = max(i, 0); e < min(i + 8, n); ++e)
+                        if (at[(uint32_t)e / a.d] == at[(uint32_t)e / a.d + 1]) q[e] = 0;
+                }
+            }
+            return;
+        }
+        if (a.lddt == (int64_t)a.d) {
+            // rows without gaps: all that follow one another at once
+            for (uint32_t r = 0; r < rows;) {
+                if (at[r] != at[r + 1]) {
+                    ++r;
+                    continue;
+                }
+                uint32_t e = r + 1;
+                while (e < rows && at[e] == at[e + 1]) ++e;
+                clear_span(a.dt + (int64_t)(t0 + r) * a.d, (int64_t)(e - r) * a.d, a.past);
+                r = e;
+            }
+            return;
+        }
         uint32_t T = 256;       // threads to a row
         while (T > 8 && T / 2 >= pieces) T /= 2;
         for (uint32_t r = threadIdx.x / T; r < rows; r += 256 / T) {
             if (at[r] != at[r + 1]) continue;
             uint16_t* q = a.dt + (int64_t)(t0 + r) * a.lddt;
-            for (uint64_t c = threadIdx.x % T * 8; c < a.d; c += T * 8) {
-                if (a.past) store8<true>(q + c, s16x8{}, (int)min(a.d - (uint32_t)c, 8u));
-                else store8(q + c, s16x8{}, (int)min(a.d - (uint32_t)c, 8u));
-            }
+            for (uint64_t c = threadIdx.x % T * 8; c < a.d; c += T * 8) store8(q + c, s16x8{}, (int)min(a.d - (uint32_t)c, 8u));
         }
         return;
     }
@@ -460,7 +498,8 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradArgs a) {
 template <int F>
 static hipError_t grad_f(EmbedGradArgs a, hipStream_t s) {
     const uint64_t threads = (uint64_t)a.chunks * ((a.d + 7) / 8);
-    const uint64_t sums = (threads + 255) / 256, zeros = a.accumulate ? 0 : ((uint64_t)a.v + ZERO_ROWS - 1) / ZERO_ROWS;
+    a.zero_rows = a.d >= 1024 ? ZERO_LEAST : ZERO_MOST;
+    const uint64_t sums = (threads + 255) / 256, zeros = a.accumulate ? 0 : ((uint64_t)a.v + a.zero_rows - 1) / a.zero_rows;
     a.chunk_groups = (uint32_t)sums;
     a.past = (int64_t)a.v * a.d * 2 > INFINITY_CACHE / 2;
     if (a.d < 8) EDKM_GO_PARTS((k_embed_grad<F, true>), sums + zeros, 256, a);

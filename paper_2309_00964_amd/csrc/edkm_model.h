@@ -48,6 +48,7 @@ struct EmbedGradArgs {
     float* part;            // [chunks][2][up8(d)]
     uint32_t m, v, d, per, chunks;
     uint32_t chunk_groups;  // workgroups that sum; those after them write the rows of no token
+    uint32_t zero_rows;     // ... so many rows each
     float scale;
     int accumulate, past;
 };
@@ -61,8 +62,8 @@ constexpr int RANK_TOKENS = 32, PLACE_LEAST = 1024, PLACE_GROUPS = 512, DIGIT_BI
 // enough, or sixteen where there are anyway and fewer parts are joined (gradients added to a table, us
 // by 8 and by 16: 1000 x 4096 15.1 and 18.5, 3000 x 4096 24.6 and 27.3, 8000 x 256 20.9 and 24.0;
 // 8192 tokens of 32000 x 4096 104.8 and 100.0); more than that for 2048 chunks at most.  And rows that one
-// workgroup looks up to write those of no token.
-constexpr int CHUNK_LEAST = 8, CHUNK_MANY = 16, CHUNKS_MOST = 2048, ZERO_ROWS = 32;
+// workgroup looks up to write those of no token, from 1024 columns on and below.
+constexpr int CHUNK_LEAST = 8, CHUNK_MANY = 16, CHUNKS_MOST = 2048, ZERO_LEAST = 32, ZERO_MOST = 256;
 constexpr int64_t CHUNK_ELEMENTS = 1 << 24;
 
 struct SortPlan {

@@ -448,12 +448,15 @@ __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
 
 // Adds the parts of the rows that go on past their first chunk: four threads for eight
 // columns, each every fourth of the chunks, whose sums are then added in order.  (By sixteen,
-// 17 us for 65536 tokens x 1024 where most rows have two parts; by four, 9.)
+// 17 us for 65536 tokens x 1024 where most rows have two parts; by four, 9.)  Rows of fewer than 64
+// pieces have up to 32 threads for each, which a workgroup has anyway (131072 tokens of 250 x 64
+// added: 32.6 us, by four 61.0).
 template <int F>
 __global__ void __launch_bounds__(256) k_embed_join(EmbedGradArgs a) {
-    __shared__ f32x4 sums[2][4][64];
-    const uint32_t pieces = (a.d + 7) / 8, blocks = (pieces + 63) / 64, group = a.first + blockIdx.x;
-    const uint32_t chunk = group / blocks, piece = group % blocks * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
+    __shared__ f32x4 sums[2][256];
+    const uint32_t pieces = (a.d + 7) / 8, lanes = 1u << a.lanes, blocks = (pieces + lanes - 1) >> a.lanes, splits = 256 >> a.lanes;
+    const uint32_t group = a.first + blockIdx.x, chunk = group / blocks;
+    const uint32_t piece = group % blocks * lanes + (threadIdx.x & (lanes - 1)), q = threadIdx.x >> a.lanes;
     const uint32_t j0 = chunk * a.per, row = a.key[j0 + a.per - 1];
     if (row >= a.v || a.key[j0 + a.per] != row || (chunk && a.key[j0 - 1] == row && a.key[j0] == row)) return;
     const uint64_t wide = (uint64_t)pieces * 8;
@@ -462,14 +465,14 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradArgs a) {
     constexpr int U = 8;
     bool on = true;
     // part 1 of the first chunk, part 0 of those after it
-    for (uint32_t k = chunk + q; on && k < a.chunks; k += 4 * U) {
+    for (uint32_t k = chunk + q; on && k < a.chunks; k += splits * U) {
         f32x4 l[U], h[U];
         uint32_t key[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t e = min(k + 4 * u, a.chunks - 1);
+            const uint32_t e = min(k + splits * u, a.chunks - 1);
             const float* p = a.part + ((uint64_t)e * 2 + (e == chunk)) * wide + c;
-            key[u] = k + 4 * u == chunk ? row : k + 4 * u < a.chunks ? a.key[e * a.per] : 0xFFFFFFFFu;
+            key[u] = k + splits * u == chunk ? row : k + splits * u < a.chunks ? a.key[e * a.per] : 0xFFFFFFFFu;
             l[u] = reinterpret_cast<const f32x4*>(p)[0];
             h[u] = reinterpret_cast<const f32x4*>(p)[1];
         }
@@ -482,14 +485,14 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradArgs a) {
             }
         }
     }
-    sums[0][q][threadIdx.x & 63] = lo;
-    sums[1][q][threadIdx.x & 63] = hi;
+    sums[0][threadIdx.x] = lo;
+    sums[1][threadIdx.x] = hi;
     __syncthreads();
     if (q || piece >= pieces) return;
-#pragma unroll
-    for (int p = 1; p < 4; ++p) {
-        lo += sums[0][p][threadIdx.x];
-        hi += sums[1][p][threadIdx.x];
+#pragma unroll 4
+    for (uint32_t p = 1; p < splits; ++p) {
+        lo += sums[0][(p << a.lanes) + threadIdx.x];
+        hi += sums[1][(p << a.lanes) + threadIdx.x];
     }
     const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     write_row<F>(a, row, c, sum);
@@ -504,7 +507,10 @@ static hipError_t grad_f(EmbedGradArgs a, hipStream_t s) {
     a.past = (int64_t)a.v * a.d * 2 > INFINITY_CACHE / 2;
     if (a.d < 8) EDKM_GO_PARTS((k_embed_grad<F, true>), sums + zeros, 256, a);
     else EDKM_GO_PARTS((k_embed_grad<F, false>), sums + zeros, 256, a);
-    if (a.chunks > 1) EDKM_GO_PARTS(k_embed_join<F>, (uint64_t)(a.chunks - 1) * (((a.d + 7) / 8 + 63) / 64), 256, a);
+    const uint32_t pieces = (a.d + 7) / 8;
+    a.lanes = 6;
+    while (a.lanes > 3 && 1u << (a.lanes - 1) >= pieces) --a.lanes;
+    if (a.chunks > 1) EDKM_GO_PARTS(k_embed_join<F>, (uint64_t)(a.chunks - 1) * ((pieces + 63) / 64), 256, a);
     return hipSuccess;
 }
 

@@ -49,6 +49,7 @@ struct EmbedGradArgs {
     uint32_t m, v, d, per, chunks;
     uint32_t chunk_groups;  // workgroups that sum; those after them write the rows of no token
     uint32_t zero_rows;     // ... so many rows each
+    uint32_t lanes;         // log2 of the threads side by side that join
     float scale;
     int accumulate, past;
 };
@@ -58,12 +59,13 @@ struct EmbedGradArgs {
 // digit's pass takes for a workgroup, at least.
 constexpr int64_t RANK_MOST = 8192;
 constexpr int RANK_TOKENS = 32, PLACE_LEAST = 1024, PLACE_GROUPS = 512, DIGIT_BITS = 10;
-// Tokens of a chunk that one thread sums for its eight columns: eight, so that there are threads
-// enough, or sixteen where there are anyway and fewer parts are joined (gradients added to a table, us
-// by 8 and by 16: 1000 x 4096 15.1 and 18.5, 3000 x 4096 24.6 and 27.3, 8000 x 256 20.9 and 24.0;
-// 8192 tokens of 32000 x 4096 104.8 and 100.0); more than that for 2048 chunks at most.  And rows that one
-// workgroup looks up to write those of no token, from 1024 columns on and below.
-constexpr int CHUNK_LEAST = 8, CHUNK_MANY = 16, CHUNKS_MOST = 2048, ZERO_LEAST = 32, ZERO_MOST = 256;
+// Tokens of a chunk that one thread sums for its eight columns: from eight, so that there are
+// threads enough, over sixteen from 16M values or 32768 tokens on to 64 at 256M, the more the fewer
+// parts are joined (gradients added to a table, us by 8, 16, 32 and 64: 2000 tokens of 2000 x 512 14.3,
+// 18.9, 24.9 and 39.9; 100000 of 40000 x 70 66, 71, 86 and 126; 8192 of 32000 x 4096 49.7, 46.7, 49.4 and
+// 62.8; 131072 of 100000 x 1000 171, 147, 135 and 143; 65536 of 50000 x 4096 253, 204, 187 and 180).  And rows
+// that one workgroup looks up to write those of no token, from 1024 columns on and below.
+constexpr int CHUNK_LEAST = 8, CHUNK_MANY = 16, CHUNK_MOST = 64, CHUNKS_FEW = 2048, ZERO_LEAST = 32, ZERO_MOST = 256;
 constexpr int64_t CHUNK_ELEMENTS = 1 << 24;
 
 struct SortPlan {
@@ -84,8 +86,9 @@ inline SortPlan sort_plan(int64_t m, int64_t v) {
     return q;
 }
 inline uint32_t chunk_tokens(int64_t m, int64_t d) {
-    const int64_t per = (m + CHUNKS_MOST - 1) / CHUNKS_MOST, least = m * d > CHUNK_ELEMENTS ? CHUNK_MANY : CHUNK_LEAST;
-    return (uint32_t)(per < least ? least : per);
+    const int64_t few = m * d > CHUNK_ELEMENTS || m / CHUNKS_FEW > CHUNK_MANY ? CHUNK_MANY : m / CHUNKS_FEW;
+    const int64_t many = m * d / (CHUNK_ELEMENTS / 4), per = few > many ? few : many;
+    return (uint32_t)(per < CHUNK_LEAST ? CHUNK_LEAST : per > CHUNK_MOST ? CHUNK_MOST : per);
 }
 
 hipError_t launch_embed(EmbedArgs a, int fmt, int index_type, int bits, hipStream_t s);

@@ -89,6 +89,21 @@ def test_embedding(fmt, m, v, d, kind):
         assert bool(more[rest].isnan().all())
 
 
+@pytest.mark.parametrize("m,v,d,kind", [(131073, 4, 8, "log"), (60000, 2, 65, "flat"), (50001, 3, 130, "flat"), (34000, 5, 257, "one"),
+                                        (33000, 1, 520, "flat"), (20000, 3, 1100, "log")])
+def test_embedding_rows_of_many_chunks(m, v, d, kind):
+    """Rows whose tokens fill hundreds of chunks, at each number of threads that join them."""
+    dt = torch.bfloat16
+    say("embedding chunks", m, v, d, kind)
+    ids, dy, old = tokens(m, m, v, kind), randn(2, m, d, dtype=dt), randn(3, v, d, dtype=dt)
+    for accumulate in (False, True):
+        g = old.clone()
+        edkm.embedding_backward(ids, dy, g, 0.5, accumulate)
+        ref, tol = M.embedding_grad(ids, dy, v, 0.5, *([old] if accumulate else []))
+        named = ids[(ids >= 0) & (ids < v)].long().unique() if accumulate else slice(None)
+        L.assert_within(g[named], ref[named], tol[named], "dtable")
+
+
 @pytest.mark.parametrize("d,lead,gap", [(64, 1, 3), (64, 8, 8), (77, 3, 0), (129, 8, 7)])
 def test_embedding_views_in_nan_buffers(d, lead, gap):
     dt, m, v = torch.bfloat16, 200, 60

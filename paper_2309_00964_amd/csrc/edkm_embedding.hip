@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
         const uint32_t t0 = (group - a.chunk_groups) * a.zero_rows, rows = min(a.zero_rows, a.v - t0);
         for (uint32_t r = threadIdx.x; r <= rows; r += 256) at[r] = lower(a.key, a.m, t0 + r);
         __syncthreads();
-        if (a.lddt == (int64_t)a.d && a.zero_rows == ZERO_MOST) {
+        if (a.lddt == (int64_t)a.d && a.d < 1024) {
             // short rows without gaps: by the 16-byte places of memory, a thread looking up whose each is
             uint16_t* q = a.dt + (int64_t)t0 * a.d;
             const int n = (int)(rows * a.d), off = (int)(((uintptr_t)q & 15) / 2);
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradArgs a) {
 template <int F>
 static hipError_t grad_f(EmbedGradArgs a, hipStream_t s) {
     const uint64_t threads = (uint64_t)a.chunks * ((a.d + 7) / 8);
-    a.zero_rows = a.d >= 1024 ? ZERO_LEAST : ZERO_MOST;
+    a.zero_rows = max(min((uint32_t)ZERO_VALUES / a.d, (uint32_t)ZERO_MOST), (uint32_t)ZERO_LEAST);
     const uint64_t sums = (threads + 255) / 256, zeros = a.accumulate ? 0 : ((uint64_t)a.v + a.zero_rows - 1) / a.zero_rows;
     a.chunk_groups = (uint32_t)sums;
     a.past = (int64_t)a.v * a.d * 2 > INFINITY_CACHE / 2;

@@ -64,8 +64,10 @@ constexpr int RANK_TOKENS = 32, PLACE_LEAST = 1024, PLACE_GROUPS = 512, DIGIT_BI
 // parts are joined (gradients added to a table, us by 8, 16, 32 and 64: 2000 tokens of 2000 x 512 14.3,
 // 18.9, 24.9 and 39.9; 100000 of 40000 x 70 66, 71, 86 and 126; 8192 of 32000 x 4096 49.7, 46.7, 49.4 and
 // 62.8; 131072 of 100000 x 1000 171, 147, 135 and 143; 65536 of 50000 x 4096 253, 204, 187 and 180).  And rows
-// that one workgroup looks up to write those of no token, from 1024 columns on and below.
-constexpr int CHUNK_LEAST = 8, CHUNK_MANY = 16, CHUNK_MOST = 64, CHUNKS_FEW = 2048, ZERO_LEAST = 32, ZERO_MOST = 256;
+// that one workgroup looks up to write those of no token: of 8192 values, 16 to 256 (gradients written, us
+// by 8192, 32768 and 262144 values: 8192 tokens of 32000 x 256 25, 38 and 56, 20000 of 50000 x 1000 61, 60
+// and 178; by 4096 that of 32000 x 256 takes 26, and 3000 of 300000 x 32 22 both ways).
+constexpr int CHUNK_LEAST = 8, CHUNK_MANY = 16, CHUNK_MOST = 64, CHUNKS_FEW = 2048, ZERO_VALUES = 8192, ZERO_LEAST = 16, ZERO_MOST = 256;
 constexpr int64_t CHUNK_ELEMENTS = 1 << 24;
 
 struct SortPlan {

@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(256) k_embed_grad(EmbedGradArgs a) {
 
 // Adds the parts of the rows that go on past their first chunk: four threads for eight
 // columns, each every fourth of the chunks, whose sums are then added in order.  (By sixteen,
-// 17 us for 65536 tokens x 1024 where most rows have two parts; by four, 9.)  Rows of fewer than 64
+// 17 us for 2048 chunks x 1024 where most rows have two parts; by four, 9.)  Rows of fewer than 64
 // pieces have up to 32 threads for each, which a workgroup has anyway (131072 tokens of 250 x 64
 // added: 32.6 us, by four 61.0).
 template <int F>

@@ -195,7 +195,8 @@ __global__ void __launch_bounds__(1024) k_pick_gather(PickArgs a, GatherArgs g, 
         }
         if (g.zero && !has[r]) clear_row(g.zero + r * g.ldz, g.k, lane, 64);
     }
-    for (int r = from; r < w.rows; r += step)
+    // unsigned: w has up to 2^31 - 1025 rows, and the step goes past 2^31
+    for (uint32_t r = from; r < (uint32_t)w.rows; r += step)
         for (int64_t c = lane * 8; c < w.cols; c += 512)
             *reinterpret_cast<s16x8*>(w.out + (int64_t)r * ((w.cols + 7) & ~7) + c) = row8(w.m + (int64_t)r * w.ld + c, w.cols - (int)c);
 }

@@ -699,3 +699,33 @@ def test_a_captured_step_through_autograd():
         torch.cuda.synchronize()
         for a, b in zip(out, step()):
             assert torch.equal(a, b)
+
+
+def test_cross_entropy_of_the_largest_vocabulary():
+    """Words up to the largest number a size can be, of rows that have to be copied: numbers of rows
+    that a step of 8192 takes past 2^31."""
+    dt, n = torch.bfloat16, 2 ** 31 - 1 - 1024
+    say("largest vocabulary")
+    x, w = torch.ones(1, 1, dtype=dt, device=DEV), torch.zeros(n, 1, dtype=dt, device=DEV)
+    w[5], w[n - 1] = 1.0, 2.0
+    targets = torch.tensor([n - 1], device=DEV)
+    total = n - 2 + np.exp(1.0) + np.exp(2.0)
+    loss, lse = torch.empty(1, device=DEV), torch.empty(1, device=DEV)
+    edkm.linear_cross_entropy(x, w, targets, loss, lse)
+    # up to 2^17 + 30 additions of equal numbers one after another, exact while the sum is below 2^24
+    # of them; what is left is the logarithm's and lse's own rounding, and a few ulps of the sum
+    assert abs(float(lse) - np.log(total)) <= 4 * M.U * np.log(total) + 40 * M.U
+    assert abs(float(loss) - (np.log(total) - 2)) <= 4 * M.U * np.log(total) + 40 * M.U
+    torch.cuda.empty_cache()
+    dx, dw = torch.empty_like(x), torch.full_like(w, float("nan"))
+    edkm.linear_cross_entropy_backward(torch.ones(1, device=DEV), x, w, targets, lse, dx, dw)
+    # lse's error is p's, relative; dz and dw are rounded once each
+    near = 2 * L.half(dt) + 2 * M.U * np.log(total) + 40 * M.U
+    for at, ref in ((5, np.exp(1.0) / total), (n - 1, np.exp(2.0) / total - 1), (0, 1 / total), (n - 2, 1 / total)):
+        assert abs(float(dw[at]) - ref) <= near * abs(ref), at
+    same = sum(int((dw[a:a + 2 ** 28] == dw[0]).sum()) for a in range(0, n, 2 ** 28))
+    assert same == n - 2
+    ref = np.exp(1.0) / total + 2 * (np.exp(2.0) / total - 1)
+    assert abs(float(dx) - ref) <= near * abs(ref)
+    del w, dw
+    torch.cuda.empty_cache()

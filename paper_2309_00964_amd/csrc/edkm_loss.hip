@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
 #pragma unroll
         for (int e = 0; e < PICK; ++e) {
             t[e] = i + e < a.m ? word_of<IDX>(a.targets, i + e, a.n) : -1;
-            g[e] = a.dloss && i + e < a.m ? a.dloss[a.reduction == RED_NONE ? i + e : 0] : 1.f;
+            g[e] = a.backward && i + e < a.m ? a.dloss[a.reduction == RED_NONE ? i + e : 0] : 1.f;
         }
 #pragma unroll
         for (int e = 0; e < PICK; ++e) {
@@ -54,11 +54,11 @@ __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
 #pragma unroll
         for (int e = 0; e < PICK; ++e) {
             if (i + e >= a.m) break;
-            if (a.dloss) a.r.slot[i + e] = t[e] >= 0 ? at : -1;
+            if (a.backward) a.r.slot[i + e] = t[e] >= 0 ? at : -1;
             if (t[e] >= 0) {
                 a.r.row[at] = (int)(i + e);
                 a.r.word[at] = t[e];
-                if (a.dloss) {
+                if (a.backward) {
                     a.r.value[at] = g[e];
                     top = fmaxf(top, fabsf(g[e]));
                 }
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
         }
     }
     if (threadIdx.x == 0) a.r.count[0] = base;
-    if (!a.dloss) return;
+    if (!a.backward) return;
 #pragma unroll
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     if (lane == 0) tops[w] = top;
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(1024) k_pick_gather(PickArgs a, GatherArgs g, 
         t[e] = word_of<IDX>(a.targets, min(i + e, m - 1), a.n);
         grad[e] = 1.f;
     }
-    if (a.dloss)
+    if (a.backward)
 #pragma unroll
         for (int e = 0; e < T; ++e) grad[e] = a.dloss[a.reduction == RED_NONE ? min(i + e, m - 1) : 0];
 #pragma unroll
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(1024) k_pick_gather(PickArgs a, GatherArgs g, 
     const bool first = blockIdx.x == 0;
     if (first && threadIdx.x == 0) {
         a.r.count[0] = count;
-        if (a.dloss) *a.r.alpha = top * (1.f / 32768.f) / (a.reduction == RED_MEAN ? (float)max(count, 1) : 1.f);
+        if (a.backward) *a.r.alpha = top * (1.f / 32768.f) / (a.reduction == RED_MEAN ? (float)max(count, 1) : 1.f);
     }
 #pragma unroll
     for (int e = 0; e < T; ++e) {
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(1024) k_pick_gather(PickArgs a, GatherArgs g, 
             if (first) {
                 a.r.row[at] = i + e;
                 a.r.word[at] = t[e];
-                if (a.dloss) a.r.value[at] = grad[e] / top * 32768.f;
+                if (a.backward) a.r.value[at] = grad[e] / top * 32768.f;
             }
             ++at;
         } else if (first && i + e < m) {

@@ -145,7 +145,8 @@ struct PickArgs {
     int reduction;
     LossRows r;
     float *loss, *lse;      // forward: zeros for tokens without a target
-    const float* dloss;     // backward
+    const float* dloss;     // backward; may be null without tokens
+    int backward;
 };
 
 // x's rows of those tokens, one after another with zeros up to ldo; nothing if all tokens

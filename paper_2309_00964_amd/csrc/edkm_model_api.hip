@@ -433,6 +433,7 @@ edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, 
     pick.reduction = reduction;
     pick.r = rows_at(base, L.rows);
     pick.dloss = dloss;
+    pick.backward = 1;
     uint16_t *xs = reinterpret_cast<uint16_t*>(base + L.rows.x), *dz = reinterpret_cast<uint16_t*>(base + L.dz);
     AlignArgs copies{};
     if (m > 0) align_rows(copies, pw, ldw, n, k, base + L.w);

@@ -729,3 +729,21 @@ def test_cross_entropy_of_the_largest_vocabulary():
     assert abs(float(dx) - ref) <= near * abs(ref)
     del w, dw
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
+@pytest.mark.parametrize("m", [0, 5, 9000])
+def test_no_targets_in_a_workspace_of_nan(m, reduction):
+    """What a backward takes from its list of no tokens is written there, not found."""
+    dt, n, k = torch.bfloat16, 90, 72
+    say("no targets, workspace of NaN", m, reduction)
+    nans = lambda size: torch.full((size,), 255, dtype=torch.uint8, device=DEV)  # noqa: E731
+    x, w = torch.full((m, k), float("nan"), dtype=dt, device=DEV), randn(1, n, k, dtype=dt)
+    targets = torch.full((m,), -100, device=DEV)
+    loss, lse = torch.ones(m if reduction == "none" else 1, device=DEV), torch.ones(m, device=DEV)
+    edkm.linear_cross_entropy(x, w, targets, loss, lse, reduction, nans(edkm.linear_cross_entropy_workspace_bytes(m, n, k)))
+    assert not bool(loss.any()) and not bool(lse.any())
+    dx, dw = torch.ones_like(x), torch.ones_like(w)
+    edkm.linear_cross_entropy_backward(torch.ones_like(loss), x, w, targets, lse, dx, dw, reduction,
+                                       nans(edkm.linear_cross_entropy_backward_workspace_bytes(m, n, k)))
+    assert not bool(dx.any()) and not bool(dw.any())

@@ -747,3 +747,41 @@ def test_no_targets_in_a_workspace_of_nan(m, reduction):
     edkm.linear_cross_entropy_backward(torch.ones_like(loss), x, w, targets, lse, dx, dw, reduction,
                                        nans(edkm.linear_cross_entropy_backward_workspace_bytes(m, n, k)))
     assert not bool(dx.any()) and not bool(dw.any())
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+@pytest.mark.parametrize("m", [5, 17, 64, 300, 1100, 9000])
+def test_certain_tokens_have_no_loss(fmt, m):
+    """A certain target has a loss of 0 and no gradient however large its logit is, by every kernel; of
+    two words as large as each other each has half.  A token's logits are one product that is not 0,
+    v or -v for v of 40 to 3040, so they are exact, and e^(-2 v) is at most 1.8e-35."""
+    dt, n, k = L.DT[fmt], 500, 64
+    say("certain tokens", fmt, m)
+    g = torch.Generator(device=DEV).manual_seed(m)
+    v = (40 + 3000 * torch.rand(m, generator=g, device=DEV)).to(dt)
+    i, j = torch.arange(m, device=DEV), torch.arange(k, device=DEV)
+    c = i % k
+    x, w = torch.zeros(m, k, dtype=dt, device=DEV), -torch.ones(n, k, dtype=dt, device=DEV)
+    x[i, c], w[j, j] = v, 1.0
+    w[k + j[32:], j[32:]] = 1.0         # the columns from 32 on have two such words
+    loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    edkm.linear_cross_entropy(x, w, c, loss, lse)
+    ref = torch.where(c < 32, 0.0, np.log(2.0)).double()
+    # the sum is 1 or 2, exactly; its logarithm is off by at most two ulps
+    assert bool((loss >= 0).all())
+    L.assert_within(loss, ref, ref * 2 * M.U, "loss")
+    L.assert_within(lse, v.double() + ref, (v.double() + ref) * M.U, "lse")
+    dloss, dx, dw = torch.full((m,), 1.0 / m, device=DEV), torch.empty_like(x), torch.empty_like(w)
+    edkm.linear_cross_entropy_backward(dloss, x, w, c, lse, dx, dw)
+    # half's error: lse's rounding, an ulp or two of e^, the rounding to 16 bits
+    each = 0.5 * (v.double() * M.U + 8 * M.U + L.half(dt)) / m
+    # both words of a pair have the same row of w: their shares, -1/2 and 1/2, cancel but for their errors
+    L.assert_within(dx, torch.zeros_like(dx).double(), torch.where(c < 32, 0.0, 2 * each * (1 + L.half(dt)))[:, None].expand(m, k) + 1e-30 + L.tiny(dt), "dx")
+    ref, tol = torch.zeros(n, k, dtype=torch.float64, device=DEV), torch.zeros(n, k, dtype=torch.float64, device=DEV)
+    two = c >= 32
+    half = 0.5 * v.double()[two] / m
+    for row, sign in ((c, -1), (c + k, 1)):
+        ref.index_put_((row[two], c[two]), sign * half, accumulate=True)
+        tol.index_put_((row[two], c[two]), each[two] * v.double()[two], accumulate=True)
+    tol = tol + ref.abs() * (L.half(dt) + (m + 4) * M.U) + 1e-30 + L.tiny(dt)
+    L.assert_within(dw, ref, tol, "dw")

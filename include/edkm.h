@@ -461,8 +461,8 @@ edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int forma
  *   dx = dz W (m x k),  dw = dz^T x (n x k without gaps), in the 16-bit format; one may be NULL.
  * Rows without a target or with g_i = 0 have dx_i = 0 and no part in dw, whatever they hold.
  * z is formed again, some thousand words at a time, and dz is rounded to 16 bits on the way
- * into the two products, as g_i's share of the largest |g_i| times 2^15 (in fp16 a token whose
- * |g_i| is below 2^-14 of the largest keeps fewer digits). */
+ * into the two products, as g_i's share of the largest finite |g_i| times 2^15 (in fp16 a token whose
+ * |g_i| is below 2^-14 of the largest keeps fewer digits).  A g_i that is not finite reaches dx_i and dw only. */
 size_t edkm_linear_cross_entropy_backward_workspace_bytes(int64_t m, int64_t n, int64_t k);
 edkm_status edkm_linear_cross_entropy_backward(int64_t m, int64_t n, int64_t k, int format, int index_type, int reduction,
                                                const float* dloss, const void* x, int64_t ldx, const void* w, int64_t ldw,

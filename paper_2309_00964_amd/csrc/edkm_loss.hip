@@ -15,6 +15,11 @@ namespace edkm {
 // gradient; a backward's factors follow, once their largest is known.  What the products
 // read has no row of any other token, so whatever those hold (NaN, Inf) reaches no gradient.
 constexpr int PICK = 8;      // tokens of a thread at a time
+
+// What a gradient counts for the largest: one that is not finite nothing, so that its token
+// alone has a factor that is not finite.  (Without any other the largest is 1.)
+__device__ __forceinline__ float size_of(float g) { return __builtin_isfinite(g) ? fabsf(g) : 0.f; }
+
 template <int IDX>
 __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
     __shared__ int waves[2][16];
@@ -60,7 +65,7 @@ __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
                 a.r.word[at] = t[e];
                 if (a.backward) {
                     a.r.value[at] = g[e];
-                    top = fmaxf(top, fabsf(g[e]));
+                    top = fmaxf(top, size_of(g[e]));
                 }
                 ++at;
             } else {
@@ -77,6 +82,7 @@ __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 16; ++q) top = fmaxf(top, tops[q]);
+    if (top == 0.f) top = 1.f;
     for (int i = threadIdx.x; i < base; i += 1024) a.r.value[i] = a.r.value[i] / top * 32768.f;
     if (threadIdx.x == 0) *a.r.alpha = top * (1.f / 32768.f) / (a.reduction == RED_MEAN ? (float)max(base, 1) : 1.f);
 }
@@ -143,7 +149,7 @@ __global__ void __launch_bounds__(1024) k_pick_gather(PickArgs a, GatherArgs g, 
     for (int e = 0; e < T; ++e) {
         if (i + e >= m || grad[e] == 0.f) t[e] = -1;
         mine += t[e] >= 0;
-        if (t[e] >= 0) top = fmaxf(top, fabsf(grad[e]));
+        if (t[e] >= 0) top = fmaxf(top, size_of(grad[e]));
     }
     int run = mine;
 #pragma unroll
@@ -164,6 +170,7 @@ __global__ void __launch_bounds__(1024) k_pick_gather(PickArgs a, GatherArgs g, 
         count += waves[p];
         top = fmaxf(top, tops[p]);
     }
+    if (top == 0.f) top = 1.f;
     const bool first = blockIdx.x == 0;
     if (first && threadIdx.x == 0) {
         a.r.count[0] = count;

@@ -785,3 +785,29 @@ def test_certain_tokens_have_no_loss(fmt, m):
         tol.index_put_((row[two], c[two]), each[two] * v.double()[two], accumulate=True)
     tol = tol + ref.abs() * (L.half(dt) + (m + 4) * M.U) + 1e-30 + L.tiny(dt)
     L.assert_within(dw, ref, tol, "dw")
+
+
+@pytest.mark.parametrize("m", [40, 2000, 9000])
+def test_an_infinite_gradient_stays_in_its_token(m):
+    """dx_i = g_i (p - onehot) W: an Inf or NaN among dL/dloss spoils its own row of dx and no other."""
+    dt, n, k = torch.float16, 100, 64
+    say("infinite dloss", m)
+    x, w = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt, scale=0.3)
+    targets = tokens(3, m, n)
+    targets[5:8] = torch.tensor([1, 2, 3], device=DEV)
+    loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    edkm.linear_cross_entropy(x, w, targets, loss, lse)
+    dloss = torch.rand(m, device=DEV) + 0.1
+    for odd in ((float("inf"), 0.5, 0.5), (-float("inf"), float("nan"), float("inf"))):
+        dloss[5:8] = torch.tensor(odd, device=DEV)
+        dx = torch.empty_like(x)
+        edkm.linear_cross_entropy_backward(dloss, x, w, targets, lse, dx)
+        finite = dloss.isfinite()
+        ref, tol = M.cross_entropy_grads(torch.where(finite, dloss, 0.0), x, w, targets, "none")["dx"]
+        L.assert_within(dx[finite], ref[finite], tol[finite], "dx")
+        assert not bool(dx[~finite].isfinite().any())
+    # none that is finite: the rows of no target are still zeros
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    edkm.linear_cross_entropy_backward(torch.full_like(dloss, float("inf")), x, w, targets, lse, dx, dw)
+    there = (targets >= 0) & (targets < n)
+    assert not bool(dx[there].isfinite().any()) and not bool(dx[~there].any()) and not bool(dw.isfinite().any())

@@ -214,9 +214,10 @@ struct LossSum : LossBegin {
   template <int TR>
   struct End {
     int row[TR][2];         // where the lane's two rows of a block go
-    float alpha;
+    float alpha[2];
     __device__ __forceinline__ void init(const LossArgs& p, int lane, int r) {
-        alpha = *p.rows_of.alpha;
+        alpha[0] = p.rows_of.alpha[0];
+        alpha[1] = p.rows_of.alpha[1];
 #pragma unroll
         for (int i = 0; i < TR; ++i)
 #pragma unroll
@@ -241,7 +242,7 @@ struct LossSum : LossBegin {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[j][e] *= alpha;
+            for (int e = 0; e < 4; ++e) acc[j][e] = acc[j][e] * alpha[0] * alpha[1];
         store_block<F>(p, lds, lane, r0, c0, acc, p.cols, [&](int q) { return p.out + (int64_t)row[i][q] * p.ldo; });
     }
   };

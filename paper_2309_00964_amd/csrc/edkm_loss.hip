@@ -19,6 +19,11 @@ constexpr int PICK = 8;      // tokens of a thread at a time
 // What a gradient counts for the largest: one that is not finite nothing, so that its token
 // alone has a factor that is not finite.  (Without any other the largest is 1.)
 __device__ __forceinline__ float size_of(float g) { return __builtin_isfinite(g) ? fabsf(g) : 0.f; }
+// In two factors, whose product may be a subnormal number although dx and dw are not.
+__device__ __forceinline__ void scales(const PickArgs& a, float top, int count) {
+    a.r.alpha[0] = 1.f / 32768.f / (a.reduction == RED_MEAN ? (float)max(count, 1) : 1.f);
+    a.r.alpha[1] = top;
+}
 
 template <int IDX>
 __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
@@ -84,7 +89,7 @@ __global__ void __launch_bounds__(1024) k_pick(PickArgs a) {
     for (int q = 0; q < 16; ++q) top = fmaxf(top, tops[q]);
     if (top == 0.f) top = 1.f;
     for (int i = threadIdx.x; i < base; i += 1024) a.r.value[i] = a.r.value[i] / top * 32768.f;
-    if (threadIdx.x == 0) *a.r.alpha = top * (1.f / 32768.f) / (a.reduction == RED_MEAN ? (float)max(base, 1) : 1.f);
+    if (threadIdx.x == 0) scales(a, top, base);
 }
 
 hipError_t launch_pick(const PickArgs& a, int index_type, hipStream_t s) {
@@ -174,7 +179,7 @@ __global__ void __launch_bounds__(1024) k_pick_gather(PickArgs a, GatherArgs g, 
     const bool first = blockIdx.x == 0;
     if (first && threadIdx.x == 0) {
         a.r.count[0] = count;
-        if (a.backward) *a.r.alpha = top * (1.f / 32768.f) / (a.reduction == RED_MEAN ? (float)max(count, 1) : 1.f);
+        if (a.backward) scales(a, top, count);
     }
 #pragma unroll
     for (int e = 0; e < T; ++e) {

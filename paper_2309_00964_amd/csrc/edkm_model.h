@@ -132,7 +132,7 @@ enum Reduction : int { RED_NONE = 0, RED_SUM = 1, RED_MEAN = 2, RED_COUNT = 3 };
 // What the tokens with a target (in a backward: and a gradient other than 0) have, in order and without gaps.
 struct LossRows {
     int32_t* count;         // [2]: how many there are
-    float* alpha;           // backward: what dz is a share of
+    float* alpha;           // [2] backward: what dz is a share of, as a product
     int32_t* row;           // [m] the token
     int32_t* word;          // [m] its target
     int32_t* slot;          // [m] backward: a token's place among them, -1 for none

@@ -811,3 +811,21 @@ def test_an_infinite_gradient_stays_in_its_token(m):
     edkm.linear_cross_entropy_backward(torch.full_like(dloss, float("inf")), x, w, targets, lse, dx, dw)
     there = (targets >= 0) & (targets < n)
     assert not bool(dx[there].isfinite().any()) and not bool(dx[~there].any()) and not bool(dw.isfinite().any())
+
+
+@pytest.mark.parametrize("m", [30, 9000])
+@pytest.mark.parametrize("g", [1.3 * 2.0 ** -132, 1.7 * 2.0 ** -122, 1.9 * 2.0 ** 110])
+@pytest.mark.parametrize("reduction", ["sum", "mean"])
+def test_gradients_of_tiny_and_huge_scale(m, g, reduction):
+    """dL/dloss down to fp32's subnormal numbers and up to where dx leaves bf16's range: what the
+    gradients are scaled by keeps its digits."""
+    dt, n, k = torch.bfloat16, 100, 64
+    say("scale of dloss", m, g, reduction)
+    x, w = randn(1, m, k, dtype=dt, scale=2.0 ** -12), randn(2, n, k, dtype=dt, scale=2.0 ** 12)
+    targets = tokens(3, m, n)
+    loss, lse = torch.empty(1, device=DEV), torch.empty(m, device=DEV)
+    edkm.linear_cross_entropy(x, w, targets, loss, lse, reduction)
+    dloss, dx, dw = torch.full((1,), g, dtype=torch.float64).float().to(DEV), torch.empty_like(x), torch.empty_like(w)
+    edkm.linear_cross_entropy_backward(dloss, x, w, targets, lse, dx, dw, reduction)
+    for key, (ref, tol) in M.cross_entropy_grads(dloss, x, w, targets, reduction).items():
+        L.assert_within({"dx": dx, "dw": dw}[key], ref, tol, key)

@@ -19,8 +19,9 @@ bool format_ok(int format) { return format == EDKM_KEYS_FP16 || format == EDKM_K
 bool index_ok(int type) { return type == EDKM_INDEX_INT32 || type == EDKM_INDEX_INT64; }
 edkm_status done(hipError_t e) { return e == hipSuccess ? EDKM_OK : EDKM_ERR_HIP; }
 
+// Its matrices are m x d and v x d.
 bool embed_ok(int64_t m, int64_t v, int64_t d, int format, int index_type) {
-    return product_ok(m, v, d, format, ACT_NONE) && index_ok(index_type);
+    return size_ok(m, 0) && size_ok(v, 1) && size_ok(d, 1) && std::max(m, v) <= MATRIX_MAX / d && format_ok(format) && index_ok(index_type);
 }
 
 // Workspace of an embedding's backward: the sorted tokens, what their passes need, and the

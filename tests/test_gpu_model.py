@@ -829,3 +829,21 @@ def test_gradients_of_tiny_and_huge_scale(m, g, reduction):
     edkm.linear_cross_entropy_backward(dloss, x, w, targets, lse, dx, dw, reduction)
     for key, (ref, tol) in M.cross_entropy_grads(dloss, x, w, targets, reduction).items():
         L.assert_within({"dx": dx, "dw": dw}[key], ref, tol, key)
+
+
+def test_embedding_of_more_tokens_times_rows_than_a_matrix_holds():
+    """2^22 + 1 tokens of a table of 2^18 rows: neither the table nor y is large."""
+    dt, m, v, d = torch.bfloat16, (1 << 22) + 1, 1 << 18, 8
+    say("embedding, many tokens and rows")
+    ids = torch.randint(-5, v + 5, (m,), device=DEV)
+    table, dy = randn(1, v, d, dtype=dt), randn(2, m, d, dtype=dt)
+    y, g = torch.empty(m, d, dtype=dt, device=DEV), torch.empty_like(table)
+    edkm.embedding(ids, table, y)
+    there = (ids >= 0) & (ids < v)
+    assert torch.equal(y, torch.where(there[:, None], table[ids.clamp(0, v - 1)], 0.0))
+    edkm.embedding_backward(ids, dy, g)
+    L.assert_within(g, *M.embedding_grad(ids, dy, v, 1.0), "dtable")
+    idx, packed, lut = L.palette(v, d, 3, 3)
+    edkm.palette_embedding(ids, torch.from_numpy(packed).to(DEV), torch.from_numpy(lut).to(DEV), v, y)
+    table = torch.from_numpy(lut).to(DEV).to(dt)[torch.from_numpy(idx).to(DEV).long()].view(v, d)
+    assert torch.equal(y, torch.where(there[:, None], table[ids.clamp(0, v - 1)], 0.0))

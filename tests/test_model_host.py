@@ -193,3 +193,15 @@ IDS, F32 = torch.zeros(4, dtype=torch.int64), torch.float32
 def test_binding_refuses_what_does_not_fit(call, what):
     with pytest.raises(ValueError, match=what):
         call()
+
+
+def test_embedding_is_bounded_by_its_matrices():
+    """m x d and v x d are the embedding's matrices; there is none of m x v."""
+    m, v = (1 << 22) + 1, 1 << 18
+    assert edkm.embedding_backward_workspace_bytes(m, v, 8) > 0
+    assert embedding_backward(m=m, v=v, d=8, lddy=8, lddt=8, ws=None) == edkm.ERR_WORKSPACE
+    for kw in (dict(m=1 << 21, v=1, d=1 << 20), dict(m=1, v=1 << 21, d=1 << 20)):
+        assert edkm.embedding_backward_workspace_bytes(**kw) == 0
+        assert embedding(**kw, ldt=1 << 20, ldy=1 << 20) == edkm.ERR_ARG
+        assert embedding_backward(**kw, lddy=1 << 20, lddt=1 << 20) == edkm.ERR_ARG
+    assert palette_embedding(m=1 << 21, v=1, d=1 << 20, ldy=1 << 20) == edkm.ERR_ARG

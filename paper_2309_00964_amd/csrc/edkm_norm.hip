@@ -396,8 +396,9 @@ __global__ void __launch_bounds__(1024) k_norm_join(NormArgs a) {
         return;
     }
     sum *= a.scale;
-    if (post) post[mine] = to_16<F>(a.gate && !a.gate_rows ? sum * to_f32<F>(a.gate[mine]) : sum);
-    if (gate) gate[mine] = to_16<F>(a.post ? sum * to_f32<F>(a.post[mine]) : sum);
+    const bool any = a.groups > 0;      // a sum of no rows is 0, whatever it would be a multiple of
+    if (post) post[mine] = to_16<F>(any && a.gate && !a.gate_rows ? sum * to_f32<F>(a.gate[mine]) : sum);
+    if (gate) gate[mine] = to_16<F>(any && a.post ? sum * to_f32<F>(a.post[mine]) : sum);
 }
 
 // ----------------------------------------------------------------------------

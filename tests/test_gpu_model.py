@@ -847,3 +847,13 @@ def test_embedding_of_more_tokens_times_rows_than_a_matrix_holds():
     edkm.palette_embedding(ids, torch.from_numpy(packed).to(DEV), torch.from_numpy(lut).to(DEV), v, y)
     table = torch.from_numpy(lut).to(DEV).to(dt)[torch.from_numpy(idx).to(DEV).long()].view(v, d)
     assert torch.equal(y, torch.where(there[:, None], table[ids.clamp(0, v - 1)], 0.0))
+
+
+def test_norm_gradients_of_no_rows_are_zeros_whatever_the_vectors_hold():
+    dt, n = torch.bfloat16, 70
+    none = torch.empty(0, n, dtype=dt, device=DEV)
+    odd = torch.full((n,), float("inf"), dtype=dt, device=DEV)
+    odd[3::7] = float("nan")
+    dw, dp, dg = (torch.ones(n, dtype=dt, device=DEV) for _ in range(3))
+    edkm.residual_norm_backward(none, none, none, odd, none, odd, odd, dweight=dw, dpost_weight=dp, dgate=dg)
+    assert not bool(dw.any()) and not bool(dp.any()) and not bool(dg.any())

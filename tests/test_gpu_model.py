@@ -857,3 +857,56 @@ def test_norm_gradients_of_no_rows_are_zeros_whatever_the_vectors_hold():
     dw, dp, dg = (torch.ones(n, dtype=dt, device=DEV) for _ in range(3))
     edkm.residual_norm_backward(none, none, none, odd, none, odd, odd, dweight=dw, dpost_weight=dp, dgate=dg)
     assert not bool(dw.any()) and not bool(dp.any()) and not bool(dg.any())
+
+
+@pytest.mark.parametrize("m", [3, 40, 1100])
+def test_cross_entropy_past_32_bits_with_exact_logits(m):
+    """A vocabulary's weights and their gradient of more than 2^32 bytes, held to bounds that a
+    missing or misplaced value does not meet: x is not 0 in three columns, where both hold multiples
+    of 1/4 up to 1, so that a logit is exact in fp32 and a row of dw has three values."""
+    dt, n, k = torch.bfloat16, 70001, 32768
+    say("loss past 32 bits, exact logits", m)
+    at = torch.tensor([0, 16385, k - 1], device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(m)
+    quarters = lambda rows: (torch.randint(1, 5, (rows, 3), generator=g, device=DEV)  # noqa: E731
+                             * (1 - 2 * torch.randint(0, 2, (rows, 3), generator=g, device=DEV)) / 4).to(dt)
+    x, w = torch.zeros(m, k, dtype=dt, device=DEV), torch.empty(n, k, dtype=dt, device=DEV)
+    for a in range(0, n, 10000):
+        w[a:a + 10000] = randn(a + 7, min(10000, n - a), k, dtype=dt)
+    x[:, at], w[:, at] = quarters(m), quarters(n)
+    targets = torch.randint(0, n, (m,), generator=g, device=DEV)
+    targets[:3] = torch.tensor([n - 1, 0, 66000])
+    z = x[:, at].double() @ w[:, at].double().t()
+    lse_ref = torch.logsumexp(z, 1)
+    want = lse_ref - z.gather(1, targets[:, None])[:, 0]
+    loss, lse = torch.empty(m, device=DEV), torch.empty(m, device=DEV)
+    edkm.linear_cross_entropy(x, w, targets, loss, lse)
+    # a term passes up to 18 additions in its block, 35 blocks of a thread and 22 joins, each with two
+    # products by e^ (an ulp each, and two of its argument); logits are multiples of 1/16
+    tol = 500 * M.U + 4 * M.U * lse_ref
+    assert float(tol.max()) < 1 / 64
+    L.assert_within(lse, lse_ref, tol, "lse")
+    L.assert_within(loss, want, tol, "loss")
+    dw, dx = torch.full_like(w, float("nan")), torch.full_like(x, float("nan"))
+    edkm.linear_cross_entropy_backward(torch.ones(m, device=DEV), x, w, targets, lse, dx, dw)
+    dz = torch.softmax(z, 1)
+    dz[torch.arange(m, device=DEV), targets] -= 1
+    # lse's error and e^'s own relative, the target's 1 by an ulp, then the rounding to 16 bits
+    ed = dz.abs() * L.half(dt) + (dz.abs() + 1e-9) * (tol + 40 * M.U)[:, None] * (1 + L.half(dt))
+    ed[torch.arange(m, device=DEV), targets] += 2 * M.U
+    ref, mag = dz.t().contiguous() @ x[:, at].double(), dz.abs().t().contiguous() @ x[:, at].double().abs()
+    bound = ed.t().contiguous() @ x[:, at].double().abs() + (m + 4) * M.U * mag
+    bound = bound + ref.abs() * L.half(dt) + L.tiny(dt)
+    assert float((bound < ref.abs()).double().mean()) > 0.9       # zeros would be refused
+    L.assert_within(dw[:, at], ref, bound, "dw")
+    dw[:, at] = 0
+    assert not any(bool(dw[a:a + 10000].any()) for a in range(0, n, 10000))
+    cols = torch.cat([at, torch.arange(5, k, 499, device=DEV)])
+    wc = torch.cat([w[a:a + 10000][:, cols] for a in range(0, n, 10000)]).double()
+    ref, mag = dz @ wc, dz.abs() @ wc.abs()
+    # sums of a tile's depths, its parts and the pieces, whatever their order: by n ulps at most
+    bound = ed @ wc.abs() + (n + 4) * M.U * mag
+    bound = bound + ref.abs() * L.half(dt) + L.tiny(dt)
+    assert float((bound < ref.abs()).double().mean()) > 0.9
+    L.assert_within(dx[:, cols], ref, bound, "dx")
+    assert bool(dx.isfinite().all())

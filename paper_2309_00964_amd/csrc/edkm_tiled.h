@@ -555,14 +555,14 @@ __global__ void __launch_bounds__(W * 64) k_join(typename ArgsOf<E>::type p, int
     }
 }
 
-template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, int BITS = 0, class E = void>
-static hipError_t tiled(typename ArgsOf<E>::type p, const ProductPlan& q, hipStream_t s) {
+template <int F, int OPA, int OPB, int B, int WM, int WN, bool DIRECT, int BITS = 0>
+static hipError_t tiled(ProductArgs p, const ProductPlan& q, hipStream_t s) {
     const int64_t tiles = ((int64_t)p.cols + B - 1) / B * (((int64_t)p.rows + B - 1) / B);
-    EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS, E>), (uint64_t)(tiles * q.splits), WM * WN * 64, p);
-    if constexpr (B == SPLIT_TILE || !std::is_void_v<E>) {
+    EDKM_GO_PARTS((k_tiled<F, OPA, OPB, B, B, WM, WN, DIRECT, BITS>), (uint64_t)(tiles * q.splits), WM * WN * 64, p);
+    if constexpr (B == SPLIT_TILE) {
         const dim3 blocks((uint32_t)(tiles * WM * WN * (B / WM / 16)));
-        if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4, E>), blocks, dim3(256), p, q.splits);
-        else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1, E>), blocks, dim3(64), p, q.splits);
+        if (q.splits > 8) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 4>), blocks, dim3(256), p, q.splits);
+        else if (q.splits > 1) EDKM_GO((k_join<F, B, B, WM, WN, OPB == OP_DEPTH, 1>), blocks, dim3(64), p, q.splits);
     }
     return hipSuccess;
 }

@@ -430,14 +430,15 @@ static hipError_t by_length(int64_t n, Go go) {
     return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
 }
 
-// Parts of a backward's sums: one for each row that is in work (two workgroups a CU, or one of the
-// longest rows), or for each wave of narrow rows.
+// Parts of a backward's sums: one for each row that is in work, or for each wave of narrow rows (up
+// to 256 values).  That is two workgroups of four waves a CU up to 512 values, and above them as many
+// workgroups, one to a row, as hold 1024 threads of a CU: eight, four, two, one.
 uint32_t norm_groups(int64_t m, int64_t n) {
     if (n <= 256) {
         const int64_t rows = n <= 128 ? Row<16>::ROWS : Row<32>::ROWS;
         return (uint32_t)std::min<int64_t>((m + rows - 1) / rows, 512) * 4;
     }
-    return (uint32_t)std::min<int64_t>(m, n <= 512 ? 2048 : n <= 1024 ? 2048 : n <= 2048 ? 1024 : n <= 4096 ? 512 : 256);
+    return (uint32_t)std::min<int64_t>(m, n <= 1024 ? 2048 : n <= 2048 ? 1024 : n <= 4096 ? 512 : 256);
 }
 
 template <int F>

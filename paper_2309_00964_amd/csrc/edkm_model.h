@@ -233,10 +233,16 @@ inline int64_t loss_piece(int64_t m, int64_t n) {
 }
 // Tokens up to which a forward makes no list of those with a target: it would be two launches
 // (9 us; 512 x 32000 x 4096 takes 131 us without, 140 with), and leaving out a quarter of the tokens
-// pays from about as many on.  And up to which each workgroup takes sixteen words for all tokens,
-// which is bound by the words' bytes (32000 x 4096: 1 token 52 us, 5.0 TB/s, 16 tokens 72; by the
-// tiles 83 and 84).
-constexpr int64_t LIST_LEAST = 1024, LOSS_FEW = 16, ONE_LIST = 8192;
+// pays from about as many on.
+constexpr int64_t LIST_LEAST = 1024, ONE_LIST = 8192;
+// Tokens up to which each workgroup takes sixteen words for all tokens: it is bound by the words'
+// bytes, but up to sixteen tokens share a wave's loads of x, and its time grows with them (losses
+// of 32000 x 4096, us by it and by the tiles: 1 token 50 and 58, 8 tokens 56 and 58, 16 tokens 68 and
+// 58; of 131072 x 2048 108 and 124, 128 and 124, 140 and 126; their mean over 300 x 64 8 and 9 to 12).  The tiles
+// need a copy of w where k is no multiple of eight, so there it is up to sixteen (1003 x 777 11.5 and 14 us,
+// 9000 x 1500 22 and 29, 50001 x 1001 64 and 61).
+constexpr int64_t LOSS_FEW = 16, LOSS_FEW_WHOLE = 8;
+inline bool loss_few(int64_t m, int64_t k) { return m > 0 && m <= (k % 8 ? LOSS_FEW : LOSS_FEW_WHOLE); }
 // Tokens of a forward's launch: as many as keep the statistics within 256 MiB, 256 at least.
 inline int64_t loss_rows(int64_t m, int64_t n) {
     const int64_t blocks = (n + 63) / 64, r = (256 << 20) / (blocks * 8) / 256 * 256;

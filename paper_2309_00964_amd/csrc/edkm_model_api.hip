@@ -83,7 +83,7 @@ LossWs loss_ws(int64_t m, int64_t n, int64_t k) {
     L.w = L.rows.total;
     L.stats = L.w + aligned_bytes(n, k);
     const int64_t rows = loss_rows(m, n);
-    L.split = L.stats + up256((size_t)(m <= LOSS_FEW ? (n + 15) / 16 : (n + 63) / 64) * rows * 8);
+    L.split = L.stats + up256((size_t)(loss_few(m, k) ? (n + 15) / 16 : (n + 63) / 64) * rows * 8);
     size_t parts = 0;
     if (m > 0) {
         parts = loss_part_bytes(rows, n, k);
@@ -350,7 +350,7 @@ edkm_status edkm_linear_cross_entropy(int64_t m, int64_t n, int64_t k, int forma
     pick.lse = lse;
     uint16_t* xs = reinterpret_cast<uint16_t*>(base + L.rows.x);
     AlignArgs copies{};
-    const bool list = m > LIST_LEAST || m == 0, few = m > 0 && m <= LOSS_FEW;
+    const bool list = m > LIST_LEAST || m == 0, few = loss_few(m, k);
     if (m > 0 && !few) align_rows(copies, pw, ldw, n, k, base + L.w);
     if (list) {
         if (begin_loss(pick, index_type, px, ldx, k, xs, nullptr, 0, copies, stream) != hipSuccess) return EDKM_ERR_HIP;

@@ -910,3 +910,19 @@ def test_cross_entropy_past_32_bits_with_exact_logits(m):
     assert float((bound < ref.abs()).double().mean()) > 0.9
     L.assert_within(dx[:, cols], ref, bound, "dx")
     assert bool(dx.isfinite().all())
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(8, 500, 304), (9, 500, 304), (16, 500, 304), (8, 500, 301), (9, 500, 301), (16, 500, 301), (17, 500, 301)])
+def test_cross_entropy_of_few_tokens(fmt, m, n, k):
+    """Both sides of the few tokens that take no tiles, with rows of whole pieces and without."""
+    dt = L.DT[fmt]
+    say("few tokens", fmt, m, n, k)
+    x, w = randn(1, m, k, dtype=dt), randn(2, n, k, dtype=dt, scale=2 * k ** -0.5)
+    targets = tokens(3, m, n, "flat")
+    for reduction in ("none", "sum", "mean"):
+        loss, lse = torch.empty(m if reduction == "none" else 1, device=DEV), torch.full((m,), float("nan"), device=DEV)
+        edkm.linear_cross_entropy(x, w, targets, loss, lse, reduction)
+        ref, tol, rl, tl = M.cross_entropy(x, w, targets, reduction)
+        L.assert_within(loss, ref.view(-1), tol.view(-1), "loss")
+        L.assert_within(lse, rl, tl, "lse")

@@ -425,7 +425,7 @@ edkm_status edkm_embedding_backward(int64_t m, int64_t v, int64_t d, int format,
  *   gate  nullable, n values, or m x n with gate_rows = 1 (ldg then counts)
  *   h     m x n (with u); may be r or u (same leading dimension);  y  m x n
  * n is 1 .. 16384, eps a normal fp32 number above 0.  y is of h before its rounding.  Squares are
- * summed in fp32: a row whose mean square is beyond its range is divided by Inf. */
+ * summed in fp32: a row whose squares' sum is beyond its range is divided by Inf. */
 #define EDKM_NORM_MAX 16384
 edkm_status edkm_residual_norm(int64_t m, int64_t n, int format, const void* r, int64_t ldr, const void* u, int64_t ldu,
                                const void* w, const void* post, const void* gate, int64_t ldg, int gate_rows,

@@ -221,8 +221,9 @@ hipError_t launch_loss_end(const LossEndArgs& a, hipStream_t s);
 hipError_t launch_loss_reduce(const LossEndArgs& a, hipStream_t s);
 
 // Words of a piece of the vocabulary whose dz is held at a time: as many as keep it within half
-// the Infinity Cache, which the two products that read it then hit; 2048 at least.  8192 x 32000 x 4096
-// with gradients takes 6925 us by 64 MiB, 6740 by 128, 6860 by 256 and 7000 by 512.
+// the Infinity Cache, which the two products that read it then hit; 2048 at least.  The gradients of 8192 x
+// 32000 x 4096 take 5280-5340 us by 64 MiB, 5140-5180 by 128 and 5230-5270 by 256, of which a quarter does not
+// count 4560, 4130-4160 and 4160: 64 is too little, and above 128 there is no more to gain.
 constexpr int64_t DZ_BYTES = 128 << 20, DZ_LEAST = 2048;
 inline int64_t loss_piece(int64_t m, int64_t n) {
     int64_t p = DZ_BYTES / (2 * (m > 0 ? m : 1));
@@ -231,9 +232,10 @@ inline int64_t loss_piece(int64_t m, int64_t n) {
     const int64_t pieces = (n + p - 1) / p;
     return (((n + pieces - 1) / pieces) + 255) / 256 * 256;
 }
-// Tokens up to which a forward makes no list of those with a target: it would be two launches
-// (9 us; 512 x 32000 x 4096 takes 131 us without, 140 with), and leaving out a quarter of the tokens
-// pays from about as many on.
+// Tokens up to which a forward makes no list of those with a target: it would be a launch more
+// (512 x 32000 x 4096 takes 119 us without, 124 with), and leaving out a quarter of the tokens pays
+// where it saves the tiles a round over the CUs (1000 x 32000 x 4096 213 and 210, of 131072 x 2048 472 and
+// 371).  At most 1024, which k_loss_reduce has threads for.
 constexpr int64_t LIST_LEAST = 1024, ONE_LIST = 8192;
 // Tokens up to which each workgroup takes sixteen words for all tokens: it is bound by the words'
 // bytes, but up to sixteen tokens share a wave's loads of x, and its time grows with them (losses

@@ -926,3 +926,9 @@ def test_cross_entropy_of_few_tokens(fmt, m, n, k):
         ref, tol, rl, tl = M.cross_entropy(x, w, targets, reduction)
         L.assert_within(loss, ref.view(-1), tol.view(-1), "loss")
         L.assert_within(lse, rl, tl, "lse")
+
+
+@pytest.mark.parametrize("m,n,k,lead,gap", [(8, 300, 264, 1, 3), (8, 300, 264, 8, 8), (3, 300, 256, 3, 5), (16, 300, 261, 1, 3), (16, 300, 264, 8, 4)])
+def test_cross_entropy_views_of_few_tokens(m, n, k, lead, gap):
+    """The same for tokens that share a workgroup's words, and for the first that do not."""
+    test_cross_entropy_views_in_nan_buffers(m, n, k, lead, gap)
